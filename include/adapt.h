@@ -368,7 +368,11 @@ enum {
   ADAPT_KERNEL_FORMAT_SEARCH = 11, /* format search: fused round / count / histograms */
   ADAPT_KERNEL_FORMAT_KLD = 12,    /* format search: divergence per (layer, format) */
   ADAPT_KERNEL_FORMAT_QUANTIZE = 13, /* stand-alone quantize to a format         */
-  ADAPT_KERNEL_KINDS = 14
+  ADAPT_KERNEL_DROPOUT = 14,       /* dropout                                    */
+  ADAPT_KERNEL_LOGPROBS = 15,      /* token log probabilities and their gradient */
+  ADAPT_KERNEL_SCAN = 16,          /* gated recurrence                           */
+  ADAPT_KERNEL_SCAN_BACKWARD = 17, /* gated recurrence, backward                 */
+  ADAPT_KERNEL_KINDS = 18
 };
 
 /* Switches per-kernel device timing on (non-zero) or off.  While on, every
@@ -495,6 +499,131 @@ int adapt_format_search(const float* const* tensors, const int64_t* lens, int n_
  *   stream      cudaStream_t or NULL */
 int adapt_format_quantize(const float* x, int64_t n, int kind, int a, int b, int round_mode,
                           uint64_t seed, int layer, float* values_out, void* stream);
+
+/* ---- operators of a training step --------------------------------------------
+ *
+ * What a language model's step needs next to the precision switch: a layer that mixes
+ * tokens (gated recurrence), dropout, and the loss (log probabilities of given tokens),
+ * each with its gradient.  The gradients that come out are what adapt_gradient_diversity
+ * and adapt_normalize_gradients take.
+ *
+ * Conventions as above.  Streams of values are fp32, fp16 or bf16 (ADAPT_DTYPE_*), all of
+ * one type within a call; arithmetic, sums, statistics and states are fp32, each output is
+ * rounded once (to nearest even).  Pointers need the alignment of their elements and no
+ * more; strides and leading dimensions count elements, the innermost stride is 1.  Calls
+ * may be captured into a CUDA graph.  A size of zero is legal and launches nothing. */
+enum { ADAPT_DTYPE_F32 = 0, ADAPT_DTYPE_F16 = 1, ADAPT_DTYPE_BF16 = 2 };
+
+/* Dropout whose mask is never stored (with an optional residual sum):
+ *   y[i][j] = residual[i][j] + (u(e) >= p 2^32 ? x[i][j] / (1 - p) : 0)
+ * e = index_base + i * cols + j is the element's number, u(e) 32 bits of a counter hash of
+ * (seed, layer, e): with j = e >> 1, z = (seed ^ D ^ (layer + 1) C1) + j C2, z ^= z >> 32,
+ * z *= C1, z ^= z >> 29, z *= C3, z ^= z >> 32 (mod 2^64; C1, C2, C3 the constants of the
+ * stochastic-rounding hash, D = 0xA54FF53A5F1D36F1 keeps the draws of one (seed, layer)
+ * apart from that one's), the high word serves even e, the low word odd e.  The same
+ * arguments give the same mask on any layout, so the backward pass is this call on dy.
+ *   x, residual, y  DEVICE [rows][cols] with leading dimensions ldx, ldr, ldy >= cols;
+ *                   residual may be NULL; y may be x or residual itself (same leading
+ *                   dimension), no other overlap
+ *   p               0 <= p <= 1, held to a multiple of 2^-32; 1 drops everything
+ * Dropped elements count as 0 whatever they hold (NaN and Inf included).
+ * Limit: rows * cols <= 2^48. */
+int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, int64_t cols,
+                  int64_t ldx, int64_t ldr, int64_t ldy, int dtype, double p, uint64_t seed,
+                  int32_t layer, uint64_t index_base, void* stream);
+
+#define ADAPT_MAX_TOP 32
+
+/* Log probabilities of given tokens, entropy, the most probable alternatives, and - in the
+ * same call where the weights are known by then - the gradient.  With z = scale * logits:
+ *   lse = ln sum_j e^z_j,  logprob = z_t - lse,  entropy = -sum_j p_j ln p_j,
+ *   dlogits_j = scale (d_logprob ([j = t] - p_j) - d_entropy p_j (ln p_j + entropy))
+ *   logits   DEVICE [rows][vocab], leading dimension ld
+ *   scale    > 0 and finite (the inverse temperature)
+ *   targets  DEVICE int64[rows] or NULL.  A negative target marks a row without one: it is
+ *            not read, its outputs are 0 (ids -1) and its gradient is 0.  A target >= vocab
+ *            gives NaN (log probability, and the gradient where d_logprob is given).
+ *            NULL: no row is left out; logprob_out and d_logprob must be NULL
+ *   n_top    0..ADAPT_MAX_TOP, at most vocab
+ *   logprob_out, entropy_out, lse_out  DEVICE float[rows], each may be NULL
+ *   top_ids_out, top_logprobs_out      DEVICE int32 / float [rows][n_top]: the n_top largest
+ *            logits, equal ones (and +-0) by the lower index, NaN before everything
+ *   d_logprob, d_entropy  DEVICE float[rows], each may be NULL: weights of the gradient
+ *   dlogits_out  DEVICE [rows][vocab], leading dimension ld_grad; given exactly when a
+ *            weight is; may be logits itself (ld_grad = ld), no other overlap
+ * z is formed in fp32; where it is -Inf the probability is 0.  A row that holds nothing
+ * else has lse, logprob and top log probabilities -Inf, entropy 0 and gradient 0.  A z of
+ * NaN or +Inf makes its row's statistics and gradient NaN.  The sums are taken in a fixed order: the same call gives the
+ * same bits.  Limit: vocab and rows < 2^31. */
+int adapt_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                         float scale, const int64_t* targets, int n_top, float* logprob_out,
+                         float* entropy_out, float* lse_out, int32_t* top_ids_out,
+                         float* top_logprobs_out, const float* d_logprob,
+                         const float* d_entropy, void* dlogits_out, int64_t ld_grad,
+                         void* stream);
+
+/* The gradient alone, from lse and entropy as adapt_token_logprobs left them (for weights
+ * that depend on the log probabilities).  lse DEVICE float[rows]; entropy needed with
+ * d_entropy, targets with d_logprob; at least one weight.  The rest as above. */
+int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t vocab, int64_t ld,
+                                  int dtype, float scale, const int64_t* targets,
+                                  const float* lse, const float* entropy,
+                                  const float* d_logprob, const float* d_entropy,
+                                  void* dlogits_out, int64_t ld_grad, void* stream);
+
+/* Gated linear recurrence over [batch][steps][channels], per channel
+ *   ADAPT_GATE_SIGMOID:  a = 1 / (1 + e^-gate),  h_t = a_t h_{t-1} + (1 - a_t) x_t
+ *   ADAPT_GATE_VALUE:    a = gate,               h_t = a_t h_{t-1} + x_t
+ * y_t = h_t.  steps = 1 with h0 and h_last is the form for single tokens.
+ *   x, y     DEVICE [batch][steps][channels]
+ *   gate     DEVICE [batch][steps][channels / gate_group]: gate k serves channels
+ *            k * gate_group .. (k + 1) * gate_group - 1.  gate_group is a power of two up
+ *            to 64 or a multiple of 64, and divides channels
+ *   strides  HOST int64[6] = {batch, step} strides of x, gate, y, or NULL: contiguous.
+ *            Inputs may have stride 0; the rows of y must not overlap.  y may be x itself
+ *            (same strides), no other overlap
+ *   h0       DEVICE float[batch][channels], the state before the first step, or NULL: 0
+ *   lengths  DEVICE int32[batch] or NULL.  Steps at or beyond a length (clamped to
+ *            0..steps) read nothing, leave the state as it is and give y = 0
+ *   reset    DEVICE uint8[batch][steps] or NULL.  At a step with a non-zero byte h_{t-1}
+ *            counts as 0, whatever it holds (a document begins)
+ *   h_last   DEVICE float[batch][channels] or NULL: the state after the last step; may be h0
+ *   carry_out  DEVICE float[batch][ceil(steps / ADAPT_SCAN_TILE)][channels] or NULL: the
+ *            state before every ADAPT_SCAN_TILE-th step, which the backward pass starts from
+ *   workspace  DEVICE scratch of adapt_gated_scan_workspace_bytes, 256-byte aligned, or NULL
+ *            to use a library-owned buffer that grows on demand: calls without a workspace
+ *            of their own must not overlap on the device
+ * Limits: steps <= 2^31 - 256, channels and batch < 2^31, batch * channels <= 2^40. */
+enum { ADAPT_GATE_SIGMOID = 0, ADAPT_GATE_VALUE = 1 };
+#define ADAPT_SCAN_TILE 128
+
+int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int32_t* lengths,
+                     const uint8_t* reset, int64_t batch, int64_t steps, int64_t channels,
+                     int gate_group, int dtype, int mode, const int64_t* strides, void* y,
+                     float* h_last, float* carry_out, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Its gradient: dh_t = dy_t + a_{t+1} dh_{t+1} (from dh_last after the last step), then
+ *   SIGMOID: dx = dh (1 - a), dgate = dh (h_{t-1} - x) a (1 - a);  VALUE: dx = dh, dgate = dh h_{t-1}
+ * (h_{t-1} = 0 at a reset), dgate summed over the channels that share a gate.  The states
+ * are recomputed in fp32 from carry; y is not needed.
+ *   carry    as adapt_gated_scan wrote it for the same inputs
+ *   dh_last  DEVICE float[batch][channels] or NULL: 0
+ *   strides  HOST int64[10] = {batch, step} strides of x, gate, dy, dx, dgate, or NULL
+ *   dx, dgate  DEVICE, 0 at and beyond a sequence's length; dx may be dy itself (same strides)
+ *   dh0      DEVICE float[batch][channels] or NULL
+ * Sums are taken in a fixed order: the same call gives the same bits. */
+int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy,
+                              const float* carry, const float* dh_last, const int32_t* lengths,
+                              const uint8_t* reset, int64_t batch, int64_t steps,
+                              int64_t channels, int gate_group, int dtype, int mode,
+                              const int64_t* strides, void* dx, void* dgate, float* dh0,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of DEVICE workspace a scan of these sizes needs (0: none, or invalid arguments);
+ * backward non-zero asks for the gradient's. */
+size_t adapt_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels,
+                                        int gate_group, int dtype, int backward);
 
 /* The bounds-checking build of the library (libadapt_b200_check.so, made by
  * `python -m paper_2107_13490_b200.build --check`; the stand-in for a memory checker

@@ -7,6 +7,7 @@ there is no fallback: a missing library raises at the first call.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -34,6 +35,8 @@ EXPORTS = (
     "adapt_kernel_times", "adapt_precision_search_static", "adapt_release",
     "adapt_format_search_workspace_bytes", "adapt_format_search", "adapt_format_quantize",
     "adapt_pushup", "adapt_bounds_check_status",
+    "adapt_dropout", "adapt_token_logprobs", "adapt_token_logprobs_backward",
+    "adapt_gated_scan", "adapt_gated_scan_backward", "adapt_gated_scan_workspace_bytes",
 )
 STRATEGY_MIN, STRATEGY_MEAN, STRATEGY_MAX = 0, 1, 2
 FMT_FIXED, FMT_BFP, FMT_FLOAT = 0, 1, 2
@@ -41,7 +44,11 @@ MAX_FORMATS = 1024
 STATIC_MAX_LAYERS, STATIC_MAX_BINS, STATIC_MAX_CAND = 8, 512, 1024
 KERNEL_KINDS = ("range", "range_finalize", "search", "kld", "select", "quantize", "plan",
                 "expand", "search_direct", "diversity", "format_resolve", "format_search",
-                "format_kld", "format_quantize")
+                "format_kld", "format_quantize", "dropout", "logprobs", "scan", "scan_backward")
+DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
+MAX_TOP = 32
+GATE_SIGMOID, GATE_VALUE = 0, 1
+SCAN_TILE = 128
 ALGO_AUTO, ALGO_KEYED, ALGO_DIRECT = 0, 1, 2
 
 
@@ -153,6 +160,21 @@ def lib():
         L.adapt_format_quantize.restype = C.c_int
         L.adapt_format_quantize.argtypes = [C.c_void_p, C.c_int64, C.c_int, C.c_int, C.c_int,
                                             C.c_int, C.c_uint64, C.c_int, C.c_void_p, C.c_void_p]
+        P, I64, I32, F32, F64, SZ = C.c_void_p, C.c_int64, C.c_int, C.c_float, C.c_double, C.c_size_t
+        L.adapt_dropout.restype = C.c_int
+        L.adapt_dropout.argtypes = [P, P, P, I64, I64, I64, I64, I64, I32, F64, C.c_uint64, C.c_int32,
+                                    C.c_uint64, P]
+        L.adapt_token_logprobs.restype = C.c_int
+        L.adapt_token_logprobs.argtypes = [P, I64, I64, I64, I32, F32, P, I32, P, P, P, P, P, P, P, P, I64, P]
+        L.adapt_token_logprobs_backward.restype = C.c_int
+        L.adapt_token_logprobs_backward.argtypes = [P, I64, I64, I64, I32, F32, P, P, P, P, P, P, I64, P]
+        L.adapt_gated_scan.restype = C.c_int
+        L.adapt_gated_scan.argtypes = [P, P, P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, P, P, SZ, P]
+        L.adapt_gated_scan_backward.restype = C.c_int
+        L.adapt_gated_scan_backward.argtypes = [P, P, P, P, P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, P,
+                                                P, SZ, P]
+        L.adapt_gated_scan_workspace_bytes.restype = SZ
+        L.adapt_gated_scan_workspace_bytes.argtypes = [I64, I64, I64, I32, I32, I32]
         _lib = L
     return _lib
 
@@ -655,3 +677,238 @@ def adapt_format_quantize(x: torch.Tensor, kind: int, a: int, b: int, round_mode
                                        out.data_ptr(), _stream_handle(stream)),
            "adapt_format_quantize")
     return out
+
+
+# ---- operators of a training step ---------------------------------------------------------
+
+_ELEM_DTYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
+
+
+def _elem(t: torch.Tensor) -> int:
+    d = _ELEM_DTYPES.get(t.dtype)
+    assert d is not None and t.is_cuda, "needs a CUDA tensor of float32, float16 or bfloat16"
+    return d
+
+
+def _on(stream):
+    """Context in which outputs and scratch are allocated: the stream that the kernels run on."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def adapt_dropout(x: torch.Tensor, p: float, seed: int = 0, layer: int = 0, index_base: int = 0,
+                  residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """adapt_dropout of adapt.h: dropout(x) (+ residual) with a mask made from (seed, layer, element
+    number), never stored; the gradient of x is the same call on dy.  ``out`` may be ``x`` or
+    ``residual`` (in place)."""
+    dtype = _elem(x)
+    if out is None:
+        with _on(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    parts = (x, out) if residual is None else (x, out, residual)
+    assert all(t.shape == x.shape and t.dtype == x.dtype and t.device == x.device for t in parts)
+    if all(t.is_contiguous() for t in parts):   # elements in order: one long row
+        rows, cols = 1, x.numel()
+        ldx = ldy = ldr = cols
+    else:
+        assert x.dim() == 2, "needs contiguous tensors, or matrices with unit inner stride"
+        rows, cols = x.shape
+        assert all(t.stride(1) == 1 or cols <= 1 for t in parts)
+        ldx, ldy, ldr = (t.stride(0) if rows > 1 else cols for t in (x, out, parts[-1]))
+    _check(lib().adapt_dropout(x.data_ptr(), _ptr(residual), out.data_ptr(), rows, cols, ldx, ldr, ldy, dtype,
+                               p, seed, layer, index_base, _stream_handle(stream)), "adapt_dropout")
+    return out
+
+
+class TokenLogprobs:
+    """Device outputs of adapt_token_logprobs (what was not asked for is None)."""
+
+    __slots__ = ("logprob", "entropy", "lse", "top_ids", "top_logprobs", "dlogits")
+
+    def __init__(self, logprob, entropy, lse, top_ids, top_logprobs, dlogits):
+        self.logprob, self.entropy, self.lse = logprob, entropy, lse
+        self.top_ids, self.top_logprobs, self.dlogits = top_ids, top_logprobs, dlogits
+
+
+def _logit_rows(t: torch.Tensor):
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "needs a matrix with unit inner stride"
+    rows, vocab = t.shape
+    return rows, vocab, t.stride(0) if rows > 1 else vocab
+
+
+def _per_row(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype):
+    assert t is None or (t.is_cuda and t.dtype == dtype and t.numel() == rows and t.is_contiguous())
+    return _ptr(t)
+
+
+def adapt_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, scale: float = 1.0,
+                         n_top: int = 0, want_entropy: bool = True,
+                         d_logprob: Optional[torch.Tensor] = None, d_entropy: Optional[torch.Tensor] = None,
+                         dlogits: Optional[torch.Tensor] = None, stream=None) -> TokenLogprobs:
+    """adapt_token_logprobs of adapt.h.  logits [rows, vocab]; targets int64 [rows], negative = none.
+    With weights ``d_logprob`` / ``d_entropy`` (float32 [rows]) the gradient comes out of the same call
+    (``dlogits`` defaults to a new tensor and may be ``logits``: in place)."""
+    dtype = _elem(logits)
+    rows, vocab, ld = _logit_rows(logits)
+    pt = _per_row(targets, rows, torch.int64)
+    pdl, pdh = _per_row(d_logprob, rows, torch.float32), _per_row(d_entropy, rows, torch.float32)
+    dev = logits.device
+    with _on(stream):
+        stats = torch.empty((3, rows), dtype=torch.float32, device=dev)
+        ids = torch.empty((rows, n_top), dtype=torch.int32, device=dev) if n_top else None
+        tops = torch.empty((rows, n_top), dtype=torch.float32, device=dev) if n_top else None
+        if dlogits is None and (d_logprob is not None or d_entropy is not None):
+            dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
+    ldg = 0
+    if dlogits is not None:
+        assert dlogits.shape == logits.shape and dlogits.dtype == logits.dtype and dlogits.device == dev
+        ldg = _logit_rows(dlogits)[2]
+    logprob, entropy, lse = stats.unbind(0)
+    if targets is None:
+        logprob = None
+    if not want_entropy:
+        entropy = None
+    _check(lib().adapt_token_logprobs(logits.data_ptr(), rows, vocab, ld, dtype, scale, pt, n_top, _ptr(logprob),
+                                      _ptr(entropy), lse.data_ptr(), _ptr(ids), _ptr(tops), pdl, pdh,
+                                      _ptr(dlogits), ldg, _stream_handle(stream)), "adapt_token_logprobs")
+    return TokenLogprobs(logprob, entropy, lse, ids, tops, dlogits)
+
+
+def adapt_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor,
+                                  d_logprob: Optional[torch.Tensor] = None,
+                                  entropy: Optional[torch.Tensor] = None,
+                                  d_entropy: Optional[torch.Tensor] = None, scale: float = 1.0,
+                                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """adapt_token_logprobs_backward of adapt.h: the gradient from lse and entropy as
+    adapt_token_logprobs returned them (``out`` may be ``logits``: in place)."""
+    dtype = _elem(logits)
+    rows, vocab, ld = _logit_rows(logits)
+    if out is None:
+        with _on(stream):
+            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    assert out.shape == logits.shape and out.dtype == logits.dtype and out.device == logits.device
+    f32 = torch.float32
+    _check(lib().adapt_token_logprobs_backward(
+        logits.data_ptr(), rows, vocab, ld, dtype, scale, _per_row(targets, rows, torch.int64),
+        _per_row(lse, rows, f32), _per_row(entropy, rows, f32), _per_row(d_logprob, rows, f32),
+        _per_row(d_entropy, rows, f32), out.data_ptr(), _logit_rows(out)[2], _stream_handle(stream)),
+        "adapt_token_logprobs_backward")
+    return out
+
+
+class ScanResult:
+    """Device outputs of adapt_gated_scan."""
+
+    __slots__ = ("y", "h_last", "carry")
+
+    def __init__(self, y, h_last, carry):
+        self.y, self.h_last, self.carry = y, h_last, carry
+
+
+class ScanGradients:
+    """Device outputs of adapt_gated_scan_backward."""
+
+    __slots__ = ("dx", "dgate", "dh0")
+
+    def __init__(self, dx, dgate, dh0):
+        self.dx, self.dgate, self.dh0 = dx, dgate, dh0
+
+
+def _scan_args(x, gate, lengths, reset):
+    dtype = _elem(x)
+    assert x.dim() == 3 and gate.dim() == 3 and gate.dtype == x.dtype and gate.device == x.device
+    batch, steps, channels = x.shape
+    gates = gate.shape[2]
+    assert gate.shape[0] == batch and gate.shape[1] == steps
+    assert channels == 0 or (gates > 0 and channels % gates == 0), "the gates have to divide the channels"
+    assert lengths is None or (lengths.is_cuda and lengths.dtype == torch.int32 and lengths.shape == (batch,)
+                               and lengths.is_contiguous())
+    assert reset is None or (reset.is_cuda and reset.dtype in (torch.uint8, torch.bool)
+                             and reset.shape == (batch, steps) and reset.is_contiguous())
+    return dtype, batch, steps, channels, channels // gates if gates else 1
+
+
+def _scan_strides(*tensors):
+    """None where every tensor is contiguous, else the {batch, step} strides of all."""
+    if all(t.is_contiguous() for t in tensors):
+        return None
+    s = []
+    for t in tensors:
+        assert t.stride(2) == 1 or t.shape[2] <= 1, "the channels need unit stride"
+        s += [t.stride(0) if t.shape[0] > 1 else max(t.stride(0), 0), t.stride(1)]
+    return (C.c_int64 * len(s))(*s)
+
+
+def _state(t: Optional[torch.Tensor], batch: int, channels: int):
+    assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.shape == (batch, channels)
+                         and t.is_contiguous())
+    return _ptr(t)
+
+
+def _scan_workspace(batch, steps, channels, group, dtype, backward, device):
+    n = lib().adapt_gated_scan_workspace_bytes(batch, steps, channels, group, dtype, backward)
+    return (torch.empty(n, dtype=torch.uint8, device=device), n) if n else (None, 0)
+
+
+def adapt_gated_scan_workspace_bytes(batch: int, steps: int, channels: int, gate_group: int = 1,
+                                     dtype: int = DTYPE_F32, backward: bool = False) -> int:
+    return int(lib().adapt_gated_scan_workspace_bytes(batch, steps, channels, gate_group, dtype,
+                                                      1 if backward else 0))
+
+
+def adapt_gated_scan(x: torch.Tensor, gate: torch.Tensor, h0: Optional[torch.Tensor] = None,
+                     lengths: Optional[torch.Tensor] = None, reset: Optional[torch.Tensor] = None,
+                     mode: int = GATE_SIGMOID, want_carry: bool = False, y: Optional[torch.Tensor] = None,
+                     h_last: Optional[torch.Tensor] = None, stream=None) -> ScanResult:
+    """adapt_gated_scan of adapt.h.  x [batch, steps, channels], gate [batch, steps, gates] with
+    channels a multiple of gates; states float32 [batch, channels].  ``y`` may be ``x`` and ``h_last``
+    may be ``h0`` (in place).  ``want_carry`` keeps what adapt_gated_scan_backward starts from."""
+    dtype, batch, steps, channels, group = _scan_args(x, gate, lengths, reset)
+    dev = x.device
+    with _on(stream):
+        if y is None:
+            y = torch.empty((batch, steps, channels), dtype=x.dtype, device=dev)
+        if h_last is None:
+            h_last = torch.empty((batch, channels), dtype=torch.float32, device=dev)
+        carry = torch.empty((batch, -(-steps // SCAN_TILE), channels), dtype=torch.float32,
+                            device=dev) if want_carry else None
+        ws, n = _scan_workspace(batch, steps, channels, group, dtype, 0, dev)
+    assert y.shape == x.shape and y.dtype == x.dtype and y.device == dev
+    _check(lib().adapt_gated_scan(x.data_ptr(), gate.data_ptr(), _state(h0, batch, channels), _ptr(lengths),
+                                  _ptr(reset), batch, steps, channels, group, dtype, mode,
+                                  _scan_strides(x, gate, y), y.data_ptr(), _state(h_last, batch, channels),
+                                  _ptr(carry), _ptr(ws), n, _stream_handle(stream)), "adapt_gated_scan")
+    return ScanResult(y, h_last, carry)
+
+
+def adapt_gated_scan_backward(x: torch.Tensor, gate: torch.Tensor, dy: torch.Tensor, carry: torch.Tensor,
+                              dh_last: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                              reset: Optional[torch.Tensor] = None, mode: int = GATE_SIGMOID,
+                              want_dh0: bool = False, dx: Optional[torch.Tensor] = None,
+                              dgate: Optional[torch.Tensor] = None, stream=None) -> ScanGradients:
+    """adapt_gated_scan_backward of adapt.h; ``carry`` from adapt_gated_scan on the same inputs.
+    ``dx`` may be ``dy`` (in place)."""
+    dtype, batch, steps, channels, group = _scan_args(x, gate, lengths, reset)
+    dev = x.device
+    assert dy.shape == x.shape and dy.dtype == x.dtype and dy.device == dev
+    assert carry.is_cuda and carry.dtype == torch.float32 and carry.is_contiguous()
+    assert carry.shape == (batch, -(-steps // SCAN_TILE), channels)
+    with _on(stream):
+        if dx is None:
+            dx = torch.empty((batch, steps, channels), dtype=x.dtype, device=dev)
+        if dgate is None:
+            dgate = torch.empty(gate.shape, dtype=x.dtype, device=dev)
+        dh0 = torch.empty((batch, channels), dtype=torch.float32, device=dev) if want_dh0 else None
+        ws, n = _scan_workspace(batch, steps, channels, group, dtype, 1, dev)
+    assert dx.shape == x.shape and dx.dtype == x.dtype and dgate.shape == gate.shape and dgate.dtype == x.dtype
+    _check(lib().adapt_gated_scan_backward(x.data_ptr(), gate.data_ptr(), dy.data_ptr(), carry.data_ptr(),
+                                           _state(dh_last, batch, channels), _ptr(lengths), _ptr(reset), batch,
+                                           steps, channels, group, dtype, mode,
+                                           _scan_strides(x, gate, dy, dx, dgate), dx.data_ptr(),
+                                           dgate.data_ptr(), _ptr(dh0), _ptr(ws), n, _stream_handle(stream)),
+           "adapt_gated_scan_backward")
+    return ScanGradients(dx, dgate, dh0)

@@ -1,0 +1,281 @@
+// C-ABI entry points of the training-step operators: dropout, token log probabilities, gated
+// recurrence.  Declarations and argument contracts live in adapt.h.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/adapt.h"
+#include "host.cuh"
+#include "k_dropout.cuh"
+#include "k_logprobs.cuh"
+#include "k_scan.cuh"
+
+namespace {
+
+using namespace adapt;
+
+static_assert(ADAPT_SCAN_TILE == kScanTile && ADAPT_MAX_TOP == kMaxTop && ADAPT_GATE_SIGMOID == kGateSigmoid &&
+              ADAPT_GATE_VALUE == kGateValue, "the kernels use the constants of the C interface");
+
+// Bytes of an element, 0 for an unknown type.
+int elem_bytes(int dtype) {
+  return dtype == ADAPT_DTYPE_F32 ? 4 : (dtype == ADAPT_DTYPE_F16 || dtype == ADAPT_DTYPE_BF16) ? 2 : 0;
+}
+
+bool misaligned(const void* p, int bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) != 0;
+}
+
+// Calls f(T{}) with the element type.
+template <typename F>
+void with_type(int dtype, F f) {
+  if (dtype == ADAPT_DTYPE_F32) f(float{});
+  else if (dtype == ADAPT_DTYPE_F16) f(__half{});
+  else f(__nv_bfloat16{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, int64_t cols, int64_t ldx,
+                  int64_t ldr, int64_t ldy, int dtype, double p, uint64_t seed, int32_t layer,
+                  uint64_t index_base, void* stream_handle) {
+  const int e = elem_bytes(dtype);
+  if (!e || rows < 0 || cols < 0 || !(p >= 0.0 && p <= 1.0)) return ADAPT_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return ADAPT_OK;
+  if (!x || !y || misaligned(x, e) || misaligned(y, e) || misaligned(residual, e)) return ADAPT_ERR_INVALID_ARG;
+  if (rows > (1ll << 48) / cols) return ADAPT_ERR_INVALID_ARG;
+  if (rows > 1 && (ldx < cols || ldy < cols || (residual && ldr < cols))) return ADAPT_ERR_INVALID_ARG;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceCache* dc = nullptr;
+  const int rc = current_cache(&dc);
+  if (rc != ADAPT_OK) return rc;
+  DropoutParams q;
+  q.x = x; q.r = residual; q.y = y;
+  q.rows = rows; q.cols = cols; q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
+  q.base = seed ^ 0xA54FF53A5F1D36F1ull ^ ((static_cast<uint64_t>(static_cast<int64_t>(layer)) + 1ull) * 0x9E3779B97F4A7C15ull);
+  q.index_base = index_base;
+  q.threshold = static_cast<unsigned long long>(std::nearbyint(p * 4294967296.0));
+  q.scale = p < 1.0 ? static_cast<float>(1.0 / (1.0 - p)) : 0.0f;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
+  const int grid = static_cast<int>(std::min<long long>((rows * cols + 255) / 256, 16ll * dc->sm_count));
+  LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
+  with_type(dtype, [&](auto t) { dropout_kernel<decltype(t)><<<grid, 256, 0, stream>>>(q); });
+  ADAPT_LAUNCH_OK("dropout");
+  return ADAPT_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+int run_logprobs(LogprobParams& q, int dtype, void* stream_handle) {
+  const int e = elem_bytes(dtype);
+  if (!e || q.rows < 0 || q.rows > 0x7FFFFFFF || q.vocab < 1 || !(q.scale > 0.0f) || !std::isfinite(q.scale))
+    return ADAPT_ERR_INVALID_ARG;
+  if (q.rows == 0) return ADAPT_OK;
+  if (!q.logits || misaligned(q.logits, e) || misaligned(q.dlogits, e)) return ADAPT_ERR_INVALID_ARG;
+  if (q.rows > 1 && (q.ld < q.vocab || (q.dlogits && q.ld_grad < q.vocab))) return ADAPT_ERR_INVALID_ARG;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
+  LaunchScope ls(ADAPT_KERNEL_LOGPROBS, stream);
+  with_type(dtype, [&](auto t) {
+    logprob_kernel<decltype(t)><<<static_cast<unsigned>(q.rows), kRowThreads, 0, stream>>>(q);
+  });
+  ADAPT_LAUNCH_OK("token log probabilities");
+  return ADAPT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adapt_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype, float scale,
+                         const int64_t* targets, int n_top, float* logprob_out, float* entropy_out,
+                         float* lse_out, int32_t* top_ids_out, float* top_logprobs_out,
+                         const float* d_logprob, const float* d_entropy, void* dlogits_out,
+                         int64_t ld_grad, void* stream) {
+  if (vocab < 1 || vocab > 0x7FFFFFFF || n_top < 0 || n_top > kMaxTop || n_top > vocab) return ADAPT_ERR_INVALID_ARG;
+  if (n_top > 0 && (!top_ids_out || !top_logprobs_out)) return ADAPT_ERR_INVALID_ARG;
+  if (!targets && (logprob_out || d_logprob)) return ADAPT_ERR_INVALID_ARG;
+  if ((dlogits_out != nullptr) != (d_logprob || d_entropy)) return ADAPT_ERR_INVALID_ARG;
+  if (misaligned(targets, 8) || misaligned(logprob_out, 4) || misaligned(entropy_out, 4) || misaligned(lse_out, 4) ||
+      misaligned(top_ids_out, 4) || misaligned(top_logprobs_out, 4) || misaligned(d_logprob, 4) || misaligned(d_entropy, 4))
+    return ADAPT_ERR_INVALID_ARG;
+  LogprobParams q = {};
+  q.logits = logits; q.rows = rows; q.ld = ld; q.ld_grad = ld_grad; q.vocab = static_cast<int>(vocab);
+  q.n_top = n_top; q.scale = scale; q.targets = reinterpret_cast<const long long*>(targets);
+  q.logprob = logprob_out; q.entropy = entropy_out; q.lse = lse_out;
+  q.top_ids = top_ids_out; q.top_logprobs = top_logprobs_out;
+  q.d_logprob = d_logprob; q.d_entropy = d_entropy; q.dlogits = dlogits_out;
+  return run_logprobs(q, dtype, stream);
+}
+
+int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t vocab, int64_t ld, int dtype,
+                                  float scale, const int64_t* targets, const float* lse,
+                                  const float* entropy, const float* d_logprob, const float* d_entropy,
+                                  void* dlogits_out, int64_t ld_grad, void* stream) {
+  if (vocab < 1 || vocab > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
+  if (!d_logprob && !d_entropy) return ADAPT_ERR_INVALID_ARG;
+  if ((d_logprob && !targets) || (d_entropy && !entropy)) return ADAPT_ERR_INVALID_ARG;
+  if (rows > 0 && (!lse || !dlogits_out)) return ADAPT_ERR_INVALID_ARG;
+  if (misaligned(targets, 8) || misaligned(lse, 4) || misaligned(entropy, 4) || misaligned(d_logprob, 4) || misaligned(d_entropy, 4))
+    return ADAPT_ERR_INVALID_ARG;
+  LogprobParams q = {};
+  q.logits = logits; q.rows = rows; q.ld = ld; q.ld_grad = ld_grad; q.vocab = static_cast<int>(vocab);
+  q.scale = scale; q.targets = reinterpret_cast<const long long*>(targets);
+  q.lse_in = lse; q.entropy_in = entropy; q.d_logprob = d_logprob; q.d_entropy = d_entropy; q.dlogits = dlogits_out;
+  return run_logprobs(q, dtype, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// Checks what forward and backward share.  Fills sizes; strides are set by the caller.
+bool scan_shape(ScanParams& q, int64_t batch, int64_t steps, int64_t channels, int group, int dtype, int mode) {
+  if (!elem_bytes(dtype) || (mode != ADAPT_GATE_SIGMOID && mode != ADAPT_GATE_VALUE)) return false;
+  if (batch < 0 || steps < 0 || channels < 0) return false;
+  if (steps > 0x7FFFFF00 || channels > 0x7FFFFFFF || batch > 0x7FFFFFFF) return false;
+  if (batch > 0 && channels > 0 && batch > (1ll << 40) / channels) return false;
+  // a gate of its own, or shared by a power of two of channels up to 64, or by a multiple of 64
+  const bool ok = group >= 1 && (group <= 64 ? (group & (group - 1)) == 0 : group % 64 == 0);
+  if (!ok || channels % group != 0) return false;
+  q.batch = batch; q.steps = steps; q.channels = channels; q.group = group;
+  return true;
+}
+
+// Stride pair: given, or that of a contiguous [batch][steps][width] array.
+void stride_pair(const int64_t* given, int k, int64_t steps, int64_t width, long long& b, long long& t) {
+  b = given ? given[2 * k] : steps * width;
+  t = given ? given[2 * k + 1] : width;
+}
+
+// Rows that are written must not overlap.
+bool out_strides_ok(long long b, long long t, const ScanParams& q, int64_t width) {
+  if (b < 0 || t < 0) return false;
+  if (q.steps > 1 && t < width) return false;
+  if (q.batch > 1 && b < width) return false;
+  if (q.steps > 1 && q.batch > 1 && b < t * q.steps && t < b * q.batch) return false;
+  return true;
+}
+
+size_t scan_workspace(const ScanParams& q, bool backward) {
+  if (!backward || q.group == 1) return 0;
+  return sizeof(float) * static_cast<size_t>(q.batch) * q.steps * q.channels;
+}
+
+// The caller's workspace, or the library's (grown on demand).
+int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, char** out) {
+  *out = nullptr;
+  if (need == 0) return ADAPT_OK;
+  if (workspace) {
+    if (have < need) return ADAPT_ERR_WORKSPACE;
+    if (misaligned(workspace, 256)) return ADAPT_ERR_INVALID_ARG;
+    *out = static_cast<char*>(workspace);
+    return ADAPT_OK;
+  }
+  const int rc = grow_device(&dc.scan_buf, &dc.scan_buf_bytes, align_up(need, 4096));
+  *out = static_cast<char*>(dc.scan_buf);
+  return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t adapt_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels, int gate_group,
+                                        int dtype, int backward) {
+  ScanParams q = {};
+  if (!scan_shape(q, batch, steps, channels, gate_group, dtype, ADAPT_GATE_SIGMOID)) return 0;
+  return scan_workspace(q, backward != 0);
+}
+
+int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int32_t* lengths,
+                     const uint8_t* reset, int64_t batch, int64_t steps, int64_t channels,
+                     int gate_group, int dtype, int mode, const int64_t* strides, void* y,
+                     float* h_last, float* carry_out, void* workspace, size_t workspace_bytes,
+                     void* stream_handle) {
+  ScanParams q = {};
+  if (!scan_shape(q, batch, steps, channels, gate_group, dtype, mode)) return ADAPT_ERR_INVALID_ARG;
+  if (batch == 0 || channels == 0) return ADAPT_OK;
+  const int e = elem_bytes(dtype);
+  if (steps > 0 && (!x || !gate || !y)) return ADAPT_ERR_INVALID_ARG;
+  if (misaligned(x, e) || misaligned(gate, e) || misaligned(y, e) || misaligned(h0, 4) || misaligned(h_last, 4) ||
+      misaligned(carry_out, 4) || misaligned(lengths, 4))
+    return ADAPT_ERR_INVALID_ARG;
+  stride_pair(strides, 0, steps, channels, q.xb, q.xt);
+  stride_pair(strides, 1, steps, channels / gate_group, q.gb, q.gt);
+  stride_pair(strides, 2, steps, channels, q.yb, q.yt);
+  if (q.xb < 0 || q.xt < 0 || q.gb < 0 || q.gt < 0 || !out_strides_ok(q.yb, q.yt, q, channels)) return ADAPT_ERR_INVALID_ARG;
+  q.x = x; q.gate = gate; q.h0 = h0; q.lengths = lengths; q.reset = reset; q.y = y; q.h_last = h_last; q.carry = carry_out;
+  (void)workspace; (void)workspace_bytes;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
+  const unsigned grid = static_cast<unsigned>((batch * channels + 127) / 128);
+  LaunchScope ls(ADAPT_KERNEL_SCAN, stream);
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (mode == ADAPT_GATE_SIGMOID) scan_serial_kernel<T, kGateSigmoid><<<grid, 128, 0, stream>>>(q);
+    else scan_serial_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
+  });
+  ADAPT_LAUNCH_OK("gated scan");
+  return ADAPT_OK;
+}
+
+int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy, const float* carry,
+                              const float* dh_last, const int32_t* lengths, const uint8_t* reset,
+                              int64_t batch, int64_t steps, int64_t channels, int gate_group,
+                              int dtype, int mode, const int64_t* strides, void* dx, void* dgate,
+                              float* dh0, void* workspace, size_t workspace_bytes,
+                              void* stream_handle) {
+  ScanParams q = {};
+  if (!scan_shape(q, batch, steps, channels, gate_group, dtype, mode)) return ADAPT_ERR_INVALID_ARG;
+  if (batch == 0 || channels == 0) return ADAPT_OK;
+  const int e = elem_bytes(dtype);
+  if (steps > 0 && (!x || !gate || !dy || !carry || !dx || !dgate)) return ADAPT_ERR_INVALID_ARG;
+  if (misaligned(x, e) || misaligned(gate, e) || misaligned(dy, e) || misaligned(dx, e) || misaligned(dgate, e) ||
+      misaligned(carry, 4) || misaligned(dh_last, 4) || misaligned(dh0, 4) || misaligned(lengths, 4))
+    return ADAPT_ERR_INVALID_ARG;
+  stride_pair(strides, 0, steps, channels, q.xb, q.xt);
+  stride_pair(strides, 1, steps, channels / gate_group, q.gb, q.gt);
+  stride_pair(strides, 2, steps, channels, q.yb, q.yt);
+  stride_pair(strides, 3, steps, channels, q.dxb, q.dxt);
+  stride_pair(strides, 4, steps, channels / gate_group, q.dgb, q.dgt);
+  if (q.xb < 0 || q.xt < 0 || q.gb < 0 || q.gt < 0 || q.yb < 0 || q.yt < 0 ||
+      !out_strides_ok(q.dxb, q.dxt, q, channels) || !out_strides_ok(q.dgb, q.dgt, q, channels / gate_group))
+    return ADAPT_ERR_INVALID_ARG;
+  q.x = x; q.gate = gate; q.dy = dy; q.carry = const_cast<float*>(carry); q.dh_last = dh_last;
+  q.lengths = lengths; q.reset = reset; q.dx = dx; q.dgate = dgate; q.dh0 = dh0;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceCache* dc = nullptr;
+  int rc = current_cache(&dc);
+  if (rc != ADAPT_OK) return rc;
+  char* scratch = nullptr;
+  rc = scan_scratch(*dc, workspace, workspace_bytes, scan_workspace(q, true), &scratch);
+  if (rc != ADAPT_OK) return rc;
+  q.partial = reinterpret_cast<float*>(scratch);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
+  const unsigned grid = static_cast<unsigned>((batch * channels + 127) / 128);
+  {
+    LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      if (mode == ADAPT_GATE_SIGMOID) scan_serial_backward_kernel<T, kGateSigmoid><<<grid, 128, 0, stream>>>(q);
+      else scan_serial_backward_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
+    });
+    ADAPT_LAUNCH_OK("gated scan, backward");
+  }
+  if (q.partial && steps > 0) {
+    const long long n = batch * steps * (channels / gate_group);
+    LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
+    with_type(dtype, [&](auto t) {
+      scan_gate_sum_kernel<decltype(t)><<<static_cast<int>(std::min<long long>((n + 255) / 256, 16ll * dc->sm_count)), 256, 0, stream>>>(q);
+    });
+    ADAPT_LAUNCH_OK("gate gradient sum");
+  }
+  return ADAPT_OK;
+}
+
+}  // extern "C"
