@@ -593,9 +593,9 @@ int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t voca
  *   workspace  DEVICE scratch of adapt_gated_scan_workspace_bytes, 256-byte aligned, or NULL
  *            to use a library-owned buffer that grows on demand: calls without a workspace
  *            of their own must not overlap on the device
- * Limits: steps <= 2^31 - 256, channels and batch < 2^31, batch * channels <= 2^40. */
+ * Limits: steps <= 2^31 - 256, channels and batch < 2^31, batch * ceil(channels / 64) <= 2^27. */
 enum { ADAPT_GATE_SIGMOID = 0, ADAPT_GATE_VALUE = 1 };
-#define ADAPT_SCAN_TILE 128
+#define ADAPT_SCAN_TILE 64
 
 int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int32_t* lengths,
                      const uint8_t* reset, int64_t batch, int64_t steps, int64_t channels,

@@ -48,7 +48,7 @@ KERNEL_KINDS = ("range", "range_finalize", "search", "kld", "select", "quantize"
 DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 MAX_TOP = 32
 GATE_SIGMOID, GATE_VALUE = 0, 1
-SCAN_TILE = 128
+SCAN_TILE = 64
 ALGO_AUTO, ALGO_KEYED, ALGO_DIRECT = 0, 1, 2
 
 

@@ -5,6 +5,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
+#include <vector>
 
 #include "../../include/adapt.h"
 #include "host.cuh"
@@ -139,7 +141,7 @@ bool scan_shape(ScanParams& q, int64_t batch, int64_t steps, int64_t channels, i
   if (!elem_bytes(dtype) || (mode != ADAPT_GATE_SIGMOID && mode != ADAPT_GATE_VALUE)) return false;
   if (batch < 0 || steps < 0 || channels < 0) return false;
   if (steps > 0x7FFFFF00 || channels > 0x7FFFFFFF || batch > 0x7FFFFFFF) return false;
-  if (batch > 0 && channels > 0 && batch > (1ll << 40) / channels) return false;
+  if (batch > 0 && channels > 0 && batch > (1ll << 27) / ((channels + kScanChannels - 1) / kScanChannels)) return false;
   // a gate of its own, or shared by a power of two of channels up to 64, or by a multiple of 64
   const bool ok = group >= 1 && (group <= 64 ? (group & (group - 1)) == 0 : group % 64 == 0);
   if (!ok || channels % group != 0) return false;
@@ -163,9 +165,79 @@ bool out_strides_ok(long long b, long long t, const ScanParams& q, int64_t width
 }
 
 size_t scan_workspace(const ScanParams& q, bool backward) {
-  if (!backward || q.group == 1) return 0;
-  return sizeof(float) * static_cast<size_t>(q.batch) * q.steps * q.channels;
+  if (!backward || q.group <= kScanChannels) return 0;
+  return sizeof(float) * static_cast<size_t>(q.batch) * q.steps * (q.channels / kScanChannels);
 }
+
+// Whether two channels can be moved at a time.
+bool scan_pairs(const ScanParams& q, int elem, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
+  if (q.channels & 1) return false;
+  for (const void* p : ptrs) if (misaligned(p, 2 * elem)) return false;
+  for (long long s : strides) if (s & 1) return false;
+  return true;
+}
+
+// CTAs of a tile kernel that the device holds at once, by kernel (first use: attributes and occupancy).
+struct ScanSlots { const void* kernel; int device, slots; };
+std::vector<ScanSlots> g_scan_slots;   // under g_mutex
+
+int scan_slots(DeviceCache& dc, const void* kernel, size_t smem, int* out) {
+  int dev = 0;
+  ADAPT_CUDA(cudaGetDevice(&dev));
+  for (const ScanSlots& s : g_scan_slots)
+    if (s.kernel == kernel && s.device == dev) { *out = s.slots; return ADAPT_OK; }
+  ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  static_cast<int>(smem + scan_totals_bytes(kScanMaxCluster))));
+  ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  int per_sm = 0;
+  ADAPT_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kScanThreads, smem + scan_totals_bytes(4)));
+  const int slots = std::max(1, per_sm) * dc.sm_count;
+  g_scan_slots.push_back({kernel, dev, slots});
+  *out = slots;
+  return ADAPT_OK;
+}
+
+// CTAs that share a chain.  The time goes with the waves of CTAs over their number per chain, and an
+// exchange costs a few per cent more for every doubling.
+int scan_cluster(long long chains, long long tiles, int slots) {
+  int best = 1;
+  double least = 1e300;
+  for (int k = 1, doublings = 0; k <= kScanMaxCluster; k *= 2, ++doublings) {
+    if (k > 1 && k / 2 >= tiles) break;
+    const long long ctas = chains * k;
+    const double cost = static_cast<double>((ctas + slots - 1) / slots) / k * (1.0 + 0.04 * doublings);
+    if (cost < least) { least = cost; best = k; }
+  }
+  return best;
+}
+
+int launch_scan(DeviceCache& dc, void (*kernel)(ScanParams), int tensors, int elem, const ScanParams& q, cudaStream_t stream) {
+  const size_t stages = kScanStages * scan_stage_bytes(tensors, elem);
+  int slots = 0;
+  const int rc = scan_slots(dc, reinterpret_cast<const void*>(kernel), stages, &slots);
+  if (rc != ADAPT_OK) return rc;
+  const long long chains = q.batch * ((q.channels + kScanChannels - 1) / kScanChannels);
+  const long long tiles = (q.steps + kScanTile - 1) / kScanTile;
+  const int cluster = scan_cluster(chains, tiles, slots);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(chains * cluster));
+  cfg.blockDim = dim3(kScanThreads);
+  cfg.dynamicSmemBytes = stages + scan_totals_bytes(cluster);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kernel, q));
+  return ADAPT_OK;
+}
+
+// Calls f(kernel) with the scan kernel of these types.
+#define ADAPT_SCAN_KERNEL(name, T, mode, pairs)                                                     \
+  ((mode) == ADAPT_GATE_SIGMOID ? ((pairs) ? name<T, kGateSigmoid, true> : name<T, kGateSigmoid, false>) \
+                                : ((pairs) ? name<T, kGateValue, true> : name<T, kGateValue, false>))
+constexpr long long kSerialSteps = 4;
 
 // The caller's workspace, or the library's (grown on demand).
 int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, char** out) {
@@ -211,15 +283,29 @@ int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int
   stride_pair(strides, 2, steps, channels, q.yb, q.yt);
   if (q.xb < 0 || q.xt < 0 || q.gb < 0 || q.gt < 0 || !out_strides_ok(q.yb, q.yt, q, channels)) return ADAPT_ERR_INVALID_ARG;
   q.x = x; q.gate = gate; q.h0 = h0; q.lengths = lengths; q.reset = reset; q.y = y; q.h_last = h_last; q.carry = carry_out;
-  (void)workspace; (void)workspace_bytes;
+  (void)workspace; (void)workspace_bytes;   // the tiles meet in shared memory
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  const unsigned grid = static_cast<unsigned>((batch * channels + 127) / 128);
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceCache* dc = nullptr;
+  int rc = current_cache(&dc);
+  if (rc != ADAPT_OK) return rc;
   LaunchScope ls(ADAPT_KERNEL_SCAN, stream);
-  with_type(dtype, [&](auto t) {
-    using T = decltype(t);
-    if (mode == ADAPT_GATE_SIGMOID) scan_serial_kernel<T, kGateSigmoid><<<grid, 128, 0, stream>>>(q);
-    else scan_serial_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
-  });
+  if (steps <= kSerialSteps) {
+    const unsigned grid = static_cast<unsigned>((batch * channels + 127) / 128);
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      if (mode == ADAPT_GATE_SIGMOID) scan_serial_kernel<T, kGateSigmoid><<<grid, 128, 0, stream>>>(q);
+      else scan_serial_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
+    });
+  } else {
+    const bool pairs = scan_pairs(q, e, {x, y, gate_group == 1 ? gate : nullptr},
+                                  {q.xb, q.xt, q.yb, q.yt, gate_group == 1 ? q.gb : 0, gate_group == 1 ? q.gt : 0});
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      rc = launch_scan(*dc, ADAPT_SCAN_KERNEL(scan_kernel, T, mode, pairs), 2, e, q, stream);
+    });
+    if (rc != ADAPT_OK) return rc;
+  }
   ADAPT_LAUNCH_OK("gated scan");
   return ADAPT_OK;
 }
@@ -257,14 +343,17 @@ int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy, c
   if (rc != ADAPT_OK) return rc;
   q.partial = reinterpret_cast<float*>(scratch);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  const unsigned grid = static_cast<unsigned>((batch * channels + 127) / 128);
   {
     LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
+    const bool own = gate_group == 1;
+    const bool pairs = scan_pairs(q, e, {x, dy, dx, own ? gate : nullptr, own ? dgate : nullptr},
+                                  {q.xb, q.xt, q.yb, q.yt, q.dxb, q.dxt, own ? q.gb : 0, own ? q.gt : 0,
+                                   own ? q.dgb : 0, own ? q.dgt : 0});
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      if (mode == ADAPT_GATE_SIGMOID) scan_serial_backward_kernel<T, kGateSigmoid><<<grid, 128, 0, stream>>>(q);
-      else scan_serial_backward_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
+      rc = launch_scan(*dc, ADAPT_SCAN_KERNEL(scan_backward_kernel, T, mode, pairs), 3, e, q, stream);
     });
+    if (rc != ADAPT_OK) return rc;
     ADAPT_LAUNCH_OK("gated scan, backward");
   }
   if (q.partial && steps > 0) {
