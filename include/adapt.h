@@ -593,7 +593,7 @@ int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t voca
  *   workspace  DEVICE scratch of adapt_gated_scan_workspace_bytes, 256-byte aligned, or NULL
  *            to use a library-owned buffer that grows on demand: calls without a workspace
  *            of their own must not overlap on the device
- * Limits: steps <= 2^31 - 256, channels and batch < 2^31, batch * ceil(channels / 64) <= 2^27. */
+ * Limits: steps <= 2^31 - 8192, channels and batch < 2^31, batch * ceil(channels / 64) <= 2^27. */
 enum { ADAPT_GATE_SIGMOID = 0, ADAPT_GATE_VALUE = 1 };
 #define ADAPT_SCAN_TILE 64
 

@@ -140,7 +140,7 @@ namespace {
 bool scan_shape(ScanParams& q, int64_t batch, int64_t steps, int64_t channels, int group, int dtype, int mode) {
   if (!elem_bytes(dtype) || (mode != ADAPT_GATE_SIGMOID && mode != ADAPT_GATE_VALUE)) return false;
   if (batch < 0 || steps < 0 || channels < 0) return false;
-  if (steps > 0x7FFFFF00 || channels > 0x7FFFFFFF || batch > 0x7FFFFFFF) return false;
+  if (steps > 0x7FFFE000 || channels > 0x7FFFFFFF || batch > 0x7FFFFFFF) return false;
   if (batch > 0 && channels > 0 && batch > (1ll << 27) / ((channels + kScanChannels - 1) / kScanChannels)) return false;
   // a gate of its own, or shared by a power of two of channels up to 64, or by a multiple of 64
   const bool ok = group >= 1 && (group <= 64 ? (group & (group - 1)) == 0 : group % 64 == 0);
@@ -169,74 +169,91 @@ size_t scan_workspace(const ScanParams& q, bool backward) {
   return sizeof(float) * static_cast<size_t>(q.batch) * q.steps * (q.channels / kScanChannels);
 }
 
-// Whether two channels can be moved at a time.
-bool scan_pairs(const ScanParams& q, int elem, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
-  if (q.channels & 1) return false;
-  for (const void* p : ptrs) if (misaligned(p, 2 * elem)) return false;
-  for (long long s : strides) if (s & 1) return false;
-  return true;
+// How many channels can be moved at a time: those of 16 bytes, two, or one.
+int scan_move(const ScanParams& q, int elem, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
+  int unit = 16 / elem;
+  auto fits = [&](int u) {
+    if (q.channels % u) return false;
+    for (const void* p : ptrs) if (misaligned(p, u * elem)) return false;
+    for (long long s : strides) if (s % u) return false;
+    return true;
+  };
+  return fits(unit) ? kMoveVec : fits(2) ? kMovePair : kMoveOne;
 }
 
 // CTAs of a tile kernel that the device holds at once, by kernel (first use: attributes and occupancy).
 struct ScanSlots { const void* kernel; int device, slots; };
 std::vector<ScanSlots> g_scan_slots;   // under g_mutex
 
-int scan_slots(DeviceCache& dc, const void* kernel, size_t smem, int* out) {
+int scan_slots(DeviceCache& dc, const void* kernel, size_t smem, int channels, int* out) {
   int dev = 0;
   ADAPT_CUDA(cudaGetDevice(&dev));
   for (const ScanSlots& s : g_scan_slots)
     if (s.kernel == kernel && s.device == dev) { *out = s.slots; return ADAPT_OK; }
   ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  static_cast<int>(smem + scan_totals_bytes(kScanMaxCluster))));
+                                  static_cast<int>(smem + scan_totals_bytes(kScanMaxCluster, channels))));
   ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   int per_sm = 0;
-  ADAPT_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kScanThreads, smem + scan_totals_bytes(4)));
+  ADAPT_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kScanThreads, smem + scan_totals_bytes(4, channels)));
   const int slots = std::max(1, per_sm) * dc.sm_count;
   g_scan_slots.push_back({kernel, dev, slots});
   *out = slots;
   return ADAPT_OK;
 }
 
-// CTAs that share a chain.  The time goes with the waves of CTAs over their number per chain, and an
-// exchange costs a few per cent more for every doubling.
-int scan_cluster(long long chains, long long tiles, int slots) {
-  int best = 1;
-  double least = 1e300;
-  for (int k = 1, doublings = 0; k <= kScanMaxCluster; k *= 2, ++doublings) {
-    if (k > 1 && k / 2 >= tiles) break;
-    const long long ctas = chains * k;
-    const double cost = static_cast<double>((ctas + slots - 1) / slots) / k * (1.0 + 0.04 * doublings);
-    if (cost < least) { least = cost; best = k; }
-  }
-  return best;
-}
+typedef void (*ScanKernel)(ScanParams);
 
-int launch_scan(DeviceCache& dc, void (*kernel)(ScanParams), int tensors, int elem, const ScanParams& q, cudaStream_t stream) {
+// The tile kernels of one type, mode and alignment, for 64, 32 and 16 channels a CTA, and the number of
+// CTAs to a chain, by the estimated time: waves of CTAs x rounds of a chain x the time of a round, in units
+// of a round without exchange (1.4 to 2.5 us).  An exchange costs 1.2 + 0.05 K of them, narrower tiles
+// 20 % a halving (more pieces to join).  Measured forward, us: 8 x 4096 x 2048 bf16 (256 chains of 64)
+// 93 with one CTA to a chain, 124 with two; 1 x 65536 x 1024 bf16 (16 chains of 64, 32 of 32) 1174 with one,
+// 220 with 16, 169 with 32 channels and 8 CTAs; over ten shapes both ways the choice is within 2 % of the best.
+int launch_scan(DeviceCache& dc, const ScanKernel (&kernels)[3], int tensors, int elem, const ScanParams& q, cudaStream_t stream) {
   const size_t stages = kScanStages * scan_stage_bytes(tensors, elem);
-  int slots = 0;
-  const int rc = scan_slots(dc, reinterpret_cast<const void*>(kernel), stages, &slots);
-  if (rc != ADAPT_OK) return rc;
-  const long long chains = q.batch * ((q.channels + kScanChannels - 1) / kScanChannels);
-  const long long tiles = (q.steps + kScanTile - 1) / kScanTile;
-  const int cluster = scan_cluster(chains, tiles, slots);
+  int width = 0, cluster = 1;
+  double least = 1e300;
+  for (int i = 0; i < 3; ++i) {
+    const int channels = kScanChannels >> i;
+    if (i && q.group > channels) break;   // a shared gate stays in one CTA
+    int slots = 0;
+    const int rc = scan_slots(dc, reinterpret_cast<const void*>(kernels[i]), stages, channels, &slots);
+    if (rc != ADAPT_OK) return rc;
+    const long long chains = q.batch * ((q.channels + channels - 1) / channels);
+    const long long tiles = (q.steps * channels + kTileElements - 1) / kTileElements;
+    for (int k = 1; k <= kScanMaxCluster; k *= 2) {
+      if (k > 1 && k / 2 >= tiles) break;
+      const double waves = static_cast<double>((chains * k + slots - 1) / slots);
+      const double rounds = static_cast<double>((tiles + k - 1) / k);
+      const double cost = waves * rounds * (k > 1 ? 1.2 + 0.05 * k : 1.0) * (1.0 + 0.2 * i);
+      if (cost < least) { least = cost; width = i; cluster = k; }
+    }
+  }
+  const int channels = kScanChannels >> width;
+  const long long chains = q.batch * ((q.channels + channels - 1) / channels);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(chains * cluster));
   cfg.blockDim = dim3(kScanThreads);
-  cfg.dynamicSmemBytes = stages + scan_totals_bytes(cluster);
+  cfg.dynamicSmemBytes = stages + scan_totals_bytes(cluster, channels);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kernel, q));
+  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kernels[width], q));
   return ADAPT_OK;
 }
 
-// Calls f(kernel) with the scan kernel of these types.
-#define ADAPT_SCAN_KERNEL(name, T, mode, pairs)                                                     \
-  ((mode) == ADAPT_GATE_SIGMOID ? ((pairs) ? name<T, kGateSigmoid, true> : name<T, kGateSigmoid, false>) \
-                                : ((pairs) ? name<T, kGateValue, true> : name<T, kGateValue, false>))
+#define ADAPT_SCAN_WIDTHS(name, T, mode, move) {name<T, mode, move, 32>, name<T, mode, move, 16>, name<T, mode, move, 8>}
+// Launches the kernels `name` of a type for the call's mode and alignment.
+#define ADAPT_SCAN_LAUNCH(name, T, tensors)                                                            \
+  {                                                                                                    \
+    static const ScanKernel kernels[2][3][3] = {                                                       \
+        {ADAPT_SCAN_WIDTHS(name, T, 0, 0), ADAPT_SCAN_WIDTHS(name, T, 0, 1), ADAPT_SCAN_WIDTHS(name, T, 0, 2)},  \
+        {ADAPT_SCAN_WIDTHS(name, T, 1, 0), ADAPT_SCAN_WIDTHS(name, T, 1, 1), ADAPT_SCAN_WIDTHS(name, T, 1, 2)}}; \
+    rc = launch_scan(*dc, kernels[mode][move], tensors, e, q, stream);                                 \
+  }
 constexpr long long kSerialSteps = 4;
 
 // The caller's workspace, or the library's (grown on demand).
@@ -298,11 +315,11 @@ int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int
       else scan_serial_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
     });
   } else {
-    const bool pairs = scan_pairs(q, e, {x, y, gate_group == 1 ? gate : nullptr},
+    const int move = scan_move(q, e, {x, y, gate_group == 1 ? gate : nullptr},
                                   {q.xb, q.xt, q.yb, q.yt, gate_group == 1 ? q.gb : 0, gate_group == 1 ? q.gt : 0});
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      rc = launch_scan(*dc, ADAPT_SCAN_KERNEL(scan_kernel, T, mode, pairs), 2, e, q, stream);
+      ADAPT_SCAN_LAUNCH(scan_kernel, T, 2);
     });
     if (rc != ADAPT_OK) return rc;
   }
@@ -346,12 +363,12 @@ int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy, c
   {
     LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
     const bool own = gate_group == 1;
-    const bool pairs = scan_pairs(q, e, {x, dy, dx, own ? gate : nullptr, own ? dgate : nullptr},
+    const int move = scan_move(q, e, {x, dy, dx, own ? gate : nullptr, own ? dgate : nullptr},
                                   {q.xb, q.xt, q.yb, q.yt, q.dxb, q.dxt, own ? q.gb : 0, own ? q.gt : 0,
                                    own ? q.dgb : 0, own ? q.dgt : 0});
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      rc = launch_scan(*dc, ADAPT_SCAN_KERNEL(scan_backward_kernel, T, mode, pairs), 3, e, q, stream);
+      ADAPT_SCAN_LAUNCH(scan_backward_kernel, T, 3);
     });
     if (rc != ADAPT_OK) return rc;
     ADAPT_LAUNCH_OK("gated scan, backward");
