@@ -74,6 +74,22 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
 
 namespace {
 
+// CTAs that share a row: enough to fill the device, with two 16-byte loads at least for each thread; and,
+// where the gradient comes out of the same call, so many that the rows under way stay in L2 for the
+// second reading.
+int logprob_parts(const LogprobParams& q, int elem, int sm_count) {
+  const long long slots = 5ll * sm_count, least = 2ll * kRowThreads * 16 / elem;
+  int parts = 1;
+  while (parts < kRowMaxCluster && q.vocab / (2 * parts) >= least) {
+    const bool idle = q.rows * parts * 2 <= slots;
+    const long long under_way = std::min<long long>(q.rows, slots / parts) * q.vocab * elem;
+    const bool spills = q.dlogits && !q.lse_in && under_way > (64ll << 20);
+    if (!idle && !spills) break;
+    parts *= 2;
+  }
+  return parts;
+}
+
 int run_logprobs(LogprobParams& q, int dtype, void* stream_handle) {
   const int e = elem_bytes(dtype);
   if (!e || q.rows < 0 || q.rows > 0x7FFFFFFF || q.vocab < 1 || !(q.scale > 0.0f) || !std::isfinite(q.scale))
@@ -83,9 +99,48 @@ int run_logprobs(LogprobParams& q, int dtype, void* stream_handle) {
   if (q.rows > 1 && (q.ld < q.vocab || (q.dlogits && q.ld_grad < q.vocab))) return ADAPT_ERR_INVALID_ARG;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   LaunchScope ls(ADAPT_KERNEL_LOGPROBS, stream);
+  if (q.vocab <= kWarpRowMax) {
+    const unsigned grid = static_cast<unsigned>((q.rows + kRowThreads / 32 - 1) / (kRowThreads / 32));
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      if (q.vocab <= 128) logprob_warp_kernel<T, 4><<<grid, kRowThreads, 0, stream>>>(q);
+      else if (q.vocab <= 512) logprob_warp_kernel<T, 16><<<grid, kRowThreads, 0, stream>>>(q);
+      else logprob_warp_kernel<T, 32><<<grid, kRowThreads, 0, stream>>>(q);
+    });
+    ADAPT_LAUNCH_OK("token log probabilities");
+    return ADAPT_OK;
+  }
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceCache* dc = nullptr;
+  int rc = current_cache(&dc);
+  if (rc != ADAPT_OK) return rc;
+  const int parts = logprob_parts(q, e, dc->sm_count);
+  const long long ctas = q.rows * parts;
+  if (ctas > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;   // (never: many rows are not split)
+  if (q.lse_in) {
+    with_type(dtype, [&](auto t) {
+      logprob_backward_kernel<decltype(t)><<<static_cast<unsigned>(ctas), kRowThreads, 0, stream>>>(q, parts);
+    });
+    ADAPT_LAUNCH_OK("token log probabilities, gradient");
+    return ADAPT_OK;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.blockDim = dim3(kRowThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
   with_type(dtype, [&](auto t) {
-    logprob_kernel<decltype(t)><<<static_cast<unsigned>(q.rows), kRowThreads, 0, stream>>>(q);
+    const auto kernel = logprob_row_kernel<decltype(t)>;
+    cudaError_t err = cudaSuccess;
+    if (parts > 8) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (err == cudaSuccess) err = cudaLaunchKernelEx(&cfg, kernel, q);
+    if (err != cudaSuccess) rc = cuda_fail(err, "token log probabilities");
   });
+  if (rc != ADAPT_OK) return rc;
   ADAPT_LAUNCH_OK("token log probabilities");
   return ADAPT_OK;
 }
