@@ -683,6 +683,22 @@ def adapt_format_quantize(x: torch.Tensor, kind: int, a: int, b: int, round_mode
 
 _ELEM_DTYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
 
+# Small calls are bound by the host: the stream's handle comes straight from torch's C layer (the
+# public object costs 3 us to make), and outputs are made only when they are asked for.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _launch_stream(t: torch.Tensor, stream) -> Optional[int]:
+    """Handle of the stream to launch on; the tensors have to be on the current device."""
+    dev = t.get_device()
+    assert dev == _current_device(), "the tensors are not on the current device"
+    if stream is not None:
+        return stream.cuda_stream or None
+    if _raw_stream is not None:
+        return _raw_stream(dev) or None
+    return _stream_handle(None)
+
 
 def _elem(t: torch.Tensor) -> int:
     d = _ELEM_DTYPES.get(t.dtype)
@@ -690,13 +706,20 @@ def _elem(t: torch.Tensor) -> int:
     return d
 
 
+_HERE_STREAM = contextlib.nullcontext()
+
+
 def _on(stream):
     """Context in which outputs and scratch are allocated: the stream that the kernels run on."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+    return torch.cuda.stream(stream) if stream is not None else _HERE_STREAM
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
+
+
+def _like(t: torch.Tensor, x: torch.Tensor) -> bool:
+    return t.shape == x.shape and t.dtype == x.dtype and t.device == x.device
 
 
 def adapt_dropout(x: torch.Tensor, p: float, seed: int = 0, layer: int = 0, index_base: int = 0,
@@ -706,43 +729,74 @@ def adapt_dropout(x: torch.Tensor, p: float, seed: int = 0, layer: int = 0, inde
     number), never stored; the gradient of x is the same call on dy.  ``out`` may be ``x`` or
     ``residual`` (in place)."""
     dtype = _elem(x)
+    flat = x.is_contiguous()
+    if residual is not None:
+        assert _like(residual, x)
+        flat = flat and residual.is_contiguous()
     if out is None:
         with _on(stream):
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    parts = (x, out) if residual is None else (x, out, residual)
-    assert all(t.shape == x.shape and t.dtype == x.dtype and t.device == x.device for t in parts)
-    if all(t.is_contiguous() for t in parts):   # elements in order: one long row
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    else:
+        assert _like(out, x)
+        flat = flat and out.is_contiguous()
+    if flat:   # elements in order: one long row
         rows, cols = 1, x.numel()
         ldx = ldy = ldr = cols
     else:
+        parts = (x, out) if residual is None else (x, out, residual)
         assert x.dim() == 2, "needs contiguous tensors, or matrices with unit inner stride"
         rows, cols = x.shape
         assert all(t.stride(1) == 1 or cols <= 1 for t in parts)
         ldx, ldy, ldr = (t.stride(0) if rows > 1 else cols for t in (x, out, parts[-1]))
-    _check(lib().adapt_dropout(x.data_ptr(), _ptr(residual), out.data_ptr(), rows, cols, ldx, ldr, ldy, dtype,
-                               p, seed, layer, index_base, _stream_handle(stream)), "adapt_dropout")
+    _check(lib().adapt_dropout(x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(),
+                               rows, cols, ldx, ldr, ldy, dtype, p, seed, layer, index_base,
+                               _launch_stream(x, stream)), "adapt_dropout")
     return out
 
 
 class TokenLogprobs:
-    """Device outputs of adapt_token_logprobs (what was not asked for is None)."""
+    """Device outputs of adapt_token_logprobs (what was not asked for is None): logprob, entropy, lse
+    float32 [rows]; top_ids int32 and top_logprobs float32 [rows, n_top]; dlogits."""
 
-    __slots__ = ("logprob", "entropy", "lse", "top_ids", "top_logprobs", "dlogits")
+    __slots__ = ("_stats", "_tops", "_asked", "dlogits")
 
-    def __init__(self, logprob, entropy, lse, top_ids, top_logprobs, dlogits):
-        self.logprob, self.entropy, self.lse = logprob, entropy, lse
-        self.top_ids, self.top_logprobs, self.dlogits = top_ids, top_logprobs, dlogits
+    def __init__(self, stats, tops, asked, dlogits):
+        self._stats, self._tops, self._asked, self.dlogits = stats, tops, asked, dlogits
+
+    @property
+    def logprob(self) -> Optional[torch.Tensor]:
+        return self._stats[0] if self._asked[0] else None
+
+    @property
+    def entropy(self) -> Optional[torch.Tensor]:
+        return self._stats[1] if self._asked[1] else None
+
+    @property
+    def lse(self) -> torch.Tensor:
+        return self._stats[2]
+
+    @property
+    def top_ids(self) -> Optional[torch.Tensor]:
+        return None if self._tops is None else self._tops[0]
+
+    @property
+    def top_logprobs(self) -> Optional[torch.Tensor]:
+        return None if self._tops is None else self._tops[1].view(torch.float32)
 
 
 def _logit_rows(t: torch.Tensor):
-    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "needs a matrix with unit inner stride"
     rows, vocab = t.shape
+    if t.is_contiguous():
+        return rows, vocab, vocab
+    assert t.stride(1) == 1 or vocab == 1, "needs a matrix with unit inner stride"
     return rows, vocab, t.stride(0) if rows > 1 else vocab
 
 
 def _per_row(t: Optional[torch.Tensor], rows: int, dtype: torch.dtype):
-    assert t is None or (t.is_cuda and t.dtype == dtype and t.numel() == rows and t.is_contiguous())
-    return _ptr(t)
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.numel() == rows and t.is_contiguous()
+    return t.data_ptr()
 
 
 def adapt_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, scale: float = 1.0,
@@ -754,28 +808,29 @@ def adapt_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] =
     (``dlogits`` defaults to a new tensor and may be ``logits``: in place)."""
     dtype = _elem(logits)
     rows, vocab, ld = _logit_rows(logits)
+    assert 0 <= n_top <= MAX_TOP
+    f32 = torch.float32
     pt = _per_row(targets, rows, torch.int64)
-    pdl, pdh = _per_row(d_logprob, rows, torch.float32), _per_row(d_entropy, rows, torch.float32)
-    dev = logits.device
+    pdl = None if d_logprob is None else _per_row(d_logprob, rows, f32)
+    pdh = None if d_entropy is None else _per_row(d_entropy, rows, f32)
+    tops, pids, ptops, ldg, pdx = None, None, None, 0, None
     with _on(stream):
-        stats = torch.empty((3, rows), dtype=torch.float32, device=dev)
-        ids = torch.empty((rows, n_top), dtype=torch.int32, device=dev) if n_top else None
-        tops = torch.empty((rows, n_top), dtype=torch.float32, device=dev) if n_top else None
-        if dlogits is None and (d_logprob is not None or d_entropy is not None):
-            dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
-    ldg = 0
+        stats = logits.new_empty((3, rows), dtype=f32)
+        if n_top:
+            tops = logits.new_empty((2, rows, n_top), dtype=torch.int32)
+            pids = tops.data_ptr()
+            ptops = pids + 4 * rows * n_top
+        if dlogits is None and (pdl is not None or pdh is not None):
+            dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
     if dlogits is not None:
-        assert dlogits.shape == logits.shape and dlogits.dtype == logits.dtype and dlogits.device == dev
-        ldg = _logit_rows(dlogits)[2]
-    logprob, entropy, lse = stats.unbind(0)
-    if targets is None:
-        logprob = None
-    if not want_entropy:
-        entropy = None
-    _check(lib().adapt_token_logprobs(logits.data_ptr(), rows, vocab, ld, dtype, scale, pt, n_top, _ptr(logprob),
-                                      _ptr(entropy), lse.data_ptr(), _ptr(ids), _ptr(tops), pdl, pdh,
-                                      _ptr(dlogits), ldg, _stream_handle(stream)), "adapt_token_logprobs")
-    return TokenLogprobs(logprob, entropy, lse, ids, tops, dlogits)
+        assert _like(dlogits, logits)
+        ldg, pdx = _logit_rows(dlogits)[2], dlogits.data_ptr()
+    ps = stats.data_ptr()
+    _check(lib().adapt_token_logprobs(logits.data_ptr(), rows, vocab, ld, dtype, scale, pt, n_top,
+                                      None if targets is None else ps, ps + 4 * rows if want_entropy else None,
+                                      ps + 8 * rows, pids, ptops, pdl, pdh, pdx, ldg,
+                                      _launch_stream(logits, stream)), "adapt_token_logprobs")
+    return TokenLogprobs(stats, tops, (targets is not None, want_entropy), dlogits)
 
 
 def adapt_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor,
@@ -789,13 +844,14 @@ def adapt_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.
     rows, vocab, ld = _logit_rows(logits)
     if out is None:
         with _on(stream):
-            out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-    assert out.shape == logits.shape and out.dtype == logits.dtype and out.device == logits.device
+            out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    else:
+        assert _like(out, logits)
     f32 = torch.float32
     _check(lib().adapt_token_logprobs_backward(
         logits.data_ptr(), rows, vocab, ld, dtype, scale, _per_row(targets, rows, torch.int64),
         _per_row(lse, rows, f32), _per_row(entropy, rows, f32), _per_row(d_logprob, rows, f32),
-        _per_row(d_entropy, rows, f32), out.data_ptr(), _logit_rows(out)[2], _stream_handle(stream)),
+        _per_row(d_entropy, rows, f32), out.data_ptr(), _logit_rows(out)[2], _launch_stream(logits, stream)),
         "adapt_token_logprobs_backward")
     return out
 
@@ -822,8 +878,8 @@ def _scan_args(x, gate, lengths, reset):
     dtype = _elem(x)
     assert x.dim() == 3 and gate.dim() == 3 and gate.dtype == x.dtype and gate.device == x.device
     batch, steps, channels = x.shape
-    gates = gate.shape[2]
-    assert gate.shape[0] == batch and gate.shape[1] == steps
+    b, t, gates = gate.shape
+    assert b == batch and t == steps
     assert channels == 0 or (gates > 0 and channels % gates == 0), "the gates have to divide the channels"
     assert lengths is None or (lengths.is_cuda and lengths.dtype == torch.int32 and lengths.shape == (batch,)
                                and lengths.is_contiguous())
@@ -834,24 +890,23 @@ def _scan_args(x, gate, lengths, reset):
 
 def _scan_strides(*tensors):
     """None where every tensor is contiguous, else the {batch, step} strides of all."""
-    if all(t.is_contiguous() for t in tensors):
+    for t in tensors:
+        if not t.is_contiguous():
+            break
+    else:
         return None
     s = []
     for t in tensors:
         assert t.stride(2) == 1 or t.shape[2] <= 1, "the channels need unit stride"
-        s += [t.stride(0) if t.shape[0] > 1 else max(t.stride(0), 0), t.stride(1)]
+        s += [t.stride(0), t.stride(1)]
     return (C.c_int64 * len(s))(*s)
 
 
 def _state(t: Optional[torch.Tensor], batch: int, channels: int):
-    assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.shape == (batch, channels)
-                         and t.is_contiguous())
-    return _ptr(t)
-
-
-def _scan_workspace(batch, steps, channels, group, dtype, backward, device):
-    n = lib().adapt_gated_scan_workspace_bytes(batch, steps, channels, group, dtype, backward)
-    return (torch.empty(n, dtype=torch.uint8, device=device), n) if n else (None, 0)
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float32 and t.shape == (batch, channels) and t.is_contiguous()
+    return t.data_ptr()
 
 
 def adapt_gated_scan_workspace_bytes(batch: int, steps: int, channels: int, gate_group: int = 1,
@@ -868,20 +923,21 @@ def adapt_gated_scan(x: torch.Tensor, gate: torch.Tensor, h0: Optional[torch.Ten
     channels a multiple of gates; states float32 [batch, channels].  ``y`` may be ``x`` and ``h_last``
     may be ``h0`` (in place).  ``want_carry`` keeps what adapt_gated_scan_backward starts from."""
     dtype, batch, steps, channels, group = _scan_args(x, gate, lengths, reset)
-    dev = x.device
+    carry = None
     with _on(stream):
         if y is None:
-            y = torch.empty((batch, steps, channels), dtype=x.dtype, device=dev)
+            y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        else:
+            assert _like(y, x)
         if h_last is None:
-            h_last = torch.empty((batch, channels), dtype=torch.float32, device=dev)
-        carry = torch.empty((batch, -(-steps // SCAN_TILE), channels), dtype=torch.float32,
-                            device=dev) if want_carry else None
-        ws, n = _scan_workspace(batch, steps, channels, group, dtype, 0, dev)
-    assert y.shape == x.shape and y.dtype == x.dtype and y.device == dev
+            h_last = x.new_empty((batch, channels), dtype=torch.float32)
+        if want_carry:
+            carry = x.new_empty((batch, -(-steps // SCAN_TILE), channels), dtype=torch.float32)
+    # (the forward pass needs no workspace)
     _check(lib().adapt_gated_scan(x.data_ptr(), gate.data_ptr(), _state(h0, batch, channels), _ptr(lengths),
                                   _ptr(reset), batch, steps, channels, group, dtype, mode,
                                   _scan_strides(x, gate, y), y.data_ptr(), _state(h_last, batch, channels),
-                                  _ptr(carry), _ptr(ws), n, _stream_handle(stream)), "adapt_gated_scan")
+                                  _ptr(carry), None, 0, _launch_stream(x, stream)), "adapt_gated_scan")
     return ScanResult(y, h_last, carry)
 
 
@@ -893,22 +949,28 @@ def adapt_gated_scan_backward(x: torch.Tensor, gate: torch.Tensor, dy: torch.Ten
     """adapt_gated_scan_backward of adapt.h; ``carry`` from adapt_gated_scan on the same inputs.
     ``dx`` may be ``dy`` (in place)."""
     dtype, batch, steps, channels, group = _scan_args(x, gate, lengths, reset)
-    dev = x.device
-    assert dy.shape == x.shape and dy.dtype == x.dtype and dy.device == dev
+    assert _like(dy, x)
     assert carry.is_cuda and carry.dtype == torch.float32 and carry.is_contiguous()
     assert carry.shape == (batch, -(-steps // SCAN_TILE), channels)
+    dh0, ws, n = None, None, 0
     with _on(stream):
         if dx is None:
-            dx = torch.empty((batch, steps, channels), dtype=x.dtype, device=dev)
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        else:
+            assert _like(dx, x)
         if dgate is None:
-            dgate = torch.empty(gate.shape, dtype=x.dtype, device=dev)
-        dh0 = torch.empty((batch, channels), dtype=torch.float32, device=dev) if want_dh0 else None
-        ws, n = _scan_workspace(batch, steps, channels, group, dtype, 1, dev)
-    assert dx.shape == x.shape and dx.dtype == x.dtype and dgate.shape == gate.shape and dgate.dtype == x.dtype
+            dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
+        else:
+            assert _like(dgate, gate)
+        if want_dh0:
+            dh0 = x.new_empty((batch, channels), dtype=torch.float32)
+        if group > 1:
+            n = lib().adapt_gated_scan_workspace_bytes(batch, steps, channels, group, dtype, 1)
+            ws = x.new_empty((n,), dtype=torch.uint8) if n else None
     _check(lib().adapt_gated_scan_backward(x.data_ptr(), gate.data_ptr(), dy.data_ptr(), carry.data_ptr(),
                                            _state(dh_last, batch, channels), _ptr(lengths), _ptr(reset), batch,
                                            steps, channels, group, dtype, mode,
                                            _scan_strides(x, gate, dy, dx, dgate), dx.data_ptr(),
-                                           dgate.data_ptr(), _ptr(dh0), _ptr(ws), n, _stream_handle(stream)),
+                                           dgate.data_ptr(), _ptr(dh0), _ptr(ws), n, _launch_stream(x, stream)),
            "adapt_gated_scan_backward")
     return ScanGradients(dx, dgate, dh0)
