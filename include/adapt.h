@@ -527,7 +527,7 @@ enum { ADAPT_DTYPE_F32 = 0, ADAPT_DTYPE_F16 = 1, ADAPT_DTYPE_BF16 = 2 };
  *                   dimension), no other overlap
  *   p               0 <= p <= 1, held to a multiple of 2^-32; 1 drops everything
  * Dropped elements count as 0 whatever they hold (NaN and Inf included).
- * Limit: rows * cols <= 2^48. */
+ * Limits: rows * cols <= 2^48, index_base <= 2^62. */
 int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, int64_t cols,
                   int64_t ldx, int64_t ldr, int64_t ldy, int dtype, double p, uint64_t seed,
                   int32_t layer, uint64_t index_base, void* stream);

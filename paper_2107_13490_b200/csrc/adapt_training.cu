@@ -49,24 +49,61 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   if (!e || rows < 0 || cols < 0 || !(p >= 0.0 && p <= 1.0)) return ADAPT_ERR_INVALID_ARG;
   if (rows == 0 || cols == 0) return ADAPT_OK;
   if (!x || !y || misaligned(x, e) || misaligned(y, e) || misaligned(residual, e)) return ADAPT_ERR_INVALID_ARG;
-  if (rows > (1ll << 48) / cols) return ADAPT_ERR_INVALID_ARG;
+  if (rows > (1ll << 48) / cols || index_base > (1ull << 62)) return ADAPT_ERR_INVALID_ARG;
   if (rows > 1 && (ldx < cols || ldy < cols || (residual && ldr < cols))) return ADAPT_ERR_INVALID_ARG;
-  std::lock_guard<std::mutex> lock(g_mutex);
-  DeviceCache* dc = nullptr;
-  const int rc = current_cache(&dc);
-  if (rc != ADAPT_OK) return rc;
+  const int unit = 16 / e;
+  if (rows == 1) ldx = ldr = ldy = cols;
+  // x, r and y alike to the 16-byte boundary, in every row
+  auto off = [&](const void* a, const void* b) { return (reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u; };
+  const bool vec = !off(x, y) && (!residual || !off(x, residual)) &&
+                   (rows == 1 || ((ldx - ldy) % unit == 0 && (!residual || (ldx - ldr) % unit == 0)));
   DropoutParams q;
-  q.x = x; q.r = residual; q.y = y;
-  q.rows = rows; q.cols = cols; q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
+  q.cols = cols; q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
   q.base = seed ^ 0xA54FF53A5F1D36F1ull ^ ((static_cast<uint64_t>(static_cast<int64_t>(layer)) + 1ull) * 0x9E3779B97F4A7C15ull);
-  q.index_base = index_base;
-  q.threshold = static_cast<unsigned long long>(std::nearbyint(p * 4294967296.0));
+  const double threshold = std::nearbyint(p * 4294967296.0);
+  q.none = threshold >= 4294967296.0;
+  q.threshold = q.none ? 0u : static_cast<unsigned>(threshold);
   q.scale = p < 1.0 ? static_cast<float>(1.0 / (1.0 - p)) : 0.0f;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  const int grid = static_cast<int>(std::min<long long>((rows * cols + 255) / 256, 16ll * dc->sm_count));
-  LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
-  with_type(dtype, [&](auto t) { dropout_kernel<decltype(t)><<<grid, 256, 0, stream>>>(q); });
-  ADAPT_LAUNCH_OK("dropout");
+  // Chunk numbers are 31-bit: longer tensors go in pieces of rows, or of one long row's columns.
+  const int64_t most = 1ll << 30;
+  const int64_t col_step = std::min<int64_t>(cols, (most - 2) * unit), per_row = std::max<int64_t>(2, (col_step + unit - 1) / unit + (vec ? 1 : 0));
+  const int64_t row_step = std::max<int64_t>(1, most / per_row);
+  for (int64_t row = 0; row < rows; row += row_step) {
+    for (int64_t col = 0; col < cols; col += col_step) {
+      const int64_t n_rows = std::min(row_step, rows - row), n_cols = std::min(col_step, cols - col);
+      q.x = static_cast<const char*>(x) + (row * ldx + col) * e;
+      q.y = static_cast<char*>(y) + (row * ldy + col) * e;
+      q.r = residual ? static_cast<const char*>(residual) + (row * ldr + col) * e : nullptr;
+      q.index_base = static_cast<long long>(index_base) + row * cols + col;
+      if (n_rows == 1) {
+        const int64_t mis = vec ? static_cast<int64_t>((reinterpret_cast<uintptr_t>(q.x) & 15u) / e) : 0;
+        q.cols = n_cols;
+        q.per_row = q.chunks = static_cast<unsigned>((mis + n_cols + unit - 1) / unit);
+        q.magic = q.shift = 0;
+      } else {   // (col_step = cols here: a row of more than 2^30 chunks goes alone)
+        q.cols = cols;
+        q.per_row = static_cast<unsigned>(per_row);
+        q.chunks = static_cast<unsigned>(per_row * n_rows);
+        // i / d for i < 2^31, d >= 2: magic = ceil(2^(32 + s) / d) with 2^s >= d / 2 (Granlund and Montgomery)
+        unsigned s = 0;
+        while ((2ull << s) < q.per_row) ++s;
+        q.shift = s;
+        q.magic = static_cast<unsigned>(((1ull << (32 + s)) + q.per_row - 1) / q.per_row);
+      }
+      const unsigned tile = kDropoutThreads * kDropoutUnroll;
+      const unsigned grid = (q.chunks + tile - 1) / tile;
+      LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
+      with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        if (vec && residual) dropout_kernel<T, true, true><<<grid, kDropoutThreads, 0, stream>>>(q);
+        else if (vec) dropout_kernel<T, true, false><<<grid, kDropoutThreads, 0, stream>>>(q);
+        else if (residual) dropout_kernel<T, false, true><<<grid, kDropoutThreads, 0, stream>>>(q);
+        else dropout_kernel<T, false, false><<<grid, kDropoutThreads, 0, stream>>>(q);
+      });
+      ADAPT_LAUNCH_OK("dropout");
+    }
+  }
   return ADAPT_OK;
 }
 

@@ -56,7 +56,7 @@ def strides(*v):
 @pytest.mark.parametrize("bad", [
     dict(x=None), dict(y=None), dict(rows=-1), dict(cols=-1), dict(dtype=3), dict(dtype=-1), dict(p=-0.01),
     dict(p=1.01), dict(p=float("nan")), dict(ldx=7), dict(ldy=7), dict(r=P, ldr=7), dict(x=P + 2), dict(y=P + 1),
-    dict(r=P + 2), dict(dtype=2, x=P + 1), dict(rows=1 << 40, cols=1 << 40)])
+    dict(r=P + 2), dict(dtype=2, x=P + 1), dict(rows=1 << 40, cols=1 << 40), dict(base=(1 << 62) + 1)])
 def test_dropout_refuses(L, bad):
     assert dropout(L, **bad) == B.ERR_INVALID_ARG
 
