@@ -564,7 +564,8 @@ int adapt_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_
 
 /* The gradient alone, from lse and entropy as adapt_token_logprobs left them (for weights
  * that depend on the log probabilities).  lse DEVICE float[rows]; entropy needed with
- * d_entropy, targets with d_logprob; at least one weight.  The rest as above. */
+ * d_entropy, targets with d_logprob; at least one weight.  The probabilities are as exact as
+ * an fp32 lse allows: relatively 2^-24 |lse|.  The rest as above. */
 int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t vocab, int64_t ld,
                                   int dtype, float scale, const int64_t* targets,
                                   const float* lse, const float* entropy,

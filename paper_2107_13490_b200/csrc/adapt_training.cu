@@ -115,7 +115,7 @@ namespace {
 // where the gradient comes out of the same call, so many that the rows under way stay in L2 for the
 // second reading.
 int logprob_parts(const LogprobParams& q, int elem, int sm_count) {
-  const long long slots = 5ll * sm_count, least = 2ll * kRowThreads * 16 / elem;
+  const long long slots = 6ll * sm_count, least = 2ll * kRowThreads * 16 / elem;
   int parts = 1;
   while (parts < kRowMaxCluster && q.vocab / (2 * parts) >= least) {
     const bool idle = q.rows * parts * 2 <= slots;
@@ -126,6 +126,12 @@ int logprob_parts(const LogprobParams& q, int elem, int sm_count) {
   }
   return parts;
 }
+
+// Many rows of up to 8192 logits take a warp each, others a CTA each: a CTA's barriers cost about 5 us a
+// row, which long rows hide and few rows do not repeat.  Measured on bf16, warp against CTA, us: 16384 x 4096
+// 31 / 76, 16384 x 8192 51 / 77, 2048 x 8192 13 / 15, 512 x 8192 with gradient 17 / 11, 2048 x 16384 21 / 19.
+constexpr int kTeamRowMax = 8192;
+constexpr int kTeamMinRows = 1024;
 
 int run_logprobs(LogprobParams& q, int dtype, void* stream_handle) {
   const int e = elem_bytes(dtype);
@@ -154,11 +160,16 @@ int run_logprobs(LogprobParams& q, int dtype, void* stream_handle) {
   const int parts = logprob_parts(q, e, dc->sm_count);
   const long long ctas = q.rows * parts;
   if (ctas > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;   // (never: many rows are not split)
-  if (q.lse_in) {
+  const bool teams = parts == 1 && q.vocab <= kTeamRowMax && q.rows >= kTeamMinRows;
+  const unsigned team_grid = static_cast<unsigned>((q.rows + kRowThreads / 32 - 1) / (kRowThreads / 32));
+  if (q.lse_in || teams) {
     with_type(dtype, [&](auto t) {
-      logprob_backward_kernel<decltype(t)><<<static_cast<unsigned>(ctas), kRowThreads, 0, stream>>>(q, parts);
+      using T = decltype(t);
+      if (!q.lse_in) logprob_row_kernel<T, 32><<<team_grid, kRowThreads, 0, stream>>>(q);
+      else if (teams) logprob_backward_kernel<T, 32><<<team_grid, kRowThreads, 0, stream>>>(q, 1);
+      else logprob_backward_kernel<T, kRowThreads><<<static_cast<unsigned>(ctas), kRowThreads, 0, stream>>>(q, parts);
     });
-    ADAPT_LAUNCH_OK("token log probabilities, gradient");
+    ADAPT_LAUNCH_OK("token log probabilities");
     return ADAPT_OK;
   }
   cudaLaunchConfig_t cfg = {};
@@ -171,7 +182,7 @@ int run_logprobs(LogprobParams& q, int dtype, void* stream_handle) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   with_type(dtype, [&](auto t) {
-    const auto kernel = logprob_row_kernel<decltype(t)>;
+    const auto kernel = logprob_row_kernel<decltype(t), kRowThreads>;
     cudaError_t err = cudaSuccess;
     if (parts > 8) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (err == cudaSuccess) err = cudaLaunchKernelEx(&cfg, kernel, q);

@@ -4,9 +4,9 @@
 //   H = ln s - (sum e^(z - m) (z - m)) / s,
 //   dx_j = scale (dlp ([j = t] - p_j) - dH p_j (ln p_j + H)).
 //
-// Forms: rows of up to 1024 logits are held in a warp's registers; longer ones are read once by
-// a CTA, or by the CTAs of a cluster, a part each, when there are few rows.  All in one launch; the
-// gradient of the same call reads the row again, from L2.
+// Forms: rows of up to 1024 logits are held in a warp's registers; longer ones are read once by a
+// warp (many rows of up to 8192), by a CTA, or by the CTAs of a cluster, a part each, when there are few
+// rows.  All in one launch; the gradient of the same call reads the row again, from L2.
 #pragma once
 
 #include "k_elem.cuh"
@@ -320,55 +320,81 @@ __device__ __forceinline__ void cluster_barrier() {
 
 constexpr int kTopSpare = 64;   // candidates that may be there when a round of up to 256 chunks begins
 
-template <typename T>
+// The threads that work on a row (or a part of one): a CTA or a warp.
+template <int kThreads>
+struct Team {
+  static_assert(kThreads == 32 || kThreads == kRowThreads, "a warp or a CTA");
+  __device__ __forceinline__ static int me() { return threadIdx.x % kThreads; }
+  __device__ __forceinline__ static void sync() {
+    if (kThreads == 32) __syncwarp();
+    else __syncthreads();
+  }
+  __device__ __forceinline__ static bool any(bool v) {
+    return kThreads == 32 ? __any_sync(~0u, v) != 0 : __syncthreads_or(v) != 0;
+  }
+  __device__ __forceinline__ static float reduce(float v, float* red, bool max) {
+    v = max ? warp_max(v) : warp_sum(v);
+    if (kThreads == 32) return v;
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int i = 1; i < kRowThreads / 32; ++i) v = max ? fmaxf(v, red[i]) : v + red[i];
+    return v;
+  }
+};
+
+template <typename T, int kThreads>
 struct RowShared {
-  static constexpr int kCandidates = kRowThreads * RowPart<T>::kCount + kTopSpare;
+  static constexpr int kCandidates = kThreads * RowPart<T>::kCount + kTopSpare;
+  static constexpr int kParts = kThreads == 32 ? 1 : kRowMaxCluster;
   float red[2][kRowThreads / 32];
-  float4 parts[kRowMaxCluster];            // m, mc, s, w of each CTA of the row
+  float4 parts[kParts];                         // m, mc, s, w of each CTA of the row
   unsigned long long keys[kCandidates];
   unsigned long long best[kMaxTop];
-  unsigned long long lists[kRowMaxCluster * kMaxTop];   // the first CTA's: alternatives of every part
+  unsigned long long lists[kParts * kMaxTop];   // the first CTA's: alternatives of every part
   float group[32];
-  unsigned char strips[kRowThreads];
+  unsigned char strips[kThreads];
   int n_keys, n_strips;
   float threshold;
-  bool special;
 };
 
 // The k largest of n keys, sorted, into best[]; n_keys = their number.  All threads.
-template <typename T>
-__device__ void top_prune(RowShared<T>& sh, const unsigned long long* keys, int n, int k) {
-  for (int i = threadIdx.x; i < n; i += kRowThreads) {
+template <typename T, int kThreads>
+__device__ void top_prune(RowShared<T, kThreads>& sh, const unsigned long long* keys, int n, int k) {
+  const int me = Team<kThreads>::me();
+  for (int i = me; i < n; i += kThreads) {
     const unsigned long long mine = keys[i];
     int rank = 0;
     for (int j = 0; j < n; ++j) rank += keys[j] > mine;
     if (rank < k) sh.best[rank] = mine;
   }
-  __syncthreads();
+  Team<kThreads>::sync();
 }
 
 // The part's k largest keys into best[].  `bound`: no element of the part below this one's order can be
 // among them (0: any can); only the chunks of the threads listed in strips[] can hold larger ones (all of
-// them if n_strips is kRowThreads).  Every round of at most kRowThreads chunks may add its elements'
+// them if n_strips is kThreads).  Every round of at most kThreads chunks may add its elements'
 // keys; beyond kTopSpare they are cut to the k largest, and the smallest of those bounds the rest.
-template <typename T>
-__device__ int top_collect(RowShared<T>& sh, const RowPart<T>& part, unsigned bound, int k) {
+template <typename T, int kThreads>
+__device__ int top_collect(RowShared<T, kThreads>& sh, const RowPart<T>& part, unsigned bound, int k) {
+  const int me = Team<kThreads>::me();
   constexpr int kCount = RowPart<T>::kCount;
-  const int n_strips = sh.n_strips, per = (part.q1 - part.q0 + kRowThreads - 1) / kRowThreads;
+  const int n_strips = sh.n_strips, per = (part.q1 - part.q0 + kThreads - 1) / kThreads;
   unsigned long long least = static_cast<unsigned long long>(bound) << 32;   // keys above this one count
-  if (threadIdx.x == 0) sh.n_keys = 0;
-  __syncthreads();
-  if (static_cast<int>(threadIdx.x) < part.edges) {
-    const int j = part.edge(threadIdx.x);
+  if (me == 0) sh.n_keys = 0;
+  Team<kThreads>::sync();
+  if (me < part.edges) {
+    const int j = part.edge(me);
     const unsigned long long key = top_key(to_float(part.x[j]), j);
     if (key > least) sh.keys[atomicAdd(&sh.n_keys, 1)] = key;
   }
   const int total = n_strips * per;
-  for (int base = 0; base < total; base += kRowThreads) {
-    const int i = base + threadIdx.x;
+  for (int base = 0; base < total; base += kThreads) {
+    const int i = base + me;
     if (i < total) {
       const int step = i / n_strips, s = i - step * n_strips;
-      const int q = part.q0 + step * kRowThreads + (n_strips == kRowThreads ? s : sh.strips[s]);
+      const int q = part.q0 + step * kThreads + (n_strips == kThreads ? s : sh.strips[s]);
       if (q < part.q1) {
         float v[kCount];
         unpack16<T>(part.chunks[q], v);
@@ -379,104 +405,97 @@ __device__ int top_collect(RowShared<T>& sh, const RowPart<T>& part, unsigned bo
         }
       }
     }
-    __syncthreads();
+    Team<kThreads>::sync();
     const int n = sh.n_keys;
-    __syncthreads();   // all have read it before the next round adds to it
-    if (n > kTopSpare && base + kRowThreads < total) {
-      top_prune<T>(sh, sh.keys, n, k);
-      if (static_cast<int>(threadIdx.x) < k) sh.keys[threadIdx.x] = sh.best[threadIdx.x];
-      if (threadIdx.x == 0) sh.n_keys = k;
+    Team<kThreads>::sync();   // all have read it before the next round adds to it
+    if (n > kTopSpare && base + kThreads < total) {
+      top_prune<T, kThreads>(sh, sh.keys, n, k);
+      if (me < k) sh.keys[me] = sh.best[me];
+      if (me == 0) sh.n_keys = k;
       least = max(least, sh.best[k - 1]);
-      __syncthreads();
+      Team<kThreads>::sync();
     }
   }
-  __syncthreads();
+  Team<kThreads>::sync();
   const int n = sh.n_keys;
-  top_prune<T>(sh, sh.keys, n, k);
+  top_prune<T, kThreads>(sh, sh.keys, n, k);
   return min(n, k);
 }
 
-// Order of the k-th largest of 32 group maxima (the maxima of 8 threads each): k elements at least are
+// Order of the k-th largest of 32 group maxima (the maxima of 8 threads each, or of one): k elements at least are
 // as large.  Kept in threshold; the threads whose own maximum reaches it are listed in strips[].
-template <typename T>
-__device__ void top_threshold(RowShared<T>& sh, float m, int k) {
+template <typename T, int kThreads>
+__device__ void top_threshold(RowShared<T, kThreads>& sh, float m, int k) {
+  const int me = Team<kThreads>::me();
+  constexpr int kWide = kThreads / 32;
   float g = m;
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
-  if ((threadIdx.x & 7) == 0) sh.group[threadIdx.x >> 3] = g;
-  if (threadIdx.x == 0) sh.n_strips = 0;
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    const float mine = sh.group[threadIdx.x];
+  for (int o = 1; o < kWide; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+  if (me % kWide == 0) sh.group[me / kWide] = g;
+  if (me == 0) sh.n_strips = 0;
+  Team<kThreads>::sync();
+  if (me < 32) {
+    const float mine = sh.group[me];
     int rank = 0;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
       const float v = __shfl_sync(~0u, mine, j);
-      rank += v > mine || (v == mine && j < static_cast<int>(threadIdx.x));
+      rank += v > mine || (v == mine && j < me);
     }
     if (rank == k - 1) sh.threshold = mine;
   }
-  __syncthreads();
-  if (m >= sh.threshold) sh.strips[atomicAdd(&sh.n_strips, 1)] = static_cast<unsigned char>(threadIdx.x);
-  __syncthreads();
-}
-
-__device__ __forceinline__ float block_reduce(float v, float* red, bool max) {
-  v = max ? warp_max(v) : warp_sum(v);
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int i = 1; i < kRowThreads / 32; ++i) v = max ? fmaxf(v, red[i]) : v + red[i];
-  return v;
+  Team<kThreads>::sync();
+  if (m >= sh.threshold) sh.strips[atomicAdd(&sh.n_strips, 1)] = static_cast<unsigned char>(me);
+  Team<kThreads>::sync();
 }
 
 // A special row (NaN, Inf, nothing but -Inf, or values where the one-pass sums would lose themselves):
 // one CTA, element by element, three passes.
-template <typename T>
-__device__ void special_row(const LogprobParams& p, RowShared<T>& sh, long long row, const T* x, T* dx, long long target) {
+template <typename T, int kThreads>
+__device__ void special_row(const LogprobParams& p, RowShared<T, kThreads>& sh, long long row, const T* x, T* dx, long long target) {
+  const int me = Team<kThreads>::me();
   float m = -INFINITY;
   bool nan = false;
-  for (int j = threadIdx.x; j < p.vocab; j += kRowThreads) {
+  for (int j = me; j < p.vocab; j += kThreads) {
     const float v = to_float(x[j]);
     nan |= v != v;
     m = fmaxf(m, v);
   }
-  nan = __syncthreads_or(nan);
-  RowStats r = {block_reduce(m, sh.red[0], true), 0.0f, 0.0f};
+  nan = Team<kThreads>::any(nan);
+  RowStats r = {Team<kThreads>::reduce(m, sh.red[0], true), 0.0f, 0.0f};
   nan |= r.m * p.scale == INFINITY;
   const bool dead = r.m * p.scale == -INFINITY;
   float s = 0.0f, w = 0.0f;
   if (!dead)
-    for (int j = threadIdx.x; j < p.vocab; j += kRowThreads) {
+    for (int j = me; j < p.vocab; j += kThreads) {
       const float v = to_float(x[j]);
       const float t = v * p.scale == -INFINITY ? -200.0f : fmaxf((v - r.m) * (p.scale * kLog2e), -200.0f);
       const float e = exp2_approx(t);
       s += e;
       w = fmaf(e, t, w);
     }
-  s = block_reduce(s, sh.red[1], false);
-  __syncthreads();
-  w = block_reduce(w, sh.red[0], false);
+  s = Team<kThreads>::reduce(s, sh.red[1], false);
+  Team<kThreads>::sync();
+  w = Team<kThreads>::reduce(w, sh.red[0], false);
   r.ln_sum = logf(s);
   r.spread = kLn2 * w / s;
   if (nan) r.ln_sum = __int_as_float(0x7FFFFFFF);
-  if (threadIdx.x == 0) put_stats(p, row, r, target, target < p.vocab ? to_float(x[target]) : 0.0f);
+  if (me == 0) put_stats(p, row, r, target, target < p.vocab ? to_float(x[target]) : 0.0f);
   if (p.n_top) {
-    if (threadIdx.x == 0) sh.n_strips = kRowThreads;
-    __syncthreads();
-    top_collect<T>(sh, RowPart<T>(x, p.vocab, 0, 1), 0u, p.n_top);
-    if (static_cast<int>(threadIdx.x) < p.n_top) {
-      const int j = top_index(sh.best[threadIdx.x]);
-      p.top_ids[row * p.n_top + threadIdx.x] = j;
-      p.top_logprobs[row * p.n_top + threadIdx.x] = row_logp(r, p.scale, to_float(x[j]));
+    if (me == 0) sh.n_strips = kThreads;
+    Team<kThreads>::sync();
+    top_collect<T, kThreads>(sh, RowPart<T>(x, p.vocab, 0, 1), 0u, p.n_top);
+    if (me < p.n_top) {
+      const int j = top_index(sh.best[me]);
+      p.top_ids[row * p.n_top + me] = j;
+      p.top_logprobs[row * p.n_top + me] = row_logp(r, p.scale, to_float(x[j]));
     }
   }
   if (!dx) return;
-  __syncthreads();
+  Team<kThreads>::sync();
   const RowWeights g = {p.d_logprob ? p.d_logprob[row] : 0.0f, p.d_entropy ? p.d_entropy[row] : 0.0f};
   const bool lost = p.d_logprob && target >= p.vocab;
-  for (int j = threadIdx.x; j < p.vocab; j += kRowThreads) {
+  for (int j = me; j < p.vocab; j += kThreads) {
     float d = dead && !nan ? 0.0f : element_grad(row_logp(r, p.scale, to_float(x[j])), j == target, g, r.ln_sum - r.spread, p.scale);
     if (lost) d = __int_as_float(0x7FFFFFFF);
     dx[j] = from_float<T>(d);
@@ -485,21 +504,21 @@ __device__ void special_row(const LogprobParams& p, RowShared<T>& sh, long long 
 
 // Writes f(x) for the part's elements to dx: 16 bytes at a time where dx is aligned as x is.  From the last
 // chunk to the first: what was read last is the likeliest to be in L2 still.
-template <typename T, bool kFloored, typename F, typename G>
+template <typename T, int kThreads, bool kFloored, typename F, typename G>
 __device__ __forceinline__ void write_part(const RowPart<T>& part, T* dx, F pairs, G one) {
   constexpr int kCount = RowPart<T>::kCount;
   const bool aligned = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(part.x)) & 15u) == 0;
   uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(dx) & ~static_cast<uintptr_t>(15));
   const int n = part.q1 - part.q0;
-  for (int i = threadIdx.x; i < n; i += kRowThreads * kRowUnroll) {
+  for (int i = Team<kThreads>::me(); i < n; i += kThreads * kRowUnroll) {
     uint4 q[kRowUnroll];
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u)
-      if (i + u * kRowThreads < n) q[u] = __ldcs(part.chunks + part.q1 - 1 - (i + u * kRowThreads));
+      if (i + u * kThreads < n) q[u] = __ldcs(part.chunks + part.q1 - 1 - (i + u * kThreads));
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u) {
-      if (i + u * kRowThreads >= n) break;
-      const int at = part.q1 - 1 - (i + u * kRowThreads);
+      if (i + u * kThreads >= n) break;
+      const int at = part.q1 - 1 - (i + u * kThreads);
       f32x2 v[kCount / 2];
       Logits<T>::pairs(kFloored ? Logits<T>::floored(q[u]) : q[u], v);
       float f[kCount];
@@ -516,46 +535,52 @@ __device__ __forceinline__ void write_part(const RowPart<T>& part, T* dx, F pair
       }
     }
   }
-  if (static_cast<int>(threadIdx.x) < part.edges) {
-    const int j = part.edge(threadIdx.x);
+  if (Team<kThreads>::me() < part.edges) {
+    const int j = part.edge(Team<kThreads>::me());
     dx[j] = from_float<T>(one(to_float(part.x[j])));
   }
 }
-template <typename T>
+template <typename T, int kThreads>
 __device__ __forceinline__ void zero_part(const RowPart<T>& part, T* dx) {
   const bool aligned = ((reinterpret_cast<uintptr_t>(dx) ^ reinterpret_cast<uintptr_t>(part.x)) & 15u) == 0;
   uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(dx) & ~static_cast<uintptr_t>(15));
-  for (int q = part.q0 + threadIdx.x; q < part.q1; q += kRowThreads) {
+  for (int q = part.q0 + Team<kThreads>::me(); q < part.q1; q += kThreads) {
     if (aligned) __stcs(out + q, make_uint4(0u, 0u, 0u, 0u));
     else for (int e = 0; e < RowPart<T>::kCount; ++e) dx[part.element(q) + e] = from_float<T>(0.0f);
   }
-  if (static_cast<int>(threadIdx.x) < part.edges) dx[part.edge(threadIdx.x)] = from_float<T>(0.0f);
+  if (Team<kThreads>::me() < part.edges) dx[part.edge(Team<kThreads>::me())] = from_float<T>(0.0f);
 }
 // Whether this thread wrote element j of the part (the target's gradient is put right by its writer).
-template <typename T>
+template <typename T, int kThreads>
 __device__ __forceinline__ bool wrote(const RowPart<T>& part, int j) {
   const int q = (j + part.mis) / RowPart<T>::kCount;
-  if (q >= part.q0 && q < part.q1) return static_cast<int>(threadIdx.x) == (part.q1 - 1 - q) % kRowThreads;
-  return static_cast<int>(threadIdx.x) < part.edges && part.edge(threadIdx.x) == j;
+  if (q >= part.q0 && q < part.q1) return Team<kThreads>::me() == (part.q1 - 1 - q) % kThreads;
+  return Team<kThreads>::me() < part.edges && part.edge(Team<kThreads>::me()) == j;
 }
 
 // What bounds it: HBM (one read of the row; with the gradient one write as well); an element costs about
 // 5 lane instructions and one exponential forward, as many for the gradient.
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 5) logprob_row_kernel(const LogprobParams p) {
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kRowThreads, kThreads == 32 ? 5 : 6) logprob_row_kernel(const LogprobParams p) {
   constexpr int kCount = RowPart<T>::kCount;
-  __shared__ RowShared<T> sh;
-  unsigned rank, parts;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
-  const long long row = blockIdx.x / parts;
+  constexpr int kRows = kRowThreads / kThreads;   // of a CTA
+  __shared__ RowShared<T, kThreads> shared[kRows];
+  RowShared<T, kThreads>& sh = shared[threadIdx.x / kThreads];
+  const int me = Team<kThreads>::me();
+  unsigned rank = 0, parts = 1;
+  if (kRows == 1) {
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+  }
+  const long long row = kRows == 1 ? blockIdx.x / parts : static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / kThreads;
+  if (row >= p.rows) return;
   const T* x = static_cast<const T*>(p.logits) + row * p.ld;
   T* dx = p.dlogits ? static_cast<T*>(p.dlogits) + row * p.ld_grad : nullptr;
   const long long target = p.targets ? p.targets[row] : 0;
   const RowPart<T> part(x, p.vocab, rank, parts);
   if (target < 0) {   // the whole cluster
-    if (rank == 0 && threadIdx.x == 0) put_ignored(p, row);
-    if (dx) zero_part<T>(part, dx);
+    if (rank == 0 && me == 0) put_ignored(p, row);
+    if (dx) zero_part<T, kThreads>(part, dx);
     return;
   }
   if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this CTA has started
@@ -587,11 +612,11 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_row_kernel(const Logpr
       w2 = fma2(ex, t, w2);
     }
   };
-  int q = part.q0 + threadIdx.x;
-  for (; q + (kRowUnroll - 1) * kRowThreads < part.q1; q += kRowUnroll * kRowThreads) {
+  int q = part.q0 + me;
+  for (; q + (kRowUnroll - 1) * kThreads < part.q1; q += kRowUnroll * kThreads) {
     uint4 v[kRowUnroll];
 #pragma unroll
-    for (int u = 0; u < kRowUnroll; ++u) v[u] = part.chunks[q + u * kRowThreads];
+    for (int u = 0; u < kRowUnroll; ++u) v[u] = part.chunks[q + u * kThreads];
     float top = Logits<T>::top(v[0]);
 #pragma unroll
     for (int u = 1; u < kRowUnroll; ++u) {
@@ -602,13 +627,13 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_row_kernel(const Logpr
 #pragma unroll
     for (int u = 0; u < kRowUnroll; ++u) add(v[u]);
   }
-  for (; q < part.q1; q += kRowThreads) {
+  for (; q < part.q1; q += kThreads) {
     const uint4 v = part.chunks[q];
     raise(Logits<T>::top(v));
     add(v);
   }
-  if (static_cast<int>(threadIdx.x) < part.edges) {
-    const float v = to_float(x[part.edge(threadIdx.x)]);
+  if (me < part.edges) {
+    const float v = to_float(x[part.edge(me)]);
     raise(v);
     const float t = fmaf(fmaxf(v, Logits<T>::kFloor), c, -a.mc), e = exp2_approx(t);
     s2 = add2(s2, pack2(e, 0.0f));
@@ -620,18 +645,18 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_row_kernel(const Logpr
     a.s = s.x + s.y; a.w = w.x + w.y;
   }
   // one maximum for the CTA, then for the row; NaN shows in the sums
-  const bool nan = __syncthreads_or(own_top != own_top);
-  float m = block_reduce(own_top, sh.red[0], true);
+  const bool nan = Team<kThreads>::any(own_top != own_top);
+  float m = Team<kThreads>::reduce(own_top, sh.red[0], true);
   a.raise(m, c);
-  const float s_cta = block_reduce(a.s, sh.red[1], false);
-  __syncthreads();
-  float w_sum = block_reduce(a.w, sh.red[0], false);
+  const float s_cta = Team<kThreads>::reduce(a.s, sh.red[1], false);
+  Team<kThreads>::sync();
+  float w_sum = Team<kThreads>::reduce(a.w, sh.red[0], false);
   float s_sum = nan ? __int_as_float(0x7FFFFFFF) : s_cta;
   if (parts > 1) {
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // and so have the others
-    if (threadIdx.x < parts) {
-      const unsigned at = cluster_smem(&sh.parts[rank], threadIdx.x);
+    if (me < static_cast<int>(parts)) {
+      const unsigned at = cluster_smem(&sh.parts[rank], me);
       asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(at), "f"(m), "f"(a.mc), "f"(s_sum), "f"(w_sum) : "memory");
     }
     cluster_barrier();
@@ -646,41 +671,41 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_row_kernel(const Logpr
   }
   // logits at the floor must have been nothing beside the maximum, and c m a number
   if (!((m - Logits<T>::kFloor) * c > 160.0f) || !(fabsf(a.mc) < 1e20f) || !(c < 1e7f) || s_sum != s_sum) {
-    if (rank == 0) special_row<T>(p, sh, row, x, dx, target);
+    if (rank == 0) special_row<T, kThreads>(p, sh, row, x, dx, target);
     return;   // (no other CTA's shared memory is touched from here on)
   }
   // s is relative to the rounded c m; delta = c m - fl(c m) takes it to the true one
   const float log2_s = log2f(s_sum), delta = fmaf(m, c, -a.mc);
   const RowStats r = {m, kLn2 * (log2_s - delta), kLn2 * (w_sum / s_sum - delta)};
-  if (rank == 0 && threadIdx.x == 0) put_stats(p, row, r, target, x_target);
+  if (rank == 0 && me == 0) put_stats(p, row, r, target, x_target);
 
   if (p.n_top) {
     const int k = p.n_top;
-    top_threshold<T>(sh, own_top, k);
+    top_threshold<T, kThreads>(sh, own_top, k);
     const bool few = !(sh.threshold > Logits<T>::kFloor);   // fewer than k above the floor: take any
     if (few) {
-      if (threadIdx.x == 0) sh.n_strips = kRowThreads;
-      __syncthreads();
+      if (me == 0) sh.n_strips = kThreads;
+      Team<kThreads>::sync();
     }
-    int n = top_collect<T>(sh, part, few ? 0u : top_order(sh.threshold), k);
+    int n = top_collect<T, kThreads>(sh, part, few ? 0u : top_order(sh.threshold), k);
     if (parts > 1) {
-      if (static_cast<int>(threadIdx.x) < k) {
-        const unsigned at = cluster_smem(&sh.lists[rank * k + threadIdx.x], 0);
-        const unsigned long long key = static_cast<int>(threadIdx.x) < n ? sh.best[threadIdx.x] : 0ull;
+      if (me < k) {
+        const unsigned at = cluster_smem(&sh.lists[rank * k + me], 0);
+        const unsigned long long key = me < n ? sh.best[me] : 0ull;
         asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(at), "l"(key) : "memory");
       }
       cluster_barrier();
-      if (rank == 0) top_prune<T>(sh, sh.lists, static_cast<int>(parts) * k, k);
+      if (rank == 0) top_prune<T, kThreads>(sh, sh.lists, static_cast<int>(parts) * k, k);
     }
-    if (rank == 0 && static_cast<int>(threadIdx.x) < k) {
-      const int j = top_index(sh.best[threadIdx.x]);
-      p.top_ids[row * k + threadIdx.x] = j;
-      p.top_logprobs[row * k + threadIdx.x] = row_logp(r, p.scale, to_float(x[j]));
+    if (rank == 0 && me < k) {
+      const int j = top_index(sh.best[me]);
+      p.top_ids[row * k + me] = j;
+      p.top_logprobs[row * k + me] = row_logp(r, p.scale, to_float(x[j]));
     }
     if (dx && parts > 1) cluster_barrier();   // the alternatives' logits are read before they are overwritten
   }
   if (!dx) return;
-  __syncthreads();
+  Team<kThreads>::sync();
   const RowWeights g = {p.d_logprob ? p.d_logprob[row] : 0.0f, p.d_entropy ? p.d_entropy[row] : 0.0f};
   const bool lost = p.d_logprob && target >= p.vocab;
   // e (a1 t + a0), e = 2^t, t = c x - fl(c m): ln p + H = ln 2 (t - mean of t)
@@ -691,29 +716,31 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_row_kernel(const Logpr
     const float t = fmaf(fmaxf(v, Logits<T>::kFloor), c, -a.mc);
     return exp2_approx(t) * fmaf(t, a1, a0);
   };
-  write_part<T, true>(part, dx, [&](f32x2 v) {
+  write_part<T, kThreads, true>(part, dx, [&](f32x2 v) {
     const f32x2 t = fma2(v, cc, back);
     const float2 f = unpack2(t);
     return mul2(pack2(exp2_approx(f.x), exp2_approx(f.y)), fma2(t, a1a1, a0a0));
   }, one);
-  if (!lost && g.dlp != 0.0f && wrote<T>(part, static_cast<int>(target)))
+  if (!lost && g.dlp != 0.0f && wrote<T, kThreads>(part, static_cast<int>(target)))
     dx[target] = from_float<T>(fmaf(p.scale, g.dlp, one(x_target)));
 }
 
 // The gradient from lse and entropy.
-template <typename T>
+template <typename T, int kThreads>
 __global__ void __launch_bounds__(kRowThreads, 5) logprob_backward_kernel(const LogprobParams p, int parts) {
-  const long long row = blockIdx.x / parts;
+  constexpr int kRows = kRowThreads / kThreads;   // of a CTA
+  const long long row = kRows == 1 ? blockIdx.x / parts : static_cast<long long>(blockIdx.x) * kRows + threadIdx.x / kThreads;
+  if (row >= p.rows) return;
   const T* x = static_cast<const T*>(p.logits) + row * p.ld;
   T* dx = static_cast<T*>(p.dlogits) + row * p.ld_grad;
   const long long target = p.targets ? p.targets[row] : 0;
-  const RowPart<T> part(x, p.vocab, blockIdx.x % parts, parts);
+  const RowPart<T> part(x, p.vocab, kRows == 1 ? blockIdx.x % parts : 0, kRows == 1 ? parts : 1);
   const float lse = p.lse_in[row];
-  if (target < 0 || lse == -INFINITY) { zero_part<T>(part, dx); return; }
+  if (target < 0 || lse == -INFINITY) { zero_part<T, kThreads>(part, dx); return; }
   const float h = p.entropy_in ? p.entropy_in[row] : 0.0f;
   const RowWeights g = {p.d_logprob ? p.d_logprob[row] : 0.0f, p.d_entropy ? p.d_entropy[row] : 0.0f};
   const bool lost = (p.d_logprob && target >= p.vocab) || lse != lse;
-  const bool mine = !lost && g.dlp != 0.0f && wrote<T>(part, static_cast<int>(target));
+  const bool mine = !lost && g.dlp != 0.0f && wrote<T, kThreads>(part, static_cast<int>(target));
   const float x_target = mine ? to_float(x[target]) : 0.0f;   // before it is overwritten in place
   // p (a1 t + a0), t = ln p = z - lse
   const float a1 = -p.scale * g.dh, a0 = lost ? __int_as_float(0x7FFFFFFF) : -p.scale * fmaf(g.dh, h, g.dlp);
@@ -723,7 +750,7 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_backward_kernel(const 
     const float t = fmaxf(fmaf(v, p.scale, -lse), -1000.0f);
     return exp2_approx(t * kLog2e) * fmaf(t, a1, a0);
   };
-  write_part<T, false>(part, dx, [&](f32x2 v) {
+  write_part<T, kThreads, false>(part, dx, [&](f32x2 v) {
     const float2 u = unpack2(fma2(v, ss, back));
     const f32x2 t = pack2(fmaxf(u.x, -1000.0f), fmaxf(u.y, -1000.0f));
     const float2 f = unpack2(mul2(t, l2));

@@ -206,6 +206,34 @@ def test_nan_and_inf(B, dtype, vocab):
     assert r.dlogits[:4].isnan().all() and r.dlogits[4].isfinite().all()
 
 
+@pytest.mark.parametrize("rows,vocab", [(1100, 1500), (1100, 7777), (40, 7777)])
+def test_special_rows_among_many(B, rows, vocab):
+    import torch
+    x = logits(rows, vocab, "bfloat16", 6)
+    x[3] = -math.inf
+    x[5, 17] = math.nan
+    x[6, :] = torch.finfo(x.dtype).min
+    x[7, 5:] = -math.inf
+    x[9] = 1.0
+    x[11, ::2] = -math.inf
+    t = torch.arange(rows, device="cuda") % 5
+    t[13] = -1
+    t[14] = vocab
+    d, e = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+    r = B.adapt_token_logprobs(x, t, n_top=9, d_logprob=d, d_entropy=e)
+    s = B.adapt_token_logprobs_backward(x, t, r.lse, d, r.entropy, e)
+    for i in (2, 3, 5, 6, 7, 9, 11, 13, 14, 15):   # a row alone takes another form of the kernel
+        one = B.adapt_token_logprobs(x[i:i + 1], t[i:i + 1], n_top=9, d_logprob=d[i:i + 1], d_entropy=e[i:i + 1])
+        assert torch.equal(r.top_ids[i], one.top_ids[0])
+        pairs = [(r.lse, one.lse), (r.entropy, one.entropy), (r.logprob, one.logprob),
+                 (r.top_logprobs, one.top_logprobs), (r.dlogits.float(), one.dlogits.float())]
+        if i != 6:   # (an fp32 lse of -3.4e38 does not hold ln vocab, so the gradient from it cannot either)
+            pairs.append((s.float(), one.dlogits.float()))
+        for a, b in pairs:
+            # the same sums in another order: 2^-17 of values up to 20, and two roundings of a gradient
+            assert torch.allclose(a[i], b[0], rtol=2.0 ** -7, atol=20 * 2.0 ** -17, equal_nan=True), i
+
+
 def test_targets_outside_the_vocabulary(B):
     import torch
     x = logits(4, 300, "float32", 1)
@@ -262,7 +290,8 @@ def test_gradient_against_differences(B):
 
 
 @pytest.mark.parametrize("rows,vocab,dtype", [(1, 131072, "bfloat16"), (3, 250001, "float16"), (64, 32000, "float32"),
-                                              (700, 40000, "bfloat16")])
+                                              (700, 40000, "bfloat16"), (1030, 8191, "float16"), (2100, 1025, "bfloat16"),
+                                              (1024, 5000, "float32")])
 def test_large_rows_against_64_bits_on_the_device(B, rows, vocab, dtype):
     import torch
     x = logits(rows, vocab, dtype, 2)
