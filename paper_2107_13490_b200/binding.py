@@ -758,10 +758,11 @@ class TokenLogprobs:
     """Device outputs of adapt_token_logprobs (what was not asked for is None): logprob, entropy, lse
     float32 [rows]; top_ids int32 and top_logprobs float32 [rows, n_top]; dlogits."""
 
-    __slots__ = ("_stats", "_tops", "_asked", "dlogits")
+    __slots__ = ("_stats", "_asked", "top_ids", "top_logprobs", "dlogits")
 
-    def __init__(self, stats, tops, asked, dlogits):
-        self._stats, self._tops, self._asked, self.dlogits = stats, tops, asked, dlogits
+    def __init__(self, stats, asked, top_ids, top_logprobs, dlogits):
+        self._stats, self._asked = stats, asked
+        self.top_ids, self.top_logprobs, self.dlogits = top_ids, top_logprobs, dlogits
 
     @property
     def logprob(self) -> Optional[torch.Tensor]:
@@ -774,14 +775,6 @@ class TokenLogprobs:
     @property
     def lse(self) -> torch.Tensor:
         return self._stats[2]
-
-    @property
-    def top_ids(self) -> Optional[torch.Tensor]:
-        return None if self._tops is None else self._tops[0]
-
-    @property
-    def top_logprobs(self) -> Optional[torch.Tensor]:
-        return None if self._tops is None else self._tops[1].view(torch.float32)
 
 
 def _logit_rows(t: torch.Tensor):
@@ -813,13 +806,13 @@ def adapt_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] =
     pt = _per_row(targets, rows, torch.int64)
     pdl = None if d_logprob is None else _per_row(d_logprob, rows, f32)
     pdh = None if d_entropy is None else _per_row(d_entropy, rows, f32)
-    tops, pids, ptops, ldg, pdx = None, None, None, 0, None
+    ids, tops, pids, ptops, ldg, pdx = None, None, None, None, 0, None
     with _on(stream):
         stats = logits.new_empty((3, rows), dtype=f32)
         if n_top:
-            tops = logits.new_empty((2, rows, n_top), dtype=torch.int32)
-            pids = tops.data_ptr()
-            ptops = pids + 4 * rows * n_top
+            ids = logits.new_empty((rows, n_top), dtype=torch.int32)
+            tops = logits.new_empty((rows, n_top), dtype=f32)
+            pids, ptops = ids.data_ptr(), tops.data_ptr()
         if dlogits is None and (pdl is not None or pdh is not None):
             dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
     if dlogits is not None:
@@ -830,7 +823,7 @@ def adapt_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] =
                                       None if targets is None else ps, ps + 4 * rows if want_entropy else None,
                                       ps + 8 * rows, pids, ptops, pdl, pdh, pdx, ldg,
                                       _launch_stream(logits, stream)), "adapt_token_logprobs")
-    return TokenLogprobs(stats, tops, (targets is not None, want_entropy), dlogits)
+    return TokenLogprobs(stats, (targets is not None, want_entropy), ids, tops, dlogits)
 
 
 def adapt_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor,

@@ -51,13 +51,13 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   if (!x || !y || misaligned(x, e) || misaligned(y, e) || misaligned(residual, e)) return ADAPT_ERR_INVALID_ARG;
   if (rows > (1ll << 48) / cols || index_base > (1ull << 62)) return ADAPT_ERR_INVALID_ARG;
   if (rows > 1 && (ldx < cols || ldy < cols || (residual && ldr < cols))) return ADAPT_ERR_INVALID_ARG;
-  const int unit = 16 / e;
   if (rows == 1) ldx = ldr = ldy = cols;
-  // x, r and y alike to the 16-byte boundary, in every row
+  // x, r and y alike to the 16-byte boundary, in every row: chunks of 16 bytes, else of a pair
   auto off = [&](const void* a, const void* b) { return (reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u; };
   const bool vec = !off(x, y) && (!residual || !off(x, residual)) &&
-                   (rows == 1 || ((ldx - ldy) % unit == 0 && (!residual || (ldx - ldr) % unit == 0)));
-  DropoutParams q;
+                   (rows == 1 || ((ldx - ldy) % (16 / e) == 0 && (!residual || (ldx - ldr) % (16 / e) == 0)));
+  const int unit = vec ? 16 / e : 2;
+  DropoutParams q = {};
   q.cols = cols; q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
   q.base = seed ^ 0xA54FF53A5F1D36F1ull ^ ((static_cast<uint64_t>(static_cast<int64_t>(layer)) + 1ull) * 0x9E3779B97F4A7C15ull);
   const double threshold = std::nearbyint(p * 4294967296.0);
@@ -67,7 +67,7 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   // Chunk numbers are 31-bit: longer tensors go in pieces of rows, or of one long row's columns.
   const int64_t most = 1ll << 30;
-  const int64_t col_step = std::min<int64_t>(cols, (most - 2) * unit), per_row = std::max<int64_t>(2, (col_step + unit - 1) / unit + (vec ? 1 : 0));
+  const int64_t col_step = std::min<int64_t>(cols, (most - 2) / 8 * unit), per_row = (col_step + unit - 1) / unit + 1;
   const int64_t row_step = std::max<int64_t>(1, most / per_row);
   for (int64_t row = 0; row < rows; row += row_step) {
     for (int64_t col = 0; col < cols; col += col_step) {
@@ -77,12 +77,12 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
       q.r = residual ? static_cast<const char*>(residual) + (row * ldr + col) * e : nullptr;
       q.index_base = static_cast<long long>(index_base) + row * cols + col;
       if (n_rows == 1) {
-        const int64_t mis = vec ? static_cast<int64_t>((reinterpret_cast<uintptr_t>(q.x) & 15u) / e) : 0;
+        q.mis = static_cast<int>(vec ? (reinterpret_cast<uintptr_t>(q.x) & 15u) / e : q.index_base & 1);
         q.cols = n_cols;
-        q.per_row = q.chunks = static_cast<unsigned>((mis + n_cols + unit - 1) / unit);
-        q.magic = q.shift = 0;
-      } else {   // (col_step = cols here: a row of more than 2^30 chunks goes alone)
-        q.cols = cols;
+        q.chunks = static_cast<unsigned>((q.mis + n_cols + unit - 1) / unit);
+        q.from = q.mis ? 1 : 0;
+        q.to = static_cast<unsigned>((q.mis + n_cols) / unit);
+      } else {   // (col_step = cols here: a longer row goes alone)
         q.per_row = static_cast<unsigned>(per_row);
         q.chunks = static_cast<unsigned>(per_row * n_rows);
         // i / d for i < 2^31, d >= 2: magic = ceil(2^(32 + s) / d) with 2^s >= d / 2 (Granlund and Montgomery)
@@ -91,15 +91,20 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
         q.shift = s;
         q.magic = static_cast<unsigned>(((1ull << (32 + s)) + q.per_row - 1) / q.per_row);
       }
-      const unsigned tile = kDropoutThreads * kDropoutUnroll;
+      const unsigned tile = kDropoutThreads * (vec ? 2 : 4);
       const unsigned grid = (q.chunks + tile - 1) / tile;
       LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        if (vec && residual) dropout_kernel<T, true, true><<<grid, kDropoutThreads, 0, stream>>>(q);
-        else if (vec) dropout_kernel<T, true, false><<<grid, kDropoutThreads, 0, stream>>>(q);
-        else if (residual) dropout_kernel<T, false, true><<<grid, kDropoutThreads, 0, stream>>>(q);
-        else dropout_kernel<T, false, false><<<grid, kDropoutThreads, 0, stream>>>(q);
+        constexpr int kVec = 16 / sizeof(T);
+        auto go = [&](auto kernel) { kernel<<<grid, kDropoutThreads, 0, stream>>>(q); };
+        if (n_rows == 1) {
+          if (vec) residual ? go(dropout_kernel<T, kVec, true, false>) : go(dropout_kernel<T, kVec, false, false>);
+          else residual ? go(dropout_kernel<T, 2, true, false>) : go(dropout_kernel<T, 2, false, false>);
+        } else {
+          if (vec) residual ? go(dropout_kernel<T, kVec, true, true>) : go(dropout_kernel<T, kVec, false, true>);
+          else residual ? go(dropout_kernel<T, 2, true, true>) : go(dropout_kernel<T, 2, false, true>);
+        }
       });
       ADAPT_LAUNCH_OK("dropout");
     }
