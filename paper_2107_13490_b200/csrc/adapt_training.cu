@@ -277,16 +277,17 @@ size_t scan_workspace(const ScanParams& q, bool backward) {
   return sizeof(float) * static_cast<size_t>(q.batch) * q.steps * (q.channels / kScanChannels);
 }
 
-// How many channels can be moved at a time: those of 16 bytes, two, or one.
+// Whether `unit` channels can be moved at a time.
+bool scan_fits(const ScanParams& q, int elem, int unit, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
+  if (q.channels % unit) return false;
+  for (const void* p : ptrs) if (misaligned(p, unit * elem)) return false;
+  for (long long s : strides) if (s % unit) return false;
+  return true;
+}
+
+// How many channels a tile kernel moves at a time: those of 16 bytes, two, or one.
 int scan_move(const ScanParams& q, int elem, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
-  int unit = 16 / elem;
-  auto fits = [&](int u) {
-    if (q.channels % u) return false;
-    for (const void* p : ptrs) if (misaligned(p, u * elem)) return false;
-    for (long long s : strides) if (s % u) return false;
-    return true;
-  };
-  return fits(unit) ? kMoveVec : fits(2) ? kMovePair : kMoveOne;
+  return scan_fits(q, elem, 16 / elem, ptrs, strides) ? kMoveVec : scan_fits(q, elem, 2, ptrs, strides) ? kMovePair : kMoveOne;
 }
 
 // CTAs of a tile kernel that the device holds at once, by kernel (first use: attributes and occupancy).
@@ -362,7 +363,12 @@ int launch_scan(DeviceCache& dc, const ScanKernel (&kernels)[3], int tensors, in
         {ADAPT_SCAN_WIDTHS(name, T, 1, 0), ADAPT_SCAN_WIDTHS(name, T, 1, 1), ADAPT_SCAN_WIDTHS(name, T, 1, 2)}}; \
     rc = launch_scan(*dc, kernels[mode][move], tensors, e, q, stream);                                 \
   }
-constexpr long long kSerialSteps = 4;
+// Short sequences take a thread for every four channels instead of tiles, which would be mostly empty.
+// Measured on bf16, us, serial against tiles: 256 x 16 x 4096 36 / 109, 256 x 32 x 4096 68 / 108,
+// 64 x 16 x 4096 12 / 29, 64 x 32 x 4096 31 / 29, 8 x 16 x 1024 8 / 8, 8 x 32 x 1024 17 / 8.
+bool scan_serial(const ScanParams& q) {
+  return q.steps <= 16 || (q.steps <= 32 && q.batch * q.channels >= (1 << 19));
+}
 
 // The caller's workspace, or the library's (grown on demand).
 int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, char** out) {
@@ -415,16 +421,20 @@ int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int
   int rc = current_cache(&dc);
   if (rc != ADAPT_OK) return rc;
   LaunchScope ls(ADAPT_KERNEL_SCAN, stream);
-  if (steps <= kSerialSteps) {
-    const unsigned grid = static_cast<unsigned>((batch * channels + 127) / 128);
+  const bool own = gate_group == 1;   // a gate for every channel
+  const std::initializer_list<const void*> ptrs = {x, y, own ? gate : nullptr};
+  const std::initializer_list<long long> lines = {q.xb, q.xt, q.yb, q.yt, own ? q.gb : 0, own ? q.gt : 0};
+  if (scan_serial(q)) {
+    const bool wide = scan_fits(q, e, 4, ptrs, lines) && (own || gate_group % 4 == 0);
+    const unsigned grid = static_cast<unsigned>((batch * channels / (wide ? 4 : 1) + 127) / 128);
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      if (mode == ADAPT_GATE_SIGMOID) scan_serial_kernel<T, kGateSigmoid><<<grid, 128, 0, stream>>>(q);
-      else scan_serial_kernel<T, kGateValue><<<grid, 128, 0, stream>>>(q);
+      auto go = [&](auto kernel) { kernel<<<grid, 128, 0, stream>>>(q); };
+      if (mode == ADAPT_GATE_SIGMOID) wide ? go(scan_serial_kernel<T, kGateSigmoid, 4>) : go(scan_serial_kernel<T, kGateSigmoid, 1>);
+      else wide ? go(scan_serial_kernel<T, kGateValue, 4>) : go(scan_serial_kernel<T, kGateValue, 1>);
     });
   } else {
-    const int move = scan_move(q, e, {x, y, gate_group == 1 ? gate : nullptr},
-                                  {q.xb, q.xt, q.yb, q.yt, gate_group == 1 ? q.gb : 0, gate_group == 1 ? q.gt : 0});
+    const int move = scan_move(q, e, ptrs, lines);
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
       ADAPT_SCAN_LAUNCH(scan_kernel, T, 2);

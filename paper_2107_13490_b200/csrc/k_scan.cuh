@@ -65,30 +65,69 @@ __device__ __forceinline__ void gate_coefs2(f32x2 g, f32x2& a, f32x2& c) {
   c = mul2(e, a);
 }
 
-// ---- short sequences: one thread a channel, step after step ------------------------------------
+// ---- short sequences: a thread runs through the steps of one or four channels -------------------------
 
-template <typename T, int kMode>
+constexpr int kSerialAhead = 4;   // steps whose inputs are under way
+
+template <typename T, int kWide> struct __align__(kWide * sizeof(T)) ScanWide { T v[kWide]; };
+
+template <typename T, int kMode, int kWide>
 __global__ void __launch_bounds__(128) scan_serial_kernel(const ScanParams p) {
+  typedef ScanWide<T, kWide> Wide;
+  const int threads = static_cast<int>(p.channels / kWide);   // of a sequence
   const long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (i >= p.batch * p.channels) return;
-  const long long b = i / p.channels, d = i - b * p.channels;
-  const long long len = p.lengths ? min(max(static_cast<long long>(p.lengths[b]), 0ll), p.steps) : p.steps;
+  if (i >= p.batch * threads) return;
+  const long long b = i / threads;
+  const int d = static_cast<int>(i - b * threads) * kWide, steps = static_cast<int>(p.steps);
+  const int len = p.lengths ? min(max(p.lengths[b], 0), steps) : steps;
   const T* x = static_cast<const T*>(p.x) + b * p.xb + d;
-  const T* g = static_cast<const T*>(p.gate) + b * p.gb + d / p.group;
+  const bool shared_gate = p.group > 1;   // (then one gate serves all of the thread's channels)
+  const T* g = static_cast<const T*>(p.gate) + b * p.gb + (shared_gate ? d / p.group : d);
   T* y = static_cast<T*>(p.y) + b * p.yb + d;
-  float h = p.h0 ? p.h0[i] : 0.0f;
-  const long long tiles = (p.steps + kScanTile - 1) / kScanTile;
-  for (long long t = 0; t < p.steps; ++t) {
-    if (p.carry && t % kScanTile == 0) p.carry[(b * tiles + t / kScanTile) * p.channels + d] = h;
-    if (t >= len) { y[t * p.yt] = from_float<T>(0.0f); continue; }
-    float a, c;
-    gate_coefs<kMode>(to_float(g[t * p.gt]), a, c);
-    const bool cut = p.reset && p.reset[b * p.steps + t];
-    const float u = kMode == kGateValue ? to_float(x[t * p.xt]) : c * to_float(x[t * p.xt]);
-    h = cut ? u : fmaf(a, h, u);
-    y[t * p.yt] = from_float<T>(h);
+  const unsigned char* reset = p.reset ? p.reset + b * p.steps : nullptr;
+  float h[kWide];
+#pragma unroll
+  for (int j = 0; j < kWide; ++j) h[j] = p.h0 ? p.h0[b * p.channels + d + j] : 0.0f;
+  const int tiles = (steps + kScanTile - 1) / kScanTile;
+  for (int t0 = 0; t0 < steps; t0 += kSerialAhead) {
+    Wide xv[kSerialAhead], gv[kSerialAhead];
+    bool cut[kSerialAhead];
+#pragma unroll
+    for (int k = 0; k < kSerialAhead; ++k) {
+      const int t = t0 + k;
+      if (t >= len) continue;
+      xv[k] = *reinterpret_cast<const Wide*>(x + t * p.xt);
+      if (shared_gate) gv[k].v[0] = g[t * p.gt];
+      else gv[k] = *reinterpret_cast<const Wide*>(g + t * p.gt);
+      cut[k] = reset && reset[t];
+    }
+#pragma unroll
+    for (int k = 0; k < kSerialAhead; ++k) {
+      const int t = t0 + k;
+      if (t >= steps) break;
+      if (p.carry && t % kScanTile == 0) {
+        float* at = p.carry + (b * tiles + t / kScanTile) * p.channels + d;
+#pragma unroll
+        for (int j = 0; j < kWide; ++j) at[j] = h[j];
+      }
+      Wide out;
+#pragma unroll
+      for (int j = 0; j < kWide; ++j) {
+        out.v[j] = from_float<T>(0.0f);
+        if (t >= len) continue;
+        float a, c;
+        gate_coefs<kMode>(to_float(gv[k].v[shared_gate ? 0 : j]), a, c);
+        const float u = kMode == kGateValue ? to_float(xv[k].v[j]) : c * to_float(xv[k].v[j]);
+        h[j] = cut[k] ? u : fmaf(a, h[j], u);
+        out.v[j] = from_float<T>(h[j]);
+      }
+      *reinterpret_cast<Wide*>(y + t * p.yt) = out;
+    }
   }
-  if (p.h_last) p.h_last[i] = h;
+  if (p.h_last) {
+#pragma unroll
+    for (int j = 0; j < kWide; ++j) p.h_last[b * p.channels + d + j] = h[j];
+  }
 }
 
 // ---- tiles -------------------------------------------------------------------------------------
