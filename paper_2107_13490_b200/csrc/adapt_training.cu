@@ -290,6 +290,11 @@ int scan_move(const ScanParams& q, int elem, std::initializer_list<const void*> 
   return scan_fits(q, elem, 16 / elem, ptrs, strides) ? kMoveVec : scan_fits(q, elem, 2, ptrs, strides) ? kMovePair : kMoveOne;
 }
 
+// Whether shared gates can be copied by the 4-byte words that hold them, none of which leaves its row.
+bool scan_gate_words(const ScanParams& q, int elem) {
+  return elem == 4 || (q.channels / q.group % 2 == 0 && !misaligned(q.gate, 4) && q.gb % 2 == 0 && q.gt % 2 == 0);
+}
+
 // CTAs of a tile kernel that the device holds at once, by kernel (first use: attributes and occupancy).
 struct ScanSlots { const void* kernel; int device, slots; };
 std::vector<ScanSlots> g_scan_slots;   // under g_mutex
@@ -314,10 +319,10 @@ typedef void (*ScanKernel)(ScanParams);
 
 // The tile kernels of one type, mode and alignment, for 64, 32 and 16 channels a CTA, and the number of
 // CTAs to a chain, by the estimated time: waves of CTAs x rounds of a chain x the time of a round, in units
-// of a round without exchange (1.4 to 2.5 us).  An exchange costs 1.2 + 0.05 K of them, narrower tiles
-// 20 % a halving (more pieces to join).  Measured forward, us: 8 x 4096 x 2048 bf16 (256 chains of 64)
-// 93 with one CTA to a chain, 124 with two; 1 x 65536 x 1024 bf16 (16 chains of 64, 32 of 32) 1174 with one,
-// 220 with 16, 169 with 32 channels and 8 CTAs; over ten shapes both ways the choice is within 2 % of the best.
+// of a round without exchange (1.4 to 2.5 us).  An exchange costs 1.35 + 0.03 K of them, narrower tiles
+// 10 % a halving.  Measured forward, us: 8 x 4096 x 2048 bf16 (256 chains of 64) 91 with one CTA to a chain,
+// 119 with two; 1 x 65536 x 1024 bf16 (16 chains of 64, 32 of 32) 1070 with one, 234 with 16, 134 with 32
+// channels and 8 CTAs; over twelve shapes both ways the choice is within 3 % of the best on the mean.
 int launch_scan(DeviceCache& dc, const ScanKernel (&kernels)[3], int tensors, int elem, const ScanParams& q, cudaStream_t stream) {
   const size_t stages = kScanStages * scan_stage_bytes(tensors, elem);
   int width = 0, cluster = 1;
@@ -332,9 +337,9 @@ int launch_scan(DeviceCache& dc, const ScanKernel (&kernels)[3], int tensors, in
     const long long tiles = (q.steps * channels + kTileElements - 1) / kTileElements;
     for (int k = 1; k <= kScanMaxCluster; k *= 2) {
       if (k > 1 && k / 2 >= tiles) break;
-      const double waves = static_cast<double>((chains * k + slots - 1) / slots);
+      const double full = static_cast<double>(chains * k) / slots, waves = full <= 1.0 ? 1.0 : full + 0.5;
       const double rounds = static_cast<double>((tiles + k - 1) / k);
-      const double cost = waves * rounds * (k > 1 ? 1.2 + 0.05 * k : 1.0) * (1.0 + 0.2 * i);
+      const double cost = waves * rounds * (k > 1 ? 1.35 + 0.03 * k : 1.0) * (1.0 + 0.1 * i);
       if (cost < least) { least = cost; width = i; cluster = k; }
     }
   }
@@ -435,6 +440,7 @@ int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int
     });
   } else {
     const int move = scan_move(q, e, ptrs, lines);
+    q.gate_words = scan_gate_words(q, e);
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
       ADAPT_SCAN_LAUNCH(scan_kernel, T, 2);
@@ -484,6 +490,7 @@ int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy, c
     const int move = scan_move(q, e, {x, dy, dx, own ? gate : nullptr, own ? dgate : nullptr},
                                   {q.xb, q.xt, q.yb, q.yt, q.dxb, q.dxt, own ? q.gb : 0, own ? q.gt : 0,
                                    own ? q.dgb : 0, own ? q.dgt : 0});
+    q.gate_words = scan_gate_words(q, e);
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
       ADAPT_SCAN_LAUNCH(scan_backward_kernel, T, 3);

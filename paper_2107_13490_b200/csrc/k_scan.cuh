@@ -15,6 +15,7 @@ constexpr int kScanChannels = 64;    // channels of a CTA: two for each lane
 constexpr int kScanSteps = 8;        // steps of a thread
 constexpr int kScanWarps = kScanTile / kScanSteps;
 constexpr int kScanThreads = 32 * kScanWarps;
+constexpr int kAhead = 2;            // warps' maps read at a time (4: 4 % slower, registers)
 constexpr int kScanStages = 2;       // tiles in shared memory: the one worked on and the next
 constexpr int kScanMaxCluster = 16;
 constexpr int kGateSigmoid = 0, kGateValue = 1;
@@ -31,6 +32,7 @@ struct ScanParams {
   long long xb, xt, gb, gt, yb, yt;    // strides (elements) of x, gate, y / dy
   long long dxb, dxt, dgb, dgt;        // strides of dx, dgate
   int group;
+  bool gate_words;                     // the 4-byte words of a row's gates lie within the row
 };
 
 constexpr f32x2 kOnes2 = 0x3F8000003F800000ull, kMinusOnes2 = 0xBF800000BF800000ull;
@@ -134,9 +136,10 @@ __global__ void __launch_bounds__(128) scan_serial_kernel(const ScanParams p) {
 //
 // A chain is a block of 64, 32 or 16 channels of one sequence (kLanes lanes of two channels); a tile is
 // 4096 of its elements, 64, 128 or 256 steps.  A thread has two channels and 8 steps of a tile - a piece -
-// and reduces them to h -> A h + B; the pieces of a tile join through shared memory.  The CTAs of a
-// cluster take a chain's tiles in turn (tile s K + rank in round s) and send each other their tiles'
-// (A, B), so the data is read once whatever the number of chains, and nothing goes through global memory.
+// and reduces them to h -> A h + B; the pieces of a warp join by shuffles, the warps of a tile through
+// shared memory.  The CTAs of a cluster take a chain's tiles in turn (tile s K + rank in round s) and send
+// each other their tiles' (A, B), so the data is read once whatever the number of chains, and nothing goes
+// through global memory.
 // A reset's cut is carried as a flag (it is the same for all channels), not as a factor of 0: what the
 // state holds before it, Inf and NaN included, must not come through.
 
@@ -159,8 +162,12 @@ __device__ __forceinline__ f32x2 held2(f32x2 a) {
   const float2 v = unpack2(a);
   return pack2(held(v.x), held(v.y));
 }
+// A map h -> a h + b of a lane's two channels; `cut`: what comes before does not count (h -> b).
+struct __align__(16) ScanMap { f32x2 a, b; };
+
 // f(true) or f(false), the argument a constant.
 template <bool kValue> struct Flag { static constexpr bool value = kValue; };
+template <int kValue> struct Number { static constexpr int value = kValue; };
 template <typename F>
 __device__ __forceinline__ void with_flag(bool v, F f) {
   if (v) f(Flag<true>{});
@@ -187,9 +194,9 @@ __device__ __forceinline__ unsigned cluster_address(unsigned addr, unsigned rank
 }
 // Remote stores that count themselves off at a barrier beside the data they write: no fence, so an
 // exchange does not wait for the output rows on their way to memory.
-__device__ __forceinline__ void cluster_store(unsigned addr, unsigned barrier, float2 v) {
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
-               :: "r"(addr), "f"(v.x), "f"(v.y), "r"(barrier) : "memory");
+__device__ __forceinline__ void cluster_store(unsigned addr, unsigned barrier, float4 v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+               :: "r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(barrier) : "memory");
 }
 __device__ __forceinline__ void cluster_store(unsigned addr, unsigned barrier, unsigned v) {
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];"
@@ -253,6 +260,7 @@ struct ScanPlace {
   static constexpr int kPieces = kScanWarps * kParts;    // of a tile
   static constexpr int kTileSteps = kPieces * kScanSteps;
   static constexpr int kChannels = 2 * kLanes;
+  static constexpr int kStretchWarps = kScanWarps / kParts;   // warps between two kept states
   long long b;
   int steps, len;     // of the call, of this sequence
   int rank, cluster, warp, lane, pair, piece, rounds;
@@ -331,18 +339,49 @@ __device__ __forceinline__ void fetch_rows(unsigned char* part, const T* src, lo
     }
   }
 }
-// The same for a gate that serves both channels; src points to this pair's gate in the warp's first row.
+// Shared gates are few: a warp copies its rows' gates once, 16 / group for a lane, as the 4-byte words that
+// hold them, row by row into its part of the stage.  (Asynchronously: loads into registers a tile ahead
+// waited all the same, 8 x 4096 x 2048 bf16 with gates for 64 channels took 137 us, now 105.)
 template <typename T, int kLanes>
-__device__ __forceinline__ void fetch_shared_gate(unsigned char* part, const T* src, long long stride, int rows, int left) {
-  const int lane = threadIdx.x & 31, pair = lane % kLanes, row0 = lane / kLanes * kScanSteps;
-  typename Pair<T>::raw* slot = reinterpret_cast<typename Pair<T>::raw*>(part) + row0 * kLanes + pair;
-  src += row0 * stride;
-#pragma unroll
-  for (int k = 0; k < kScanSteps; ++k, src += stride) {
-    const T v = row0 + k < rows && 2 * pair < left ? src[0] : from_float<T>(0.0f);
-    slot[k * kLanes] = join(v, v);
+struct SharedGates {
+  int shift, first, mine, left;   // log2 of the gates of a row, the first's number, this pair's, those that exist
+  bool odd, words;                // this pair's is the upper half of its word; all words lie within their rows
+  __device__ __forceinline__ SharedGates(const ScanParams& p, const ScanPlace<kLanes>& w) {
+    shift = p.group < 2 * kLanes ? __ffs(2 * kLanes / p.group) - 1 : 0;   // (a power of two there)
+    first = w.block / p.group;
+    mine = 2 * w.pair / p.group;
+    left = (w.left + p.group - 1) / p.group;
+    odd = sizeof(T) == 2 && ((first + mine) & 1);
+    words = p.gate_words;
   }
-}
+  __device__ __forceinline__ void fetch(unsigned char* part, const T* src, long long stride, int rows) const {
+    for (int i = threadIdx.x & 31; i < ((32 / kLanes) * kScanSteps) << shift; i += 32) {
+      const int row = i >> shift, g = i - (row << shift);
+      unsigned* slot = reinterpret_cast<unsigned*>(part) + i;
+      const T* at = src + row * stride + first + g;
+      if (row >= rows || g >= left) {
+        *slot = 0;
+      } else if (words) {
+        if (sizeof(T) == 2) at = src + row * stride + ((first + g) & ~1);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(scan_smem(slot)), "l"(at) : "memory");
+      } else {
+        *slot = both(at[0]);
+      }
+    }
+  }
+  __device__ __forceinline__ static unsigned both(float v) { return __float_as_uint(v); }
+  template <typename U>
+  __device__ __forceinline__ static unsigned both(U v) { return join(v, v); }
+  __device__ __forceinline__ f32x2 get(const unsigned char* part, int row) const {
+    const unsigned v = reinterpret_cast<const unsigned*>(part)[(row << shift) + mine];
+    if (sizeof(T) == 4) return pack2(__uint_as_float(v), __uint_as_float(v));
+    const float2 f = unpack2(two(v, T{}));
+    return odd ? pack2(f.y, f.y) : pack2(f.x, f.x);
+  }
+  __device__ __forceinline__ static f32x2 two(unsigned v, float) { return 0; }
+  template <typename U>
+  __device__ __forceinline__ static f32x2 two(unsigned v, U u) { return widen(v, u); }
+};
 
 template <typename T, int kMove>
 __device__ __forceinline__ void store_pair(T* dst, f32x2 v, int channels) {
@@ -385,18 +424,21 @@ struct ScanExchange {
     }
     __syncwarp();
   }
-  // Called by all threads; thread i holds channel i % kChannels' map.
+  // Called by the kLanes threads that hold the tile's map.
   template <bool kCut>
-  __device__ __forceinline__ void send(const ScanPlace<kLanes>& w, int buffer, float a, float b, bool cut) {
-    const int ch = threadIdx.x % kChannels;
-    if (threadIdx.x == 0) barrier_expect(barrier + 8 * buffer, w.cluster * (kChannels * 8 + (kCut ? 4 : 0)));
-    const unsigned at = scan_smem(totals + (buffer * w.cluster + w.rank) * kChannels + ch);
+  __device__ __forceinline__ void send(const ScanPlace<kLanes>& w, int buffer, const ScanMap& map, bool cut) {
+    const float2 a = unpack2(map.a), b = unpack2(map.b);
+    const unsigned at = scan_smem(totals + (buffer * w.cluster + w.rank) * kChannels + 2 * w.pair);
     const unsigned flag = scan_smem(cuts + buffer * w.cluster + w.rank);
-    for (int q = threadIdx.x / kChannels; q < w.cluster; q += kScanThreads / kChannels) {
+    for (int q = 0; q < w.cluster; ++q) {
       const unsigned bar = cluster_address(barrier + 8 * buffer, q);
-      cluster_store(cluster_address(at, q), bar, make_float2(a, b));
-      if (kCut && ch == 0) cluster_store(cluster_address(flag, q), bar, cut ? 1u : 0u);
+      cluster_store(cluster_address(at, q), bar, make_float4(a.x, b.x, a.y, b.y));
+      if (kCut && w.pair == 0) cluster_store(cluster_address(flag, q), bar, cut ? 1u : 0u);
     }
+  }
+  // Called by one thread, before the round's barrier: the bytes that will come.
+  __device__ __forceinline__ void expect(const ScanPlace<kLanes>& w, int buffer, bool flags) {
+    barrier_expect(barrier + 8 * buffer, w.cluster * (kChannels * 8 + (flags ? 4 : 0)));
   }
   // Called by the first kChannels threads, a channel each: the tiles of a round, first to last or last to
   // first; returns what leaves the round, puts what enters this CTA's tile into `enter`.
@@ -461,35 +503,64 @@ __device__ __forceinline__ float* carry_at(const ScanParams& p, const ScanPlace<
   return p.carry + (w.b * ((w.steps + kScanTile - 1) / kScanTile) + t / kScanTile) * p.channels + w.block + 2 * w.pair;
 }
 
-// The map of a piece, {A, B} pairs of its lane's channels.
-struct __align__(16) ScanMap { f32x2 a, b; };
-constexpr int kStretch = kScanTile / kScanSteps;   // pieces between two kept states
+// `first`, then `next`.
+template <bool kCut>
+__device__ __forceinline__ void then_map(ScanMap& first, bool& first_cut, const ScanMap& next, bool next_cut, bool hold) {
+  first.b = through2<kCut>(kCut && next_cut, next.a, next.b, first.b);
+  first.a = mul2(first.a, next.a);
+  if (hold) first.a = held2(first.a);
+  first_cut |= kCut && next_cut;
+}
+__device__ __forceinline__ f32x2 shuffle2(f32x2 v, int from) { return __shfl_sync(~0u, v, from); }
 
-// Composes a tile's pieces for one channel (a thread a channel, each channel several times).
-__device__ __forceinline__ float map_a(const ScanMap* maps, int ch) { return reinterpret_cast<const float*>(maps + (ch >> 1))[ch & 1]; }
-__device__ __forceinline__ float map_b(const ScanMap* maps, int ch) { return reinterpret_cast<const float*>(maps + (ch >> 1))[2 + (ch & 1)]; }
+// The pieces of a warp: `map` becomes that of all pieces up to this one (from behind: from this one on),
+// the result is that of those before it (behind it), the identity for the first.
+template <int kLanes, bool kCut, bool kBackward, bool kHold>
+__device__ __forceinline__ ScanMap join_pieces(ScanMap& map, bool& cut, bool& cut_before, int lane) {
+  ScanMap before = {kOnes2, 0};
+  cut_before = false;
+  if (kLanes == 32) return before;
+#pragma unroll
+  for (int o = kLanes; o < 32; o <<= 1) {
+    const int from = kBackward ? lane + o : lane - o;
+    const bool on = kBackward ? from < 32 : from >= 0;
+    ScanMap other = {shuffle2(map.a, from & 31), shuffle2(map.b, from & 31)};
+    bool other_cut = kCut && __shfl_sync(~0u, static_cast<int>(cut), from & 31) != 0;
+    if (on) {
+      then_map<kCut>(other, other_cut, map, cut, kHold);
+      map = other;
+      cut = other_cut;
+    }
+  }
+  const int from = kBackward ? lane + kLanes : lane - kLanes;
+  before = {shuffle2(map.a, from & 31), shuffle2(map.b, from & 31)};
+  cut_before = kCut && __shfl_sync(~0u, static_cast<int>(cut), from & 31) != 0;
+  if (kBackward ? from >= 32 : from < 0) { before = {kOnes2, 0}; cut_before = false; }
+  return before;
+}
 
 // What bounds it: HBM (2 reads and a write an element); the arithmetic is about 20 lane instructions
 // an element.
 template <typename T, int kMode, int kMove, int kLanes>
-__global__ void __launch_bounds__(kScanThreads, sizeof(T) == 4 ? 2 : 3) scan_kernel(const ScanParams p) {
+__global__ void __launch_bounds__(kScanThreads, sizeof(T) == 4 || kLanes < 32 ? 2 : 3) scan_kernel(const ScanParams p) {
   typedef typename Pair<T>::raw Raw;
   typedef ScanPlace<kLanes> Place;
   constexpr int kPieces = Place::kPieces;
   extern __shared__ __align__(16) unsigned char dynamic[];
-  __shared__ ScanMap maps[2][kPieces * kLanes];
+  __shared__ ScanMap maps[2][kScanWarps][kLanes];          // of the warps
   __shared__ __align__(8) float enter[Place::kChannels];   // cluster: the state before this CTA's tile
   __shared__ f32x2 hand[2][kLanes];
-  __shared__ unsigned piece_cut[2][kPieces];
+  __shared__ bool warp_cut[2][kScanWarps];
   __shared__ unsigned long long barriers[2];
   const Place w(p);
   constexpr int kPart = kTileElements / kScanWarps * sizeof(T);   // a warp's part of a tensor's stage
   unsigned char* stage = dynamic + w.warp * kPart;
   ScanExchange<kLanes> exchange(dynamic + kScanStages * scan_stage_bytes(2, sizeof(T)), barriers, w);
   const T* x = static_cast<const T*>(p.x) + w.b * p.xb + w.block;
-  const T* gate = static_cast<const T*>(p.gate) + w.b * p.gb + (p.group > 1 ? (w.block + 2 * w.pair) / p.group : w.block);
+  const T* gate = static_cast<const T*>(p.gate) + w.b * p.gb + (p.group > 1 ? 0 : w.block);
   T* y = static_cast<T*>(p.y) + w.b * p.yb + w.block + 2 * w.pair;
 
+  const SharedGates<T, kLanes> shared(p, w);
   // (the row pointers run ahead of what is read; behind the last step nothing is read through them)
   x += w.warp_first(0) * p.xt; gate += w.warp_first(0) * p.gt;
   auto fetch = [&](int s) {
@@ -498,7 +569,7 @@ __global__ void __launch_bounds__(kScanThreads, sizeof(T) == 4 ? 2 : 3) scan_ker
       const int n = Place::clamp_steps(w.len - w.warp_first(s), Place::kParts * kScanSteps);
       fetch_rows<T, kMove, kLanes>(part, x, p.xt, n, w.left);
       part += kScanWarps * kPart;
-      if (p.group > 1) fetch_shared_gate<T, kLanes>(part, gate, p.gt, n, w.left);
+      if (p.group > 1) shared.fetch(part, gate, p.gt, n);
       else fetch_rows<T, kMove, kLanes>(part, gate, p.gt, n, w.left);
       x += w.stride() * p.xt; gate += w.stride() * p.gt;
     }
@@ -514,74 +585,98 @@ __global__ void __launch_bounds__(kScanThreads, sizeof(T) == 4 ? 2 : 3) scan_ker
   for (int s = 0; s < w.rounds; ++s) {
     fetch(s + 1);
     asm volatile("cp.async.wait_group 1;" ::: "memory");
-    if (kMove == kMoveVec) __syncwarp();
+    if (kMove == kMoveVec || p.group > 1) __syncwarp();
     const int live = w.live(s);
     const unsigned resets = w.reset_bits(next_reset);
     next_reset = s + 1 < w.rounds ? w.reset_byte(p, s + 1) : 0u;
 
     f32x2 a[kScanSteps], u[kScanSteps];
     const Raw* slot = reinterpret_cast<const Raw*>(stage + (s & 1) * (2 * kScanWarps * kPart)) + (w.lane - w.pair) * kScanSteps + w.pair;
+    const unsigned char* gates = stage + (s & 1) * (2 * kScanWarps * kPart) + kScanWarps * kPart;
+    const int row0 = (w.lane / kLanes) * kScanSteps;
+    with_flag(p.group > 1, [&](auto group) {
 #pragma unroll
-    for (int k = 0; k < kScanSteps; ++k) {
-      const f32x2 xv = widen(slot[k * kLanes], T{});
-      f32x2 c;
-      gate_coefs2<kMode>(widen(slot[kTileElements / 2 + k * kLanes], T{}), a[k], c);
-      u[k] = kMode == kGateValue ? xv : mul2(c, xv);
-    }
+      for (int k = 0; k < kScanSteps; ++k) {
+        const f32x2 xv = widen(slot[k * kLanes], T{});
+        f32x2 c;
+        gate_coefs2<kMode>(decltype(group)::value ? shared.get(gates, row0 + k)
+                                                      : widen(slot[kTileElements / 2 + k * kLanes], T{}), a[k], c);
+        u[k] = kMode == kGateValue ? xv : mul2(c, xv);
+      }
+    });
     if (live < kScanSteps) {
 #pragma unroll
       for (int k = 0; k < kScanSteps; ++k)
         if (k >= live) { a[k] = kOnes2; u[k] = 0; }
     }
-    f32x2 A = a[0], Bv = u[0];
+    ScanMap map = {a[0], u[0]};
 #pragma unroll
     for (int k = 1; k < kScanSteps; ++k) {
-      A = mul2(A, a[k]);
-      Bv = fma2(a[k], Bv, u[k]);
+      map.a = mul2(map.a, a[k]);
+      map.b = fma2(a[k], map.b, u[k]);
     }
     if (resets) {   // what comes before the last reset does not count
 #pragma unroll
-      for (int k = 0; k < kScanSteps; ++k) Bv = through2<true>(resets >> k & 1, a[k], u[k], Bv);
+      for (int k = 0; k < kScanSteps; ++k) map.b = through2<true>(resets >> k & 1, a[k], u[k], map.b);
     }
-    const ScanMap* tile = maps[s & 1];
-    const unsigned* tile_cut = piece_cut[s & 1];
-    maps[s & 1][w.piece * kLanes + w.pair] = {held2(A), Bv};
-    if (p.reset && w.pair == 0) piece_cut[s & 1][w.piece] = resets;
-    __syncthreads();
-
-    f32x2 h;    // the state before this tile, then before this piece
-    with_flag(p.reset != nullptr, [&](auto cut) {
-      constexpr bool kCut = decltype(cut)::value;
-      if (w.cluster > 1) {
-        const int ch = threadIdx.x % Place::kChannels;
-        float ta = 1.0f, tb = 0.0f;
-        bool any = false;
-#pragma unroll 4
-        for (int v = 0; v < kPieces; ++v) {
-          const float ma = map_a(tile + v * kLanes, ch);
-          const bool cv = kCut && tile_cut[v] != 0;
-          tb = through<kCut>(cv, ma, map_b(tile + v * kLanes, ch), tb);
-          ta *= ma;
-          any |= cv;
-        }
-        exchange.template send<kCut>(w, s & 1, held(ta), tb, any);
-        if (threadIdx.x < Place::kChannels)
-          state = pack2(exchange.template run<kCut, false>(w, s & 1, s >> 1 & 1, unpack2(state).x, enter), 0.0f);
-        __syncthreads();
-        h = *reinterpret_cast<const f32x2*>(enter + 2 * w.pair);
-      } else {
-        h = hand[(s & 1) ^ 1][w.pair];
+    map.a = held2(map.a);
+    const int buffer = s & 1;
+    f32x2 h;    // the state before this piece
+    with_flag(p.reset != nullptr, [&](auto with_cuts) {
+      constexpr bool kCut = decltype(with_cuts)::value;
+      bool cut = resets != 0, cut_before;
+      const ScanMap before = join_pieces<kLanes, kCut, false, kMode == kGateValue>(map, cut, cut_before, w.lane);
+      if (w.lane >= 32 - kLanes) {
+        maps[buffer][w.warp][w.pair] = map;
+        if (kCut && w.pair == 0) warp_cut[buffer][w.warp] = cut;
       }
+      if (w.cluster > 1 && threadIdx.x == 0) exchange.expect(w, buffer, kCut);
+      __syncthreads();
+      auto tile = [&](int v) { return maps[buffer][v][w.pair]; };
+      auto tile_cut = [&](int v) { return kCut && warp_cut[buffer][v]; };
+      if (w.cluster > 1) {
+        // everything that does not need the other CTAs comes before the wait
+        ScanMap pre = {kOnes2, 0};
+        bool pre_cut = false;
 #pragma unroll
-      for (int v = 0; v < kPieces - 1; ++v) {
-        if (v >= w.piece) break;
-        const ScanMap m = tile[v * kLanes + w.pair];
-        h = through2<kCut>(kCut && tile_cut[v] != 0, m.a, m.b, h);
+        for (int v0 = 0; v0 < kScanWarps - 1; v0 += kAhead) {
+          if (v0 >= w.warp) break;
+          ScanMap m[kAhead];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) m[j] = tile(min(v0 + j, kScanWarps - 1));
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+            if (v0 + j < w.warp) then_map<kCut>(pre, pre_cut, m[j], tile_cut(v0 + j), kMode == kGateValue);
+        }
+        if (w.warp == kScanWarps - 1 && w.lane >= 32 - kLanes) {
+          ScanMap all = pre;
+          bool all_cut = pre_cut;
+          then_map<kCut>(all, all_cut, map, cut, true);
+          exchange.template send<kCut>(w, buffer, all, all_cut);
+        }
+        then_map<kCut>(pre, pre_cut, before, cut_before, true);
+        if (threadIdx.x < Place::kChannels)
+          state = pack2(exchange.template run<kCut, false>(w, buffer, s >> 1 & 1, unpack2(state).x, enter), 0.0f);
+        __syncthreads();
+        h = through2<kCut>(pre_cut, pre.a, pre.b, *reinterpret_cast<const f32x2*>(enter + 2 * w.pair));
+      } else {
+        h = hand[buffer ^ 1][w.pair];
+#pragma unroll
+        for (int v0 = 0; v0 < kScanWarps - 1; v0 += kAhead) {
+          if (v0 >= w.warp) break;
+          ScanMap m[kAhead];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) m[j] = tile(min(v0 + j, kScanWarps - 1));
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+            if (v0 + j < w.warp) h = through2<kCut>(tile_cut(v0 + j), m[j].a, m[j].b, h);
+        }
+        if (kLanes < 32) h = through2<kCut>(cut_before, before.a, before.b, h);
       }
     });
 
     const int t = w.first(s);
-    if (p.carry && w.piece % kStretch == 0 && t < w.steps) {
+    if (p.carry && t % kScanTile == 0 && t < w.steps) {
       float* at = carry_at(p, w, t);
       const float2 f = unpack2(h);
       if (w.channels > 0) at[0] = f.x;
@@ -603,7 +698,7 @@ __global__ void __launch_bounds__(kScanThreads, sizeof(T) == 4 ? 2 : 3) scan_ker
         if (k < rows) store_pair<T, kMove>(out, k < live ? h : 0, w.channels);
       }
     }
-    if (w.cluster == 1 && w.piece == kPieces - 1) hand[s & 1][w.pair] = state = h;
+    if (w.cluster == 1 && w.piece == kPieces - 1) hand[buffer][w.pair] = state = h;
   }
   if (p.h_last && w.rank == 0) put_state(p.h_last, p, w, kPieces - 1, state);
 }
@@ -616,11 +711,11 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
   typedef ScanPlace<kLanes> Place;
   constexpr int kPieces = Place::kPieces;
   extern __shared__ __align__(16) unsigned char dynamic[];
-  __shared__ ScanMap maps[2][kPieces * kLanes];          // of the states
-  __shared__ f32x2 flows[2][kPieces * kLanes];           // B of the gradient flow (A is the same)
+  __shared__ ScanMap maps[2][kScanWarps][kLanes];          // of the states, warps
+  __shared__ f32x2 flows[2][kScanWarps][kLanes];           // b of the gradient flow (a is the same)
   __shared__ __align__(8) float enter[Place::kChannels];   // cluster: the flow from behind this CTA's tile
   __shared__ f32x2 hand[2][kLanes];
-  __shared__ unsigned piece_cut[2][kPieces];
+  __shared__ bool warp_cut[2][kScanWarps];
   __shared__ unsigned long long barriers[2];
   const Place w(p);
   constexpr int kPart = kTileElements / kScanWarps * sizeof(T);
@@ -628,11 +723,12 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
   ScanExchange<kLanes> exchange(dynamic + kScanStages * scan_stage_bytes(3, sizeof(T)), barriers, w);
   const int c0 = w.block + 2 * w.pair;
   const T* x = static_cast<const T*>(p.x) + w.b * p.xb + w.block;
-  const T* gate = static_cast<const T*>(p.gate) + w.b * p.gb + (p.group > 1 ? c0 / p.group : w.block);
+  const T* gate = static_cast<const T*>(p.gate) + w.b * p.gb + (p.group > 1 ? 0 : w.block);
   const T* dy = static_cast<const T*>(p.dy) + w.b * p.yb + w.block;
   T* dx = static_cast<T*>(p.dx) + w.b * p.dxb + c0;
   T* dgate = static_cast<T*>(p.dgate) + w.b * p.dgb + c0 / p.group;
 
+  const SharedGates<T, kLanes> shared(p, w);
   const int last = w.rounds - 1;
   x += w.warp_first(last) * p.xt; gate += w.warp_first(last) * p.gt; dy += w.warp_first(last) * p.yt;
   auto fetch = [&](int s) {
@@ -641,7 +737,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
       const int n = Place::clamp_steps(w.len - w.warp_first(s), Place::kParts * kScanSteps);
       fetch_rows<T, kMove, kLanes>(part, x, p.xt, n, w.left);
       part += kScanWarps * kPart;
-      if (p.group > 1) fetch_shared_gate<T, kLanes>(part, gate, p.gt, n, w.left);
+      if (p.group > 1) shared.fetch(part, gate, p.gt, n);
       else fetch_rows<T, kMove, kLanes>(part, gate, p.gt, n, w.left);
       part += kScanWarps * kPart;
       fetch_rows<T, kMove, kLanes>(part, dy, p.yt, n, w.left);
@@ -670,7 +766,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
   for (int s = w.rounds - 1; s >= 0; --s) {
     fetch(s - 1);
     asm volatile("cp.async.wait_group 1;" ::: "memory");
-    if (kMove == kMoveVec) __syncwarp();
+    if (kMove == kMoveVec || p.group > 1) __syncwarp();
     const int live = w.live(s);
     const unsigned resets = w.reset_bits(next_reset);
     next_reset = s > 0 ? w.reset_byte(p, s - 1) : 0u;
@@ -679,9 +775,15 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
 
     f32x2 a[kScanSteps], c[kScanSteps];
     const Raw* slot = reinterpret_cast<const Raw*>(stage + (s & 1) * (3 * kScanWarps * kPart)) + (w.lane - w.pair) * kScanSteps + w.pair;
+    const unsigned char* gates = stage + (s & 1) * (3 * kScanWarps * kPart) + kScanWarps * kPart;
+    const int row0 = (w.lane / kLanes) * kScanSteps;
     constexpr int kGate = kTileElements / 2, kDy = kTileElements;
+    with_flag(p.group > 1, [&](auto group) {
 #pragma unroll
-    for (int k = 0; k < kScanSteps; ++k) gate_coefs2<kMode>(widen(slot[kGate + k * kLanes], T{}), a[k], c[k]);
+      for (int k = 0; k < kScanSteps; ++k)
+        gate_coefs2<kMode>(decltype(group)::value ? shared.get(gates, row0 + k)
+                                                      : widen(slot[kGate + k * kLanes], T{}), a[k], c[k]);
+    });
     if (live < kScanSteps) {
 #pragma unroll
       for (int k = 0; k < kScanSteps; ++k)
@@ -691,63 +793,88 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
       const f32x2 xv = widen(slot[k * kLanes], T{});
       return kMode == kGateValue ? xv : mul2(c[k], xv);
     };
-    f32x2 A = kOnes2, Bv = 0, Q = 0;
-    with_flag(resets != 0, [&](auto cut) {
-      constexpr bool kCut = decltype(cut)::value;
+    ScanMap map = {kOnes2, 0}, back = {kOnes2, 0};   // of the states, of the flow
+    with_flag(resets != 0, [&](auto with_cuts) {
+      constexpr bool kCut = decltype(with_cuts)::value;
 #pragma unroll
       for (int k = 0; k < kScanSteps; ++k) {
-        A = k ? mul2(A, a[k]) : a[k];
-        Bv = through2<kCut>(kCut && resets >> k & 1, a[k], added(k), Bv);
+        map.a = k ? mul2(map.a, a[k]) : a[k];
+        map.b = through2<kCut>(kCut && resets >> k & 1, a[k], added(k), map.b);
       }
 #pragma unroll
       for (int k = kScanSteps - 1; k >= 0; --k) {
-        Q = mul2(a[k], add2(widen(slot[kDy + k * kLanes], T{}), Q));
-        if (kCut && resets >> k & 1) Q = 0;
+        back.b = mul2(a[k], add2(widen(slot[kDy + k * kLanes], T{}), back.b));
+        if (kCut && resets >> k & 1) back.b = 0;
       }
     });
+    back.a = map.a = held2(map.a);
     const int round = w.rounds - 1 - s, buffer = round & 1;
-    const ScanMap* tile = maps[buffer];
-    const f32x2* tile_flow = flows[buffer];
-    const unsigned* tile_cut = piece_cut[buffer];
-    maps[buffer][w.piece * kLanes + w.pair] = {held2(A), Bv};
-    flows[buffer][w.piece * kLanes + w.pair] = Q;
-    if (p.reset && w.pair == 0) piece_cut[buffer][w.piece] = resets;
-    __syncthreads();
-
-    with_flag(p.reset != nullptr, [&](auto cut) {
-      constexpr bool kCut = decltype(cut)::value;
+    with_flag(p.reset != nullptr, [&](auto with_cuts) {
+      constexpr bool kCut = decltype(with_cuts)::value, kHold = kMode == kGateValue;
+      bool cut = resets != 0, cut_back = cut, cut_before, cut_behind;
+      const ScanMap before = join_pieces<kLanes, kCut, false, kHold>(map, cut, cut_before, w.lane);
+      const ScanMap behind = join_pieces<kLanes, kCut, true, kHold>(back, cut_back, cut_behind, w.lane);
+      if (w.lane >= 32 - kLanes) {
+        maps[buffer][w.warp][w.pair] = map;
+        if (kCut && w.pair == 0) warp_cut[buffer][w.warp] = cut;
+      }
+      if (w.lane < kLanes) flows[buffer][w.warp][w.pair] = back.b;
+      if (w.cluster > 1 && threadIdx.x == 0) exchange.expect(w, buffer, kCut);
+      __syncthreads();
+      auto tile = [&](int v) { return maps[buffer][v][w.pair]; };
+      auto tile_back = [&](int v) { return ScanMap{maps[buffer][v][w.pair].a, flows[buffer][v][w.pair]}; };
+      auto tile_cut = [&](int v) { return kCut && warp_cut[buffer][v]; };
       if (w.cluster > 1) {
-        const int ch = threadIdx.x % Place::kChannels;
-        float ta = 1.0f, tb = 0.0f;
-        bool any = false;
-#pragma unroll 4
-        for (int v = kPieces - 1; v >= 0; --v) {
-          const float ma = map_a(tile + v * kLanes, ch);
-          const bool cv = kCut && tile_cut[v] != 0;
-          tb = through<kCut>(cv, ma, reinterpret_cast<const float*>(tile_flow + v * kLanes)[ch], tb);
-          ta *= ma;
-          any |= cv;
+        ScanMap pre = {kOnes2, 0};
+        bool pre_cut = false;
+#pragma unroll
+        for (int v0 = kScanWarps - 1; v0 > 0; v0 -= kAhead) {
+          if (v0 <= w.warp) break;
+          ScanMap m[kAhead];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) m[j] = tile_back(max(v0 - j, 0));
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+            if (v0 - j > w.warp) then_map<kCut>(pre, pre_cut, m[j], tile_cut(v0 - j), kHold);
         }
-        exchange.template send<kCut>(w, buffer, held(ta), tb, any);
+        if (w.warp == 0 && w.lane < kLanes) {
+          ScanMap all = pre;
+          bool all_cut = pre_cut;
+          then_map<kCut>(all, all_cut, back, cut_back, true);
+          exchange.template send<kCut>(w, buffer, all, all_cut);
+        }
+        then_map<kCut>(pre, pre_cut, behind, cut_behind, true);
         if (threadIdx.x < Place::kChannels)
           flow = pack2(exchange.template run<kCut, true>(w, buffer, round >> 1 & 1, unpack2(flow).x, enter), 0.0f);
         __syncthreads();
-        r = *reinterpret_cast<const f32x2*>(enter + 2 * w.pair);
+        r = through2<kCut>(pre_cut, pre.a, pre.b, *reinterpret_cast<const f32x2*>(enter + 2 * w.pair));
       } else {
         r = hand[buffer ^ 1][w.pair];
-      }
 #pragma unroll
-      for (int v = kPieces - 1; v > 0; --v) {
-        if (v <= w.piece) break;
-        r = through2<kCut>(kCut && tile_cut[v] != 0, tile[v * kLanes + w.pair].a, tile_flow[v * kLanes + w.pair], r);
-      }
-      const int from = w.piece / kStretch * kStretch;
+        for (int v0 = kScanWarps - 1; v0 > 0; v0 -= kAhead) {
+          if (v0 <= w.warp) break;
+          ScanMap m[kAhead];
 #pragma unroll
-      for (int v = 0; v < kStretch - 1; ++v) {
-        if (from + v >= w.piece) break;
-        const ScanMap m = tile[(from + v) * kLanes + w.pair];
-        h = through2<kCut>(kCut && tile_cut[from + v] != 0, m.a, m.b, h);
+          for (int j = 0; j < kAhead; ++j) m[j] = tile_back(max(v0 - j, 0));
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+            if (v0 - j > w.warp) r = through2<kCut>(tile_cut(v0 - j), m[j].a, m[j].b, r);
+        }
+        if (kLanes < 32) r = through2<kCut>(cut_behind, behind.a, behind.b, r);
       }
+      // the states from the kept one before this stretch
+      const int from = w.warp / Place::kStretchWarps * Place::kStretchWarps;
+#pragma unroll
+      for (int v0 = 0; v0 < Place::kStretchWarps - 1; v0 += kAhead) {
+        if (from + v0 >= w.warp) break;
+        ScanMap m[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) m[j] = tile(min(from + v0 + j, kScanWarps - 1));
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+          if (from + v0 + j < w.warp) h = through2<kCut>(tile_cut(from + v0 + j), m[j].a, m[j].b, h);
+      }
+      if (kLanes < 32) h = through2<kCut>(cut_before, before.a, before.b, h);
     });
 
     const int t = w.first(s);
@@ -764,7 +891,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
       }
       T* gx_at = dx;
       T* gg_at = dgate;
-      const int lanes = min(p.group, kScanChannels) / 2;   // that share a gate
+      float sums[kScanSteps];   // of the gate's gradient over the thread's channels
 #pragma unroll
       for (int k = kScanSteps - 1; k >= 0; --k, gx_at -= p.dxt, gg_at -= p.dgt) {
         const f32x2 dh = add2(widen(slot[kDy + k * kLanes], T{}), r);
@@ -786,15 +913,45 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
         if (p.group == 1) {
           if (on) store_pair<T, kMove>(gg_at, gg, w.channels);
         } else {
-          // sum over the gate's channels: the lanes that share it, by doubling distances
           const float2 f = unpack2(gg);
-          float sum = w.channels > 0 ? f.x + (w.channels > 1 ? f.y : 0.0f) : 0.0f;
-          for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(~0u, sum, o);
-          if (on && w.channels > 0 && (w.pair & (lanes - 1)) == 0) {
+          sums[k] = w.channels > 0 ? f.x + (w.channels > 1 ? f.y : 0.0f) : 0.0f;
+        }
+      }
+      if (p.group > 1) {
+        // the lanes that share a gate add their sums, each keeping half of the steps as long as it has
+        // several: 9 shuffles instead of 40 for 32 lanes
+        const int lanes = min(p.group, kScanChannels) / 2;
+        int kept = 0, count = kScanSteps, o = lanes >> 1;   // first step and number of those kept
+        auto halve = [&](auto half_of) {
+          constexpr int kHalf = decltype(half_of)::value;
+          if (o) {
+            const bool upper = w.pair & o;
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j) {
+              const float got = __shfl_xor_sync(~0u, upper ? sums[j] : sums[j + kHalf], o);
+              sums[j] = (upper ? sums[j + kHalf] : sums[j]) + got;
+            }
+            kept += upper ? kHalf : 0;
+            count = kHalf;
+            o >>= 1;
+          }
+        };
+        halve(Number<4>{});
+        halve(Number<2>{});
+        halve(Number<1>{});
+        const int rest = o ? 2 * o - 1 : 0;
+        for (; o; o >>= 1) sums[0] += __shfl_xor_sync(~0u, sums[0], o);
+        if (w.channels > 0 && (w.pair & rest) == 0) {
+          gg_at = dgate - (kScanSteps - 1) * p.dgt;   // the piece's first row
+#pragma unroll
+          for (int j = 0; j < kScanSteps; ++j) {
+            if (j >= count) break;
+            const int k = kept + j;
+            if (!kWhole && k >= rows) continue;
             if (p.partial)
-              p.partial[(w.b * p.steps + t + k) * (p.channels / kScanChannels) + c0 / kScanChannels] = sum;
+              p.partial[(w.b * p.steps + t + k) * (p.channels / kScanChannels) + c0 / kScanChannels] = sums[j];
             else
-              *gg_at = from_float<T>(sum);
+              gg_at[k * p.dgt] = from_float<T>(sums[j]);
           }
         }
       }
