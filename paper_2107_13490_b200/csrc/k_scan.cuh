@@ -519,23 +519,24 @@ template <int kLanes, bool kCut, bool kBackward, bool kHold>
 __device__ __forceinline__ ScanMap join_pieces(ScanMap& map, bool& cut, bool& cut_before, int lane) {
   ScanMap before = {kOnes2, 0};
   cut_before = false;
-  if (kLanes == 32) return before;
+  if constexpr (kLanes < 32) {
 #pragma unroll
-  for (int o = kLanes; o < 32; o <<= 1) {
-    const int from = kBackward ? lane + o : lane - o;
-    const bool on = kBackward ? from < 32 : from >= 0;
-    ScanMap other = {shuffle2(map.a, from & 31), shuffle2(map.b, from & 31)};
-    bool other_cut = kCut && __shfl_sync(~0u, static_cast<int>(cut), from & 31) != 0;
-    if (on) {
-      then_map<kCut>(other, other_cut, map, cut, kHold);
-      map = other;
-      cut = other_cut;
+    for (int o = kLanes; o < 32; o <<= 1) {
+      const int from = kBackward ? lane + o : lane - o;
+      const bool on = kBackward ? from < 32 : from >= 0;
+      ScanMap other = {shuffle2(map.a, from & 31), shuffle2(map.b, from & 31)};
+      bool other_cut = kCut && __shfl_sync(~0u, static_cast<int>(cut), from & 31) != 0;
+      if (on) {
+        then_map<kCut>(other, other_cut, map, cut, kHold);
+        map = other;
+        cut = other_cut;
+      }
     }
+    const int from = kBackward ? lane + kLanes : lane - kLanes;
+    before = {shuffle2(map.a, from & 31), shuffle2(map.b, from & 31)};
+    cut_before = kCut && __shfl_sync(~0u, static_cast<int>(cut), from & 31) != 0;
+    if (kBackward ? from >= 32 : from < 0) { before = {kOnes2, 0}; cut_before = false; }
   }
-  const int from = kBackward ? lane + kLanes : lane - kLanes;
-  before = {shuffle2(map.a, from & 31), shuffle2(map.b, from & 31)};
-  cut_before = kCut && __shfl_sync(~0u, static_cast<int>(cut), from & 31) != 0;
-  if (kBackward ? from >= 32 : from < 0) { before = {kOnes2, 0}; cut_before = false; }
   return before;
 }
 
@@ -709,7 +710,6 @@ template <typename T, int kMode, int kMove, int kLanes>
 __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const ScanParams p) {
   typedef typename Pair<T>::raw Raw;
   typedef ScanPlace<kLanes> Place;
-  constexpr int kPieces = Place::kPieces;
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ ScanMap maps[2][kScanWarps][kLanes];          // of the states, warps
   __shared__ f32x2 flows[2][kScanWarps][kLanes];           // b of the gradient flow (a is the same)
