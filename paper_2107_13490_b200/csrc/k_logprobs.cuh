@@ -219,7 +219,7 @@ template <> struct Logits<float> {
   }
 };
 template <> struct Logits<__nv_bfloat16> {
-  static constexpr float kFloor = -998358383820800.0f;   // 0xD863: -1.7734375 2^49
+  static constexpr float kFloor = -998356558020608.0f;   // 0xD863: -1.7734375 2^49
   __device__ __forceinline__ static __nv_bfloat162 two(unsigned v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); }
   __device__ __forceinline__ static unsigned floored(unsigned v) {
     const __nv_bfloat162 r = __hmax2(two(v), two(0xD863D863u));
@@ -297,11 +297,14 @@ struct RowPart {
   __device__ __forceinline__ int element(int q) const { return q * kCount - mis; }                   // of a chunk's first
 };
 
-// Running maximum and sums of a thread; t = c x - c m in units of ln 2.
+// Running maximum and sums of a thread; t = c x - mc in units of ln 2, mc = c m rounded up, so that t <= 0
+// whatever the size of m: a thread that has met only barred logits (-Inf, the type's lowest, -1e10) sums
+// numbers up to 1 until a larger maximum wipes them.  (To nearest, their t could be a rounding error of 10^7,
+// and the row took the three-pass form: 64 x 32000 fp32 with a tenth barred 154 us for some masks, 12 for others.)
 struct RowSums {
   float m, mc, s, w;
   __device__ __forceinline__ void raise(float to, float c) {
-    const float mc2 = to * c, d = mc - mc2, f = exp2_approx(d);
+    const float mc2 = __fmul_ru(to, c), d = mc - mc2, f = exp2_approx(d);
     w = f * fmaf(d, s, w);
     s *= f;
     m = to; mc = mc2;
@@ -375,7 +378,10 @@ __device__ void top_prune(RowShared<T, kThreads>& sh, const unsigned long long* 
 // The part's k largest keys into best[].  `bound`: no element of the part below this one's order can be
 // among them (0: any can); only the chunks of the threads listed in strips[] can hold larger ones (all of
 // them if n_strips is kThreads).  Every round of at most kThreads chunks may add its elements'
-// keys; beyond kTopSpare they are cut to the k largest, and the smallest of those bounds the rest.
+// keys; beyond kTopSpare they are cut to the k largest, and the smallest of those bounds the rest.  Where most
+// threads' chunks and several rounds are to come, the first round is of kTopSpare keys and is cut as well: equal
+// logits, or barred ones where the bound is none, would fill a whole round (about 2000 keys, whose ranks take
+// 70 us) and are then below the bound.  (1 x 131072 bf16, all equal, 8 alternatives: 151 -> 14 us.)
 template <typename T, int kThreads>
 __device__ int top_collect(RowShared<T, kThreads>& sh, const RowPart<T>& part, unsigned bound, int k) {
   const int me = Team<kThreads>::me();
@@ -390,9 +396,11 @@ __device__ int top_collect(RowShared<T, kThreads>& sh, const RowPart<T>& part, u
     if (key > least) sh.keys[atomicAdd(&sh.n_keys, 1)] = key;
   }
   const int total = n_strips * per;
-  for (int base = 0; base < total; base += kThreads) {
+  for (int base = 0, width; base < total; base += width) {
+    const bool probe = base == 0 && total > kThreads && 2 * n_strips > kThreads;
+    width = probe ? min(kThreads, kTopSpare / kCount) : kThreads;
     const int i = base + me;
-    if (i < total) {
+    if (me < width && i < total) {
       const int step = i / n_strips, s = i - step * n_strips;
       const int q = part.q0 + step * kThreads + (n_strips == kThreads ? s : sh.strips[s]);
       if (q < part.q1) {
@@ -408,7 +416,7 @@ __device__ int top_collect(RowShared<T, kThreads>& sh, const RowPart<T>& part, u
     Team<kThreads>::sync();
     const int n = sh.n_keys;
     Team<kThreads>::sync();   // all have read it before the next round adds to it
-    if (n > kTopSpare && base + kThreads < total) {
+    if ((n > kTopSpare || (probe && n >= k)) && base + width < total) {
       top_prune<T, kThreads>(sh, sh.keys, n, k);
       if (me < k) sh.keys[me] = sh.best[me];
       if (me == 0) sh.n_keys = k;
@@ -587,7 +595,7 @@ __global__ void __launch_bounds__(kRowThreads, kThreads == 32 ? 5 : 6) logprob_r
   const float x_target = target < p.vocab ? to_float(x[target]) : 0.0f;
   const float c = p.scale * kLog2e;
 
-  RowSums a = {Logits<T>::kFloor, Logits<T>::kFloor * c, 0.0f, 0.0f};
+  RowSums a = {Logits<T>::kFloor, __fmul_ru(Logits<T>::kFloor, c), 0.0f, 0.0f};
   f32x2 s2 = 0, w2 = 0;
   const f32x2 cc = pack2(c, c);
   f32x2 shift = pack2(-a.mc, -a.mc);
@@ -669,8 +677,8 @@ __global__ void __launch_bounds__(kRowThreads, kThreads == 32 ? 5 : 6) logprob_r
     }
     m = all.m; a.mc = all.mc; s_sum = all.s; w_sum = all.w;
   }
-  // logits at the floor must have been nothing beside the maximum, and c m a number
-  if (!((m - Logits<T>::kFloor) * c > 160.0f) || !(fabsf(a.mc) < 1e20f) || !(c < 1e7f) || s_sum != s_sum) {
+  // logits at the floor must have been nothing beside the maximum, and c m within 32 of mc
+  if (!((m - Logits<T>::kFloor) * c > 160.0f) || !(fabsf(a.mc) < 5e8f) || !(c < 1e7f) || s_sum != s_sum) {
     if (rank == 0) special_row<T, kThreads>(p, sh, row, x, dx, target);
     return;   // (no other CTA's shared memory is touched from here on)
   }

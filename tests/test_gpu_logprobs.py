@@ -314,3 +314,41 @@ def test_large_rows_against_64_bits_on_the_device(B, rows, vocab, dtype):
     off = (r.dlogits.double() - ref).abs()
     bound = d.double().abs()[:, None] * (p * (6 * tol * (2 + logp.abs() + h[:, None])) + 2.0 ** -22 * hot) + UNIT[dtype] * ref.abs() + TINY[dtype]
     assert (off <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1.0, 1 / 0.7, 3.3])
+def test_most_logits_barred_by_any_value(B, dtype, scale):
+    import torch
+    vocab = 9001
+    top = float(torch.finfo(getattr(torch, dtype)).max)
+    x = logits(6, vocab, dtype, 12)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    keep = torch.randperm(vocab, generator=g, device="cuda")[:40]
+    barred = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    barred[keep] = False
+    for row, value in enumerate((-math.inf, -top, -1e10, -3e13, -math.inf, -1e9)):
+        x[row, barred] = max(value, -top) if math.isfinite(value) else value
+    x[4, keep[5:]] = -math.inf     # fewer are left than alternatives are asked for
+    compare(B, x, [int(v) for v in keep[:6]], scale=scale, k=32)
+
+
+@pytest.mark.parametrize("scale", [0.3, 1.0, 1.7])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_one_large_maximum(B, scale, sign):
+    import torch
+    x = logits(24, 2000, "float32", 14)
+    for row in range(24):   # (the rounding of scale x is then larger than what the other logits differ by)
+        x[row] += sign * 3e7 * 1.37 ** row
+    compare(B, x, list(range(24)), scale=scale, k=2, weights=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_alternatives_of_equal_and_rising_rows(B, dtype):
+    import torch
+    vocab = 20000
+    x = torch.zeros(4, vocab, device="cuda")
+    x[1, 1::2] = 1.0
+    x[2] = torch.arange(vocab, device="cuda") // 64 / 64.0
+    x[3] = x[2].flip(0)
+    compare(B, x.to(getattr(torch, dtype)), [0, 1, 2, 3], k=32, weights=False)
