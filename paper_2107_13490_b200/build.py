@@ -1,4 +1,5 @@
-"""Builds libadapt_b200.so (CUDA kernels + C ABI) for sm_100a with nvcc, in-tree.
+"""Builds libadapt_b200.so (CUDA kernels + C ABI) for sm_100a with nvcc, and _adapt_torch.so (the calls of the
+training-step operators from torch tensors, g++), in-tree.
 
     python -m paper_2107_13490_b200.build [--force] [--check]
 
@@ -11,11 +12,13 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libadapt_b200.so")
 CHECK_LIB = os.path.join(HERE, "libadapt_b200_check.so")
+CALLS = os.path.join(HERE, "_adapt_torch.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -46,7 +49,28 @@ def build(force: bool = False, verbose: bool = False, check: bool = False) -> st
             (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + sources()
         subprocess.run(cmd, check=True)
         os.replace(tmp, lib)
+    build_calls(force)
     return lib
+
+
+def build_calls(force: bool = False) -> str:
+    """Builds the extension behind binding.py's training-step operators if it is stale."""
+    source, header = os.path.join(CSRC, "torch_calls.cpp"), os.path.join(os.path.dirname(HERE), "include", "adapt.h")
+    stale = (not os.path.exists(CALLS)) or any(
+        os.path.getmtime(d) > os.path.getmtime(CALLS) for d in (source, header))
+    if force or stale:
+        import torch
+        root = os.path.dirname(torch.__file__)
+        cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+        tmp = CALLS + ".tmp%d" % os.getpid()
+        cmd = ["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-Wall"]
+        cmd += ["-I" + d for d in (os.path.join(root, "include"), os.path.join(root, "include/torch/csrc/api/include"),
+                                   sysconfig.get_paths()["include"], os.path.join(cuda, "include"))]
+        cmd += [source, "-o", tmp, "-L" + os.path.join(root, "lib")]
+        cmd += ["-l" + n for n in ("torch_python", "torch", "torch_cpu", "torch_cuda", "c10", "c10_cuda")]
+        subprocess.run(cmd, check=True)
+        os.replace(tmp, CALLS)
+    return CALLS
 
 
 if __name__ == "__main__":
