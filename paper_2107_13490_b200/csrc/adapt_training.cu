@@ -52,11 +52,11 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   if (rows > (1ll << 48) / cols || index_base > (1ull << 62)) return ADAPT_ERR_INVALID_ARG;
   if (rows > 1 && (ldx < cols || ldy < cols || (residual && ldr < cols))) return ADAPT_ERR_INVALID_ARG;
   if (rows == 1) ldx = ldr = ldy = cols;
-  // x, r and y alike to the 16-byte boundary, in every row: chunks of 16 bytes, else of a pair
+  // whether x, r and y lie alike to the 16-byte boundary, in every row
   auto off = [&](const void* a, const void* b) { return (reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u; };
   const bool vec = !off(x, y) && (!residual || !off(x, residual)) &&
                    (rows == 1 || ((ldx - ldy) % (16 / e) == 0 && (!residual || (ldx - ldr) % (16 / e) == 0)));
-  const int unit = vec ? 16 / e : 2;
+  const int unit = 16 / e;
   DropoutParams q = {};
   q.cols = cols; q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
   q.base = seed ^ 0xA54FF53A5F1D36F1ull ^ ((static_cast<uint64_t>(static_cast<int64_t>(layer)) + 1ull) * 0x9E3779B97F4A7C15ull);
@@ -75,9 +75,11 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
       q.x = static_cast<const char*>(x) + (row * ldx + col) * e;
       q.y = static_cast<char*>(y) + (row * ldy + col) * e;
       q.r = residual ? static_cast<const char*>(residual) + (row * ldr + col) * e : nullptr;
+      q.x_end = static_cast<const char*>(q.x) + ((n_rows - 1) * ldx + n_cols) * e;
+      q.r_end = residual ? static_cast<const char*>(q.r) + ((n_rows - 1) * ldr + n_cols) * e : nullptr;
       q.index_base = static_cast<long long>(index_base) + row * cols + col;
       if (n_rows == 1) {
-        q.mis = static_cast<int>(vec ? (reinterpret_cast<uintptr_t>(q.x) & 15u) / e : q.index_base & 1);
+        q.mis = static_cast<int>((reinterpret_cast<uintptr_t>(q.y) & 15u) / e);
         q.cols = n_cols;
         q.chunks = static_cast<unsigned>((q.mis + n_cols + unit - 1) / unit);
         q.from = q.mis ? 1 : 0;
@@ -91,19 +93,18 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
         q.shift = s;
         q.magic = static_cast<unsigned>(((1ull << (32 + s)) + q.per_row - 1) / q.per_row);
       }
-      const unsigned tile = kDropoutThreads * (vec ? 2 : 4);
+      const unsigned tile = kDropoutThreads * (vec ? kDropoutUnroll : kShiftUnroll);
       const unsigned grid = (q.chunks + tile - 1) / tile;
       LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        constexpr int kVec = 16 / sizeof(T);
         auto go = [&](auto kernel) { kernel<<<grid, kDropoutThreads, 0, stream>>>(q); };
         if (n_rows == 1) {
-          if (vec) residual ? go(dropout_kernel<T, kVec, true, false>) : go(dropout_kernel<T, kVec, false, false>);
-          else residual ? go(dropout_kernel<T, 2, true, false>) : go(dropout_kernel<T, 2, false, false>);
+          if (vec) residual ? go(dropout_kernel<T, false, true, false>) : go(dropout_kernel<T, false, false, false>);
+          else residual ? go(dropout_kernel<T, true, true, false>) : go(dropout_kernel<T, true, false, false>);
         } else {
-          if (vec) residual ? go(dropout_kernel<T, kVec, true, true>) : go(dropout_kernel<T, kVec, false, true>);
-          else residual ? go(dropout_kernel<T, 2, true, true>) : go(dropout_kernel<T, 2, false, true>);
+          if (vec) residual ? go(dropout_kernel<T, false, true, true>) : go(dropout_kernel<T, false, false, true>);
+          else residual ? go(dropout_kernel<T, true, true, true>) : go(dropout_kernel<T, true, false, true>);
         }
       });
       ADAPT_LAUNCH_OK("dropout");

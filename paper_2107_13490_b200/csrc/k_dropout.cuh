@@ -10,13 +10,15 @@
 namespace adapt {
 
 constexpr int kDropoutThreads = 256;
+constexpr int kDropoutUnroll = 2, kShiftUnroll = 1;   // chunks of a thread (kShift with 2: 8.3 us for 7.8, 4099 x 1001 fp16)
 
 struct DropoutParams {
   const void* x;
   const void* r;          // may be null
   void* y;
+  const void *x_end, *r_end;
   long long cols, ldx, ldr, ldy;
-  unsigned chunks;        // of 16 bytes of x, or of two elements, over all rows
+  unsigned chunks;        // of 16 bytes of y, over all rows
   unsigned per_row;       // chunks of a row (the most that any alignment needs)
   unsigned magic, shift;  // i / per_row = (i * magic >> 32) >> shift
   unsigned from, to;      // one row: its whole chunks
@@ -61,21 +63,49 @@ __device__ __forceinline__ void dropout_words(unsigned long long base, long long
   }
 }
 
-// A chunk is 16 bytes where the rows of x, r and y lie alike to the 16-byte boundary (kCount = 16 /
-// sizeof(T)), a hash's pair of elements otherwise (kCount = 2; then neighbouring threads read and write
-// neighbouring pairs: 4099 x 1001 fp16 into rows of another alignment takes 7 us, 17 with 8 elements a
-// thread).  Chunks over a row's ends go element by element.  kRows: several rows.
-template <typename T, int kCount, bool kResidual, bool kRows>
+// 16 bytes from any address: the aligned blocks that hold them (the second only where it is needed, so that
+// an operand that lies like y - the one y may be - is read by the thread that writes it).  False, and nothing
+// read, where a block reaches beyond the operand.
+__device__ __forceinline__ bool fetch_blocks(const void* from, const void* begin, const void* end, uint4& low, uint4& high) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(from), block = a & ~static_cast<uintptr_t>(15);
+  const bool two = (a & 15u) != 0;
+  if (block < reinterpret_cast<uintptr_t>(begin) || block + (two ? 32 : 16) > reinterpret_cast<uintptr_t>(end)) return false;
+  low = *reinterpret_cast<const uint4*>(block);
+  high = two ? *reinterpret_cast<const uint4*>(block + 16) : make_uint4(0u, 0u, 0u, 0u);
+  return true;
+}
+__device__ __forceinline__ uint4 join_blocks(const uint4& low, const uint4& high, const void* from) {
+  const unsigned off = static_cast<unsigned>(reinterpret_cast<uintptr_t>(from) & 15u);
+  unsigned a[8] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
+  if (off & 8) {
+#pragma unroll
+    for (int k = 0; k < 6; ++k) a[k] = a[k + 2];
+  }
+  if (off & 4) {
+#pragma unroll
+    for (int k = 0; k < 5; ++k) a[k] = a[k + 1];
+  }
+  const unsigned bits = (off & 3) * 8;
+  return make_uint4(__funnelshift_r(a[0], a[1], bits), __funnelshift_r(a[1], a[2], bits),
+                    __funnelshift_r(a[2], a[3], bits), __funnelshift_r(a[3], a[4], bits));
+}
+
+// A chunk is 16 bytes of y.  Where the rows of x, r and y lie alike to the 16-byte boundary, so is its part of
+// x and r, and chunks over a row's ends go element by element (whole blocks there too: 16384 x 4096 bf16 51 us,
+// 49 without).  Otherwise (kShift) x and r are shifted out of the aligned blocks around them, over a row's ends
+// too: 16384 x 4095 bf16 into rows of another alignment 66 us, 111 with pairs of elements; 4099 x 1001 fp16 7.8
+// and 10.4; rows of 10 elements are too short for it (10^6 x 10 31 and 23 us).  kRows: several rows.
+template <typename T, bool kShift, bool kResidual, bool kRows>
 __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutParams p) {
-  constexpr bool kVec = kCount * sizeof(T) == 16;
-  constexpr int kUnroll = kVec ? 2 : 4;
+  constexpr int kCount = 16 / sizeof(T);
+  constexpr int kUnroll = kShift ? kShiftUnroll : kDropoutUnroll;
   const unsigned first = blockIdx.x * (kDropoutThreads * kUnroll) + threadIdx.x;
   const T *x[kUnroll], *r[kUnroll];
   T* y[kUnroll];
   long long e[kUnroll];        // number of the chunk's first element (kRows)
   int from[kUnroll], to[kUnroll];   // its elements that exist
-  uint4 vx[kUnroll], vr[kUnroll];
-  T sx[kUnroll][2], sr[kUnroll][2];
+  bool blocks[kUnroll];             // its operands are in vx and vr
+  uint4 vx[kUnroll], vr[kUnroll], hx[kUnroll], hr[kUnroll];
 #pragma unroll
   for (int i = 0; i < kUnroll; ++i) {
     const unsigned c = first + i * kDropoutThreads;
@@ -84,14 +114,13 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutP
     if (kRows) {
       const unsigned row = __umulhi(c, p.magic) >> p.shift;
       const unsigned q = c - row * p.per_row;
-      const T* start = static_cast<const T*>(p.x) + row * p.ldx;
-      const long long number = p.index_base + row * p.cols;
-      const int mis = kVec ? static_cast<int>((reinterpret_cast<uintptr_t>(start) & 15u) / sizeof(T)) : static_cast<int>(number & 1);
+      T* start = static_cast<T*>(p.y) + row * p.ldy;
+      const int mis = static_cast<int>((reinterpret_cast<uintptr_t>(start) & 15u) / sizeof(T));
       const int col = static_cast<int>(q) * kCount - mis, cols = static_cast<int>(p.cols);
-      x[i] = start + col;
-      y[i] = static_cast<T*>(p.y) + row * p.ldy + col;
+      x[i] = static_cast<const T*>(p.x) + row * p.ldx + col;
+      y[i] = start + col;
       if (kResidual) r[i] = static_cast<const T*>(p.r) + row * p.ldr + col;
-      e[i] = number + col;
+      e[i] = p.index_base + row * p.cols + col;
       from[i] = max(0, -col);
       to[i] = min(kCount, cols - col);
     } else {
@@ -105,17 +134,14 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutP
       }
     }
     if (c >= p.chunks) to[i] = 0;
-    if (kVec) {
-      if (to[i] - from[i] == kCount) {
+    if (kShift) {
+      blocks[i] = to[i] > from[i] && fetch_blocks(x[i], p.x, p.x_end, vx[i], hx[i]);
+      if (kResidual) blocks[i] = blocks[i] && fetch_blocks(r[i], p.r, p.r_end, vr[i], hr[i]);
+    } else {
+      blocks[i] = to[i] - from[i] == kCount;
+      if (blocks[i]) {
         vx[i] = *reinterpret_cast<const uint4*>(x[i]);
         if (kResidual) vr[i] = *reinterpret_cast<const uint4*>(r[i]);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const bool on = k >= from[i] && k < to[i];
-        sx[i][k] = on ? x[i][k] : from_float<T>(0.0f);
-        if (kResidual) sr[i][k] = on ? r[i][k] : from_float<T>(0.0f);
       }
     }
   }
@@ -131,22 +157,28 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutP
 #pragma unroll
       for (int k = 0; k < kCount; ++k) u[k] = 0;
     }
-    if (kVec && to[i] - from[i] == kCount) {
+    if (blocks[i]) {
       float f[kCount], g[kCount];
-      unpack16<T>(vx[i], *reinterpret_cast<float(*)[16 / sizeof(T)]>(&f));
-      if (kResidual) unpack16<T>(vr[i], *reinterpret_cast<float(*)[16 / sizeof(T)]>(&g));
+      unpack16<T>(kShift ? join_blocks(vx[i], hx[i], x[i]) : vx[i], f);
+      if (kResidual) unpack16<T>(kShift ? join_blocks(vr[i], hr[i], r[i]) : vr[i], g);
 #pragma unroll
       for (int k = 0; k < kCount; ++k) {
         f[k] = u[k] >= least ? f[k] * p.scale : 0.0f;
         if (kResidual) f[k] += g[k];
       }
-      *reinterpret_cast<uint4*>(y[i]) = pack16<T>(*reinterpret_cast<float(*)[16 / sizeof(T)]>(&f));
+      if (!kShift || to[i] - from[i] == kCount) {
+        *reinterpret_cast<uint4*>(y[i]) = pack16<T>(f);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kCount; ++k)
+          if (k >= from[i] && k < to[i]) y[i][k] = from_float<T>(f[k]);
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < kCount; ++k) {
         if (k < from[i] || k >= to[i]) continue;
-        float f = u[k] >= least ? to_float(kVec ? x[i][k] : sx[i][k & 1]) * p.scale : 0.0f;
-        if (kResidual) f += to_float(kVec ? r[i][k] : sr[i][k & 1]);
+        float f = u[k] >= least ? to_float(x[i][k]) * p.scale : 0.0f;
+        if (kResidual) f += to_float(r[i][k]);
         y[i][k] = from_float<T>(f);
       }
     }

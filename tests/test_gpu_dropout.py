@@ -143,3 +143,36 @@ def test_large_tensor_samples(B):
     for start in (0, 12345678, n - 64):
         assert np.array_equal(y[start:start + 64].float().cpu().numpy() != 0, R.dropout_keep(64, 0.5, 21, 1, start))
     assert abs(float((y != 0).double().mean()) - 0.5) < 5 * 0.5 / n ** 0.5
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("cols", [3, 8, 37, 256, 1003])
+def test_every_pair_of_alignments(B, dtype, cols):
+    import torch
+    dt = getattr(torch, dtype)
+    lane = 16 // torch.empty(0, dtype=dt).element_size()
+    rows = 5
+    keep = R.dropout_keep(rows * cols, 0.4, 12, 3)
+    g = torch.Generator(device="cuda").manual_seed(cols)
+
+    def matrix(shift, pad):
+        # the matrix ends where its buffer ends, so that a read beyond it would leave the buffer
+        buf = torch.randn(shift + (rows - 1) * (cols + pad) + cols, generator=g, device="cuda").to(dt)
+        return buf, torch.as_strided(buf, (rows, cols), (cols + pad, 1), shift)
+
+    for shift in range(lane):
+        _, x = matrix(shift, 3)
+        _, r = matrix((3 * shift + 1) % lane, 5)
+        for pad in (0, 2):
+            buf, y = matrix((shift * 5 + 2) % lane, pad)
+            before = buf.clone()
+            check(B.adapt_dropout(x, 0.4, 12, 3, residual=r, out=y), x, r, 0.4, keep, dtype)
+            y.copy_(torch.as_strided(before, y.shape, y.stride(), y.storage_offset()))
+            assert torch.equal(buf.view(torch.uint8), before.view(torch.uint8))
+        for same in (x, r):   # in place, the other operand at another alignment
+            want = B.adapt_dropout(x, 0.4, 12, 3, residual=r)
+            held = same.clone()
+            assert torch.equal(B.adapt_dropout(x, 0.4, 12, 3, residual=r, out=same), want)
+            same.copy_(held)
+    line, other = matrix(1, 0)[1].reshape(-1), matrix(2, 0)[1].reshape(-1)   # one long row
+    check(B.adapt_dropout(line, 0.4, 12, 3, residual=other), line, other, 0.4, keep, dtype)
