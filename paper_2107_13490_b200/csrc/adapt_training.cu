@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "../../include/adapt.h"
+#include "dropout_pieces.h"
 #include "host.cuh"
 #include "k_dropout.cuh"
 #include "k_logprobs.cuh"
@@ -65,52 +66,46 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   q.threshold = q.none ? 0u : static_cast<unsigned>(threshold);
   q.scale = p < 1.0 ? static_cast<float>(1.0 / (1.0 - p)) : 0.0f;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  // Chunk numbers are 31-bit: longer tensors go in pieces of rows, or of one long row's columns.
-  const int64_t most = 1ll << 30;
-  const int64_t col_step = std::min<int64_t>(cols, (most - 2) / 8 * unit), per_row = (col_step + unit - 1) / unit + 1;
-  const int64_t row_step = std::max<int64_t>(1, most / per_row);
-  for (int64_t row = 0; row < rows; row += row_step) {
-    for (int64_t col = 0; col < cols; col += col_step) {
-      const int64_t n_rows = std::min(row_step, rows - row), n_cols = std::min(col_step, cols - col);
-      q.x = static_cast<const char*>(x) + (row * ldx + col) * e;
-      q.y = static_cast<char*>(y) + (row * ldy + col) * e;
-      q.r = residual ? static_cast<const char*>(residual) + (row * ldr + col) * e : nullptr;
-      q.x_end = static_cast<const char*>(q.x) + ((n_rows - 1) * ldx + n_cols) * e;
-      q.r_end = residual ? static_cast<const char*>(q.r) + ((n_rows - 1) * ldr + n_cols) * e : nullptr;
-      q.index_base = static_cast<long long>(index_base) + row * cols + col;
-      if (n_rows == 1) {
-        q.mis = static_cast<int>((reinterpret_cast<uintptr_t>(q.y) & 15u) / e);
-        q.cols = n_cols;
-        q.chunks = static_cast<unsigned>((q.mis + n_cols + unit - 1) / unit);
-        q.from = q.mis ? 1 : 0;
-        q.to = static_cast<unsigned>((q.mis + n_cols) / unit);
-      } else {   // (col_step = cols here: a longer row goes alone)
-        q.per_row = static_cast<unsigned>(per_row);
-        q.chunks = static_cast<unsigned>(per_row * n_rows);
-        // i / d for i < 2^31, d >= 2: magic = ceil(2^(32 + s) / d) with 2^s >= d / 2 (Granlund and Montgomery)
-        unsigned s = 0;
-        while ((2ull << s) < q.per_row) ++s;
-        q.shift = s;
-        q.magic = static_cast<unsigned>(((1ull << (32 + s)) + q.per_row - 1) / q.per_row);
-      }
-      const unsigned tile = kDropoutThreads * (vec ? kDropoutUnroll : kShiftUnroll);
-      const unsigned grid = (q.chunks + tile - 1) / tile;
-      LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
-      with_type(dtype, [&](auto t) {
-        using T = decltype(t);
-        auto go = [&](auto kernel) { kernel<<<grid, kDropoutThreads, 0, stream>>>(q); };
-        if (n_rows == 1) {
-          if (vec) residual ? go(dropout_kernel<T, false, true, false>) : go(dropout_kernel<T, false, false, false>);
-          else residual ? go(dropout_kernel<T, true, true, false>) : go(dropout_kernel<T, true, false, false>);
-        } else {
-          if (vec) residual ? go(dropout_kernel<T, false, true, true>) : go(dropout_kernel<T, false, false, true>);
-          else residual ? go(dropout_kernel<T, true, true, true>) : go(dropout_kernel<T, true, false, true>);
-        }
-      });
-      ADAPT_LAUNCH_OK("dropout");
+  const DropoutPieces pieces(rows, cols, e);
+  return pieces.each([&](int64_t row, int64_t col, int64_t n_rows, int64_t n_cols) -> int {
+    q.x = static_cast<const char*>(x) + (row * ldx + col) * e;
+    q.y = static_cast<char*>(y) + (row * ldy + col) * e;
+    q.r = residual ? static_cast<const char*>(residual) + (row * ldr + col) * e : nullptr;
+    q.x_end = static_cast<const char*>(q.x) + ((n_rows - 1) * ldx + n_cols) * e;
+    q.r_end = residual ? static_cast<const char*>(q.r) + ((n_rows - 1) * ldr + n_cols) * e : nullptr;
+    q.index_base = static_cast<long long>(index_base) + row * cols + col;
+    if (n_rows == 1) {
+      q.mis = static_cast<int>((reinterpret_cast<uintptr_t>(q.y) & 15u) / e);
+      q.cols = n_cols;
+      q.chunks = static_cast<unsigned>((q.mis + n_cols + unit - 1) / unit);
+      q.from = q.mis ? 1 : 0;
+      q.to = static_cast<unsigned>((q.mis + n_cols) / unit);
+    } else {   // whole rows
+      q.per_row = static_cast<unsigned>(pieces.per_row);
+      q.chunks = static_cast<unsigned>(pieces.per_row * n_rows);
+      // i / d for i < 2^31, d >= 2: magic = ceil(2^(32 + s) / d) with 2^s >= d / 2 (Granlund and Montgomery)
+      unsigned s = 0;
+      while ((2ull << s) < q.per_row) ++s;
+      q.shift = s;
+      q.magic = static_cast<unsigned>(((1ull << (32 + s)) + q.per_row - 1) / q.per_row);
     }
-  }
-  return ADAPT_OK;
+    const unsigned tile = kDropoutThreads * (vec ? kDropoutUnroll : kShiftUnroll);
+    const unsigned grid = (q.chunks + tile - 1) / tile;
+    LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      auto go = [&](auto kernel) { kernel<<<grid, kDropoutThreads, 0, stream>>>(q); };
+      if (n_rows == 1) {
+        if (vec) residual ? go(dropout_kernel<T, false, true, false>) : go(dropout_kernel<T, false, false, false>);
+        else residual ? go(dropout_kernel<T, true, true, false>) : go(dropout_kernel<T, true, false, false>);
+      } else {
+        if (vec) residual ? go(dropout_kernel<T, false, true, true>) : go(dropout_kernel<T, false, false, true>);
+        else residual ? go(dropout_kernel<T, true, true, true>) : go(dropout_kernel<T, true, false, true>);
+      }
+    });
+    ADAPT_LAUNCH_OK("dropout");
+    return ADAPT_OK;
+  });
 }
 
 }  // extern "C"
