@@ -34,10 +34,13 @@ struct LogprobParams {
 };
 
 // Order of the alternatives: larger logit first, equal ones (and +-0) by the lower index, NaN before
-// everything.  One 64-bit key, all keys of a row distinct, none 0.
+// everything.  One 64-bit key, all keys of a row distinct, none 0 and none ~0 (which a selection from above starts
+// at: NaN at index 0 would not be below it).
+constexpr unsigned kNanOrder = 0xFFFFFFFEu;
+static_assert(kNanOrder > (0x7F800000u | 0x80000000u) && kNanOrder != 0xFFFFFFFFu, "above +Inf, below the start");
 __device__ __forceinline__ unsigned top_order(float v) {
   const unsigned b = __float_as_uint(__fadd_rn(v, 0.0f));
-  return v != v ? 0xFFFFFFFFu : (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+  return v != v ? kNanOrder : (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 __device__ __forceinline__ unsigned long long top_key(float v, int j) {
   return (static_cast<unsigned long long>(top_order(v)) << 32) | (0xFFFFFFFFu - static_cast<unsigned>(j));

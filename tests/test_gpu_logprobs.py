@@ -352,3 +352,18 @@ def test_alternatives_of_equal_and_rising_rows(B, dtype):
     x[2] = torch.arange(vocab, device="cuda") // 64 / 64.0
     x[3] = x[2].flip(0)
     compare(B, x.to(getattr(torch, dtype)), [0, 1, 2, 3], k=32, weights=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [1, 3, 32, 50, 129, 1000, 2600])
+def test_nan_at_the_first_token_and_rows_of_nothing_else(B, dtype, vocab):
+    x = logits(4, vocab, dtype, vocab + 1)
+    x[0, 0] = math.nan
+    x[1] = math.nan
+    x[2, 0] = math.nan
+    x[2, vocab - 1] = math.inf
+    for k in {1, min(vocab, 5), min(vocab, 32)}:     # vocab itself where it is small
+        for t in ([0, vocab - 1, 0, vocab // 2], None):
+            r = compare(B, x, t, k=k, weights=False)
+            assert r.top_ids[1].tolist() == list(range(k)) and r.top_ids[0, 0] == 0
+            assert int(r.top_ids.min()) == 0 and int(r.top_ids.max()) < vocab
