@@ -299,7 +299,7 @@ struct ScanPlace {
 // Copies a warp's rows of a tile into its part of a stage, asynchronously where the alignment allows;
 // rows at or beyond `rows` and channels at or beyond `left` are filled with zeros.  src points to the
 // warp's first row, the block's first channel.  With kMoveVec a lane's pairs come by other lanes'
-// copies: __syncwarp() after the wait.
+// copies: __syncwarp() after the wait, and before the copies where the warp's reads of the part may not be over.
 template <typename T, int kMove, int kLanes>
 __device__ __forceinline__ void fetch_rows(unsigned char* part, const T* src, long long stride, int rows, int left) {
   typedef typename Pair<T>::raw Raw;
@@ -764,6 +764,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
   unsigned next_reset = w.rounds ? w.reset_byte(p, w.rounds - 1) : 0u;
   f32x2 next_state = w.rounds ? kept_state(w.rounds - 1) : 0;
   for (int s = w.rounds - 1; s >= 0; --s) {
+    // the round before read its stage to its end, this fetch fills it again: with other lanes' slots too
+    if (kMove == kMoveVec || p.group > 1) __syncwarp();
     fetch(s - 1);
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     if (kMove == kMoveVec || p.group > 1) __syncwarp();

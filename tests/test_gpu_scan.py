@@ -337,3 +337,18 @@ def test_graph_capture_and_changed_inputs(B):
         want = run(B, c, True)
         assert torch.equal(r.y, want["y"]) and torch.equal(g.dx, want["dx"]) and torch.equal(g.dgate, want["dgate"])
     del ws_f
+
+
+# About 500 chains of 64 channels: one CTA each on 148 SMs, so the state goes from tile to tile inside the CTA.
+# 4000 channels move 16 bytes at a time, 3998 two channels (16-bit: 4-byte rows), 3999 one.
+@pytest.mark.parametrize("sigmoid", [True, False])
+@pytest.mark.parametrize("dtype,channels,group", [("bfloat16", 4000, 1), ("float16", 3998, 1), ("bfloat16", 3999, 1),
+                                                  ("float32", 4000, 1), ("float32", 3999, 1), ("float16", 4096, 8),
+                                                  ("bfloat16", 4096, 64), ("float32", 4096, 128)])
+def test_many_chains_run_through_their_tiles(B, sigmoid, dtype, channels, group):
+    steps = 150     # two whole tiles and 22 steps
+    check(B, case(dtype, 8, steps, channels, group, channels + group, sigmoid), sigmoid)
+    lengths = [0, 1, steps, steps - 1, 64, 65, 128, 127]
+    c = case(dtype, 8, steps, channels, group, channels, sigmoid, lengths=lengths, resets=True)
+    c["reset"][2, 64] = c["reset"][2, 127] = True      # at a tile's first and last step
+    check(B, c, sigmoid)
