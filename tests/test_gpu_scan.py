@@ -352,3 +352,17 @@ def test_many_chains_run_through_their_tiles(B, sigmoid, dtype, channels, group)
     c = case(dtype, 8, steps, channels, group, channels, sigmoid, lengths=lengths, resets=True)
     c["reset"][2, 64] = c["reset"][2, 127] = True      # at a tile's first and last step
     check(B, c, sigmoid)
+
+
+# Few chains: narrower blocks in clusters, over several rounds of exchange (on 148 SMs 32 channels by 8 CTAs, 16
+# channels by 16 CTAs, and 64 channels by 16 CTAs with the gate of 64 channels).
+@pytest.mark.parametrize("sigmoid", [True, False])
+@pytest.mark.parametrize("dtype,batch,steps,channels,group", [
+    ("bfloat16", 2, 9001, 512, 1), ("float32", 2, 9001, 510, 1), ("float16", 2, 9001, 511, 1), ("bfloat16", 1, 9100, 256, 1),
+    ("float32", 1, 9100, 250, 2), ("float16", 1, 9100, 256, 64)])
+def test_few_chains_run_through_their_rounds(B, sigmoid, dtype, batch, steps, channels, group):
+    c = case(dtype, batch, steps, channels, group, steps + group, sigmoid, lengths=[steps, steps - 4000][:batch], resets=True)
+    if not sigmoid:
+        c["gate"] = c["gate"].clamp(-1, 1)      # (longer products of decays than in the cases above)
+    check(B, c, sigmoid)
+    check(B, dict(c, reset=None, lengths=None), sigmoid)
