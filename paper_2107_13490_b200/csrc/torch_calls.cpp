@@ -158,14 +158,15 @@ Matrix matrix(const at::Tensor& t) {
   need(cols <= 1 || t.stride(1) == 1, "needs a matrix with unit inner stride");
   return {rows, cols, rows > 1 ? t.stride(0) : cols};
 }
-const void* per_row(const at::Tensor* t, int64_t rows, at::ScalarType type) {
+// What goes with the rows of x: on its device, an element a row.
+const void* per_row(const at::Tensor* t, const at::Tensor& x, at::ScalarType type) {
   if (!t) return nullptr;
-  need(t->is_cuda() && t->scalar_type() == type && t->numel() == rows && t->is_contiguous(),
-       "needs a contiguous CUDA tensor with an element a row (targets int64, others float32)");
+  need(t->device() == x.device() && t->scalar_type() == type && t->numel() == x.size(0) && t->is_contiguous(),
+       "needs a contiguous tensor on the logits' device with an element a row (targets int64, others float32)");
   return t->const_data_ptr();
 }
-const float* floats(const at::Tensor* t, int64_t rows) { return static_cast<const float*>(per_row(t, rows, at::kFloat)); }
-const int64_t* numbers(const at::Tensor* t, int64_t rows) { return static_cast<const int64_t*>(per_row(t, rows, at::kLong)); }
+const float* floats(const at::Tensor* t, const at::Tensor& x) { return static_cast<const float*>(per_row(t, x, at::kFloat)); }
+const int64_t* numbers(const at::Tensor* t, const at::Tensor& x) { return static_cast<const int64_t*>(per_row(t, x, at::kLong)); }
 template <typename T>
 T* out_data(const at::Tensor& t) { return t.defined() ? static_cast<T*>(t.mutable_data_ptr()) : nullptr; }
 
@@ -179,8 +180,8 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float scale = static_cast<float>(real(a[2]));
     const int32_t k = whole(a[3]);
     need(k >= 0 && k <= ADAPT_MAX_TOP, "between 0 and 32 alternatives");
-    const int64_t* pt = numbers(maybe(a[1]), m.rows);
-    const float *pdl = floats(maybe(a[5]), m.rows), *pdh = floats(maybe(a[6]), m.rows);
+    const int64_t* pt = numbers(maybe(a[1]), x);
+    const float *pdl = floats(maybe(a[5]), x), *pdh = floats(maybe(a[6]), x);
     const at::Tensor* given = maybe(a[7]);
     at::Tensor logprob, entropy, lse = make(x, {m.rows}, at::kFloat), ids, tops, dx;
     if (a[1] != Py_None) logprob = make(x, {m.rows}, at::kFloat);
@@ -210,9 +211,9 @@ PyObject* logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = tensor(a[0]);
     const int dtype = elem(x);
     const Matrix m = matrix(x);
-    const int64_t* pt = numbers(maybe(a[1]), m.rows);
-    const float *pl = floats(maybe(a[2]), m.rows), *pdl = floats(maybe(a[3]), m.rows), *ph = floats(maybe(a[4]), m.rows),
-                *pdh = floats(maybe(a[5]), m.rows);
+    const int64_t* pt = numbers(maybe(a[1]), x);
+    const float *pl = floats(maybe(a[2]), x), *pdl = floats(maybe(a[3]), x), *ph = floats(maybe(a[4]), x),
+                *pdh = floats(maybe(a[5]), x);
     const float scale = static_cast<float>(real(a[6]));
     const at::Tensor out = out_like(maybe(a[7]), x);
     const int64_t ldg = matrix(out).ld;
@@ -243,19 +244,19 @@ struct ScanCall {
     need(channels == 0 || (gates > 0 && channels % gates == 0), "the gates have to divide the channels");
     group = static_cast<int>(gates ? channels / gates : 1);
     if (const at::Tensor* t = maybe(lengths_)) {
-      need(t->is_cuda() && t->scalar_type() == at::kInt && t->dim() == 1 && t->size(0) == batch && t->is_contiguous(),
-           "lengths: int32 [batch]");
+      need(t->device() == x.device() && t->scalar_type() == at::kInt && t->dim() == 1 && t->size(0) == batch && t->is_contiguous(),
+           "lengths: int32 [batch], on the device of x");
       lengths = static_cast<const int32_t*>(t->const_data_ptr());
     }
     if (const at::Tensor* t = maybe(reset_)) {
-      need(t->is_cuda() && (t->scalar_type() == at::kByte || t->scalar_type() == at::kBool) && t->dim() == 2 &&
-               t->size(0) == batch && t->size(1) == steps && t->is_contiguous(), "reset: uint8 or bool [batch, steps]");
+      need(t->device() == x.device() && (t->scalar_type() == at::kByte || t->scalar_type() == at::kBool) && t->dim() == 2 &&
+               t->size(0) == batch && t->size(1) == steps && t->is_contiguous(), "reset: uint8 or bool [batch, steps], on the device of x");
       reset = static_cast<const uint8_t*>(t->const_data_ptr());
     }
   }
   void need_state(const at::Tensor& t) const {
-    need(t.is_cuda() && t.scalar_type() == at::kFloat && t.dim() == 2 && t.size(0) == batch && t.size(1) == channels &&
-             t.is_contiguous(), "states: float32 [batch, channels]");
+    need(t.device() == x.device() && t.scalar_type() == at::kFloat && t.dim() == 2 && t.size(0) == batch &&
+             t.size(1) == channels && t.is_contiguous(), "states: float32 [batch, channels], on the device of x");
   }
   const float* state(const at::Tensor* t) const {
     if (!t) return nullptr;
@@ -310,7 +311,7 @@ PyObject* scan_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const ScanCall c(a[0], a[1], a[5], a[6]);
     const at::Tensor &dy = tensor(a[2]), &carry = tensor(a[3]);
     need_like(dy, c.x);
-    need(carry.is_cuda() && carry.scalar_type() == at::kFloat && carry.is_contiguous() && carry.dim() == 3 &&
+    need(carry.device() == c.x.device() && carry.scalar_type() == at::kFloat && carry.is_contiguous() && carry.dim() == 3 &&
              carry.size(0) == c.batch && carry.size(1) == c.kept() && carry.size(2) == c.channels,
          "carry: as adapt_gated_scan made it");
     const float* dh = c.state(maybe(a[4]));

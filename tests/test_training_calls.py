@@ -97,3 +97,38 @@ def test_outputs_that_are_not_asked_for_are_none():
     assert B.adapt_dropout(x[:0], 0.5).shape == (0, 50) and B.adapt_token_logprobs(x[:0]).lse.shape == (0,)
     # seeds and layers beyond 32 bits and negative ones are taken modulo their width
     assert torch.equal(B.adapt_dropout(x, 0.5, seed=-1), B.adapt_dropout(x, 0.5, seed=2 ** 64 - 1))
+
+
+@pytest.mark.gpu
+def test_side_tensors_of_another_device_are_refused(monkeypatch):
+    """Targets, weights, lengths, resets and states that lie on another GPU.  (Fake tensors: they carry a device,
+    and no memory that a kernel could reach.)"""
+    from torch._subclasses import fake_tensor
+    monkeypatch.setattr(fake_tensor, "init_gpu_context", lambda device: None)   # (it would allocate on that device)
+
+    def away(*shape, dtype=torch.float32):
+        with fake_tensor.FakeTensorMode():
+            return torch.empty(shape, dtype=dtype, device="cuda:1")
+
+    x = torch.zeros(6, 40, device="cuda")
+    t, d = torch.zeros(6, dtype=torch.int64, device="cuda"), torch.zeros(6, device="cuda")
+    s, g, h = torch.zeros(2, 5, 64, device="cuda"), torch.zeros(2, 5, 16, device="cuda"), away(2, 64)
+    carry = B.adapt_gated_scan(s, g, want_carry=True).carry
+    ft, fd = away(6, dtype=torch.int64), away(6)
+    assert ft.device == torch.device("cuda:1") and ft.is_cuda
+    back = lambda **k: B.adapt_gated_scan_backward(s, g, **{"dy": s, "carry": carry, **k})  # noqa: E731
+    before = B.adapt_kernel_launch_count()
+    for call in (lambda: B.adapt_token_logprobs(x, ft), lambda: B.adapt_token_logprobs(x, t, d_logprob=fd),
+                 lambda: B.adapt_token_logprobs(x, t, d_entropy=fd),
+                 lambda: B.adapt_token_logprobs_backward(x, ft, d, d), lambda: B.adapt_token_logprobs_backward(x, t, fd, d),
+                 lambda: B.adapt_token_logprobs_backward(x, t, d, fd),
+                 lambda: B.adapt_token_logprobs_backward(x, t, d, d, fd, d),
+                 lambda: B.adapt_token_logprobs_backward(x, t, d, d, d, fd),
+                 lambda: B.adapt_gated_scan(s, g, h0=h), lambda: B.adapt_gated_scan(s, g, h_last=h),
+                 lambda: B.adapt_gated_scan(s, g, lengths=away(2, dtype=torch.int32)),
+                 lambda: B.adapt_gated_scan(s, g, reset=away(2, 5, dtype=torch.uint8)),
+                 lambda: back(dh_last=h), lambda: back(carry=away(*carry.shape)),
+                 lambda: back(lengths=away(2, dtype=torch.int32)), lambda: back(reset=away(2, 5, dtype=torch.bool))):
+        with pytest.raises(AssertionError):
+            call()
+    assert B.adapt_kernel_launch_count() == before
