@@ -576,6 +576,8 @@ int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t voca
  *   ADAPT_GATE_SIGMOID:  a = 1 / (1 + e^-gate),  h_t = a_t h_{t-1} + (1 - a_t) x_t
  *   ADAPT_GATE_VALUE:    a = gate,               h_t = a_t h_{t-1} + x_t
  * y_t = h_t.  steps = 1 with h0 and h_last is the form for single tokens.
+ * Sequences of many steps are joined from stretches of up to 256: in the value form the product of the
+ * decays of a stretch counts as 3e38 in magnitude where it is larger (a zero state stays zero under it).
  *   x, y     DEVICE [batch][steps][channels]
  *   gate     DEVICE [batch][steps][channels / gate_group]: gate k serves channels
  *            k * gate_group .. (k + 1) * gate_group - 1.  gate_group is a power of two up

@@ -162,6 +162,20 @@ __device__ __forceinline__ f32x2 held2(f32x2 a) {
   const float2 v = unpack2(a);
   return pack2(held(v.x), held(v.y));
 }
+// The product of a piece's decays, held.  Where it ran to infinity on the way and met a decay of 0 (NaN), it is
+// formed again, held at every step.  (Decays of the sigmoid form are at most 1.)
+template <int kMode>
+__device__ __forceinline__ f32x2 held_product(f32x2 product, const f32x2 (&a)[kScanSteps]) {
+  if (kMode == kGateValue) {
+    const float2 v = unpack2(product);
+    if (v.x != v.x || v.y != v.y) {
+      product = a[0];
+#pragma unroll
+      for (int k = 1; k < kScanSteps; ++k) product = mul2(held2(product), a[k]);
+    }
+  }
+  return held2(product);
+}
 // A map h -> a h + b of a lane's two channels; `cut`: what comes before does not count (h -> b).
 struct __align__(16) ScanMap { f32x2 a, b; };
 
@@ -620,7 +634,7 @@ __global__ void __launch_bounds__(kScanThreads, sizeof(T) == 4 || kLanes < 32 ? 
 #pragma unroll
       for (int k = 0; k < kScanSteps; ++k) map.b = through2<true>(resets >> k & 1, a[k], u[k], map.b);
     }
-    map.a = held2(map.a);
+    map.a = held_product<kMode>(map.a, a);
     const int buffer = s & 1;
     f32x2 h;    // the state before this piece
     with_flag(p.reset != nullptr, [&](auto with_cuts) {
@@ -809,7 +823,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
         if (kCut && resets >> k & 1) back.b = 0;
       }
     });
-    back.a = map.a = held2(map.a);
+    back.a = map.a = held_product<kMode>(map.a, a);
     const int round = w.rounds - 1 - s, buffer = round & 1;
     with_flag(p.reset != nullptr, [&](auto with_cuts) {
       constexpr bool kCut = decltype(with_cuts)::value, kHold = kMode == kGateValue;

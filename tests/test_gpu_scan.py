@@ -366,3 +366,21 @@ def test_few_chains_run_through_their_rounds(B, sigmoid, dtype, batch, steps, ch
         c["gate"] = c["gate"].clamp(-1, 1)      # (longer products of decays than in the cases above)
     check(B, c, sigmoid)
     check(B, dict(c, reset=None, lengths=None), sigmoid)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("batch,steps,channels", [(2, 16, 64), (2, 17, 64), (2, 40, 33), (1, 300, 64), (1, 9000, 64),
+                                                  (8, 130, 4000)])
+def test_zero_states_stay_zero_under_large_decays(B, dtype, batch, steps, channels):
+    import torch
+    big = 3e4 if dtype == "float16" else 1e25      # eight of them (fp16: ten) pass the range of fp32
+    gate = torch.full((batch, steps, channels), big, dtype=getattr(torch, dtype), device="cuda")
+    zero = torch.zeros_like(gate)
+    for at in ([7], [9, 15], list(range(5, steps, 6)), []):
+        g = gate.clone()
+        for t in at:
+            g[:, t] = 0
+        r = B.adapt_gated_scan(zero, g, h0=torch.zeros(batch, channels, device="cuda"), mode=B.GATE_VALUE, want_carry=True)
+        b = B.adapt_gated_scan_backward(zero, g, zero, r.carry, mode=B.GATE_VALUE, want_dh0=True)
+        for name, v in (("y", r.y), ("h_last", r.h_last), ("carry", r.carry), ("dx", b.dx), ("dgate", b.dgate), ("dh0", b.dh0)):
+            assert (v == 0).all(), (name, at)
