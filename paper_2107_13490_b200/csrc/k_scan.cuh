@@ -903,7 +903,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) scan_backward_kernel(const Sc
       for (int k = 0; k < kScanSteps; ++k) {
         if (!kWhole && resets >> k & 1) h = 0;
         before[k] = h;
-        h = fma2(a[k], h, added(k));
+        // (a decay of the value form may be Inf or NaN at a reset; where one of the sigmoid form is, so is its 1 - a)
+        h = through2<!kWhole && kMode == kGateValue>(resets >> k & 1, a[k], added(k), h);
       }
       T* gx_at = dx;
       T* gg_at = dgate;

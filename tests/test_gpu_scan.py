@@ -384,3 +384,21 @@ def test_zero_states_stay_zero_under_large_decays(B, dtype, batch, steps, channe
         b = B.adapt_gated_scan_backward(zero, g, zero, r.carry, mode=B.GATE_VALUE, want_dh0=True)
         for name, v in (("y", r.y), ("h_last", r.h_last), ("carry", r.carry), ("dx", b.dx), ("dgate", b.dgate), ("dh0", b.dh0)):
             assert (v == 0).all(), (name, at)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("batch,steps,channels,group", [(2, 6, 32, 1), (2, 40, 32, 1), (1, 300, 96, 4), (1, 2500, 64, 1),
+                                                        (8, 150, 4000, 1)])
+def test_decays_at_a_reset_do_not_count(B, dtype, batch, steps, channels, group):
+    import torch
+    c = case(dtype, batch, steps, channels, group, steps, False)
+    c["reset"] = torch.zeros(batch, steps, dtype=torch.bool, device="cuda")
+    at = [t for t in (0, 3, 5, 12, 31, 64, 130, 131, steps - 1) if t < steps]
+    c["reset"][:, at] = True
+    want = run(B, c, False)
+    for bad in (math.nan, math.inf, -math.inf, 0.0):
+        gate = c["gate"].clone()
+        gate[:, at] = bad
+        got = run(B, dict(c, gate=gate), False)
+        for name in want:
+            assert torch.equal(got[name], want[name]), (name, bad)
