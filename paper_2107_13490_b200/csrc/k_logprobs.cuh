@@ -10,6 +10,7 @@
 #pragma once
 
 #include "k_elem.cuh"
+#include "row_part.h"
 
 namespace adapt {
 
@@ -273,31 +274,15 @@ template <> struct Logits<__half> {
   }
 };
 
-// One CTA's part of a row: whole 16-byte chunks [q0, q1) in the row's aligned indexing (element
-// q kCount - mis is the first of chunk q), and, in the first part, the elements beside them.
+// One CTA's part of a row (row_part.h), in chunks of 16 bytes.
 template <typename T>
-struct RowPart {
+struct RowPart : RowRange {
   static constexpr int kCount = 16 / sizeof(T);
   const uint4* chunks;   // chunk 0 (it may begin before the row)
   const T* x;
-  int mis, q0, q1, head, tail_from, edges;
-  __device__ __forceinline__ RowPart(const T* row, int vocab, int rank, int parts) {
-    x = row;
-    const uintptr_t a = reinterpret_cast<uintptr_t>(row);
-    mis = static_cast<int>((a & 15u) / sizeof(T));
-    chunks = reinterpret_cast<const uint4*>(a & ~static_cast<uintptr_t>(15));
-    const int qa = mis ? 1 : 0;
-    const long long end = static_cast<long long>(mis) + vocab;
-    const int qb = max(qa, static_cast<int>(end / kCount));
-    const int per = (qb - qa + parts - 1) / parts;
-    q0 = min(qb, qa + rank * per);
-    q1 = min(qb, q0 + per);
-    head = mis ? min(kCount - mis, vocab) : 0;
-    tail_from = max(head, qb * kCount - mis);
-    edges = rank == 0 ? head + max(0, vocab - tail_from) : 0;
-  }
-  __device__ __forceinline__ int edge(int i) const { return i < head ? i : tail_from + i - head; }   // element number
-  __device__ __forceinline__ int element(int q) const { return q * kCount - mis; }                   // of a chunk's first
+  __device__ __forceinline__ RowPart(const T* row, int vocab, int rank, int parts)
+      : RowRange(kCount, static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)), vocab, rank, parts),
+        chunks(reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(row) & ~static_cast<uintptr_t>(15))), x(row) {}
 };
 
 // Running maximum and sums of a thread; t = c x - mc in units of ln 2, mc = c m rounded up, so that t <= 0
@@ -465,9 +450,10 @@ __device__ void top_threshold(RowShared<T, kThreads>& sh, float m, int k) {
 template <typename T, int kThreads>
 __device__ void special_row(const LogprobParams& p, RowShared<T, kThreads>& sh, long long row, const T* x, T* dx, long long target) {
   const int me = Team<kThreads>::me();
+  const unsigned vocab = p.vocab;   // (a signed count beyond it would overflow near 2^31)
   float m = -INFINITY;
   bool nan = false;
-  for (int j = me; j < p.vocab; j += kThreads) {
+  for (unsigned j = me; j < vocab; j += kThreads) {
     const float v = to_float(x[j]);
     nan |= v != v;
     m = fmaxf(m, v);
@@ -478,7 +464,7 @@ __device__ void special_row(const LogprobParams& p, RowShared<T, kThreads>& sh, 
   const bool dead = r.m * p.scale == -INFINITY;
   float s = 0.0f, w = 0.0f;
   if (!dead)
-    for (int j = me; j < p.vocab; j += kThreads) {
+    for (unsigned j = me; j < vocab; j += kThreads) {
       const float v = to_float(x[j]);
       const float t = v * p.scale == -INFINITY ? -200.0f : fmaxf((v - r.m) * (p.scale * kLog2e), -200.0f);
       const float e = exp2_approx(t);
@@ -506,7 +492,7 @@ __device__ void special_row(const LogprobParams& p, RowShared<T, kThreads>& sh, 
   Team<kThreads>::sync();
   const RowWeights g = {p.d_logprob ? p.d_logprob[row] : 0.0f, p.d_entropy ? p.d_entropy[row] : 0.0f};
   const bool lost = p.d_logprob && target >= p.vocab;
-  for (int j = me; j < p.vocab; j += kThreads) {
+  for (unsigned j = me; j < vocab; j += kThreads) {
     float d = dead && !nan ? 0.0f : element_grad(row_logp(r, p.scale, to_float(x[j])), j == target, g, r.ln_sum - r.spread, p.scale);
     if (lost) d = __int_as_float(0x7FFFFFFF);
     dx[j] = from_float<T>(d);
@@ -564,7 +550,7 @@ __device__ __forceinline__ void zero_part(const RowPart<T>& part, T* dx) {
 // Whether this thread wrote element j of the part (the target's gradient is put right by its writer).
 template <typename T, int kThreads>
 __device__ __forceinline__ bool wrote(const RowPart<T>& part, int j) {
-  const int q = (j + part.mis) / RowPart<T>::kCount;
+  const int q = part.chunk(j);
   if (q >= part.q0 && q < part.q1) return Team<kThreads>::me() == (part.q1 - 1 - q) % kThreads;
   return Team<kThreads>::me() < part.edges && part.edge(Team<kThreads>::me()) == j;
 }

@@ -367,3 +367,26 @@ def test_nan_at_the_first_token_and_rows_of_nothing_else(B, dtype, vocab):
             r = compare(B, x, t, k=k, weights=False)
             assert r.top_ids[1].tolist() == list(range(k)) and r.top_ids[0, 0] == 0
             assert int(r.top_ids.min()) == 0 and int(r.top_ids.max()) < vocab
+
+
+def test_the_longest_vocabulary(B):
+    import torch
+    vocab = 2 ** 31 - 1
+    buf = torch.zeros(vocab + 8, dtype=torch.bfloat16, device="cuda")
+    for shift in (0, 5):
+        x = buf[shift:shift + vocab][None]
+        buf.zero_()
+        x[0, -1], x[0, -2], x[0, 7] = 30.0, 29.0, 28.0
+        t, d = torch.tensor([vocab - 1], device="cuda"), torch.ones(1, device="cuda")
+        r = B.adapt_token_logprobs(x, t, n_top=3, d_logprob=d, dlogits=x)
+        assert r.top_ids.tolist() == [[vocab - 1, vocab - 2, 7]]
+        total = vocab - 3 + sum(math.exp(v) for v in (28, 29, 30))
+        # a CTA's 256 threads and two chains sum a 16th of the zeros: 2^18 terms each, then chains of 512
+        tol = 2.0 ** -21 * (2 + 30) + (2 ** 18 + 512) * 2.0 ** -24
+        assert abs(float(r.lse) - math.log(total)) <= tol
+        assert abs(float(r.logprob) - (30 - math.log(total))) <= 2 * tol
+        want = {vocab - 1: 1 - math.exp(30) / total, vocab - 2: -math.exp(29) / total, 7: -math.exp(28) / total, 0: -1 / total,
+                vocab // 2: -1 / total, vocab - 3: -1 / total}
+        for j, g in want.items():
+            assert abs(float(x[0, j]) - g) <= (2.0 ** -8 + 4 * tol) * abs(g) + 2 * tol * (j == vocab - 1), j
+        assert (buf[:shift] == 0).all() and (buf[shift + vocab:] == 0).all()      # nothing beside the row is written
