@@ -204,9 +204,11 @@ int adapt_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_
                          const float* d_logprob, const float* d_entropy, void* dlogits_out,
                          int64_t ld_grad, void* stream) {
   if (vocab < 1 || vocab > 0x7FFFFFFF || n_top < 0 || n_top > kMaxTop || n_top > vocab) return ADAPT_ERR_INVALID_ARG;
-  if (n_top > 0 && (!top_ids_out || !top_logprobs_out)) return ADAPT_ERR_INVALID_ARG;
-  if (!targets && (logprob_out || d_logprob)) return ADAPT_ERR_INVALID_ARG;
-  if ((dlogits_out != nullptr) != (d_logprob || d_entropy)) return ADAPT_ERR_INVALID_ARG;
+  if (rows > 0) {   // (arrays of no rows may have no address)
+    if (n_top > 0 && (!top_ids_out || !top_logprobs_out)) return ADAPT_ERR_INVALID_ARG;
+    if (!targets && (logprob_out || d_logprob)) return ADAPT_ERR_INVALID_ARG;
+    if ((dlogits_out != nullptr) != (d_logprob || d_entropy)) return ADAPT_ERR_INVALID_ARG;
+  }
   if (misaligned(targets, 8) || misaligned(logprob_out, 4) || misaligned(entropy_out, 4) || misaligned(lse_out, 4) ||
       misaligned(top_ids_out, 4) || misaligned(top_logprobs_out, 4) || misaligned(d_logprob, 4) || misaligned(d_entropy, 4))
     return ADAPT_ERR_INVALID_ARG;
@@ -224,9 +226,11 @@ int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t voca
                                   const float* entropy, const float* d_logprob, const float* d_entropy,
                                   void* dlogits_out, int64_t ld_grad, void* stream) {
   if (vocab < 1 || vocab > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
-  if (!d_logprob && !d_entropy) return ADAPT_ERR_INVALID_ARG;
-  if ((d_logprob && !targets) || (d_entropy && !entropy)) return ADAPT_ERR_INVALID_ARG;
-  if (rows > 0 && (!lse || !dlogits_out)) return ADAPT_ERR_INVALID_ARG;
+  if (rows > 0) {
+    if (!d_logprob && !d_entropy) return ADAPT_ERR_INVALID_ARG;
+    if ((d_logprob && !targets) || (d_entropy && !entropy)) return ADAPT_ERR_INVALID_ARG;
+    if (!lse || !dlogits_out) return ADAPT_ERR_INVALID_ARG;
+  }
   if (misaligned(targets, 8) || misaligned(lse, 4) || misaligned(entropy, 4) || misaligned(d_logprob, 4) || misaligned(d_entropy, 4))
     return ADAPT_ERR_INVALID_ARG;
   LogprobParams q = {};

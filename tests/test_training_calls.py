@@ -132,3 +132,13 @@ def test_side_tensors_of_another_device_are_refused(monkeypatch):
         with pytest.raises(AssertionError):
             call()
     assert B.adapt_kernel_launch_count() == before
+
+
+@pytest.mark.gpu
+def test_batches_of_no_rows():
+    x, t, d = (torch.zeros(0, 40, device="cuda"), torch.zeros(0, dtype=torch.int64, device="cuda"),
+               torch.zeros(0, device="cuda"))
+    r = B.adapt_token_logprobs(x, t, n_top=4, d_logprob=d, d_entropy=d)
+    assert r.top_ids.shape == r.top_logprobs.shape == (0, 4) and r.dlogits.shape == (0, 40)
+    assert r.logprob.shape == r.entropy.shape == r.lse.shape == (0,)
+    assert B.adapt_token_logprobs_backward(x, t, r.lse, d, r.entropy, d).shape == (0, 40)

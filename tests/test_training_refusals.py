@@ -115,6 +115,16 @@ def test_sizes_of_zero_are_legal(L):
     assert scan_backward(L, batch=0) == B.OK
 
 
+def test_arrays_of_no_rows_need_no_address(L):
+    none = dict(rows=0, x=None, t=None)
+    assert logprobs(L, **none, lp=None, ent=None, lse=None, ids=None, tops=None) == B.OK
+    assert logprobs(L, **none, lp=None, ent=None, lse=None, ids=None, tops=None, dlp=P) == B.OK
+    assert logprobs_backward(L, **none, lse=None, ent=None, dlp=None, dh=None, dx=None) == B.OK
+    # what does not hang on the rows is still refused
+    assert logprobs(L, **none, top=33) == logprobs(L, **none, dtype=4) == logprobs(L, **none, scale=0.0) == B.ERR_INVALID_ARG
+    assert logprobs_backward(L, **none, vocab=0) == logprobs_backward(L, **none, scale=-1.0) == B.ERR_INVALID_ARG
+
+
 def test_workspace_query(L):
     assert B.adapt_gated_scan_workspace_bytes(2, 3, 64) >= 0
     assert B.adapt_gated_scan_workspace_bytes(2, 3, 64, gate_group=3) == 0
