@@ -51,7 +51,20 @@ uint64_t bits(PyObject* o) {
   if (v == ~0ull && PyErr_Occurred()) throw Refused{nullptr};
   return v;
 }
-int32_t whole(PyObject* o) { return static_cast<int32_t>(bits(o)); }
+int32_t whole(PyObject* o) { return static_cast<int32_t>(bits(o)); }   // modulo 2^32
+// A number that has to be meant as it stands.
+int32_t between(PyObject* o, int32_t least, int32_t most, const char* why) {
+  int beyond = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &beyond);
+  if (v == -1 && !beyond && PyErr_Occurred()) throw Refused{nullptr};
+  need(!beyond && v >= least && v <= most, why);
+  return static_cast<int32_t>(v);
+}
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Refused{nullptr};
+  return v != 0;
+}
 
 // The element type of a tensor on the current device.
 int elem(const at::Tensor& t) {
@@ -178,14 +191,13 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int dtype = elem(x);
     const Matrix m = matrix(x);
     const float scale = static_cast<float>(real(a[2]));
-    const int32_t k = whole(a[3]);
-    need(k >= 0 && k <= ADAPT_MAX_TOP, "between 0 and 32 alternatives");
+    const int32_t k = between(a[3], 0, ADAPT_MAX_TOP, "between 0 and 32 alternatives");
     const int64_t* pt = numbers(maybe(a[1]), x);
     const float *pdl = floats(maybe(a[5]), x), *pdh = floats(maybe(a[6]), x);
     const at::Tensor* given = maybe(a[7]);
     at::Tensor logprob, entropy, lse = make(x, {m.rows}, at::kFloat), ids, tops, dx;
     if (a[1] != Py_None) logprob = make(x, {m.rows}, at::kFloat);
-    if (PyObject_IsTrue(a[4])) entropy = make(x, {m.rows}, at::kFloat);
+    if (truth(a[4])) entropy = make(x, {m.rows}, at::kFloat);
     if (k) {
       ids = make(x, {m.rows, k}, at::kInt);
       tops = make(x, {m.rows, k}, at::kFloat);
@@ -287,13 +299,13 @@ PyObject* scan(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&] {
     const ScanCall c(a[0], a[1], a[3], a[4]);
     const float* h0 = c.state(maybe(a[2]));
-    const int mode = whole(a[5]);
+    const int mode = between(a[5], INT32_MIN, INT32_MAX, "no such gate");
     const at::Tensor y = out_like(maybe(a[7]), c.x);
     const at::Tensor* given = maybe(a[8]);
     const at::Tensor h = given ? *given : make(c.x, {c.batch, c.channels}, at::kFloat);
     c.need_state(h);
     at::Tensor carry;
-    if (PyObject_IsTrue(a[6])) carry = make(c.x, {c.batch, c.kept(), c.channels}, at::kFloat);
+    if (truth(a[6])) carry = make(c.x, {c.batch, c.kept(), c.channels}, at::kFloat);
     const Strides s{&c.x, &c.gate, &y};
     const void *px = c.x.const_data_ptr(), *pg = c.gate.const_data_ptr();
     void* stream = stream_of(c.x);
@@ -315,10 +327,10 @@ PyObject* scan_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
              carry.size(0) == c.batch && carry.size(1) == c.kept() && carry.size(2) == c.channels,
          "carry: as adapt_gated_scan made it");
     const float* dh = c.state(maybe(a[4]));
-    const int mode = whole(a[7]);
+    const int mode = between(a[7], INT32_MIN, INT32_MAX, "no such gate");
     const at::Tensor dx = out_like(maybe(a[9]), c.x), dgate = out_like(maybe(a[10]), c.gate);
     at::Tensor dh0, workspace;
-    if (PyObject_IsTrue(a[8])) dh0 = make(c.x, {c.batch, c.channels}, at::kFloat);
+    if (truth(a[8])) dh0 = make(c.x, {c.batch, c.channels}, at::kFloat);
     size_t bytes = 0;
     if (c.group > 1) {
       bytes = g_scan_workspace(c.batch, c.steps, c.channels, c.group, c.dtype, 1);

@@ -142,3 +142,21 @@ def test_batches_of_no_rows():
     assert r.top_ids.shape == r.top_logprobs.shape == (0, 4) and r.dlogits.shape == (0, 40)
     assert r.logprob.shape == r.entropy.shape == r.lse.shape == (0,)
     assert B.adapt_token_logprobs_backward(x, t, r.lse, d, r.entropy, d).shape == (0, 40)
+
+
+@pytest.mark.gpu
+def test_numbers_are_taken_as_they_stand():
+    x = torch.randn(3, 50, device="cuda")
+    s = torch.randn(2, 5, 64, device="cuda")
+    carry = B.adapt_gated_scan(s, s, want_carry=True).carry
+    for call in (lambda: B.adapt_token_logprobs(x, n_top=2 ** 32 + 1), lambda: B.adapt_token_logprobs(x, n_top=2 ** 64),
+                 lambda: B.adapt_token_logprobs(x, n_top=-2 ** 70), lambda: B.adapt_gated_scan(s, s, mode=2 ** 32),
+                 lambda: B.adapt_gated_scan_backward(s, s, s, carry, mode=2 ** 32 + 1)):
+        with pytest.raises(AssertionError):
+            call()
+    # a flag without a truth value is an error of its own kind
+    many = torch.zeros(2)
+    for call in (lambda: B.adapt_token_logprobs(x, want_entropy=many), lambda: B.adapt_gated_scan(s, s, want_carry=many),
+                 lambda: B.adapt_gated_scan_backward(s, s, s, carry, want_dh0=many)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            call()
