@@ -1,45 +1,16 @@
-// C-ABI entry points of the training-step operators: dropout, token log probabilities, gated
-// recurrence.  Declarations and argument contracts live in adapt.h.
-#include <cuda_runtime.h>
-
-#include <algorithm>
+// C-ABI entry points of the training-step operators dropout and token log probabilities.  Declarations and
+// argument contracts live in adapt.h.
 #include <cmath>
 #include <cstdint>
-#include <initializer_list>
-#include <vector>
 
-#include "../../include/adapt.h"
 #include "dropout_pieces.h"
-#include "host.cuh"
 #include "k_dropout.cuh"
 #include "k_logprobs.cuh"
-#include "k_scan.cuh"
-
-namespace {
+#include "training_host.cuh"
 
 using namespace adapt;
 
-static_assert(ADAPT_SCAN_TILE == kScanTile && ADAPT_MAX_TOP == kMaxTop && ADAPT_GATE_SIGMOID == kGateSigmoid &&
-              ADAPT_GATE_VALUE == kGateValue, "the kernels use the constants of the C interface");
-
-// Bytes of an element, 0 for an unknown type.
-int elem_bytes(int dtype) {
-  return dtype == ADAPT_DTYPE_F32 ? 4 : (dtype == ADAPT_DTYPE_F16 || dtype == ADAPT_DTYPE_BF16) ? 2 : 0;
-}
-
-bool misaligned(const void* p, int bytes) {
-  return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) != 0;
-}
-
-// Calls f(T{}) with the element type.
-template <typename F>
-void with_type(int dtype, F f) {
-  if (dtype == ADAPT_DTYPE_F32) f(float{});
-  else if (dtype == ADAPT_DTYPE_F16) f(__half{});
-  else f(__nv_bfloat16{});
-}
-
-}  // namespace
+static_assert(ADAPT_MAX_TOP == kMaxTop, "the kernels use the constant of the C interface");
 
 extern "C" {
 
@@ -238,275 +209,6 @@ int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t voca
   q.scale = scale; q.targets = reinterpret_cast<const long long*>(targets);
   q.lse_in = lse; q.entropy_in = entropy; q.d_logprob = d_logprob; q.d_entropy = d_entropy; q.dlogits = dlogits_out;
   return run_logprobs(q, dtype, stream);
-}
-
-}  // extern "C"
-
-namespace {
-
-// Checks what forward and backward share.  Fills sizes; strides are set by the caller.
-bool scan_shape(ScanParams& q, int64_t batch, int64_t steps, int64_t channels, int group, int dtype, int mode) {
-  if (!elem_bytes(dtype) || (mode != ADAPT_GATE_SIGMOID && mode != ADAPT_GATE_VALUE)) return false;
-  if (batch < 0 || steps < 0 || channels < 0) return false;
-  if (steps > 0x7FFFE000 || channels > 0x7FFFFFFF || batch > 0x7FFFFFFF) return false;
-  if (batch > 0 && channels > 0 && batch > (1ll << 27) / ((channels + kScanChannels - 1) / kScanChannels)) return false;
-  // a gate of its own, or shared by a power of two of channels up to 64, or by a multiple of 64
-  const bool ok = group >= 1 && (group <= 64 ? (group & (group - 1)) == 0 : group % 64 == 0);
-  if (!ok || channels % group != 0) return false;
-  q.batch = batch; q.steps = steps; q.channels = channels; q.group = group;
-  return true;
-}
-
-// Stride pair: given, or that of a contiguous [batch][steps][width] array.
-void stride_pair(const int64_t* given, int k, int64_t steps, int64_t width, long long& b, long long& t) {
-  b = given ? given[2 * k] : steps * width;
-  t = given ? given[2 * k + 1] : width;
-}
-
-// Rows that are written must not overlap.
-bool out_strides_ok(long long b, long long t, const ScanParams& q, int64_t width) {
-  if (b < 0 || t < 0) return false;
-  if (q.steps > 1 && t < width) return false;
-  if (q.batch > 1 && b < width) return false;
-  if (q.steps > 1 && q.batch > 1 && b < t * q.steps && t < b * q.batch) return false;
-  return true;
-}
-
-size_t scan_workspace(const ScanParams& q, bool backward) {
-  if (!backward || q.group <= kScanChannels) return 0;
-  return sizeof(float) * static_cast<size_t>(q.batch) * q.steps * (q.channels / kScanChannels);
-}
-
-// Whether `unit` channels can be moved at a time.
-bool scan_fits(const ScanParams& q, int elem, int unit, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
-  if (q.channels % unit) return false;
-  for (const void* p : ptrs) if (misaligned(p, unit * elem)) return false;
-  for (long long s : strides) if (s % unit) return false;
-  return true;
-}
-
-// How many channels a tile kernel moves at a time: those of 16 bytes, two, or one.
-int scan_move(const ScanParams& q, int elem, std::initializer_list<const void*> ptrs, std::initializer_list<long long> strides) {
-  return scan_fits(q, elem, 16 / elem, ptrs, strides) ? kMoveVec : scan_fits(q, elem, 2, ptrs, strides) ? kMovePair : kMoveOne;
-}
-
-// Whether shared gates can be copied by the 4-byte words that hold them, none of which leaves its row.
-bool scan_gate_words(const ScanParams& q, int elem) {
-  return elem == 4 || (q.channels / q.group % 2 == 0 && !misaligned(q.gate, 4) && q.gb % 2 == 0 && q.gt % 2 == 0);
-}
-
-// CTAs of a tile kernel that the device holds at once, by kernel (first use: attributes and occupancy).
-struct ScanSlots { const void* kernel; int device, slots; };
-std::vector<ScanSlots> g_scan_slots;   // under g_mutex
-
-int scan_slots(DeviceCache& dc, const void* kernel, size_t smem, int channels, int* out) {
-  int dev = 0;
-  ADAPT_CUDA(cudaGetDevice(&dev));
-  for (const ScanSlots& s : g_scan_slots)
-    if (s.kernel == kernel && s.device == dev) { *out = s.slots; return ADAPT_OK; }
-  ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  static_cast<int>(smem + scan_totals_bytes(kScanMaxCluster, channels))));
-  ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-  int per_sm = 0;
-  ADAPT_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kScanThreads, smem + scan_totals_bytes(4, channels)));
-  const int slots = std::max(1, per_sm) * dc.sm_count;
-  g_scan_slots.push_back({kernel, dev, slots});
-  *out = slots;
-  return ADAPT_OK;
-}
-
-typedef void (*ScanKernel)(ScanParams);
-
-// The tile kernels of one type, mode and alignment, for 64, 32 and 16 channels a CTA, and the number of
-// CTAs to a chain, by the estimated time: waves of CTAs x rounds of a chain x the time of a round, in units
-// of a round without exchange (1.4 to 2.5 us).  An exchange costs 1.35 + 0.03 K of them, narrower tiles
-// 10 % a halving.  Measured forward, us: 8 x 4096 x 2048 bf16 (256 chains of 64) 91 with one CTA to a chain,
-// 119 with two; 1 x 65536 x 1024 bf16 (16 chains of 64, 32 of 32) 1070 with one, 234 with 16, 134 with 32
-// channels and 8 CTAs; over twelve shapes both ways the choice is within 3 % of the best on the mean.
-int launch_scan(DeviceCache& dc, const ScanKernel (&kernels)[3], int tensors, int elem, const ScanParams& q, cudaStream_t stream) {
-  const size_t stages = kScanStages * scan_stage_bytes(tensors, elem);
-  int width = 0, cluster = 1;
-  double least = 1e300;
-  for (int i = 0; i < 3; ++i) {
-    const int channels = kScanChannels >> i;
-    if (i && q.group > channels) break;   // a shared gate stays in one CTA
-    int slots = 0;
-    const int rc = scan_slots(dc, reinterpret_cast<const void*>(kernels[i]), stages, channels, &slots);
-    if (rc != ADAPT_OK) return rc;
-    const long long chains = q.batch * ((q.channels + channels - 1) / channels);
-    const long long tiles = (q.steps * channels + kTileElements - 1) / kTileElements;
-    for (int k = 1; k <= kScanMaxCluster; k *= 2) {
-      if (k > 1 && k / 2 >= tiles) break;
-      const double full = static_cast<double>(chains * k) / slots, waves = full <= 1.0 ? 1.0 : full + 0.5;
-      const double rounds = static_cast<double>((tiles + k - 1) / k);
-      const double cost = waves * rounds * (k > 1 ? 1.35 + 0.03 * k : 1.0) * (1.0 + 0.1 * i);
-      if (cost < least) { least = cost; width = i; cluster = k; }
-    }
-  }
-  const int channels = kScanChannels >> width;
-  const long long chains = q.batch * ((q.channels + channels - 1) / channels);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(chains * cluster));
-  cfg.blockDim = dim3(kScanThreads);
-  cfg.dynamicSmemBytes = stages + scan_totals_bytes(cluster, channels);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kernels[width], q));
-  return ADAPT_OK;
-}
-
-#define ADAPT_SCAN_WIDTHS(name, T, mode, move) {name<T, mode, move, 32>, name<T, mode, move, 16>, name<T, mode, move, 8>}
-// Launches the kernels `name` of a type for the call's mode and alignment.
-#define ADAPT_SCAN_LAUNCH(name, T, tensors)                                                            \
-  {                                                                                                    \
-    static const ScanKernel kernels[2][3][3] = {                                                       \
-        {ADAPT_SCAN_WIDTHS(name, T, 0, 0), ADAPT_SCAN_WIDTHS(name, T, 0, 1), ADAPT_SCAN_WIDTHS(name, T, 0, 2)},  \
-        {ADAPT_SCAN_WIDTHS(name, T, 1, 0), ADAPT_SCAN_WIDTHS(name, T, 1, 1), ADAPT_SCAN_WIDTHS(name, T, 1, 2)}}; \
-    rc = launch_scan(*dc, kernels[mode][move], tensors, e, q, stream);                                 \
-  }
-// Short sequences take a thread for every four channels instead of tiles, which would be mostly empty.
-// Measured on bf16, us, serial against tiles: 256 x 16 x 4096 36 / 109, 256 x 32 x 4096 68 / 108,
-// 64 x 16 x 4096 12 / 29, 64 x 32 x 4096 31 / 29, 8 x 16 x 1024 8 / 8, 8 x 32 x 1024 17 / 8.
-bool scan_serial(const ScanParams& q) {
-  return q.steps <= 16 || (q.steps <= 32 && q.batch * q.channels >= (1 << 19));
-}
-
-// The caller's workspace, or the library's (grown on demand).
-int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, char** out) {
-  *out = nullptr;
-  if (need == 0) return ADAPT_OK;
-  if (workspace) {
-    if (have < need) return ADAPT_ERR_WORKSPACE;
-    if (misaligned(workspace, 256)) return ADAPT_ERR_INVALID_ARG;
-    *out = static_cast<char*>(workspace);
-    return ADAPT_OK;
-  }
-  const int rc = grow_device(&dc.scan_buf, &dc.scan_buf_bytes, align_up(need, 4096));
-  *out = static_cast<char*>(dc.scan_buf);
-  return rc;
-}
-
-}  // namespace
-
-extern "C" {
-
-size_t adapt_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels, int gate_group,
-                                        int dtype, int backward) {
-  ScanParams q = {};
-  if (!scan_shape(q, batch, steps, channels, gate_group, dtype, ADAPT_GATE_SIGMOID)) return 0;
-  return scan_workspace(q, backward != 0);
-}
-
-int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int32_t* lengths,
-                     const uint8_t* reset, int64_t batch, int64_t steps, int64_t channels,
-                     int gate_group, int dtype, int mode, const int64_t* strides, void* y,
-                     float* h_last, float* carry_out, void* workspace, size_t workspace_bytes,
-                     void* stream_handle) {
-  ScanParams q = {};
-  if (!scan_shape(q, batch, steps, channels, gate_group, dtype, mode)) return ADAPT_ERR_INVALID_ARG;
-  if (batch == 0 || channels == 0) return ADAPT_OK;
-  const int e = elem_bytes(dtype);
-  if (steps > 0 && (!x || !gate || !y)) return ADAPT_ERR_INVALID_ARG;
-  if (misaligned(x, e) || misaligned(gate, e) || misaligned(y, e) || misaligned(h0, 4) || misaligned(h_last, 4) ||
-      misaligned(carry_out, 4) || misaligned(lengths, 4))
-    return ADAPT_ERR_INVALID_ARG;
-  stride_pair(strides, 0, steps, channels, q.xb, q.xt);
-  stride_pair(strides, 1, steps, channels / gate_group, q.gb, q.gt);
-  stride_pair(strides, 2, steps, channels, q.yb, q.yt);
-  if (q.xb < 0 || q.xt < 0 || q.gb < 0 || q.gt < 0 || !out_strides_ok(q.yb, q.yt, q, channels)) return ADAPT_ERR_INVALID_ARG;
-  q.x = x; q.gate = gate; q.h0 = h0; q.lengths = lengths; q.reset = reset; q.y = y; q.h_last = h_last; q.carry = carry_out;
-  (void)workspace; (void)workspace_bytes;   // the tiles meet in shared memory
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  std::lock_guard<std::mutex> lock(g_mutex);
-  DeviceCache* dc = nullptr;
-  int rc = current_cache(&dc);
-  if (rc != ADAPT_OK) return rc;
-  LaunchScope ls(ADAPT_KERNEL_SCAN, stream);
-  const bool own = gate_group == 1;   // a gate for every channel
-  const std::initializer_list<const void*> ptrs = {x, y, own ? gate : nullptr};
-  const std::initializer_list<long long> lines = {q.xb, q.xt, q.yb, q.yt, own ? q.gb : 0, own ? q.gt : 0};
-  if (scan_serial(q)) {
-    const bool wide = scan_fits(q, e, 4, ptrs, lines) && (own || gate_group % 4 == 0);
-    const unsigned grid = static_cast<unsigned>((batch * channels / (wide ? 4 : 1) + 127) / 128);
-    with_type(dtype, [&](auto t) {
-      using T = decltype(t);
-      auto go = [&](auto kernel) { kernel<<<grid, 128, 0, stream>>>(q); };
-      if (mode == ADAPT_GATE_SIGMOID) wide ? go(scan_serial_kernel<T, kGateSigmoid, 4>) : go(scan_serial_kernel<T, kGateSigmoid, 1>);
-      else wide ? go(scan_serial_kernel<T, kGateValue, 4>) : go(scan_serial_kernel<T, kGateValue, 1>);
-    });
-  } else {
-    const int move = scan_move(q, e, ptrs, lines);
-    q.gate_words = scan_gate_words(q, e);
-    with_type(dtype, [&](auto t) {
-      using T = decltype(t);
-      ADAPT_SCAN_LAUNCH(scan_kernel, T, 2);
-    });
-    if (rc != ADAPT_OK) return rc;
-  }
-  ADAPT_LAUNCH_OK("gated scan");
-  return ADAPT_OK;
-}
-
-int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy, const float* carry,
-                              const float* dh_last, const int32_t* lengths, const uint8_t* reset,
-                              int64_t batch, int64_t steps, int64_t channels, int gate_group,
-                              int dtype, int mode, const int64_t* strides, void* dx, void* dgate,
-                              float* dh0, void* workspace, size_t workspace_bytes,
-                              void* stream_handle) {
-  ScanParams q = {};
-  if (!scan_shape(q, batch, steps, channels, gate_group, dtype, mode)) return ADAPT_ERR_INVALID_ARG;
-  if (batch == 0 || channels == 0) return ADAPT_OK;
-  const int e = elem_bytes(dtype);
-  if (steps > 0 && (!x || !gate || !dy || !carry || !dx || !dgate)) return ADAPT_ERR_INVALID_ARG;
-  if (misaligned(x, e) || misaligned(gate, e) || misaligned(dy, e) || misaligned(dx, e) || misaligned(dgate, e) ||
-      misaligned(carry, 4) || misaligned(dh_last, 4) || misaligned(dh0, 4) || misaligned(lengths, 4))
-    return ADAPT_ERR_INVALID_ARG;
-  stride_pair(strides, 0, steps, channels, q.xb, q.xt);
-  stride_pair(strides, 1, steps, channels / gate_group, q.gb, q.gt);
-  stride_pair(strides, 2, steps, channels, q.yb, q.yt);
-  stride_pair(strides, 3, steps, channels, q.dxb, q.dxt);
-  stride_pair(strides, 4, steps, channels / gate_group, q.dgb, q.dgt);
-  if (q.xb < 0 || q.xt < 0 || q.gb < 0 || q.gt < 0 || q.yb < 0 || q.yt < 0 ||
-      !out_strides_ok(q.dxb, q.dxt, q, channels) || !out_strides_ok(q.dgb, q.dgt, q, channels / gate_group))
-    return ADAPT_ERR_INVALID_ARG;
-  q.x = x; q.gate = gate; q.dy = dy; q.carry = const_cast<float*>(carry); q.dh_last = dh_last;
-  q.lengths = lengths; q.reset = reset; q.dx = dx; q.dgate = dgate; q.dh0 = dh0;
-  std::lock_guard<std::mutex> lock(g_mutex);
-  DeviceCache* dc = nullptr;
-  int rc = current_cache(&dc);
-  if (rc != ADAPT_OK) return rc;
-  char* scratch = nullptr;
-  rc = scan_scratch(*dc, workspace, workspace_bytes, scan_workspace(q, true), &scratch);
-  if (rc != ADAPT_OK) return rc;
-  q.partial = reinterpret_cast<float*>(scratch);
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  {
-    LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
-    const bool own = gate_group == 1;
-    const int move = scan_move(q, e, {x, dy, dx, own ? gate : nullptr, own ? dgate : nullptr},
-                                  {q.xb, q.xt, q.yb, q.yt, q.dxb, q.dxt, own ? q.gb : 0, own ? q.gt : 0,
-                                   own ? q.dgb : 0, own ? q.dgt : 0});
-    q.gate_words = scan_gate_words(q, e);
-    with_type(dtype, [&](auto t) {
-      using T = decltype(t);
-      ADAPT_SCAN_LAUNCH(scan_backward_kernel, T, 3);
-    });
-    if (rc != ADAPT_OK) return rc;
-    ADAPT_LAUNCH_OK("gated scan, backward");
-  }
-  if (q.partial && steps > 0) {
-    const long long n = batch * steps * (channels / gate_group);
-    LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
-    with_type(dtype, [&](auto t) {
-      scan_gate_sum_kernel<decltype(t)><<<static_cast<int>(std::min<long long>((n + 255) / 256, 16ll * dc->sm_count)), 256, 0, stream>>>(q);
-    });
-    ADAPT_LAUNCH_OK("gate gradient sum");
-  }
-  return ADAPT_OK;
 }
 
 }  // extern "C"
