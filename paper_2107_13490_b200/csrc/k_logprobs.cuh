@@ -57,6 +57,14 @@ __device__ __forceinline__ float exp2_approx(float v) {
 }
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// log2 e scale (v - m), the exponent of v beside the maximum.  (From a scale of 2.4e38 on log2 e scale leaves the range:
+// then v and m, which are small there, count twice and the factor half.)
+struct Exponent {
+  float unit, c;
+  __device__ __forceinline__ explicit Exponent(float scale) : unit(scale > 1e38f ? 2.0f : 1.0f), c(scale / unit * kLog2e) {}
+  __device__ __forceinline__ float operator()(float v, float unit_m) const { return fmaf(v, unit, -unit_m) * c; }
+};
+
 // What a row without a target leaves.
 __device__ __forceinline__ void put_ignored(const LogprobParams& p, long long row) {
   if (p.logprob) p.logprob[row] = 0.0f;
@@ -143,12 +151,13 @@ __global__ void __launch_bounds__(kRowThreads) logprob_warp_kernel(const Logprob
     m = warp_max(m);
     nan = __any_sync(~0u, nan) || m * p.scale == INFINITY;
     r.m = m;
-    const float c = p.scale * kLog2e;
+    const Exponent exponent(p.scale);
+    const float unit_m = exponent.unit * m;
     float s = 0.0f, w = 0.0f;
     if (m * p.scale != -INFINITY) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const float t = v[i] * p.scale == -INFINITY ? -200.0f : fmaxf((v[i] - m) * c, -200.0f);
+        const float t = v[i] * p.scale == -INFINITY ? -200.0f : fmaxf(exponent(v[i], unit_m), -200.0f);
         const float e = exp2_approx(t);
         s += e;
         w = fmaf(e, t, w);
@@ -462,11 +471,13 @@ __device__ void special_row(const LogprobParams& p, RowShared<T, kThreads>& sh, 
   RowStats r = {Team<kThreads>::reduce(m, sh.red[0], true), 0.0f, 0.0f};
   nan |= r.m * p.scale == INFINITY;
   const bool dead = r.m * p.scale == -INFINITY;
+  const Exponent exponent(p.scale);
+  const float unit_m = exponent.unit * r.m;
   float s = 0.0f, w = 0.0f;
   if (!dead)
     for (unsigned j = me; j < vocab; j += kThreads) {
       const float v = to_float(x[j]);
-      const float t = v * p.scale == -INFINITY ? -200.0f : fmaxf((v - r.m) * (p.scale * kLog2e), -200.0f);
+      const float t = v * p.scale == -INFINITY ? -200.0f : fmaxf(exponent(v, unit_m), -200.0f);
       const float e = exp2_approx(t);
       s += e;
       w = fmaf(e, t, w);

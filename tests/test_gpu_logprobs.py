@@ -390,3 +390,14 @@ def test_the_longest_vocabulary(B):
         for j, g in want.items():
             assert abs(float(x[0, j]) - g) <= (2.0 ** -8 + 4 * tol) * abs(g) + 2 * tol * (j == vocab - 1), j
         assert (buf[:shift] == 0).all() and (buf[shift + vocab:] == 0).all()      # nothing beside the row is written
+
+
+@pytest.mark.parametrize("vocab", [50, 1000, 2600, 20000])
+def test_scales_at_the_end_of_the_range(B, vocab):
+    for scale in (2.0 ** 127, float(np.float32(3.4e38)), 2.0 ** 120, 2.0 ** -120, 2.0 ** -126):
+        x = logits(4, vocab, "float32", vocab)
+        x *= 1 / scale if scale > 1 else 1.0        # z of order 3, or next to nothing
+        x[1, ::3] = -math.inf
+        x[2] -= 2 / scale if scale > 1 else 0.0
+        r = compare(B, x, [0, 1, 2, 3], scale=scale, k=3, weights=False)
+        assert r.lse.isfinite().all() and r.entropy.isfinite().all()
