@@ -28,7 +28,8 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   auto off = [&](const void* a, const void* b) { return (reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u; };
   const bool vec = !off(x, y) && (!residual || !off(x, residual)) &&
                    (rows == 1 || ((ldx - ldy) % (16 / e) == 0 && (!residual || (ldx - ldr) % (16 / e) == 0)));
-  const int unit = 16 / e;
+  const bool pairs = !vec && rows > 1 && cols < kPairsBelow;
+  const int unit = pairs ? 2 : 16 / e;
   DropoutParams q = {};
   q.cols = cols; q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
   q.base = seed ^ 0xA54FF53A5F1D36F1ull ^ ((static_cast<uint64_t>(static_cast<int64_t>(layer)) + 1ull) * 0x9E3779B97F4A7C15ull);
@@ -37,7 +38,7 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
   q.threshold = q.none ? 0u : static_cast<unsigned>(threshold);
   q.scale = p < 1.0 ? static_cast<float>(1.0 / (1.0 - p)) : 0.0f;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  const DropoutPieces pieces(rows, cols, e);
+  const DropoutPieces pieces(rows, cols, unit);
   return pieces.each([&](int64_t row, int64_t col, int64_t n_rows, int64_t n_cols) -> int {
     q.x = static_cast<const char*>(x) + (row * ldx + col) * e;
     q.y = static_cast<char*>(y) + (row * ldy + col) * e;
@@ -45,7 +46,7 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
     q.x_end = static_cast<const char*>(q.x) + ((n_rows - 1) * ldx + n_cols) * e;
     q.r_end = residual ? static_cast<const char*>(q.r) + ((n_rows - 1) * ldr + n_cols) * e : nullptr;
     q.index_base = static_cast<long long>(index_base) + row * cols + col;
-    if (n_rows == 1) {
+    if (n_rows == 1 && !pairs) {
       q.mis = static_cast<int>((reinterpret_cast<uintptr_t>(q.y) & 15u) / e);
       q.cols = n_cols;
       q.chunks = static_cast<unsigned>((q.mis + n_cols + unit - 1) / unit);
@@ -60,13 +61,15 @@ int adapt_dropout(const void* x, const void* residual, void* y, int64_t rows, in
       q.shift = s;
       q.magic = static_cast<unsigned>(((1ull << (32 + s)) + q.per_row - 1) / q.per_row);
     }
-    const unsigned tile = kDropoutThreads * (vec ? kDropoutUnroll : kShiftUnroll);
+    const unsigned tile = kDropoutThreads * (pairs ? kPairsUnroll : vec ? kDropoutUnroll : kShiftUnroll);
     const unsigned grid = (q.chunks + tile - 1) / tile;
     LaunchScope ls(ADAPT_KERNEL_DROPOUT, stream);
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
       auto go = [&](auto kernel) { kernel<<<grid, kDropoutThreads, 0, stream>>>(q); };
-      if (n_rows == 1) {
+      if (pairs) {
+        residual ? go(dropout_pairs_kernel<T, true>) : go(dropout_pairs_kernel<T, false>);
+      } else if (n_rows == 1) {
         if (vec) residual ? go(dropout_kernel<T, false, true, false>) : go(dropout_kernel<T, false, false, false>);
         else residual ? go(dropout_kernel<T, true, true, false>) : go(dropout_kernel<T, true, false, false>);
       } else {

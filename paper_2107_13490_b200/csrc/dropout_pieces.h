@@ -1,5 +1,6 @@
-// The launches of a dropout call.  A launch numbers the 16-byte chunks of its rows in 31 bits, so larger tensors go
-// in pieces of whole rows, and a row that is too long for one launch goes alone, in pieces of its columns.
+// The launches of a dropout call.  A launch numbers the chunks of its rows (16 bytes, or a pair of elements) in 31
+// bits, so larger tensors go in pieces of whole rows, and a row that is too long for one launch goes alone, in pieces
+// of its columns.
 #pragma once
 
 #include <algorithm>
@@ -13,7 +14,7 @@ struct DropoutPieces {
   int64_t per_row;              // chunks of a row (the most that any alignment needs)
   int64_t row_step, col_step;   // rows and columns of a piece (col_step a multiple of unit where it cuts a row)
 
-  DropoutPieces(int64_t rows, int64_t cols, int elem) : rows(rows), cols(cols), unit(16 / elem) {
+  DropoutPieces(int64_t rows, int64_t cols, int64_t unit) : rows(rows), cols(cols), unit(unit) {
     constexpr int64_t kMost = 1ll << 30;   // chunks of a launch
     col_step = std::min<int64_t>(cols, (kMost - 2) / 8 * unit);
     per_row = (col_step + unit - 1) / unit + 1;

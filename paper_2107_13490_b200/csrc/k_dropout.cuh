@@ -11,6 +11,8 @@ namespace adapt {
 
 constexpr int kDropoutThreads = 256;
 constexpr int kDropoutUnroll = 2, kShiftUnroll = 1;   // chunks of a thread (kShift with 2: 8.3 us for 7.8, 4099 x 1001 fp16)
+constexpr int kPairsUnroll = 4;                       // pairs of a thread
+constexpr int kPairsBelow = 16;                       // shorter rows of other alignments go in pairs
 
 struct DropoutParams {
   const void* x;
@@ -94,7 +96,7 @@ __device__ __forceinline__ uint4 join_blocks(const uint4& low, const uint4& high
 // x and r, and chunks over a row's ends go element by element (whole blocks there too: 16384 x 4096 bf16 51 us,
 // 49 without).  Otherwise (kShift) x and r are shifted out of the aligned blocks around them, over a row's ends
 // too: 16384 x 4095 bf16 into rows of another alignment 66 us, 111 with pairs of elements; 4099 x 1001 fp16 7.8
-// and 10.4; rows of 10 elements are too short for it (10^6 x 10 31 and 23 us).  kRows: several rows.
+// and 10.4; rows of fewer than kPairsBelow elements go in pairs (below).  kRows: several rows.
 template <typename T, bool kShift, bool kResidual, bool kRows>
 __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutParams p) {
   constexpr int kCount = 16 / sizeof(T);
@@ -181,6 +183,46 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutP
         if (kResidual) f += to_float(r[i][k]);
         y[i][k] = from_float<T>(f);
       }
+    }
+  }
+}
+
+// Short rows of other alignments: a chunk is a hash's pair of elements, so a row of 10 takes five or six threads of
+// one hash, not two or three of four.  Always several rows.  Measured on 10^7 elements, us, pairs against shifted
+// chunks: bf16 rows of 3 33 / 60, of 10 21 / 31, of 15 21 / 23, of 16 21 / 18, of 64 19 / 14; fp32 of 3 31 / 43, of
+// 10 21 / 27, of 15 21 / 23, of 16 21 / 21, of 64 20 / 19.
+template <typename T, bool kResidual>
+__global__ void __launch_bounds__(kDropoutThreads) dropout_pairs_kernel(const DropoutParams p) {
+  const unsigned first = blockIdx.x * (kDropoutThreads * kPairsUnroll) + threadIdx.x;
+  T x[kPairsUnroll][2], r[kPairsUnroll][2], *y[kPairsUnroll];
+  bool on[kPairsUnroll][2];
+  long long e[kPairsUnroll];   // number of the pair's first element, an even one
+#pragma unroll
+  for (int i = 0; i < kPairsUnroll; ++i) {
+    const unsigned c = first + i * kDropoutThreads;
+    const unsigned row = __umulhi(c, p.magic) >> p.shift;
+    const long long number = p.index_base + row * p.cols;
+    const int col = static_cast<int>(c - row * p.per_row) * 2 - static_cast<int>(number & 1);
+    e[i] = number + col;
+    y[i] = static_cast<T*>(p.y) + row * p.ldy + col;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      on[i][k] = c < p.chunks && col + k >= 0 && col + k < static_cast<int>(p.cols);
+      if (on[i][k]) x[i][k] = static_cast<const T*>(p.x)[row * p.ldx + col + k];
+      if (kResidual && on[i][k]) r[i][k] = static_cast<const T*>(p.r)[row * p.ldr + col + k];
+    }
+  }
+  const unsigned least = p.none ? 1u : p.threshold;
+#pragma unroll
+  for (int i = 0; i < kPairsUnroll; ++i) {
+    const uint2 w = dropout_hash(p.base + static_cast<unsigned long long>(e[i] >> 1) * kPairStep);
+    const unsigned u[2] = {p.none ? 0u : w.x, p.none ? 0u : w.y};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (!on[i][k]) continue;
+      float f = u[k] >= least ? to_float(x[i][k]) * p.scale : 0.0f;
+      if (kResidual) f += to_float(r[i][k]);
+      y[i][k] = from_float<T>(f);
     }
   }
 }

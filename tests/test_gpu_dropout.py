@@ -176,3 +176,30 @@ def test_every_pair_of_alignments(B, dtype, cols):
             same.copy_(held)
     line, other = matrix(1, 0)[1].reshape(-1), matrix(2, 0)[1].reshape(-1)   # one long row
     check(B.adapt_dropout(line, 0.4, 12, 3, residual=other), line, other, 0.4, keep, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("cols", [1, 2, 5, 10, 15, 16, 17])
+def test_short_rows_of_other_alignments(B, dtype, cols):
+    import torch
+    dt, rows = getattr(torch, dtype), 700       # more than a CTA's pairs
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn(rows, cols + 3, generator=g, device="cuda").to(dt)[:, 1:1 + cols]
+    r = torch.randn(rows, cols + 2, generator=g, device="cuda").to(dt)[:, 2:]
+    for base in (0, 7):
+        keep = R.dropout_keep(rows * cols, 0.3, 5, 6, base)
+        out = torch.full((rows, cols + 5), 7.0, device="cuda", dtype=dt)
+        y = out[:, 3:3 + cols]
+        check(B.adapt_dropout(x, 0.3, 5, 6, base, out=y), x, None, 0.3, keep, dtype)
+        check(B.adapt_dropout(x, 0.3, 5, 6, base, residual=r, out=y), x, r, 0.3, keep, dtype)
+        assert (out[:, :3] == 7).all() and (out[:, 3 + cols:] == 7).all()
+    want = B.adapt_dropout(x, 0.3, 5, 6, 7, residual=r)
+    for same in (x, r):
+        held = same.clone()
+        assert torch.equal(B.adapt_dropout(x, 0.3, 5, 6, 7, residual=r, out=same), want)
+        same.copy_(held)
+    assert torch.equal(B.adapt_dropout(x, 1.0, 5, 6, residual=r, out=y), r)
+    assert torch.equal(B.adapt_dropout(x, 0.0, 5, 6, out=y), x)
+    x[::2] = float("nan")
+    y = B.adapt_dropout(x, 0.3, 5, 6, out=y).float().cpu().numpy().ravel()
+    assert np.array_equal(np.isnan(y), R.dropout_keep(rows * cols, 0.3, 5, 6) & np.repeat(np.arange(rows) % 2 == 0, cols))
