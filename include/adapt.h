@@ -632,7 +632,7 @@ size_t adapt_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t ch
  * `python -m paper_2107_13490_b200.build --check`; the stand-in for a memory checker
  * where none can be run).  In it every table index that the kernels form from
  * the data - cell positions taken from float bit patterns, bins, sub-cells, queue
- * slots - is tested against its table's size; an index outside is skipped (never
+ * slots, places of candidate tokens, tokens - is tested against its table's size; an index outside is skipped (never
  * dereferenced, nothing traps) and the first such event is kept in a device word.
  *   out  HOST uint32[4] or NULL: {events since the library was loaded or the word
  *        was last cleared, site number of the first event, its index, its limit}

@@ -1656,14 +1656,18 @@ int adapt_precision_search_static(const float* const* tensors, const int64_t* le
 int adapt_bounds_check_status(uint32_t* out, int clear) {
   if (out) out[0] = out[1] = out[2] = out[3] = 0;
 #ifdef ADAPT_CHECK_BOUNDS
-  unsigned word[4] = {0, 0, 0, 0};
-  if (cudaDeviceSynchronize() != cudaSuccess ||
-      cudaMemcpyFromSymbol(word, adapt::g_bounds_error, sizeof(word)) != cudaSuccess)
-    return -ADAPT_ERR_CUDA;
-  if (out) for (int i = 0; i < 4; ++i) out[i] = word[i];
-  if (clear) {
-    const unsigned zero[4] = {0, 0, 0, 0};
-    if (cudaMemcpyToSymbol(adapt::g_bounds_error, zero, sizeof(zero)) != cudaSuccess) return -ADAPT_ERR_CUDA;
+  if (cudaDeviceSynchronize() != cudaSuccess) return -ADAPT_ERR_CUDA;
+  for (int k = 0; k < adapt::g_bounds_word_count; ++k) {
+    unsigned word[4] = {0, 0, 0, 0};
+    if (cudaMemcpyFromSymbol(word, adapt::g_bounds_words[k], sizeof(word)) != cudaSuccess) return -ADAPT_ERR_CUDA;
+    if (out && word[0]) {
+      if (!out[0]) for (int i = 1; i < 4; ++i) out[i] = word[i];
+      out[0] += word[0];
+    }
+    if (clear) {
+      const unsigned zero[4] = {0, 0, 0, 0};
+      if (cudaMemcpyToSymbol(adapt::g_bounds_words[k], zero, sizeof(zero)) != cudaSuccess) return -ADAPT_ERR_CUDA;
+    }
   }
   return 1;
 #else

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "bounds.cuh"
+
 namespace adapt {
 
 __device__ __forceinline__ float to_float(float v) { return v; }

@@ -182,8 +182,9 @@ __global__ void __launch_bounds__(kRowThreads) logprob_warp_kernel(const Logprob
       }
       last = best = warp_max(best);
       if (lane == 0) {
-        p.top_ids[row * p.n_top + k] = top_index(best);
-        p.top_logprobs[row * p.n_top + k] = row_logp(r, p.scale, to_float(x[top_index(best)]));
+        const int j = top_index(best);
+        p.top_ids[row * p.n_top + k] = j;
+        if (ADAPT_IN_BOUNDS(j, p.vocab, 60)) p.top_logprobs[row * p.n_top + k] = row_logp(r, p.scale, to_float(x[j]));
       }
     }
     h = r.ln_sum - r.spread;
@@ -367,9 +368,15 @@ __device__ void top_prune(RowShared<T, kThreads>& sh, const unsigned long long* 
     const unsigned long long mine = keys[i];
     int rank = 0;
     for (int j = 0; j < n; ++j) rank += keys[j] > mine;
-    if (rank < k) sh.best[rank] = mine;
+    if (rank < k && ADAPT_IN_BOUNDS(rank, kMaxTop, 61)) sh.best[rank] = mine;
   }
   Team<kThreads>::sync();
+}
+
+template <typename T, int kThreads>
+__device__ __forceinline__ void add_key(RowShared<T, kThreads>& sh, unsigned long long key) {
+  const int at = atomicAdd(&sh.n_keys, 1);
+  if (ADAPT_IN_BOUNDS(at, (RowShared<T, kThreads>::kCandidates), 62)) sh.keys[at] = key;
 }
 
 // The part's k largest keys into best[].  `bound`: no element of the part below this one's order can be
@@ -390,7 +397,7 @@ __device__ int top_collect(RowShared<T, kThreads>& sh, const RowPart<T>& part, u
   if (me < part.edges) {
     const int j = part.edge(me);
     const unsigned long long key = top_key(to_float(part.x[j]), j);
-    if (key > least) sh.keys[atomicAdd(&sh.n_keys, 1)] = key;
+    if (key > least) add_key(sh, key);
   }
   const int total = n_strips * per;
   for (int base = 0, width; base < total; base += width) {
@@ -406,7 +413,7 @@ __device__ int top_collect(RowShared<T, kThreads>& sh, const RowPart<T>& part, u
 #pragma unroll
         for (int e = 0; e < kCount; ++e) {
           const unsigned long long key = top_key(v[e], part.element(q) + e);
-          if (key > least) sh.keys[atomicAdd(&sh.n_keys, 1)] = key;
+          if (key > least) add_key(sh, key);
         }
       }
     }
@@ -450,7 +457,10 @@ __device__ void top_threshold(RowShared<T, kThreads>& sh, float m, int k) {
     if (rank == k - 1) sh.threshold = mine;
   }
   Team<kThreads>::sync();
-  if (m >= sh.threshold) sh.strips[atomicAdd(&sh.n_strips, 1)] = static_cast<unsigned char>(me);
+  if (m >= sh.threshold) {
+    const int at = atomicAdd(&sh.n_strips, 1);
+    if (ADAPT_IN_BOUNDS(at, kThreads, 63)) sh.strips[at] = static_cast<unsigned char>(me);
+  }
   Team<kThreads>::sync();
 }
 
@@ -496,7 +506,7 @@ __device__ void special_row(const LogprobParams& p, RowShared<T, kThreads>& sh, 
     if (me < p.n_top) {
       const int j = top_index(sh.best[me]);
       p.top_ids[row * p.n_top + me] = j;
-      p.top_logprobs[row * p.n_top + me] = row_logp(r, p.scale, to_float(x[j]));
+      if (ADAPT_IN_BOUNDS(j, p.vocab, 64)) p.top_logprobs[row * p.n_top + me] = row_logp(r, p.scale, to_float(x[j]));
     }
   }
   if (!dx) return;
@@ -708,7 +718,7 @@ __global__ void __launch_bounds__(kRowThreads, kThreads == 32 ? 5 : 6) logprob_r
     if (rank == 0 && me < k) {
       const int j = top_index(sh.best[me]);
       p.top_ids[row * k + me] = j;
-      p.top_logprobs[row * k + me] = row_logp(r, p.scale, to_float(x[j]));
+      if (ADAPT_IN_BOUNDS(j, p.vocab, 65)) p.top_logprobs[row * k + me] = row_logp(r, p.scale, to_float(x[j]));
     }
     if (dx && parts > 1) cluster_barrier();   // the alternatives' logits are read before they are overwritten
   }
@@ -729,7 +739,7 @@ __global__ void __launch_bounds__(kRowThreads, kThreads == 32 ? 5 : 6) logprob_r
     const float2 f = unpack2(t);
     return mul2(pack2(exp2_approx(f.x), exp2_approx(f.y)), fma2(t, a1a1, a0a0));
   }, one);
-  if (!lost && g.dlp != 0.0f && wrote<T, kThreads>(part, static_cast<int>(target)))
+  if (!lost && g.dlp != 0.0f && ADAPT_IN_BOUNDS(target, p.vocab, 66) && wrote<T, kThreads>(part, static_cast<int>(target)))
     dx[target] = from_float<T>(fmaf(p.scale, g.dlp, one(x_target)));
 }
 
@@ -748,7 +758,8 @@ __global__ void __launch_bounds__(kRowThreads, 5) logprob_backward_kernel(const 
   const float h = p.entropy_in ? p.entropy_in[row] : 0.0f;
   const RowWeights g = {p.d_logprob ? p.d_logprob[row] : 0.0f, p.d_entropy ? p.d_entropy[row] : 0.0f};
   const bool lost = (p.d_logprob && target >= p.vocab) || lse != lse;
-  const bool mine = !lost && g.dlp != 0.0f && wrote<T, kThreads>(part, static_cast<int>(target));
+  const bool mine = !lost && g.dlp != 0.0f && ADAPT_IN_BOUNDS(target, p.vocab, 67) &&
+                    wrote<T, kThreads>(part, static_cast<int>(target));
   const float x_target = mine ? to_float(x[target]) : 0.0f;   // before it is overwritten in place
   // p (a1 t + a0), t = ln p = z - lse
   const float a1 = -p.scale * g.dh, a0 = lost ? __int_as_float(0x7FFFFFFF) : -p.scale * fmaf(g.dh, h, g.dlp);

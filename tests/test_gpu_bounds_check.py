@@ -75,3 +75,28 @@ def test_no_table_index_leaves_its_table():
     line = [ln for ln in out.stdout.splitlines() if ln.startswith("BOUNDS")][-1].split()
     assert line[1] == "1"                       # the checking build did run
     assert line[2:] == ["0", "0", "0", "0"], f"an index left its table: events, site, index, limit = {line[2:]}"
+
+
+OPERATORS = r"""
+import sys
+import pytest
+from paper_2107_13490_b200 import binding as B
+checking, word = B.adapt_bounds_check_status(clear=True)
+assert checking, "the bounds-checking build was not loaded"
+rc = pytest.main(["-q", "-x", "-p", "no:cacheprovider", "tests/test_gpu_logprobs.py", "tests/test_gpu_dropout.py",
+                  "tests/test_gpu_scan.py", "-k", "not longest_vocabulary and not many_chains and not few_chains"])
+assert rc == 0, rc
+checking, word = B.adapt_bounds_check_status()
+print("BOUNDS", int(checking), *[int(v) for v in word])
+"""
+
+
+def test_the_training_step_operators_on_the_checking_build():
+    from paper_2107_13490_b200 import build
+    lib = build.build(check=True)
+    env = dict(os.environ, ADAPT_B200_LIBRARY=lib, PYTHONPATH=ROOT)
+    out = subprocess.run([sys.executable, "-c", OPERATORS], cwd=ROOT, env=env, capture_output=True, text=True,
+                         timeout=1500)
+    assert out.returncode == 0, out.stdout[-4000:] + out.stderr[-4000:]
+    line = [ln for ln in out.stdout.splitlines() if ln.startswith("BOUNDS")][-1].split()
+    assert line[1:] == ["1", "0", "0", "0", "0"], line
