@@ -593,9 +593,7 @@ int adapt_token_logprobs_backward(const void* logits, int64_t rows, int64_t voca
  *   h_last   DEVICE float[batch][channels] or NULL: the state after the last step; may be h0
  *   carry_out  DEVICE float[batch][ceil(steps / ADAPT_SCAN_TILE)][channels] or NULL: the
  *            state before every ADAPT_SCAN_TILE-th step, which the backward pass starts from
- *   workspace  DEVICE scratch of adapt_gated_scan_workspace_bytes, 256-byte aligned, or NULL
- *            to use a library-owned buffer that grows on demand: calls without a workspace
- *            of their own must not overlap on the device
+ *   workspace, workspace_bytes  not used: the forward pass needs none, whatever is given
  * Limits: steps <= 2^31 - 8192, channels and batch < 2^31, batch * ceil(channels / 64) <= 2^27. */
 enum { ADAPT_GATE_SIGMOID = 0, ADAPT_GATE_VALUE = 1 };
 #define ADAPT_SCAN_TILE 64
@@ -615,6 +613,10 @@ int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int
  *   strides  HOST int64[10] = {batch, step} strides of x, gate, dy, dx, dgate, or NULL
  *   dx, dgate  DEVICE, 0 at and beyond a sequence's length; dx may be dy itself (same strides)
  *   dh0      DEVICE float[batch][channels] or NULL
+ *   workspace  DEVICE scratch of adapt_gated_scan_workspace_bytes (0 unless a gate serves more than 64
+ *            channels), 256-byte aligned, or NULL to use a library-owned buffer that grows on demand: calls
+ *            without a workspace of their own must not overlap on the device, and one that needs
+ *            scratch returns ADAPT_ERR_INVALID_ARG on a stream that is being captured
  * Sums are taken in a fixed order: the same call gives the same bits. */
 int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy,
                               const float* carry, const float* dh_last, const int32_t* lengths,

@@ -41,7 +41,7 @@ int adapt_gated_scan(const void* x, const void* gate, const float* h0, const int
   stride_pair(strides, 2, steps, channels, q.yb, q.yt);
   if (q.xb < 0 || q.xt < 0 || q.gb < 0 || q.gt < 0 || !out_strides_ok(q.yb, q.yt, q, channels)) return ADAPT_ERR_INVALID_ARG;
   q.x = x; q.gate = gate; q.h0 = h0; q.lengths = lengths; q.reset = reset; q.y = y; q.h_last = h_last; q.carry = carry_out;
-  (void)workspace; (void)workspace_bytes;   // the tiles meet in shared memory
+  (void)workspace; (void)workspace_bytes;   // not needed: the tiles meet in shared memory
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   std::lock_guard<std::mutex> lock(g_mutex);
   DeviceCache* dc = nullptr;

@@ -6,8 +6,8 @@ using namespace adapt;
 
 namespace {
 
-// The caller's workspace, or the library's (grown on demand).
-int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, char** out) {
+// The caller's workspace, or the library's (grown on demand: a graph would keep an address that a later call frees).
+int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, cudaStream_t stream, char** out) {
   *out = nullptr;
   if (need == 0) return ADAPT_OK;
   if (workspace) {
@@ -15,6 +15,13 @@ int scan_scratch(DeviceCache& dc, void* workspace, size_t have, size_t need, cha
     if (misaligned(workspace, 256)) return ADAPT_ERR_INVALID_ARG;
     *out = static_cast<char*>(workspace);
     return ADAPT_OK;
+  }
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  ADAPT_CUDA(cudaStreamIsCapturing(stream, &capturing));
+  if (capturing != cudaStreamCaptureStatusNone) {
+    std::snprintf(g_last_error, sizeof(g_last_error),
+                  "adapt_gated_scan_backward: the stream is being captured and the call has no workspace of its own");
+    return ADAPT_ERR_INVALID_ARG;
   }
   const int rc = grow_device(&dc.scan_buf, &dc.scan_buf_bytes, align_up(need, 4096));
   *out = static_cast<char*>(dc.scan_buf);
@@ -54,10 +61,10 @@ int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy, c
   int rc = current_cache(&dc);
   if (rc != ADAPT_OK) return rc;
   char* scratch = nullptr;
-  rc = scan_scratch(*dc, workspace, workspace_bytes, scan_workspace(q, true), &scratch);
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
+  rc = scan_scratch(*dc, workspace, workspace_bytes, scan_workspace(q, true), stream, &scratch);
   if (rc != ADAPT_OK) return rc;
   q.partial = reinterpret_cast<float*>(scratch);
-  cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   {
     LaunchScope ls(ADAPT_KERNEL_SCAN_BACKWARD, stream);
     const bool own = gate_group == 1;

@@ -402,3 +402,33 @@ def test_decays_at_a_reset_do_not_count(B, dtype, batch, steps, channels, group)
         got = run(B, dict(c, gate=gate), False)
         for name in want:
             assert torch.equal(got[name], want[name]), (name, bad)
+
+
+def test_capture_needs_a_workspace_of_the_call_s_own(B):
+    import torch
+    c = case("float32", 2, 70, 256, 128, 6, True)
+    want = run(B, c, True)
+    carry = B.adapt_gated_scan(c["x"], c["gate"], h0=c["h0"], want_carry=True).carry
+    dx, dgate = torch.zeros_like(c["x"]), torch.zeros_like(c["gate"])
+    need = B.adapt_gated_scan_workspace_bytes(2, 70, 256, 128, B.DTYPE_F32, backward=True)
+    assert need > 0 and B.adapt_gated_scan_workspace_bytes(2, 70, 256, 64, B.DTYPE_F32, backward=True) == 0
+    scratch = torch.zeros(need, dtype=torch.uint8, device="cuda")
+
+    def call(workspace, size, stream):
+        return B.lib().adapt_gated_scan_backward(c["x"].data_ptr(), c["gate"].data_ptr(), c["dy"].data_ptr(), carry.data_ptr(),
+                                                 c["dl"].data_ptr(), None, None, 2, 70, 256, 128, B.DTYPE_F32, B.GATE_SIGMOID,
+                                                 None, dx.data_ptr(), dgate.data_ptr(), None, workspace, size, stream)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        stream = torch.cuda.current_stream().cuda_stream
+        assert call(None, 0, stream) == B.ERR_INVALID_ARG and b"captured" in B.lib().adapt_last_error()
+        assert call(scratch.data_ptr(), need - 1, stream) == B.ERR_WORKSPACE
+        assert call(scratch.data_ptr(), need, stream) == B.OK
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want["dx"]) and torch.equal(dgate, want["dgate"])
+    dgate.zero_()
+    assert call(None, 0, torch.cuda.current_stream().cuda_stream) == B.OK      # outside a capture: the library's buffer
+    torch.cuda.synchronize()
+    assert torch.equal(dgate, want["dgate"])
