@@ -53,13 +53,13 @@ class DropoutAdd(torch.autograd.Function):
 
 
 class TokenLoss(torch.autograd.Function):
-    """Mean negative log probability of the targets (negative ones are left out); the gradient comes out
-    of the forward call."""
+    """Mean negative log probability of the targets (negative ones are left out; without any it is 0); the gradient
+    comes out of the forward call."""
 
     @staticmethod
     def forward(ctx, logits, targets):
         live = targets >= 0
-        weight = -live.float() / live.sum()
+        weight = -live.float() / live.sum().clamp(min=1)
         r = B.adapt_token_logprobs(logits, targets, want_entropy=False, d_logprob=weight)
         ctx.save_for_backward(r.dlogits)
         return (r.logprob * weight).sum()

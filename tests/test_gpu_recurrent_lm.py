@@ -59,3 +59,11 @@ def test_single_tokens_give_the_sequence_s_logits(LM):
     lse = torch.logsumexp(whole[:, -1].double(), 1)
     assert torch.allclose(r.lse.double(), lse, rtol=1e-5, atol=1e-5)
     assert LM.continue_text(model, tokens[:, :4], 5).shape == (3, 5)
+
+
+def test_a_batch_without_targets_has_no_loss(LM):
+    import torch
+    model = LM.RecurrentLM(30, 16, 1, dtype=torch.float32)
+    tokens, targets, reset = LM.synthetic_text(2, 20, 30, 3)
+    loss, gradients = model.loss_and_gradients(tokens, torch.full_like(targets, -1), reset)
+    assert float(loss) == 0 and all((g == 0).all() for g in gradients)
