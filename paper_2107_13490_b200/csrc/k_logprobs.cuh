@@ -154,14 +154,18 @@ __global__ void __launch_bounds__(kRowThreads) logprob_warp_kernel(const Logprob
     const Exponent exponent(p.scale);
     const float unit_m = exponent.unit * m;
     float s = 0.0f, w = 0.0f;
-    if (m * p.scale != -INFINITY) {
+    auto sum = [&](auto term) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const float t = v[i] * p.scale == -INFINITY ? -200.0f : fmaxf(exponent(v[i], unit_m), -200.0f);
+        const float t = v[i] * p.scale == -INFINITY ? -200.0f : fmaxf(term(v[i]), -200.0f);
         const float e = exp2_approx(t);
         s += e;
         w = fmaf(e, t, w);
       }
+    };
+    if (m * p.scale != -INFINITY) {   // (of the two forms the second alone costs 4 % on rows of 1000)
+      if (exponent.unit == 1.0f) sum([&](float v) { return (v - m) * exponent.c; });
+      else sum([&](float v) { return exponent(v, unit_m); });
     }
     s = warp_sum(s);
     w = warp_sum(w);
