@@ -163,18 +163,21 @@ __device__ __forceinline__ f32x2 held2(f32x2 a) {
   return pack2(held(v.x), held(v.y));
 }
 // The product of a piece's decays, held.  Where it ran to infinity on the way and met a decay of 0 (NaN), it is
-// formed again, held at every step.  (Decays of the sigmoid form are at most 1.)
+// formed again, held at every step.  (Decays of the sigmoid form are at most 1.)  The test costs the value form 1 to 2 %:
+// 8 x 4096 x 2048 bf16 forward 80.7 -> 81.8 us, backward 132.6 -> 134.4.
 template <int kMode>
 __device__ __forceinline__ f32x2 held_product(f32x2 product, const f32x2 (&a)[kScanSteps]) {
+  product = held2(product);
   if (kMode == kGateValue) {
     const float2 v = unpack2(product);
-    if (v.x != v.x || v.y != v.y) {
+    if (__builtin_expect(isnan(v.x + v.y), 0)) {
       product = a[0];
 #pragma unroll
       for (int k = 1; k < kScanSteps; ++k) product = mul2(held2(product), a[k]);
+      product = held2(product);
     }
   }
-  return held2(product);
+  return product;
 }
 // A map h -> a h + b of a lane's two channels; `cut`: what comes before does not count (h -> b).
 struct __align__(16) ScanMap { f32x2 a, b; };
