@@ -686,6 +686,10 @@ def adapt_format_quantize(x: torch.Tensor, kind: int, a: int, b: int, round_mode
 # in C++ (csrc/torch_calls.cpp), which gets the entry points of the library loaded here.  Us a call, from Python
 # through ctypes / through the extension: dropout 8.1 / 4.8, log probabilities 9.4 / 7.3, with 8 alternatives
 # 14.1 / 8.6, one step of the recurrence 11.9 / 5.2.
+#
+# The calls record nothing for autograd: their results have no gradient function, whatever the inputs require.  A
+# training program calls the backward entry points itself, or wraps both in a torch.autograd.Function, as
+# examples/recurrent_lm.py does for each of the three.
 
 _calls = None
 
