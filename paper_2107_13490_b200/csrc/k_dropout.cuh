@@ -10,7 +10,7 @@
 namespace adapt {
 
 constexpr int kDropoutThreads = 256;
-constexpr int kDropoutUnroll = 2, kShiftUnroll = 1;   // chunks of a thread (kShift with 2: 8.3 us for 7.8, 4099 x 1001 fp16)
+constexpr int kDropoutUnroll = 2, kShiftUnroll = 1;   // chunks of a thread (kShift with 2 is within 2 % of 1)
 constexpr int kPairsUnroll = 4;                       // pairs of a thread
 constexpr int kPairsBelow = 16;                       // shorter rows of other alignments go in pairs
 
@@ -95,8 +95,8 @@ __device__ __forceinline__ uint4 join_blocks(const uint4& low, const uint4& high
 // A chunk is 16 bytes of y.  Where the rows of x, r and y lie alike to the 16-byte boundary, so is its part of
 // x and r, and chunks over a row's ends go element by element (whole blocks there too: 16384 x 4096 bf16 51 us,
 // 49 without).  Otherwise (kShift) x and r are shifted out of the aligned blocks around them, over a row's ends
-// too: 16384 x 4095 bf16 into rows of another alignment 66 us, 111 with pairs of elements; 4099 x 1001 fp16 7.8
-// and 10.4; rows of fewer than kPairsBelow elements go in pairs (below).  kRows: several rows.
+// too: 16384 x 4095 bf16 into rows of another alignment 64 us (device time), 96 with pairs of elements; 4099 x 1001
+// fp16 5.3 and 7.3; rows of fewer than kPairsBelow elements go in pairs (below).  kRows: several rows.
 template <typename T, bool kShift, bool kResidual, bool kRows>
 __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const DropoutParams p) {
   constexpr int kCount = 16 / sizeof(T);
