@@ -188,7 +188,8 @@ def _plain_codes(x):
     """Codes and scales of the rows: code = x (127 / largest) to the nearest, the quotient in fp32 and the
     product unrounded; scale = largest / 127."""
     largest = x.float().abs().amax(1).clamp(min=_TINY)
-    codes = torch.round(x.double() * (127 / largest).double()[:, None]).clamp(-127, 127)
+    inverse = torch.full_like(largest, 127.0) / largest     # (127 / largest would multiply by a reciprocal)
+    codes = torch.round(x.double() * inverse.double()[:, None]).clamp(-127, 127)
     return codes.float(), largest / 127
 
 
@@ -210,7 +211,8 @@ def _exact_int8(s):
         scales = s["xs"].double()
     else:
         largest = x.abs().max(1).values.clamp(min=_TINY)
-        inverse = (127 / largest.float()).double()      # fp32 by definition
+        # fp32 by definition: rounding the quotient of two fp32 numbers in 64 bits once more is the same
+        inverse = torch.div(torch.tensor(127.0, dtype=torch.float64, device=x.device).expand_as(largest), largest).float().double()
         x, scales = torch.round(x * inverse[:, None]), largest / 127
     y = torch.einsum("rk,nk->rn", x, s["w"].double()) * torch.outer(scales, s["ws"].double().expand(s["w"].shape[0]))
     return y if s["bias"] is None else y + s["bias"].double()
