@@ -372,7 +372,13 @@ enum {
   ADAPT_KERNEL_LOGPROBS = 15,      /* token log probabilities and their gradient */
   ADAPT_KERNEL_SCAN = 16,          /* gated recurrence                           */
   ADAPT_KERNEL_SCAN_BACKWARD = 17, /* gated recurrence, backward                 */
-  ADAPT_KERNEL_KINDS = 18
+  ADAPT_KERNEL_EMBEDDING = 18,     /* token embedding                            */
+  ADAPT_KERNEL_EMBEDDING_BACKWARD = 19, /* its gradient: sort, sums, joins       */
+  ADAPT_KERNEL_BLOCK_NORM = 20,    /* norms around a block                       */
+  ADAPT_KERNEL_BLOCK_NORM_BACKWARD = 21, /* their gradient, column sums           */
+  ADAPT_KERNEL_INT8_ROWS = 22,     /* rows to 8-bit codes                        */
+  ADAPT_KERNEL_INT8_LINEAR = 23,   /* product of 8-bit codes                     */
+  ADAPT_KERNEL_KINDS = 24
 };
 
 /* Switches per-kernel device timing on (non-zero) or off.  While on, every
@@ -629,6 +635,142 @@ int adapt_gated_scan_backward(const void* x, const void* gate, const void* dy,
  * backward non-zero asks for the gradient's. */
 size_t adapt_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels,
                                         int gate_group, int dtype, int backward);
+
+/* ---- around a language model's layers -----------------------------------------
+ *
+ * What stands in front of, between and inside the layers: the embedding of tokens with its
+ * gradient, the norms before and after a block with their gradients, and the product with
+ * weights held as 8-bit codes (adapt_quantize's with code_bits 8, or adapt_int8_rows').
+ * Conventions as for the operators of a training step; parameters and their gradients
+ * (norm weights, a gate shared by all rows, scales, bias) are fp32.  A stride or leading
+ * dimension of a matrix of one row is not looked at. */
+
+/* Token embedding: out[i] = scale * table[ids[i]].
+ *   table  DEVICE [vocab][dim], leading dimension ld_table >= dim
+ *   ids    DEVICE int64[n].  A negative one marks a place without a token: its row is 0; one
+ *          that is >= vocab gives a row of NaN
+ *   scale  finite
+ *   out    DEVICE [n][dim], leading dimension ld_out >= dim, of the table's type; no overlap
+ * Limits: vocab, n, dim < 2^31. */
+int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_table, int dtype,
+                    const int64_t* ids, int64_t n, float scale, void* out, int64_t ld_out,
+                    void* stream);
+
+/* Its gradient: dtable[v] = scale * sum of dy[i] over the i with ids[i] = v (+ dtable[v] where
+ * accumulate is non-zero).  The tokens are sorted, so that the sums are taken in fp32 in a
+ * fixed order and each row is rounded once: the same call gives the same bits.
+ *   dy          DEVICE [n][dim], leading dimension ld_dy >= dim.  Rows whose id is negative or
+ *               >= vocab are not read
+ *   dtable      DEVICE [vocab][dim], leading dimension ld_grad >= dim, of grad_dtype, which is
+ *               dtype or ADAPT_DTYPE_F32.  Rows of tokens that do not occur are 0, or, with
+ *               accumulate, left as they are
+ *   workspace   DEVICE scratch of adapt_embedding_workspace_bytes, 256-byte aligned; needed
+ * Limits: vocab, n, dim < 2^31. */
+int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_dy, int dtype,
+                             const int64_t* ids, int64_t vocab, float scale, int accumulate,
+                             void* dtable, int64_t ld_grad, int grad_dtype, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace the gradient of these sizes needs (0: none, or invalid arguments). */
+size_t adapt_embedding_workspace_bytes(int64_t n, int64_t dim, int64_t vocab);
+
+/* Norms after a block and before the next one, with the block's gate and the residual sum:
+ *   y      = residual_scale * residual + scale * g(gate) * norm_after(block) * weight_after
+ *   normed = norm_before(y) * weight_before
+ *   ADAPT_NORM_RMS:    norm(v) = v / sqrt(mean(v^2) + eps)
+ *   ADAPT_NORM_LAYER:  norm(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps)
+ *   ADAPT_NORM_NONE:   norm(v) = v, without a weight; before = NONE: no second output
+ * g(gate) = 1 / (1 + e^-gate) (ADAPT_GATE_SIGMOID) or gate (ADAPT_GATE_VALUE).  normed is formed
+ * from y before its rounding.  With residual and gate NULL, after = NONE and scale = 1 this is
+ * a norm alone (y may then be NULL: it is block).
+ *   block, residual, gate, y, normed  DEVICE [rows][dim]; residual, gate may be NULL (a gate of
+ *            1), y and normed where they are not wanted, not both.  normed needs before
+ *   gate_shared   non-zero: gate is DEVICE float[dim], the same for all rows
+ *   strides  HOST int64[5] = leading dimensions of block, residual, gate, y, normed, or NULL: dim.
+ *            Inputs may have 0 (one row for all).  y may be block, residual or a gate of each row
+ *            (same leading dimension), normed too where y is not it; no other overlap
+ *   weight_after, weight_before  DEVICE float[dim] or NULL: 1
+ *   eps      >= 0 and finite; scale, residual_scale finite
+ *   stats_out  DEVICE float[rows][4] or NULL: {mean, 1 / deviation} of block and of y, what the
+ *            backward pass starts from
+ * Limits: rows < 2^31, dim <= ADAPT_NORM_MAX_DIM. */
+enum { ADAPT_NORM_NONE = 0, ADAPT_NORM_RMS = 1, ADAPT_NORM_LAYER = 2 };
+#define ADAPT_NORM_MAX_DIM 32768
+
+typedef struct adapt_norm_args {
+  int32_t after, before, gate_mode, gate_shared; /* ADAPT_NORM_*, ADAPT_GATE_*, flag  */
+  float scale, residual_scale, eps;
+} adapt_norm_args;
+
+int adapt_block_norm(const void* block, const void* residual, const void* gate,
+                     const float* weight_after, const float* weight_before, int64_t rows,
+                     int64_t dim, int dtype, const adapt_norm_args* args,
+                     const int64_t* strides, void* y, void* normed, float* stats_out,
+                     void* stream);
+
+/* Its gradient.  y is recomputed in fp32 from the inputs, which must be as they were.
+ *   stats     as adapt_block_norm wrote it for the same inputs
+ *   d_y, d_normed  DEVICE [rows][dim], gradients of y and normed; either may be NULL (0), not
+ *             both; d_normed needs before
+ *   d_block, d_residual, d_gate  DEVICE [rows][dim], each may be NULL; a shared gate's d_gate is
+ *             DEVICE float[dim], the sum over the rows.  d_residual may be d_y (same leading
+ *             dimension), no other overlap
+ *   d_weight_after, d_weight_before  DEVICE float[dim], each may be NULL
+ *   strides   HOST int64[8] = leading dimensions of block, residual, gate, d_y, d_normed,
+ *             d_block, d_residual, d_gate, or NULL: dim.  Inputs may have 0
+ *   workspace DEVICE scratch of adapt_block_norm_workspace_bytes, 256-byte aligned; needed where a
+ *             gradient is summed over the rows
+ * Sums over rows are taken in a fixed order: the same call gives the same bits. */
+int adapt_block_norm_backward(const void* block, const void* residual, const void* gate,
+                              const float* weight_after, const float* weight_before,
+                              const float* stats, const void* d_y, const void* d_normed,
+                              int64_t rows, int64_t dim, int dtype,
+                              const adapt_norm_args* args, const int64_t* strides,
+                              void* d_block, void* d_residual, void* d_gate,
+                              float* d_weight_after, float* d_weight_before, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace a backward call of these sizes needs, whichever gradients it gives. */
+size_t adapt_block_norm_workspace_bytes(int64_t rows, int64_t dim);
+
+/* Rows (tokens of activations, channels of weights) to 8-bit codes with a scale each:
+ *   m = max(largest |x| of the row, 2^-100),  code = rne(x * r) with r = 127 / m in fp32 and the
+ *   product unrounded (so |code| <= 127),  scale = m / 127 in fp32
+ * A row that holds NaN or Inf gets codes 0 and the scale NaN.
+ *   x       DEVICE [rows][cols], leading dimension ldx
+ *   codes   DEVICE int8 [rows][cols], leading dimension ld_codes >= cols
+ *   scales  DEVICE float[rows]
+ * Limits: rows < 2^31, cols < 2^31. */
+int adapt_int8_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype,
+                    int8_t* codes, int64_t ld_codes, float* scales, void* stream);
+
+#define ADAPT_DTYPE_I8 3
+#define ADAPT_INT8_MAX_K 131071
+
+/* Product with weights held as 8-bit codes:
+ *   y[i][j] = x_scale_i * weight_scale_j * sum_k x[i][k] * weight[j][k] (+ bias[j])
+ *   x        DEVICE [rows][k], leading dimension ldx.  Codes (x_dtype ADAPT_DTYPE_I8) with x_scales, or
+ *            fp32, fp16, bf16 with x_scales NULL: then the rows are quantised within the call,
+ *            as adapt_int8_rows does
+ *   x_scales DEVICE float[rows], or one for all (x_scale_count 1)
+ *   weight   DEVICE int8 [n][k], leading dimension ldw
+ *   weight_scales  DEVICE float[n], or one for all (weight_scale_count 1)
+ *   bias     DEVICE float[n] or NULL
+ *   y        DEVICE [rows][n], leading dimension ldy >= n, of dtype (fp32, fp16, bf16); no overlap
+ *   workspace  DEVICE scratch of adapt_int8_linear_workspace_bytes, 256-byte aligned (NULL where that is 0)
+ * Any codes are legal, -128 too.  The sum is exact (int32); then come the scales, one after the
+ * other, and the bias in fp32.  Weights with a 16-byte aligned address and a leading dimension
+ * that is a multiple of 16 are read as they are; others are first copied to the workspace where
+ * there are many rows.  Limits: rows, n < 2^31, k <= ADAPT_INT8_MAX_K. */
+int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t x_scale_count,
+                      const int8_t* weight, const float* weight_scales,
+                      int64_t weight_scale_count, const float* bias, int64_t rows, int64_t n,
+                      int64_t k, int64_t ldx, int64_t ldw, void* y, int64_t ldy, int dtype,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace a product of these sizes may need (0: none, or invalid arguments). */
+size_t adapt_int8_linear_workspace_bytes(int64_t rows, int64_t n, int64_t k, int64_t ldw,
+                                         int x_dtype);
 
 /* The bounds-checking build of the library (libadapt_b200_check.so, made by
  * `python -m paper_2107_13490_b200.build --check`; the stand-in for a memory checker

@@ -38,6 +38,9 @@ EXPORTS = (
     "adapt_pushup", "adapt_bounds_check_status",
     "adapt_dropout", "adapt_token_logprobs", "adapt_token_logprobs_backward",
     "adapt_gated_scan", "adapt_gated_scan_backward", "adapt_gated_scan_workspace_bytes",
+    "adapt_embedding", "adapt_embedding_backward", "adapt_embedding_workspace_bytes",
+    "adapt_block_norm", "adapt_block_norm_backward", "adapt_block_norm_workspace_bytes",
+    "adapt_int8_rows", "adapt_int8_linear", "adapt_int8_linear_workspace_bytes",
 )
 STRATEGY_MIN, STRATEGY_MEAN, STRATEGY_MAX = 0, 1, 2
 FMT_FIXED, FMT_BFP, FMT_FLOAT = 0, 1, 2
@@ -45,11 +48,15 @@ MAX_FORMATS = 1024
 STATIC_MAX_LAYERS, STATIC_MAX_BINS, STATIC_MAX_CAND = 8, 512, 1024
 KERNEL_KINDS = ("range", "range_finalize", "search", "kld", "select", "quantize", "plan",
                 "expand", "search_direct", "diversity", "format_resolve", "format_search",
-                "format_kld", "format_quantize", "dropout", "logprobs", "scan", "scan_backward")
-DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
+                "format_kld", "format_quantize", "dropout", "logprobs", "scan", "scan_backward",
+                "embedding", "embedding_backward", "block_norm", "block_norm_backward", "int8_rows", "int8_linear")
+DTYPE_F32, DTYPE_F16, DTYPE_BF16, DTYPE_I8 = 0, 1, 2, 3
 MAX_TOP = 32
 GATE_SIGMOID, GATE_VALUE = 0, 1
 SCAN_TILE = 64
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+NORM_MAX_DIM = 32768
+INT8_MAX_K = 131071
 ALGO_AUTO, ALGO_KEYED, ALGO_DIRECT = 0, 1, 2
 
 
@@ -64,6 +71,11 @@ class AdaptSearchOpts(C.Structure):
                 ("hist_out", C.c_void_p), ("range_out", C.c_void_p), ("algorithm", C.c_int32),
                 ("n_bins_per_layer", C.c_void_p), ("start_wl_fl", C.c_void_p),
                 ("status_out", C.c_void_p)]
+
+
+class AdaptNormArgs(C.Structure):
+    _fields_ = [("after", C.c_int32), ("before", C.c_int32), ("gate_mode", C.c_int32), ("gate_shared", C.c_int32),
+                ("scale", C.c_float), ("residual_scale", C.c_float), ("eps", C.c_float)]
 
 
 class AdaptFormat(C.Structure):
@@ -176,6 +188,24 @@ def lib():
                                                 P, SZ, P]
         L.adapt_gated_scan_workspace_bytes.restype = SZ
         L.adapt_gated_scan_workspace_bytes.argtypes = [I64, I64, I64, I32, I32, I32]
+        L.adapt_embedding.restype = C.c_int
+        L.adapt_embedding.argtypes = [P, I64, I64, I64, I32, P, I64, F32, P, I64, P]
+        L.adapt_embedding_backward.restype = C.c_int
+        L.adapt_embedding_backward.argtypes = [P, I64, I64, I64, I32, P, I64, F32, I32, P, I64, I32, P, SZ, P]
+        L.adapt_embedding_workspace_bytes.restype = SZ
+        L.adapt_embedding_workspace_bytes.argtypes = [I64, I64, I64]
+        L.adapt_block_norm.restype = C.c_int
+        L.adapt_block_norm.argtypes = [P, P, P, P, P, I64, I64, I32, P, P, P, P, P, P]
+        L.adapt_block_norm_backward.restype = C.c_int
+        L.adapt_block_norm_backward.argtypes = [P, P, P, P, P, P, P, P, I64, I64, I32, P, P, P, P, P, P, P, P, SZ, P]
+        L.adapt_block_norm_workspace_bytes.restype = SZ
+        L.adapt_block_norm_workspace_bytes.argtypes = [I64, I64]
+        L.adapt_int8_rows.restype = C.c_int
+        L.adapt_int8_rows.argtypes = [P, I64, I64, I64, I32, P, I64, P, P]
+        L.adapt_int8_linear.restype = C.c_int
+        L.adapt_int8_linear.argtypes = [P, I32, P, I64, P, P, I64, P, I64, I64, I64, I64, I64, P, I64, I32, P, SZ, P]
+        L.adapt_int8_linear_workspace_bytes.restype = SZ
+        L.adapt_int8_linear_workspace_bytes.argtypes = [I64, I64, I64, I64, I32]
         _lib = L
     return _lib
 
@@ -708,7 +738,10 @@ def _native():
         spec.loader.exec_module(m)
         m.bind(*(C.cast(f, C.c_void_p).value for f in (
             L.adapt_dropout, L.adapt_token_logprobs, L.adapt_token_logprobs_backward, L.adapt_gated_scan,
-            L.adapt_gated_scan_backward, L.adapt_gated_scan_workspace_bytes)), AdaptError)
+            L.adapt_gated_scan_backward, L.adapt_gated_scan_workspace_bytes, L.adapt_embedding,
+            L.adapt_embedding_backward, L.adapt_embedding_workspace_bytes, L.adapt_block_norm,
+            L.adapt_block_norm_backward, L.adapt_block_norm_workspace_bytes, L.adapt_int8_rows, L.adapt_int8_linear,
+            L.adapt_int8_linear_workspace_bytes)), AdaptError)
         _calls = m
     return _calls
 
@@ -806,3 +839,105 @@ def adapt_gated_scan_backward(x: torch.Tensor, gate: torch.Tensor, dy: torch.Ten
     ``dx`` may be ``dy`` (in place)."""
     return ScanGradients(*_run("scan_backward", stream, x, gate, dy, carry, dh_last, lengths, reset, mode, want_dh0,
                                dx, dgate))
+
+
+# ---- around a language model's layers -------------------------------------------------------
+#
+# By the same extension.  Nothing is recorded for autograd here either.
+
+def adapt_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """adapt_embedding of adapt.h: scale * table[ids].  table [vocab, dim]; ids int64 of any shape, negative =
+    no token (a row of 0); returns [*ids.shape, dim]."""
+    return _run("embedding", stream, table, ids, scale, out)
+
+
+def adapt_embedding_workspace_bytes(n: int, dim: int, vocab: int) -> int:
+    return int(lib().adapt_embedding_workspace_bytes(n, dim, vocab))
+
+
+def adapt_embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0,
+                             dtype: Optional[torch.dtype] = None, dtable: Optional[torch.Tensor] = None,
+                             accumulate: bool = False, stream=None) -> torch.Tensor:
+    """adapt_embedding_backward of adapt.h: the gradient of the table [vocab, dim], of ``dtype`` (that of dy or
+    float32; default: dy's).  With ``accumulate`` it is added to ``dtable``."""
+    return _run("embedding_backward", stream, dy, ids, vocab, scale, dtype, dtable, accumulate)
+
+
+class BlockNorm:
+    """Device outputs of adapt_block_norm (what was not asked for is None)."""
+
+    __slots__ = ("y", "normed", "stats")
+
+    def __init__(self, y, normed, stats):
+        self.y, self.normed, self.stats = y, normed, stats
+
+
+class BlockNormGradients:
+    """Device outputs of adapt_block_norm_backward (what was not asked for is None)."""
+
+    __slots__ = ("d_block", "d_residual", "d_gate", "d_weight_after", "d_weight_before")
+
+    def __init__(self, d_block, d_residual, d_gate, d_weight_after, d_weight_before):
+        self.d_block, self.d_residual, self.d_gate = d_block, d_residual, d_gate
+        self.d_weight_after, self.d_weight_before = d_weight_after, d_weight_before
+
+
+def adapt_block_norm(block: torch.Tensor, residual: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                     weight_after: Optional[torch.Tensor] = None, weight_before: Optional[torch.Tensor] = None,
+                     after: int = NORM_NONE, before: int = NORM_RMS, gate_mode: int = GATE_SIGMOID, scale: float = 1.0,
+                     residual_scale: float = 1.0, eps: float = 1e-6, want_y: bool = True, want_stats: bool = False,
+                     y: Optional[torch.Tensor] = None, normed: Optional[torch.Tensor] = None, stream=None) -> BlockNorm:
+    """adapt_block_norm of adapt.h: y = residual_scale residual + scale g(gate) norm_after(block), and normed =
+    norm_before(y) where ``before`` is not NORM_NONE.  block [..., dim]; a gate of one dimension (float32 [dim]) is
+    shared by all rows.  ``want_stats`` keeps what adapt_block_norm_backward starts from."""
+    return BlockNorm(*_run("block_norm", stream, block, residual, gate, weight_after, weight_before, after, before,
+                           gate_mode, scale, residual_scale, eps, want_y, before != NORM_NONE, want_stats, y, normed))
+
+
+def adapt_block_norm_workspace_bytes(rows: int, dim: int) -> int:
+    return int(lib().adapt_block_norm_workspace_bytes(rows, dim))
+
+
+def adapt_block_norm_backward(block: torch.Tensor, stats: torch.Tensor, d_y: Optional[torch.Tensor] = None,
+                              d_normed: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                              gate: Optional[torch.Tensor] = None, weight_after: Optional[torch.Tensor] = None,
+                              weight_before: Optional[torch.Tensor] = None, after: int = NORM_NONE,
+                              before: int = NORM_RMS, gate_mode: int = GATE_SIGMOID, scale: float = 1.0,
+                              residual_scale: float = 1.0, eps: float = 1e-6, want_block: bool = True,
+                              want_residual: bool = True, want_gate: bool = True, want_weights: bool = True,
+                              d_residual: Optional[torch.Tensor] = None, stream=None) -> BlockNormGradients:
+    """adapt_block_norm_backward of adapt.h, for the inputs and options of adapt_block_norm and its ``stats``;
+    gradients of what was given there and is wanted.  ``d_residual`` may be ``d_y`` (in place)."""
+    return BlockNormGradients(*_run("block_norm_backward", stream, block, residual, gate, weight_after, weight_before,
+                                    after, before, gate_mode, scale, residual_scale, eps, stats, d_y, d_normed,
+                                    want_block, want_residual, want_gate, want_weights, d_residual))
+
+
+class Int8Rows:
+    """Device outputs of adapt_int8_rows: codes int8 [rows, cols], scales float32 [rows]."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes, scales):
+        self.codes, self.scales = codes, scales
+
+
+def adapt_int8_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                    stream=None) -> Int8Rows:
+    """adapt_int8_rows of adapt.h: the rows of a matrix (tokens, or the channels of a weight) as 8-bit codes with a
+    scale each."""
+    return Int8Rows(*_run("int8_rows", stream, x, codes, scales))
+
+
+def adapt_int8_linear_workspace_bytes(rows: int, n: int, k: int, ldw: int, x_dtype: int) -> int:
+    return int(lib().adapt_int8_linear_workspace_bytes(rows, n, k, ldw, x_dtype))
+
+
+def adapt_int8_linear(x: torch.Tensor, weight: torch.Tensor, weight_scales: torch.Tensor,
+                      x_scales: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                      dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """adapt_int8_linear of adapt.h: x [rows, k] times weight [channels, k], int8 codes with a scale for each
+    channel or one for all (2^-FL for adapt_quantize's codes).  x is float32, float16 or bfloat16 and quantised by
+    rows within the call, or int8 with ``x_scales``.  The result is of ``dtype`` (default: x's, float32 for codes)."""
+    return _run("int8_linear", stream, x, weight, weight_scales, x_scales, bias, dtype, out)

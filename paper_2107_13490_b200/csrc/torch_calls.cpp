@@ -1,4 +1,4 @@
-// The training-step operators' calls from torch tensors: checks, outputs, the current stream, and the entry
+// The language-model operators' calls from torch tensors: checks, outputs, the current stream, and the entry
 // point of adapt.h.  Same checks and calls as ctypes would make, in C++ because a small call is bound by
 // the host: see binding.py for what it measured.
 //
@@ -10,12 +10,14 @@
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
 #include <initializer_list>
 #include <optional>
+#include <type_traits>
 
 #include "../../include/adapt.h"
 
@@ -27,6 +29,15 @@ decltype(&adapt_token_logprobs_backward) g_logprobs_backward;
 decltype(&adapt_gated_scan) g_scan;
 decltype(&adapt_gated_scan_backward) g_scan_backward;
 decltype(&adapt_gated_scan_workspace_bytes) g_scan_workspace;
+decltype(&adapt_embedding) g_embedding;
+decltype(&adapt_embedding_backward) g_embedding_backward;
+decltype(&adapt_embedding_workspace_bytes) g_embedding_workspace;
+decltype(&adapt_block_norm) g_norm;
+decltype(&adapt_block_norm_backward) g_norm_backward;
+decltype(&adapt_block_norm_workspace_bytes) g_norm_workspace;
+decltype(&adapt_int8_rows) g_int8_rows;
+decltype(&adapt_int8_linear) g_int8_linear;
+decltype(&adapt_int8_linear_workspace_bytes) g_int8_workspace;
 PyObject* g_error;   // called with (status, entry point): the exception to raise
 
 // An argument that does not fit (AssertionError); the Python error is set already where there is no text.
@@ -82,6 +93,10 @@ void need_like(const at::Tensor& t, const at::Tensor& x) {
 }
 at::Tensor make(const at::Tensor& x, at::IntArrayRef sizes, at::ScalarType type) {
   return at::empty(sizes, at::TensorOptions().dtype(type).device(x.device()));
+}
+// Scratch for a call, undefined where none is needed.
+at::Tensor scratch(const at::Tensor& x, size_t bytes) {
+  return bytes ? make(x, {static_cast<int64_t>(bytes)}, at::kByte) : at::Tensor();
 }
 at::Tensor make_like(const at::Tensor& x) { return make(x, x.sizes(), x.scalar_type()); }
 // `given`, which has to be as x is, or a new tensor.
@@ -349,26 +364,288 @@ PyObject* scan_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (addresses of the six entry points, error)
-PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+at::ScalarType floating(PyObject* o) {   // a torch.dtype that the operators know
+  need(THPDtype_Check(o), "needs a torch.dtype");
+  const at::ScalarType t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+  need(t == at::kFloat || t == at::kHalf || t == at::kBFloat16, "needs float32, float16 or bfloat16");
+  return t;
+}
+int elem_of(at::ScalarType t) { return t == at::kFloat ? ADAPT_DTYPE_F32 : t == at::kHalf ? ADAPT_DTYPE_F16 : ADAPT_DTYPE_BF16; }
+int64_t count(PyObject* o, const char* why) {
+  int beyond = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &beyond);
+  if (v == -1 && !beyond && PyErr_Occurred()) throw Refused{nullptr};
+  need(!beyond && v >= 0, why);
+  return v;
+}
+const int64_t* tokens(const at::Tensor& ids, const at::Tensor& x) {
+  need(ids.device() == x.device() && ids.scalar_type() == at::kLong && ids.is_contiguous(),
+       "tokens: a contiguous int64 tensor on the device of its partner");
+  return static_cast<const int64_t*>(ids.const_data_ptr());
+}
+// [tokens..., dim] as rows: contiguous, or a matrix with unit inner stride.
+Matrix rows_of(const at::Tensor& t, int64_t n, int64_t dim) {
+  need(t.dim() >= 1 && t.size(t.dim() - 1) == dim && t.numel() == n * dim, "a row for each token");
+  if (t.is_contiguous()) return {n, dim, dim};
+  need(t.dim() == 2 && (dim <= 1 || t.stride(1) == 1), "needs contiguous rows, or a matrix with unit inner stride");
+  return {n, dim, n > 1 ? t.stride(0) : dim};
+}
+
+// (table, ids, scale, out) -> out
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 4, [&] {
+    const at::Tensor &table = tensor(a[0]), &ids = tensor(a[1]);
+    const int dtype = elem(table);
+    const Matrix m = matrix(table);
+    const int64_t* pi = tokens(ids, table);
+    const float scale = static_cast<float>(real(a[2]));
+    at::Tensor out;
+    if (const at::Tensor* given = maybe(a[3])) {
+      out = *given;
+      need(out.scalar_type() == table.scalar_type() && out.device() == table.device(), "out: of the table's type, on its device");
+    } else {
+      c10::SmallVector<int64_t, 6> sizes(ids.sizes().begin(), ids.sizes().end());
+      sizes.push_back(m.cols);
+      out = make(table, sizes, table.scalar_type());
+    }
+    const Matrix r = rows_of(out, ids.numel(), m.cols);
+    const void* pt = table.const_data_ptr();
+    void* stream = stream_of(table);
+    call("adapt_embedding", [&] { return g_embedding(pt, m.rows, m.cols, m.ld, dtype, pi, r.rows, scale, out_data<void>(out), r.ld, stream); });
+    return wrap(out);
+  });
+}
+
+// (dy, ids, vocab, scale, dtype, dtable, accumulate) -> dtable
+PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&] {
-    void* at[6];
-    for (int i = 0; i < 6; ++i) at[i] = reinterpret_cast<void*>(static_cast<uintptr_t>(bits(a[i])));
-    g_dropout = reinterpret_cast<decltype(g_dropout)>(at[0]);
-    g_logprobs = reinterpret_cast<decltype(g_logprobs)>(at[1]);
-    g_logprobs_backward = reinterpret_cast<decltype(g_logprobs_backward)>(at[2]);
-    g_scan = reinterpret_cast<decltype(g_scan)>(at[3]);
-    g_scan_backward = reinterpret_cast<decltype(g_scan_backward)>(at[4]);
-    g_scan_workspace = reinterpret_cast<decltype(g_scan_workspace)>(at[5]);
+    const at::Tensor &dy = tensor(a[0]), &ids = tensor(a[1]);
+    const int dtype = elem(dy);
+    need(dy.dim() >= 1, "a row for each token");
+    const int64_t* pi = tokens(ids, dy);
+    const Matrix m = rows_of(dy, ids.numel(), dy.size(dy.dim() - 1));
+    const int64_t vocab = count(a[2], "the vocabulary is a whole number");
+    const float scale = static_cast<float>(real(a[3]));
+    const bool accumulate = truth(a[6]);
+    at::Tensor grad;
+    if (const at::Tensor* given = maybe(a[5])) {
+      grad = *given;
+      need(grad.device() == dy.device() && (grad.scalar_type() == dy.scalar_type() || grad.scalar_type() == at::kFloat),
+           "dtable: of the type of dy or float32, on its device");
+      need(a[4] == Py_None || floating(a[4]) == grad.scalar_type(), "dtable is of another type than asked for");
+      need(grad.dim() == 2 && grad.size(0) == vocab && grad.size(1) == m.cols, "dtable: [vocab, dim]");
+    } else {
+      need(!accumulate, "accumulation needs a dtable");
+      const at::ScalarType t = a[4] == Py_None ? dy.scalar_type() : floating(a[4]);
+      grad = make(dy, {vocab, m.cols}, t);
+    }
+    const Matrix g = matrix(grad);
+    const size_t bytes = g_embedding_workspace(m.rows, m.cols, vocab);
+    const at::Tensor workspace = scratch(dy, bytes);
+    const void* pd = dy.const_data_ptr();
+    void* stream = stream_of(dy);
+    call("adapt_embedding_backward", [&] {
+      return g_embedding_backward(pd, m.rows, m.cols, m.ld, dtype, pi, vocab, scale, accumulate, out_data<void>(grad), g.ld,
+                                  elem_of(grad.scalar_type()), out_data<void>(workspace), bytes, stream);
+    });
+    return wrap(grad);
+  });
+}
+
+// What the forward and the backward call of the norms share.  The rows are the first tensor's without its last
+// dimension; all are contiguous, or all are matrices with unit inner stride.
+struct NormCall {
+  const at::Tensor& x;
+  const int dtype;
+  int64_t rows, dim;
+  adapt_norm_args args;
+  const at::Tensor *residual, *gate;
+  const float *weight_after, *weight_before;
+  int64_t lines[8];
+  // (block, residual, gate, weight_after, weight_before, after, before, gate_mode, scale, residual_scale, eps)
+  explicit NormCall(PyObject* const* a) : x(tensor(a[0])), dtype(elem(x)), residual(maybe(a[1])), gate(maybe(a[2])) {
+    need(x.dim() >= 1, "needs rows");
+    dim = x.size(x.dim() - 1);
+    rows = 1;
+    for (int64_t d = 0; d + 1 < x.dim(); ++d) rows *= x.size(d);
+    args.after = between(a[5], INT32_MIN, INT32_MAX, "no such norm");
+    args.before = between(a[6], INT32_MIN, INT32_MAX, "no such norm");
+    args.gate_mode = between(a[7], INT32_MIN, INT32_MAX, "no such gate");
+    args.scale = static_cast<float>(real(a[8]));
+    args.residual_scale = static_cast<float>(real(a[9]));
+    args.eps = static_cast<float>(real(a[10]));
+    args.gate_shared = gate && gate->dim() == 1 && x.dim() != 1;
+    weight_after = parameter(maybe(a[3]));
+    weight_before = parameter(maybe(a[4]));
+    for (int64_t& v : lines) v = dim;
+    lines[0] = line(x);
+    if (residual) { need_like(*residual, x); lines[1] = line(*residual); }
+    if (gate) {
+      if (args.gate_shared) parameter(gate);
+      else { need_like(*gate, x); lines[2] = line(*gate); }
+    }
+  }
+  const float* parameter(const at::Tensor* t) const {
+    if (!t) return nullptr;
+    need(t->device() == x.device() && t->scalar_type() == at::kFloat && t->dim() == 1 && t->size(0) == dim && t->is_contiguous(),
+         "weights and shared gates: float32 [dim], on the device of the rows");
+    return static_cast<const float*>(t->const_data_ptr());
+  }
+  int64_t line(const at::Tensor& t) const {
+    if (t.is_contiguous() || rows == 1) {
+      need(dim <= 1 || t.stride(t.dim() - 1) == 1, "needs unit inner stride");
+      return dim;
+    }
+    need(t.dim() == 2 && (dim <= 1 || t.stride(1) == 1), "needs contiguous tensors, or matrices with unit inner stride");
+    return t.stride(0);
+  }
+  static const void* data(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
+};
+
+// (..., want_y, want_normed, want_stats, y, normed) -> (y, normed, stats)
+PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&] {
+    NormCall c(a);
+    at::Tensor y, normed, stats;
+    if (truth(a[11])) { y = out_like(maybe(a[14]), c.x); c.lines[3] = c.line(y); }
+    else need(a[14] == Py_None, "y is given but not wanted");
+    if (truth(a[12])) { normed = out_like(maybe(a[15]), c.x); c.lines[4] = c.line(normed); }
+    else need(a[15] == Py_None, "normed is given but not wanted");
+    if (truth(a[13])) stats = make(c.x, {c.rows, 4}, at::kFloat);
+    const void* px = c.x.const_data_ptr();
+    void* stream = stream_of(c.x);
+    call("adapt_block_norm", [&] {
+      return g_norm(px, NormCall::data(c.residual), NormCall::data(c.gate), c.weight_after, c.weight_before, c.rows, c.dim, c.dtype,
+                    &c.args, c.lines, out_data<void>(y), out_data<void>(normed), out_data<float>(stats), stream);
+    });
+    return wrap({&y, &normed, &stats});
+  });
+}
+
+// (..., stats, d_y, d_normed, want_block, want_residual, want_gate, want_weights, d_residual)
+// -> (d_block, d_residual, d_gate, d_weight_after, d_weight_before)
+PyObject* block_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 19, [&] {
+    NormCall c(a);
+    const at::Tensor &stats = tensor(a[11]), *d_y = maybe(a[12]), *d_normed = maybe(a[13]);
+    need(stats.device() == c.x.device() && stats.scalar_type() == at::kFloat && stats.is_contiguous() && stats.dim() == 2 &&
+             stats.size(0) == c.rows && stats.size(1) == 4, "stats: as adapt_block_norm made them");
+    if (d_y) { need_like(*d_y, c.x); c.lines[3] = c.line(*d_y); }
+    if (d_normed) { need_like(*d_normed, c.x); c.lines[4] = c.line(*d_normed); }
+    at::Tensor d_block, d_residual, d_gate, d_after, d_before;
+    if (truth(a[14])) d_block = make_like(c.x);
+    if (truth(a[15]) && c.residual) { d_residual = out_like(maybe(a[18]), c.x); c.lines[6] = c.line(d_residual); }
+    else need(a[18] == Py_None, "d_residual is given but there is none");
+    if (truth(a[16]) && c.gate) d_gate = c.args.gate_shared ? make(c.x, {c.dim}, at::kFloat) : make_like(c.x);
+    const bool weights = truth(a[17]);
+    if (weights && c.weight_after) d_after = make(c.x, {c.dim}, at::kFloat);
+    if (weights && c.weight_before && d_normed) d_before = make(c.x, {c.dim}, at::kFloat);
+    size_t bytes = 0;
+    if (d_after.defined() || d_before.defined() || (d_gate.defined() && c.args.gate_shared)) bytes = g_norm_workspace(c.rows, c.dim);
+    const at::Tensor workspace = scratch(c.x, bytes);
+    const void* px = c.x.const_data_ptr();
+    const float* ps = static_cast<const float*>(stats.const_data_ptr());
+    void* stream = stream_of(c.x);
+    call("adapt_block_norm_backward", [&] {
+      return g_norm_backward(px, NormCall::data(c.residual), NormCall::data(c.gate), c.weight_after, c.weight_before, ps,
+                             NormCall::data(d_y), NormCall::data(d_normed), c.rows, c.dim, c.dtype, &c.args, c.lines,
+                             out_data<void>(d_block), out_data<void>(d_residual), out_data<void>(d_gate), out_data<float>(d_after),
+                             out_data<float>(d_before), out_data<void>(workspace), bytes, stream);
+    });
+    return wrap({&d_block, &d_residual, &d_gate, &d_after, &d_before});
+  });
+}
+
+// (x, codes, scales) -> (codes, scales)
+PyObject* int8_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 3, [&] {
+    const at::Tensor& x = tensor(a[0]);
+    const int dtype = elem(x);
+    const Matrix m = matrix(x);
+    const at::Tensor *given = maybe(a[1]), *given_scales = maybe(a[2]);
+    const at::Tensor codes = given ? *given : make(x, x.sizes(), at::kChar);
+    need(codes.scalar_type() == at::kChar && codes.device() == x.device() && codes.sizes() == x.sizes(), "codes: int8, of the shape of x, on its device");
+    const at::Tensor scales = given_scales ? *given_scales : make(x, {m.rows}, at::kFloat);
+    per_row(&scales, x, at::kFloat);
+    const Matrix c = matrix(codes);
+    const void* px = x.const_data_ptr();
+    void* stream = stream_of(x);
+    call("adapt_int8_rows", [&] {
+      return g_int8_rows(px, m.rows, m.cols, m.ld, dtype, out_data<int8_t>(codes), c.ld, out_data<float>(scales), stream);
+    });
+    return wrap({&codes, &scales});
+  });
+}
+
+// (x, weight, weight_scales, x_scales, bias, dtype, out) -> out
+PyObject* int8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&] {
+    const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]), &ws = tensor(a[2]);
+    const at::Tensor *xs = maybe(a[3]), *bias = maybe(a[4]), *given = maybe(a[6]);
+    const bool coded = x.scalar_type() == at::kChar;
+    need(x.is_cuda() && (!coded || x.get_device() == c10::cuda::current_device()), "needs CUDA tensors on the current device");
+    const int x_dtype = coded ? ADAPT_DTYPE_I8 : elem(x);
+    need(w.device() == x.device() && w.scalar_type() == at::kChar, "the weights are int8, on the device of x");
+    const Matrix m = matrix(x), mw = matrix(w);
+    need(mw.cols == m.cols, "x and the weights have the same number of columns");
+    auto scales = [&](const at::Tensor& t, int64_t most) {
+      need(t.device() == x.device() && t.scalar_type() == at::kFloat && t.is_contiguous() && t.dim() <= 1 && (t.numel() == 1 || t.numel() == most),
+           "scales: contiguous float32, one for all or one for each row, on the device of x");
+      return static_cast<const float*>(t.const_data_ptr());
+    };
+    need(coded == (xs != nullptr), "codes come with their scales, other types without");
+    const float *pws = scales(ws, mw.rows), *pxs = xs ? scales(*xs, m.rows) : nullptr;
+    const float* pb = nullptr;
+    if (bias) {
+      need(bias->device() == x.device() && bias->scalar_type() == at::kFloat && bias->is_contiguous() && bias->dim() == 1 && bias->size(0) == mw.rows,
+           "bias: float32, one for each row of the weights, on the device of x");
+      pb = static_cast<const float*>(bias->const_data_ptr());
+    }
+    at::Tensor out;
+    if (given) {
+      out = *given;
+      need(out.device() == x.device() && out.dim() == 2 && out.size(0) == m.rows && out.size(1) == mw.rows, "out: [rows, channels], on the device of x");
+      need(a[5] == Py_None || floating(a[5]) == out.scalar_type(), "out is of another type than asked for");
+    } else {
+      const at::ScalarType t = a[5] != Py_None ? floating(a[5]) : coded ? at::kFloat : x.scalar_type();
+      out = make(x, {m.rows, mw.rows}, t);
+    }
+    const int dtype = elem(out);
+    const Matrix o = matrix(out);
+    const size_t bytes = g_int8_workspace(m.rows, mw.rows, m.cols, mw.ld, x_dtype);
+    const at::Tensor workspace = scratch(x, bytes);
+    const void *px = x.const_data_ptr();
+    const int8_t* pw = static_cast<const int8_t*>(w.const_data_ptr());
+    const int64_t xn = xs ? xs->numel() : 0, wn = ws.numel();
+    void* stream = stream_of(x);
+    call("adapt_int8_linear", [&] {
+      return g_int8_linear(px, x_dtype, pxs, xn, pw, pws, wn, pb, m.rows, mw.rows, m.cols, m.ld, mw.ld, out_data<void>(out), o.ld, dtype,
+                           out_data<void>(workspace), bytes, stream);
+    });
+    return wrap(out);
+  });
+}
+
+// Entry points' addresses in the order of binding.py, then the error.
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 16, [&] {
+    int i = 0;
+    auto take = [&](auto& f) { f = reinterpret_cast<std::remove_reference_t<decltype(f)>>(static_cast<uintptr_t>(bits(a[i++]))); };
+    take(g_dropout); take(g_logprobs); take(g_logprobs_backward); take(g_scan); take(g_scan_backward); take(g_scan_workspace);
+    take(g_embedding); take(g_embedding_backward); take(g_embedding_workspace);
+    take(g_norm); take(g_norm_backward); take(g_norm_workspace);
+    take(g_int8_rows); take(g_int8_linear); take(g_int8_workspace);
     Py_XDECREF(g_error);
-    g_error = Py_NewRef(a[6]);
+    g_error = Py_NewRef(a[i]);
     return Py_NewRef(Py_None);
   });
 }
 
 #define ADAPT_CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {ADAPT_CALL(dropout), ADAPT_CALL(logprobs), ADAPT_CALL(logprobs_backward), ADAPT_CALL(scan),
-                           ADAPT_CALL(scan_backward), ADAPT_CALL(bind), {nullptr, nullptr, 0, nullptr}};
+                           ADAPT_CALL(scan_backward), ADAPT_CALL(embedding),
+                           ADAPT_CALL(embedding_backward), ADAPT_CALL(block_norm), ADAPT_CALL(block_norm_backward),
+                           ADAPT_CALL(int8_rows), ADAPT_CALL(int8_linear), ADAPT_CALL(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_adapt_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
