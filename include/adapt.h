@@ -759,18 +759,20 @@ int adapt_int8_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
  *   y        DEVICE [rows][n], leading dimension ldy >= n, of dtype (fp32, fp16, bf16); no overlap
  *   workspace  DEVICE scratch of adapt_int8_linear_workspace_bytes, 256-byte aligned (NULL where that is 0)
  * Any codes are legal, -128 too.  The sum is exact (int32); then come the scales, one after the
- * other, and the bias in fp32.  Weights with a 16-byte aligned address and a leading dimension
- * that is a multiple of 16 are read as they are; others are first copied to the workspace where
- * there are many rows.  Limits: rows, n < 2^31, k <= ADAPT_INT8_MAX_K. */
+ * other, and the bias in fp32.  Codes with a 16-byte aligned address and a leading dimension
+ * that is a multiple of 16 are read as they are; where there are more than 8 rows, others are
+ * first copied to the workspace.  Limits: rows, n < 2^31, k <= ADAPT_INT8_MAX_K. */
 int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t x_scale_count,
                       const int8_t* weight, const float* weight_scales,
                       int64_t weight_scale_count, const float* bias, int64_t rows, int64_t n,
                       int64_t k, int64_t ldx, int64_t ldw, void* y, int64_t ldy, int dtype,
                       void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace a product of these sizes may need (0: none, or invalid arguments). */
-size_t adapt_int8_linear_workspace_bytes(int64_t rows, int64_t n, int64_t k, int64_t ldw,
-                                         int x_dtype);
+/* Bytes of workspace a product needs (0: none, or invalid arguments).  Of x and weight only the
+ * addresses are looked at. */
+size_t adapt_int8_linear_workspace_bytes(const void* x, int x_dtype, const int8_t* weight,
+                                         int64_t rows, int64_t n, int64_t k, int64_t ldx,
+                                         int64_t ldw);
 
 /* The bounds-checking build of the library (libadapt_b200_check.so, made by
  * `python -m paper_2107_13490_b200.build --check`; the stand-in for a memory checker

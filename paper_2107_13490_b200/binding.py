@@ -205,7 +205,7 @@ def lib():
         L.adapt_int8_linear.restype = C.c_int
         L.adapt_int8_linear.argtypes = [P, I32, P, I64, P, P, I64, P, I64, I64, I64, I64, I64, P, I64, I32, P, SZ, P]
         L.adapt_int8_linear_workspace_bytes.restype = SZ
-        L.adapt_int8_linear_workspace_bytes.argtypes = [I64, I64, I64, I64, I32]
+        L.adapt_int8_linear_workspace_bytes.argtypes = [P, I32, P, I64, I64, I64, I64, I64]
         _lib = L
     return _lib
 
@@ -930,8 +930,10 @@ def adapt_int8_rows(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale
     return Int8Rows(*_run("int8_rows", stream, x, codes, scales))
 
 
-def adapt_int8_linear_workspace_bytes(rows: int, n: int, k: int, ldw: int, x_dtype: int) -> int:
-    return int(lib().adapt_int8_linear_workspace_bytes(rows, n, k, ldw, x_dtype))
+def adapt_int8_linear_workspace_bytes(x: torch.Tensor, weight: torch.Tensor) -> int:
+    kinds = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.int8: DTYPE_I8}
+    return int(lib().adapt_int8_linear_workspace_bytes(x.data_ptr(), kinds[x.dtype], weight.data_ptr(), x.shape[0], weight.shape[0],
+                                                       x.shape[1], x.stride(0), weight.stride(0)))
 
 
 def adapt_int8_linear(x: torch.Tensor, weight: torch.Tensor, weight_scales: torch.Tensor,

@@ -1,6 +1,8 @@
 // C-ABI entry points of the 8-bit codes and their product.  Declarations and argument contracts live in adapt.h.
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "k_int8.cuh"
 #include "training_host.cuh"
@@ -9,26 +11,186 @@ using namespace adapt;
 
 namespace {
 
+constexpr int kSms = 148;   // of a B200
+
 bool in_int(int64_t v, int64_t least) { return v >= least && v <= 0x7FFFFFFF; }
 
 int run_rows(const RowsParams& q, int dtype, cudaStream_t stream) {
+  const int e = elem_bytes(dtype), wide = 16 / e;
+  // a row in the registers of up to 256 threads, 8 chunks each
+  const bool vec = q.cols % wide == 0 && q.cols <= kRowsThreads * 8 * wide && !misaligned(q.x, 16) && !misaligned(q.codes, wide) &&
+                   (q.rows == 1 || (q.ldx % wide == 0 && q.ld_codes % wide == 0));
   LaunchScope ls(ADAPT_KERNEL_INT8_ROWS, stream);
-  with_type(dtype, [&](auto t) { int8_rows_kernel<decltype(t)><<<static_cast<unsigned>(q.rows), kRowsThreads, 0, stream>>>(q); });
+  const unsigned grid = static_cast<unsigned>(q.rows);
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (!vec) { int8_rows_any_kernel<T><<<grid, kRowsThreads, 0, stream>>>(q); return; }
+    const int chunks = q.cols / wide;
+    auto threads = [&](int per) { return static_cast<unsigned>(std::max(32, (chunks + per * 32 - 1) / (per * 32) * 32)); };
+    if (chunks <= kRowsThreads * 2) int8_rows_kernel<T, 2><<<grid, threads(2), 0, stream>>>(q);
+    else if (chunks <= kRowsThreads * 4) int8_rows_kernel<T, 4><<<grid, threads(4), 0, stream>>>(q);
+    else int8_rows_kernel<T, 8><<<grid, threads(8), 0, stream>>>(q);
+  });
   ADAPT_LAUNCH_OK("rows to 8-bit codes");
   return ADAPT_OK;
 }
 
-// Codes (rows of 16-byte multiples) and scales of activations that are quantised within a product.
+int run_copy(const CopyParams& q, cudaStream_t stream) {
+  LaunchScope ls(ADAPT_KERNEL_INT8_ROWS, stream);
+  int8_copy_kernel<<<static_cast<unsigned>(q.rows), kCopyThreads, 0, stream>>>(q);
+  ADAPT_LAUNCH_OK("rows of codes");
+  return ADAPT_OK;
+}
+
+// Whether the TMA unit can read rows of codes as they lie.
+bool tma_rows(const void* p, int64_t ld, int64_t rows) {
+  return !misaligned(p, 16) && (rows == 1 || (ld > 0 && ld % 16 == 0));
+}
+
+// What a product keeps in its workspace: codes of activations that it quantises, and copies of codes that do not
+// lie on 16-byte boundaries.  A few tokens need neither.
 struct LinearLayout {
-  size_t codes = 0, scales = 0, bytes = 0;
+  size_t x = 0, scales = 0, w = 0, bytes = 0;
+  bool quantise = false, copy_x = false, copy_w = false;
   long long ld = 0;
-  LinearLayout(int64_t rows, int64_t k, int x_dtype) {
-    if (x_dtype == ADAPT_DTYPE_I8) return;
+  LinearLayout(const void* px, int x_dtype, const void* pw, int64_t rows, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
+    if (rows <= kDotMaxRows || k == 0) return;
+    quantise = x_dtype != ADAPT_DTYPE_I8;
+    copy_x = !quantise && !tma_rows(px, ldx, rows);
+    copy_w = !tma_rows(pw, ldw, n);
     ld = (k + 15) / 16 * 16;
-    scales = align_up(static_cast<size_t>(rows) * ld, 256);
-    bytes = align_up(scales + 4 * static_cast<size_t>(rows), 256);
+    auto take = [&](size_t b) { const size_t here = bytes; bytes = align_up(bytes + b, 256); return here; };
+    if (quantise || copy_x) x = take(static_cast<size_t>(rows) * ld);
+    if (quantise) scales = take(4 * static_cast<size_t>(rows));
+    if (copy_w) w = take(static_cast<size_t>(n) * ld);
   }
 };
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encode_tiled(EncodeTiled* out) {
+  static std::atomic<void*> known{nullptr};
+  void* f = known.load();
+  if (!f) {
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    ADAPT_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found));
+    if (found != cudaDriverEntryPointSuccess || !f) return cuda_fail(cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+    known.store(f);
+  }
+  *out = reinterpret_cast<EncodeTiled>(f);
+  return ADAPT_OK;
+}
+
+// Tiles of `height` rows by kDepth codes; what lies outside the matrix reads as 0.
+int tile_map(CUtensorMap* map, const void* p, int64_t rows, int64_t k, int64_t ld, int height) {
+  EncodeTiled encode = nullptr;
+  const int rc = encode_tiled(&encode);
+  if (rc != ADAPT_OK) return rc;
+  const cuuint64_t sizes[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(rows == 1 ? (k + 15) / 16 * 16 : ld)};
+  const cuuint32_t box[2] = {kDepth, static_cast<cuuint32_t>(height)}, step[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), sizes, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return cuda_fail(cudaErrorInvalidValue, "tensor map of 8-bit codes");
+  return ADAPT_OK;
+}
+
+// Launches a product.  `early`: it may begin before the kernel in front of it, one of this call's, has ended.
+template <typename... A>
+int launch(void (*kernel)(A...), unsigned x, unsigned y, int threads, int smem, int cluster, bool early, cudaStream_t stream, A... args) {
+  ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(x, y);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  unsigned n = 0;
+  if (early) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = cluster; attr[n].val.clusterDim.y = 1; attr[n++].val.clusterDim.z = 1;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+  return ADAPT_OK;
+}
+
+int run_dot(const LinearParams& q, const void* x, int x_dtype, int dtype, int64_t ldw, cudaStream_t stream) {
+  DotParams d = {};
+  d.p = q;
+  d.x = x;
+  const bool shift = misaligned(q.w, 16) || (q.n > 1 && ldw % 16 != 0);
+  const unsigned grid = static_cast<unsigned>((q.n + kDotThreads / 32 * kDotChannels - 1) / (kDotThreads / 32 * kDotChannels));
+  LaunchScope ls(ADAPT_KERNEL_INT8_LINEAR, stream);
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto go = [&](auto v) {
+      using X = decltype(v);
+      auto rows = [&](auto r) {
+        constexpr int R = decltype(r)::value;
+        if (shift) int8_dot_kernel<T, X, R, true><<<grid, kDotThreads, 0, stream>>>(d);
+        else int8_dot_kernel<T, X, R, false><<<grid, kDotThreads, 0, stream>>>(d);
+      };
+      if (q.rows == 1) rows(std::integral_constant<int, 1>{});
+      else if (q.rows <= 2) rows(std::integral_constant<int, 2>{});
+      else if (q.rows <= 4) rows(std::integral_constant<int, 4>{});
+      else rows(std::integral_constant<int, 8>{});
+    };
+    if (x_dtype == ADAPT_DTYPE_I8) go(static_cast<signed char>(0)); else with_type(x_dtype, go);
+  });
+  ADAPT_LAUNCH_OK("8-bit product");
+  return ADAPT_OK;
+}
+
+int run_tiles(const LinearParams& q, int dtype, bool early, cudaStream_t stream) {
+  const int e = elem_bytes(dtype), blocks = (q.k + kDepth - 1) / kDepth, sms = kSms;
+  CUtensorMap x_map, w_map;
+  int rc = ADAPT_OK;
+  WideParams wide = {};
+  wide.across = (q.n + kWideTile - 1) / kWideTile;
+  wide.down = (q.rows + kWideTile - 1) / kWideTile;
+  const int64_t tiles = static_cast<int64_t>(wide.across) * wide.down;
+  if (tiles > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
+  LaunchScope ls(ADAPT_KERNEL_INT8_LINEAR, stream);
+  if (tiles >= sms / 4) {
+    if ((rc = tile_map(&x_map, q.x, q.rows, q.k, q.ldx, kCtaRows)) != ADAPT_OK || (rc = tile_map(&w_map, q.w, q.n, q.k, q.ldw, kCtaRows)) != ADAPT_OK)
+      return rc;
+    wide.p = q;
+    wide.wide_stores = !misaligned(q.y, 32) && (q.rows == 1 || q.ldy * e % 32 == 0);
+    const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sms / 2));
+    with_type(dtype, [&](auto t) {
+      rc = launch(int8_wide_kernel<decltype(t)>, grid, 1u, kWideThreads, kWideSmem, 0, early, stream, x_map, w_map, wide);
+    });
+    return rc;
+  }
+  const int tokens = q.rows <= 16 ? 16 : q.rows <= 32 ? 32 : q.rows <= 64 ? 64 : q.rows <= 128 ? 128 : 256;
+  const int across = (q.n + kCtaRows - 1) / kCtaRows, down = (q.rows + tokens - 1) / tokens;
+  int split = 1;
+  while (split < kNarrowMaxSplit && static_cast<int64_t>(across) * down * split * 2 <= sms && blocks >= split * 4) split *= 2;
+  if (down > 65535 || static_cast<int64_t>(across) * split > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
+  if ((rc = tile_map(&x_map, q.x, q.rows, q.k, q.ldx, tokens)) != ADAPT_OK || (rc = tile_map(&w_map, q.w, q.n, q.k, q.ldw, kCtaRows)) != ADAPT_OK)
+    return rc;
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto go = [&](auto c) {
+      constexpr int N = decltype(c)::value;
+      rc = launch(int8_narrow_kernel<T, N>, static_cast<unsigned>(across * split), static_cast<unsigned>(down), kNarrowThreads, narrow_smem(N), split,
+                  early, stream, x_map, w_map, q);
+    };
+    if (tokens == 16) go(std::integral_constant<int, 16>{});
+    else if (tokens == 32) go(std::integral_constant<int, 32>{});
+    else if (tokens == 64) go(std::integral_constant<int, 64>{});
+    else if (tokens == 128) go(std::integral_constant<int, 128>{});
+    else go(std::integral_constant<int, 256>{});
+  });
+  return rc;
+}
 
 }  // namespace
 
@@ -48,10 +210,10 @@ int adapt_int8_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
   return run_rows(q, dtype, static_cast<cudaStream_t>(stream));
 }
 
-size_t adapt_int8_linear_workspace_bytes(int64_t rows, int64_t n, int64_t k, int64_t ldw, int x_dtype) {
-  (void)ldw;
+size_t adapt_int8_linear_workspace_bytes(const void* x, int x_dtype, const int8_t* weight, int64_t rows, int64_t n, int64_t k, int64_t ldx,
+                                         int64_t ldw) {
   if (!in_int(rows, 1) || !in_int(n, 1) || k < 0 || k > ADAPT_INT8_MAX_K || (x_dtype != ADAPT_DTYPE_I8 && !elem_bytes(x_dtype))) return 0;
-  return LinearLayout(rows, k, x_dtype).bytes;
+  return LinearLayout(x, x_dtype, weight, rows, n, k, ldx, ldw).bytes;
 }
 
 int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t x_scale_count, const int8_t* weight,
@@ -69,35 +231,46 @@ int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t
     return ADAPT_ERR_INVALID_ARG;
   if (rows > 1 && ((ldx < k && ldx != 0) || ldy < n)) return ADAPT_ERR_INVALID_ARG;
   if (n > 1 && ldw < k && ldw != 0) return ADAPT_ERR_INVALID_ARG;
-  const LinearLayout lay(rows, k, x_dtype);
+  const LinearLayout lay(x, x_dtype, weight, rows, n, k, ldx, ldw);
   if (lay.bytes) {
     if (!workspace || misaligned(workspace, 256)) return ADAPT_ERR_INVALID_ARG;
     if (workspace_bytes < lay.bytes) return ADAPT_ERR_WORKSPACE;
   }
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   LinearParams q = {};
+  q.x = static_cast<const signed char*>(x); q.x_scales = x_scales; q.ldx = ldx; q.x_one = coded && x_scale_count == 1;
   q.w = weight; q.w_scales = weight_scales; q.bias = bias; q.y = y; q.ldw = ldw; q.ldy = ldy;
   q.rows = static_cast<int>(rows); q.n = static_cast<int>(n); q.k = static_cast<int>(k);
   q.w_one = weight_scale_count == 1;
-  if (coded) {
-    q.x = static_cast<const signed char*>(x); q.x_scales = x_scales; q.ldx = ldx; q.x_one = x_scale_count == 1;
-  } else {
+  if (k == 0) {
+    LaunchScope ls(ADAPT_KERNEL_INT8_LINEAR, stream);
+    with_type(dtype, [&](auto t) { int8_bias_kernel<decltype(t)><<<static_cast<unsigned>(rows), 256, 0, stream>>>(q); });
+    ADAPT_LAUNCH_OK("8-bit product");
+    return ADAPT_OK;
+  }
+  if (rows <= kDotMaxRows) return run_dot(q, x, x_dtype, dtype, ldw, stream);
+  signed char* ws = static_cast<signed char*>(workspace);
+  int rc = ADAPT_OK;
+  if (lay.copy_w) {
+    const CopyParams c = {weight, ws + lay.w, n > 1 ? ldw : 0, lay.ld, q.n, q.k};
+    if ((rc = run_copy(c, stream)) != ADAPT_OK) return rc;
+    q.w = c.to; q.ldw = lay.ld;
+  }
+  if (lay.copy_x) {
+    const CopyParams c = {q.x, ws + lay.x, ldx, lay.ld, q.rows, q.k};
+    if ((rc = run_copy(c, stream)) != ADAPT_OK) return rc;
+    q.x = c.to; q.ldx = lay.ld;
+  }
+  if (lay.quantise) {
     RowsParams r = {};
     r.x = x; r.ldx = ldx; r.ld_codes = lay.ld; r.rows = q.rows; r.cols = q.k;
-    r.codes = static_cast<signed char*>(workspace) + lay.codes;
-    r.scales = reinterpret_cast<float*>(static_cast<char*>(workspace) + lay.scales);
-    const int rc = run_rows(r, x_dtype, stream);
-    if (rc != ADAPT_OK) return rc;
+    r.codes = ws + lay.x;
+    r.scales = reinterpret_cast<float*>(ws + lay.scales);
+    if ((rc = run_rows(r, x_dtype, stream)) != ADAPT_OK) return rc;
     q.x = r.codes; q.x_scales = r.scales; q.ldx = lay.ld;
   }
-  const int64_t across = (n + kTile - 1) / kTile, down = (rows + kTile - 1) / kTile;
-  if (down > 65535) return ADAPT_ERR_INVALID_ARG;
-  LaunchScope ls(ADAPT_KERNEL_INT8_LINEAR, stream);
-  with_type(dtype, [&](auto t) {
-    int8_any_kernel<decltype(t)><<<dim3(static_cast<unsigned>(across), static_cast<unsigned>(down)), 256, 0, stream>>>(q);
-  });
-  ADAPT_LAUNCH_OK("8-bit product");
-  return ADAPT_OK;
+  // (it reads weights before it waits for the kernel in front, which therefore must not be the one that writes them)
+  return run_tiles(q, dtype, lay.quantise || lay.copy_x, stream);
 }
 
 }  // extern "C"

@@ -612,10 +612,10 @@ PyObject* int8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const int dtype = elem(out);
     const Matrix o = matrix(out);
-    const size_t bytes = g_int8_workspace(m.rows, mw.rows, m.cols, mw.ld, x_dtype);
-    const at::Tensor workspace = scratch(x, bytes);
     const void *px = x.const_data_ptr();
     const int8_t* pw = static_cast<const int8_t*>(w.const_data_ptr());
+    const size_t bytes = g_int8_workspace(px, x_dtype, pw, m.rows, mw.rows, m.cols, m.ld, mw.ld);
+    const at::Tensor workspace = scratch(x, bytes);
     const int64_t xn = xs ? xs->numel() : 0, wn = ws.numel();
     void* stream = stream_of(x);
     call("adapt_int8_linear", [&] {

@@ -127,7 +127,8 @@ def test_int8_rows_refuses(L, bad):
 @pytest.mark.parametrize("bad", [
     dict(x=None), dict(xs=None), dict(w=None), dict(ws=None), dict(y=None), dict(rows=-1), dict(n=-1), dict(k=-1), dict(rows=BIG), dict(n=BIG),
     dict(k=B.INT8_MAX_K + 1), dict(ldx=7), dict(ldw=7), dict(ldy=5), dict(ldx=-8), dict(dtype=3), dict(x_dtype=4), dict(xsn=2), dict(wsn=2),
-    dict(x_dtype=0), dict(x_dtype=0, xs=None, x=P + 2), dict(x_dtype=0, xs=None, work=None), dict(x_dtype=2, xs=None, work=P + 64),
+    dict(x_dtype=0), dict(x_dtype=0, xs=None, x=P + 2), dict(x_dtype=0, xs=None, rows=40, work=None),
+    dict(x_dtype=2, xs=None, rows=40, work=P + 64),
     dict(y=P + 2), dict(bias=P + 2), dict(xs=P + 1), dict(ws=P + 2)])
 def test_int8_linear_refuses(L, bad):
     assert int8_linear(L, **bad) == B.ERR_INVALID_ARG
@@ -138,14 +139,17 @@ def test_workspaces_that_are_too_small(L):
     assert need > 0 and embedding_backward(L, wsn=need - 1) == B.ERR_WORKSPACE
     need = B.adapt_block_norm_workspace_bytes(4, 8)
     assert need > 0 and norm_backward(L, wsn=need - 1) == B.ERR_WORKSPACE
-    need = B.adapt_int8_linear_workspace_bytes(4, 6, 8, 8, B.DTYPE_BF16)
-    assert need > 0 and int8_linear(L, x_dtype=2, xs=None, workn=need - 1) == B.ERR_WORKSPACE
+    need = B.lib().adapt_int8_linear_workspace_bytes(P, B.DTYPE_BF16, P, 40, 6, 8, 8, 16)
+    assert need > 0 and int8_linear(L, rows=40, x_dtype=2, xs=None, ldw=16, workn=need - 1) == B.ERR_WORKSPACE
+    more = B.lib().adapt_int8_linear_workspace_bytes(P, B.DTYPE_BF16, P, 40, 6, 8, 8, 8)     # codes between 16-byte boundaries are copied
+    assert more > need and int8_linear(L, rows=40, x_dtype=2, xs=None, workn=more - 1) == B.ERR_WORKSPACE
 
 
 def test_workspace_queries_of_invalid_sizes():
     assert B.adapt_embedding_workspace_bytes(-1, 8, 10) == B.adapt_embedding_workspace_bytes(4, 8, 0) == 0
     assert B.adapt_block_norm_workspace_bytes(0, 8) == B.adapt_block_norm_workspace_bytes(4, B.NORM_MAX_DIM + 1) == 0
-    assert B.adapt_int8_linear_workspace_bytes(4, 6, B.INT8_MAX_K + 1, 1 << 18, 0) == B.adapt_int8_linear_workspace_bytes(4, 6, 8, 8, 9) == 0
+    query = B.lib().adapt_int8_linear_workspace_bytes
+    assert query(P, 0, P, 40, 6, B.INT8_MAX_K + 1, 1 << 18, 1 << 18) == query(P, 9, P, 40, 6, 8, 8, 8) == 0
 
 
 def test_sizes_of_zero_are_legal(L):
