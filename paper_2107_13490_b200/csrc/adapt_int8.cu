@@ -97,9 +97,16 @@ int tile_map(CUtensorMap* map, const void* p, int64_t rows, int64_t k, int64_t l
 }
 
 // Launches a product.  `early`: it may begin before the kernel in front of it, one of this call's, has ended.
-template <typename... A>
-int launch(void (*kernel)(A...), unsigned x, unsigned y, int threads, int smem, int cluster, bool early, cudaStream_t stream, A... args) {
-  ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+template <auto kKernel, typename... A>
+int launch(unsigned x, unsigned y, int threads, int smem, int cluster, bool early, cudaStream_t stream, A... args) {
+  static std::atomic<uint64_t> ready{0};   // (one for each kernel) devices that know its shared memory
+  int device = 0;
+  ADAPT_CUDA(cudaGetDevice(&device));
+  const uint64_t bit = 1ull << (device & 63);
+  if (!(ready.load() & bit)) {
+    ADAPT_CUDA(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    ready.fetch_or(bit);
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(x, y);
   cfg.blockDim = dim3(threads);
@@ -117,7 +124,7 @@ int launch(void (*kernel)(A...), unsigned x, unsigned y, int threads, int smem, 
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kKernel, args...));
   return ADAPT_OK;
 }
 
@@ -165,14 +172,15 @@ int run_tiles(const LinearParams& q, int dtype, bool early, cudaStream_t stream)
     wide.wide_stores = !misaligned(q.y, 32) && (q.rows == 1 || q.ldy * e % 32 == 0);
     const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sms / 2));
     with_type(dtype, [&](auto t) {
-      rc = launch(int8_wide_kernel<decltype(t)>, grid, 1u, kWideThreads, kWideSmem, 0, early, stream, x_map, w_map, wide);
+      rc = launch<int8_wide_kernel<decltype(t)>>(grid, 1u, kWideThreads, kWideSmem, 0, early, stream, x_map, w_map, wide);
     });
     return rc;
   }
-  const int tokens = q.rows <= 16 ? 16 : q.rows <= 32 ? 32 : q.rows <= 64 ? 64 : q.rows <= 128 ? 128 : 256;
+  int tokens = q.rows <= 16 ? 16 : q.rows <= 32 ? 32 : q.rows <= 64 ? 64 : q.rows <= 128 ? 128 : 256;
   const int across = (q.n + kCtaRows - 1) / kCtaRows, down = (q.rows + tokens - 1) / tokens;
   int split = 1;
   while (split < kNarrowMaxSplit && static_cast<int64_t>(across) * down * split * 2 <= sms && blocks >= split * 4) split *= 2;
+  tokens = std::max(tokens, 4 * split);   // (columns are exchanged by fours)
   if (down > 65535 || static_cast<int64_t>(across) * split > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   if ((rc = tile_map(&x_map, q.x, q.rows, q.k, q.ldx, tokens)) != ADAPT_OK || (rc = tile_map(&w_map, q.w, q.n, q.k, q.ldw, kCtaRows)) != ADAPT_OK)
     return rc;
@@ -180,7 +188,7 @@ int run_tiles(const LinearParams& q, int dtype, bool early, cudaStream_t stream)
     using T = decltype(t);
     auto go = [&](auto c) {
       constexpr int N = decltype(c)::value;
-      rc = launch(int8_narrow_kernel<T, N>, static_cast<unsigned>(across * split), static_cast<unsigned>(down), kNarrowThreads, narrow_smem(N), split,
+      rc = launch<int8_narrow_kernel<T, N>>(static_cast<unsigned>(across * split), static_cast<unsigned>(down), kNarrowThreads, narrow_smem(N), split,
                   early, stream, x_map, w_map, q);
     };
     if (tokens == 16) go(std::integral_constant<int, 16>{});

@@ -115,34 +115,28 @@ struct LinearParams {
   bool x_one, w_one;   // one scale for all
 };
 
-// Tokens as the lanes' rows: 32 sums of one token from channel j on (all of them where `full`).
+// 32 results of one token to 32-byte aligned memory, in whole sectors.
 template <typename T>
-__device__ __forceinline__ void store_run(T* to, const float (&f)[32], int count, bool wide) {
-  if (wide && count >= 32) {
-    constexpr int kPer = 32 / sizeof(T);   // values of a 32-byte store: whole sectors
+__device__ __forceinline__ void store_run(T* to, const float (&f)[32]) {
+  constexpr int kPer = 32 / sizeof(T);   // values of a 32-byte store
 #pragma unroll
-    for (int i = 0; i < 32; i += kPer) {
-      unsigned w[8];
-      if constexpr (sizeof(T) == 4) {
+  for (int i = 0; i < 32; i += kPer) {
+    unsigned w[8];
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(f[i + k]);
-      } else {
+      for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(f[i + k]);
+    } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float part[8];
+      for (int h = 0; h < 2; ++h) {
+        float part[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) part[k] = f[i + 8 * h + k];
-          const uint4 p = pack16<T>(part);
-          w[4 * h] = p.x; w[4 * h + 1] = p.y; w[4 * h + 2] = p.z; w[4 * h + 3] = p.w;
-        }
+        for (int k = 0; k < 8; ++k) part[k] = f[i + 8 * h + k];
+        const uint4 p = pack16<T>(part);
+        w[4 * h] = p.x; w[4 * h + 1] = p.y; w[4 * h + 2] = p.z; w[4 * h + 3] = p.w;
       }
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" :: "l"(to + i), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
     }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 32; ++k)
-      if (k < count) to[k] = from_float<T>(f[k]);
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" :: "l"(to + i), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
   }
 }
 
@@ -182,6 +176,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kWideThreads, 1) void int
   __shared__ __align__(8) unsigned long long bars[2 * kWideStages + 4];
   __shared__ unsigned sums_at;
   __shared__ float scale_of[2][kWideTile], bias_of[2][kWideTile];
+  __shared__ float turned[4][32][33];   // a warp's 32 x 32 results, for rows that are not aligned
   const unsigned stages = (shared_address(wide_smem) + 1023u) & ~1023u;
   const unsigned full = shared_address(bars), empty = full + 8 * kWideStages, done = empty + 8 * kWideStages, open = done + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -278,7 +273,19 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kWideThreads, 1) void int
           const float y = static_cast<float>(v[k]) * scale * scale_of[buffer][c + k];
           f[k] = ok ? (q.p.bias ? y + bias_of[buffer][c + k] : y) : __int_as_float(0x7FC00000);   // a wait that ran out leaves NaN
         }
-        if (row < q.p.rows) store_run<T>(out + c, f, q.p.n - col - c, q.wide_stores);
+        const int count = q.p.n - col - c;
+        if (q.wide_stores && count >= 32) {
+          if (row < q.p.rows) store_run<T>(out + c, f);
+        } else {   // a row of 32 results by the warp
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) turned[quarter][lane][k] = f[k];
+          __syncwarp();
+          T* line = static_cast<T*>(q.p.y) + (row - lane) * q.p.ldy + col + c + lane;
+          const int rows = min(32, q.p.rows - (row - lane));
+          if (lane < count)
+            for (int r = 0; r < rows; ++r) line[r * q.p.ldy] = from_float<T>(turned[quarter][r][lane]);
+        }
       }
       tensor_fence_before();
       __syncwarp();
@@ -309,10 +316,11 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
                                                                     const __grid_constant__ CUtensorMap w_map, const LinearParams q) {
   constexpr int kStages = narrow_stages(kTokens), kStageBytes = narrow_stage_bytes(kTokens);
   constexpr unsigned kColumns = kTokens < 32 ? 32 : kTokens;
-  static_assert(kNarrowMaxSplit * kTokens / kNarrowMaxSplit * kCtaRows * 4 <= kStages * kStageBytes, "the exchange fits the stages");
+  static_assert(kTokens * kCtaRows * 4 <= kStages * kStageBytes, "the exchange fits the stages");
   extern __shared__ unsigned char narrow_smem_[];
   __shared__ __align__(8) unsigned long long bars[2 * kStages + 1];
-  __shared__ unsigned sums_at;
+  __shared__ unsigned sums_at, sums_ok[kNarrowMaxSplit];
+  __shared__ float scale_of[kTokens];
   const unsigned aligned = (shared_address(narrow_smem_) + 1023u) & ~1023u;
   const unsigned full = shared_address(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -372,65 +380,70 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
   }
   __syncwarp();
   wait_for_previous_kernel();
+  const int count = min(kTokens, q.rows - token0);
+  for (int c = threadIdx.x; c < count; c += kNarrowThreads) scale_of[c] = q.x_scales[q.x_one ? 0 : token0 + c];
+  const int channel = channel0 + threadIdx.x;
+  const bool in = channel < q.n;
+  const float w_scale = in ? q.w_scales[q.w_one ? 0 : channel] : 0.0f;
+  const float bias = in && q.bias ? q.bias[channel] : 0.0f;
+  __syncthreads();
   bool ok = barrier_wait(done, 0);   // (then every copy has been used)
   ok = __all_sync(~0u, ok);
   tensor_fence_after();
-  const float nan = __int_as_float(0x7FC00000);
   const unsigned mine = sums + (static_cast<unsigned>(warp * 32) << 16);
-  const int channel = channel0 + threadIdx.x;
-  const float w_scale = channel < q.n ? q.w_scales[q.w_one ? 0 : channel] : 0.0f;
-  const float bias = channel < q.n && q.bias ? q.bias[channel] : 0.0f;
-  auto finish = [&](int sum, int token, bool good) {
-    if (token >= q.rows || channel >= q.n) return;
-    float y = static_cast<float>(sum) * q.x_scales[q.x_one ? 0 : token] * w_scale;
+  T* const out = static_cast<T*>(q.y) + token0 * q.ldy + channel;
+  auto finish = [&](int sum, int c, bool good) {   // c: the token's column
+    float y = static_cast<float>(sum) * scale_of[c] * w_scale;
     if (q.bias) y += bias;
-    static_cast<T*>(q.y)[token * q.ldy + channel] = from_float<T>(good ? y : nan);
+    if (in && c < count) out[c * q.ldy] = from_float<T>(good ? y : __int_as_float(0x7FC00000));
   };
   if (split == 1) {
 #pragma unroll 1
-    for (int c = 0; c < kTokens; c += 16) {
-      if (token0 + c >= q.rows) break;
+    for (int c = 0; c < count; c += 16) {
       int v[16];
       tensor_read16(mine + c, v);
       tensor_read_wait();
 #pragma unroll
-      for (int k = 0; k < 16; ++k) finish(v[k], token0 + c + k, ok);
+      for (int k = 0; k < 16; ++k) finish(v[k], c + k, ok);
     }
   } else {
-    // [from][column of the share][channel]; a CTA that gave up sends nothing that is read as a sum: its flag is in `sums_ok`
-    __shared__ unsigned sums_ok[kNarrowMaxSplit];
-    const int share = kTokens / static_cast<int>(split);
+    // Every CTA gets its share of the columns, four at a time: [from][four columns][channel].  One whose wait
+    // ran out says so.
+    const int share = kTokens / static_cast<int>(split);   // a multiple of 4
     meet_cluster();   // everyone's products are done: the stages are free
     if (threadIdx.x < split) {
       const unsigned at = peer_address(shared_address(&sums_ok[rank]), threadIdx.x);
       asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(at), "r"(static_cast<unsigned>(ok)) : "memory");
     }
 #pragma unroll 1
-    for (int c = 0; c < kTokens; c += 16) {
-      if (token0 + c >= q.rows) break;
+    for (int c = 0; c < count; c += 16) {
       int v[16];
       tensor_read16(mine + c, v);
       tensor_read_wait();
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        const int owner = (c + k) / share, column = (c + k) - owner * share;
-        const unsigned at = peer_address(aligned + ((rank * share + column) * kCtaRows + threadIdx.x) * 4, owner);
-        asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(at), "r"(v[k]) : "memory");
+      for (int k = 0; k < 16; k += 4) {
+        const int owner = (c + k) / share, four = ((c + k) - owner * share) / 4;
+        const unsigned at = peer_address(aligned + ((rank * (share / 4) + four) * kCtaRows + threadIdx.x) * 16, owner);
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(v[k]), "r"(v[k + 1]), "r"(v[k + 2]), "r"(v[k + 3]) : "memory");
       }
     }
     meet_cluster();
     bool good = true;
     for (unsigned r = 0; r < split; ++r) good = good && sums_ok[r];
-    for (int c = 0; c < share; ++c) {
-      const int token = token0 + static_cast<int>(rank) * share + c;
-      if (token >= q.rows) break;
-      int sum = 0;
+    const int first = static_cast<int>(rank) * share;
+    for (int c = 0; c < share && first + c < count; c += 4) {
+      int4 sum = make_int4(0, 0, 0, 0);
+#pragma unroll 4
       for (unsigned r = 0; r < split; ++r) {
-        int v;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(aligned + ((r * share + c) * kCtaRows + threadIdx.x) * 4) : "memory");
-        sum += v;
+        int4 v;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(aligned + ((r * (share / 4) + c / 4) * kCtaRows + threadIdx.x) * 16) : "memory");
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
       }
-      finish(sum, token, good);
+      finish(sum.x, first + c, good);
+      finish(sum.y, first + c + 1, good);
+      finish(sum.z, first + c + 2, good);
+      finish(sum.w, first + c + 3, good);
     }
   }
   tensor_fence_before();
