@@ -760,7 +760,7 @@ int adapt_int8_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
  *   workspace  DEVICE scratch of adapt_int8_linear_workspace_bytes, 256-byte aligned (NULL where that is 0)
  * Any codes are legal, -128 too.  The sum is exact (int32); then come the scales, one after the
  * other, and the bias in fp32.  Codes with a 16-byte aligned address and a leading dimension
- * that is a multiple of 16 are read as they are; where there are more than 8 rows, others are
+ * that is a multiple of 16 are read as they are; where there are more than 2 rows, others are
  * first copied to the workspace.  Limits: rows, n < 2^31, k <= ADAPT_INT8_MAX_K. */
 int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t x_scale_count,
                       const int8_t* weight, const float* weight_scales,

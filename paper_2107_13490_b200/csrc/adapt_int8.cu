@@ -145,9 +145,7 @@ int run_dot(const LinearParams& q, const void* x, int x_dtype, int dtype, int64_
         else int8_dot_kernel<T, X, R, false><<<grid, kDotThreads, 0, stream>>>(d);
       };
       if (q.rows == 1) rows(std::integral_constant<int, 1>{});
-      else if (q.rows <= 2) rows(std::integral_constant<int, 2>{});
-      else if (q.rows <= 4) rows(std::integral_constant<int, 4>{});
-      else rows(std::integral_constant<int, 8>{});
+      else rows(std::integral_constant<int, kDotMaxRows>{});
     };
     if (x_dtype == ADAPT_DTYPE_I8) go(static_cast<signed char>(0)); else with_type(x_dtype, go);
   });
@@ -155,8 +153,31 @@ int run_dot(const LinearParams& q, const void* x, int x_dtype, int dtype, int64_
   return ADAPT_OK;
 }
 
+// How a product is cut: into tiles of pairs (tokens 0), or into tiles of so many tokens by 128 channels whose sums are dealt to
+// `split` CTAs.  Estimated in clocks: a code of the sum's index takes a tile the clocks of its products (8192 a
+// clock and SM) or those of its operands' way from L2 (about 50 bytes a clock and SM), a CTA some thousand to begin
+// and a sum that is dealt some thousand more.
+struct Cut { int tokens, split; };
+Cut choose_cut(int64_t rows, int64_t n, int64_t k) {
+  auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const int64_t blocks = up(k, kDepth), across = up(n, kCtaRows);
+  Cut best = {0, 1};
+  int64_t least = up(up(rows, kWideTile) * up(n, kWideTile), kSms / 2) * (blocks * kDepth * 9 / 2 + 1000) + 6000;
+  for (int tokens = 16; tokens <= 256; tokens *= 2) {
+    if (tokens >= 2 * rows && tokens > 16) break;
+    for (int split = 1; split <= narrow_split(tokens) && blocks >= 2 * split; split *= 2) {
+      const int64_t waves = up(across * up(rows, tokens) * split, kSms), depth = up(blocks, split) * kDepth;
+      const int64_t per = std::max<int64_t>(2 * (kCtaRows + tokens), 100 * tokens / 64);   // hundredths of a clock a code
+      const int64_t clocks = waves * (depth * per / 100 + 2000 + 12 * tokens) + (split > 1 ? 2000 + 8 * tokens : 0) + 2000;
+      if (clocks < least) { least = clocks; best = {tokens, split}; }
+    }
+  }
+  return best;
+}
+
 int run_tiles(const LinearParams& q, int dtype, bool early, cudaStream_t stream) {
-  const int e = elem_bytes(dtype), blocks = (q.k + kDepth - 1) / kDepth, sms = kSms;
+  const int e = elem_bytes(dtype);
+  const Cut cut = choose_cut(q.rows, q.n, q.k);
   CUtensorMap x_map, w_map;
   int rc = ADAPT_OK;
   WideParams wide = {};
@@ -165,22 +186,18 @@ int run_tiles(const LinearParams& q, int dtype, bool early, cudaStream_t stream)
   const int64_t tiles = static_cast<int64_t>(wide.across) * wide.down;
   if (tiles > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   LaunchScope ls(ADAPT_KERNEL_INT8_LINEAR, stream);
-  if (tiles >= sms / 4) {
+  if (cut.tokens == 0) {
     if ((rc = tile_map(&x_map, q.x, q.rows, q.k, q.ldx, kCtaRows)) != ADAPT_OK || (rc = tile_map(&w_map, q.w, q.n, q.k, q.ldw, kCtaRows)) != ADAPT_OK)
       return rc;
     wide.p = q;
     wide.wide_stores = !misaligned(q.y, 32) && (q.rows == 1 || q.ldy * e % 32 == 0);
-    const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sms / 2));
+    const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, kSms / 2));
     with_type(dtype, [&](auto t) {
       rc = launch<int8_wide_kernel<decltype(t)>>(grid, 1u, kWideThreads, kWideSmem, 0, early, stream, x_map, w_map, wide);
     });
     return rc;
   }
-  int tokens = q.rows <= 16 ? 16 : q.rows <= 32 ? 32 : q.rows <= 64 ? 64 : q.rows <= 128 ? 128 : 256;
-  const int across = (q.n + kCtaRows - 1) / kCtaRows, down = (q.rows + tokens - 1) / tokens;
-  int split = 1;
-  while (split < kNarrowMaxSplit && static_cast<int64_t>(across) * down * split * 2 <= sms && blocks >= split * 4) split *= 2;
-  tokens = std::max(tokens, 4 * split);   // (columns are exchanged by fours)
+  const int tokens = cut.tokens, split = cut.split, across = (q.n + kCtaRows - 1) / kCtaRows, down = (q.rows + tokens - 1) / tokens;
   if (down > 65535 || static_cast<int64_t>(across) * split > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   if ((rc = tile_map(&x_map, q.x, q.rows, q.k, q.ldx, tokens)) != ADAPT_OK || (rc = tile_map(&w_map, q.w, q.n, q.k, q.ldw, kCtaRows)) != ADAPT_OK)
     return rc;

@@ -306,9 +306,11 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kWideThreads, 1) void int
 // share of the tokens' columns from all of them through shared memory.
 
 constexpr int kNarrowThreads = 128;
-constexpr int kNarrowMaxSplit = 8;
 __host__ __device__ constexpr int narrow_stage_bytes(int tokens) { return (kCtaRows + tokens) * kDepth; }
 __host__ __device__ constexpr int narrow_stages(int tokens) { return tokens <= 64 ? 8 : tokens == 128 ? 6 : 4; }
+// CTAs that share a sum at most, and the columns that one of them sends.
+__host__ __device__ constexpr int narrow_split(int tokens) { return tokens <= 16 ? 4 : tokens <= 128 ? 8 : 4; }
+__host__ __device__ constexpr int narrow_sent(int tokens) { return tokens / narrow_split(tokens) * (narrow_split(tokens) - 1); }
 __host__ __device__ constexpr int narrow_smem(int tokens) { return narrow_stages(tokens) * narrow_stage_bytes(tokens) + 1024; }
 
 template <typename T, int kTokens>
@@ -316,13 +318,13 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
                                                                     const __grid_constant__ CUtensorMap w_map, const LinearParams q) {
   constexpr int kStages = narrow_stages(kTokens), kStageBytes = narrow_stage_bytes(kTokens);
   constexpr unsigned kColumns = kTokens < 32 ? 32 : kTokens;
-  static_assert(kTokens * kCtaRows * 4 <= kStages * kStageBytes, "the exchange fits the stages");
+  static_assert(2 * narrow_sent(kTokens) * kCtaRows * 4 <= kStages * kStageBytes, "what is sent and received fits the stages");
   extern __shared__ unsigned char narrow_smem_[];
-  __shared__ __align__(8) unsigned long long bars[2 * kStages + 1];
-  __shared__ unsigned sums_at, sums_ok[kNarrowMaxSplit];
+  __shared__ __align__(8) unsigned long long bars[2 * kStages + 2];
+  __shared__ unsigned sums_at;
   __shared__ float scale_of[kTokens];
   const unsigned aligned = (shared_address(narrow_smem_) + 1023u) & ~1023u;
-  const unsigned full = shared_address(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
+  const unsigned full = shared_address(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, exchange = done + 8;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned rank = cta_in_cluster(), split = ctas_of_cluster();
   const int channel0 = blockIdx.x / split * kCtaRows, token0 = blockIdx.y * kTokens;
@@ -331,6 +333,7 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
     barrier_init(done, 1);
+    barrier_init(exchange, 1);
     barrier_init_fence();
     tile_map_prefetch(&w_map);
     tile_map_prefetch(&x_map);
@@ -407,14 +410,11 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
       for (int k = 0; k < 16; ++k) finish(v[k], c + k, ok);
     }
   } else {
-    // Every CTA gets its share of the columns, four at a time: [from][four columns][channel].  One whose wait
-    // ran out says so.
-    const int share = kTokens / static_cast<int>(split);   // a multiple of 4
-    meet_cluster();   // everyone's products are done: the stages are free
-    if (threadIdx.x < split) {
-      const unsigned at = peer_address(shared_address(&sums_ok[rank]), threadIdx.x);
-      asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(at), "r"(static_cast<unsigned>(ok)) : "memory");
-    }
+    // Every CTA adds up its share of the columns: those of the others' come by bulk copies, in slots of
+    // [four columns][channel].  One whose wait ran out sends nothing, so that the others' run out too.
+    const int share = kTokens / static_cast<int>(split), first = static_cast<int>(rank) * share;   // a multiple of 4
+    const unsigned slot = share * kCtaRows * 4, received = aligned + (split - 1) * slot;
+    if (threadIdx.x == 0) barrier_expect_bytes(exchange, (split - 1) * slot);
 #pragma unroll 1
     for (int c = 0; c < count; c += 16) {
       int v[16];
@@ -423,28 +423,35 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
 #pragma unroll
       for (int k = 0; k < 16; k += 4) {
         const int owner = (c + k) / share, four = ((c + k) - owner * share) / 4;
-        const unsigned at = peer_address(aligned + ((rank * (share / 4) + four) * kCtaRows + threadIdx.x) * 16, owner);
-        asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(v[k]), "r"(v[k + 1]), "r"(v[k + 2]), "r"(v[k + 3]) : "memory");
+        if (owner == static_cast<int>(rank)) continue;
+        const unsigned at = aligned + (owner - (owner > static_cast<int>(rank))) * slot + (four * kCtaRows + threadIdx.x) * 16;
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(at), "r"(v[k]), "r"(v[k + 1]), "r"(v[k + 2]), "r"(v[k + 3]) : "memory");
       }
     }
-    meet_cluster();
-    bool good = true;
-    for (unsigned r = 0; r < split; ++r) good = good && sums_ok[r];
-    const int first = static_cast<int>(rank) * share;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    meet_cluster();   // everyone's products are done, so that the stages are free, and everyone's sums are in place
+    if (threadIdx.x < split && threadIdx.x != rank && ok) {
+      const unsigned to_rank = threadIdx.x, out_slot = to_rank - (to_rank > rank), in_slot = rank - (rank > to_rank);
+      asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                   :: "r"(peer_address(received + in_slot * slot, to_rank)), "r"(aligned + out_slot * slot), "r"(slot),
+                      "r"(peer_address(exchange, to_rank)) : "memory");
+    }
+    bool good = ok && barrier_wait(exchange, 0);
     for (int c = 0; c < share && first + c < count; c += 4) {
-      int4 sum = make_int4(0, 0, 0, 0);
-#pragma unroll 4
-      for (unsigned r = 0; r < split; ++r) {
+      int sum[4];
+      tensor_read4(mine + first + c, sum);
+      tensor_read_wait();
+      for (unsigned r = 0; r + 1 < split; ++r) {
         int4 v;
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "r"(aligned + ((r * (share / 4) + c / 4) * kCtaRows + threadIdx.x) * 16) : "memory");
-        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+                     : "r"(received + r * slot + (c / 4 * kCtaRows + threadIdx.x) * 16) : "memory");
+        sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
       }
-      finish(sum.x, first + c, good);
-      finish(sum.y, first + c + 1, good);
-      finish(sum.z, first + c + 2, good);
-      finish(sum.w, first + c + 3, good);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) finish(sum[k], first + c + k, good);
     }
+    __syncwarp();
+    meet_cluster();   // what was sent has arrived
   }
   tensor_fence_before();
   __syncthreads();
@@ -503,7 +510,7 @@ constexpr int kDotThreads = 256;
 constexpr int kDotChannels = 2;                    // of a warp
 constexpr int kDotStrips = 8;                      // blocks of 16 bytes that a lane has under way for a channel
 constexpr int kDotChunk = kDotStrips * 32 * 16;    // codes of a row at a time
-constexpr int kDotMaxRows = 8;
+constexpr int kDotMaxRows = 2;
 
 struct DotParams {
   LinearParams p;
