@@ -23,39 +23,44 @@ constexpr int kNormMaxRowForward = 32 * kNormMaxThreads;   // and forward
 
 // Elements of a thread and threads of a CTA for a row, and CTAs of an SM.  Backward: 128 registers a thread.
 int norm_elems(int64_t dim) { return dim <= 2048 ? 8 : dim <= kNormMaxRow ? 16 : 32; }
-int norm_threads(int64_t dim) {
+int norm_threads(int64_t dim) {   // (with room for up to 7 elements between a boundary and an odd row)
   const int e = norm_elems(dim);
-  return std::min<int>(kNormMaxThreads, static_cast<int>((dim + 32 * e - 1) / (32 * e)) * 32);
+  return std::min<int>(kNormMaxThreads, static_cast<int>((dim + (dim % 8 ? 7 : 0) + 32 * e - 1) / (32 * e)) * 32);
 }
 int norm_per_sm(int64_t dim) { return std::max(1, std::min(8, kNormMaxThreads / norm_threads(dim))); }
 
 // CTAs of a backward pass, each with sums of its own over its rows.
 int64_t norm_ctas(int64_t rows, int64_t dim) { return std::min<int64_t>(rows, kSms * norm_per_sm(dim)); }
+// A multiple of the period, so that a CTA's rows lie alike; the CTAs that has more have no rows, and sums of 0.
+unsigned norm_grid(int64_t ctas, int period) { return static_cast<unsigned>((ctas + period - 1) / period * period); }
 
-// How the rows come: through how many stages of shared memory (0: as they lie), of which streams.
+// How the rows come through shared memory, if they do: all tensors have to lie alike to the 16-byte boundary, row by row.
 struct NormPlan {
   NormRing ring = {};
-  int smem = 0;
-  bool staged = true;
-  // the rows that are read, and what is read or written beside them in 16 bytes
-  NormPlan(const NormParams& q, int e, int per_sm, std::initializer_list<std::pair<const void*, long long>> in,
+  int smem = 0, period = 1;   // rows whose numbers differ by a multiple of the period lie alike
+  bool staged = true, edges = false;
+  NormPlan(const NormParams& q, int e, int per_sm, int elems, int threads, std::initializer_list<std::pair<const void*, long long>> in,
            std::initializer_list<std::pair<const void*, long long>> out) {
-    const int unit = 16 / e;
-    auto fits = [&](const std::pair<const void*, long long>& p) { return !p.first || (!misaligned(p.first, 16) && (q.rows == 1 || p.second % unit == 0)); };
-    staged = q.dim % unit == 0;
+    auto phase = [](const void* p) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 15u); };
+    auto step = [&](long long ld) { return q.rows == 1 ? 0u : static_cast<unsigned>(ld * e & 15); };
+    const unsigned first = phase(q.block), by = step(q.ld_block);
+    auto alike = [&](const std::pair<const void*, long long>& p) { return !p.first || (phase(p.first) == first && step(p.second) == by); };
     int i = 0;
     for (const auto& p : in) {
-      staged = staged && fits(p);
+      staged = staged && alike(p);
       ring.slot[i++] = p.first ? ring.streams++ : -1;
     }
-    for (const auto& p : out) staged = staged && fits(p);
+    for (const auto& p : out) staged = staged && alike(p);
+    edges = first != 0 || by != 0 || q.dim * e % 16 != 0;
     for (const void* p : {static_cast<const void*>(q.weight_after), static_cast<const void*>(q.weight_before), q.shared ? q.gate : nullptr})
-      staged = staged && !misaligned(p, 16);
-    const int row = ring.streams * q.dim * e, most = 200 * 1024 / per_sm;
-    ring.stages = std::min({kNormMaxStages, most / row, 220 * 1024 / row});
-    if (ring.stages < 1 && row <= 220 * 1024) ring.stages = 1;
+      edges = edges || misaligned(p, 16);
+    while (period * by % 16) period *= 2;
+    ring.stage_row = edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
+    if (edges && q.dim + 16 / e - 1 > elems * threads) staged = false;   // the elements before a boundary take room too
+    const int stage = ring.streams * ring.stage_row;
+    ring.stages = std::min(kNormMaxStages, std::max(200 * 1024 / per_sm / stage, 220 * 1024 / stage > 0 ? 1 : 0));
     staged = staged && ring.stages > 0;
-    smem = staged ? ring.stages * row : 0;
+    smem = ring.stages * stage;
   }
 };
 
@@ -125,21 +130,23 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
   LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM, stream);
   if (dim <= kNormMaxRowForward) {
     const int elems = norm_elems(dim), threads = norm_threads(dim), per_sm = std::max(1, std::min(16, (elems <= 16 ? 1024 : 512) / threads));
-    const NormPlan plan(q, e, per_sm, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate}, {nullptr, 0}, {nullptr, 0}},
-                        {{y, q.ld_y}, {normed, q.ld_normed}});
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(rows, kSms * per_sm));
-    with_type(dtype, [&](auto t) {
-      using T = decltype(t);
-      auto go = [&](auto n) {
-        constexpr int N = decltype(n)::value;
-        if (plan.staged) rc = norm_launch<norm_row_kernel<T, N, true>>(grid, threads, plan.smem, stream, q, plan.ring);
-        else rc = norm_launch<norm_row_kernel<T, N, false>>(grid, threads, 0, stream, q, plan.ring);
-      };
-      if (elems == 8) go(std::integral_constant<int, 8>{});
-      else if (elems == 16) go(std::integral_constant<int, 16>{});
-      else go(std::integral_constant<int, 32>{});
-    });
-    return rc;
+    const NormPlan plan(q, e, per_sm, elems, threads, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
+                        {nullptr, 0}, {nullptr, 0}}, {{y, q.ld_y}, {normed, q.ld_normed}});
+    if (plan.staged) {
+      const unsigned grid = norm_grid(std::min<int64_t>(rows, kSms * per_sm), plan.period);
+      with_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        auto go = [&](auto n) {
+          constexpr int N = decltype(n)::value;
+          if (plan.edges) rc = norm_launch<norm_row_kernel<T, N, true>>(grid, threads, plan.smem, stream, q, plan.ring);
+          else rc = norm_launch<norm_row_kernel<T, N, false>>(grid, threads, plan.smem, stream, q, plan.ring);
+        };
+        if (elems == 8) go(std::integral_constant<int, 8>{});
+        else if (elems == 16) go(std::integral_constant<int, 16>{});
+        else go(std::integral_constant<int, 32>{});
+      });
+      return rc;
+    }
   }
   with_type(dtype, [&](auto t) {
     const auto kernel = norm_any_kernel<decltype(t)>;
@@ -154,7 +161,7 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
 
 size_t adapt_block_norm_workspace_bytes(int64_t rows, int64_t dim) {
   if (rows < 1 || rows > 0x7FFFFFFF || dim < 1 || dim > ADAPT_NORM_MAX_DIM) return 0;
-  return 3 * sizeof(float) * static_cast<size_t>(norm_ctas(rows, dim)) * dim;
+  return 3 * sizeof(float) * static_cast<size_t>(norm_grid(norm_ctas(rows, dim), 8)) * dim;
 }
 
 int adapt_block_norm_backward(const void* block, const void* residual, const void* gate, const float* weight_after,
@@ -202,11 +209,13 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   int rc = ADAPT_OK;
   {
     LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM_BACKWARD, stream);
-    const unsigned grid = static_cast<unsigned>(ctas);
-    if (dim <= kNormMaxRow) {
-      const int threads = norm_threads(dim);
-      const NormPlan plan(q, e, norm_per_sm(dim), {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y},
-                          {d_normed, q.ld_d_normed}}, {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
+    const int threads = norm_threads(dim);
+    const NormPlan plan(q, e, norm_per_sm(dim), norm_elems(dim), threads, {{block, q.ld_block}, {residual, q.ld_residual},
+                        {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
+                        {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
+    if (plan.staged && dim <= kNormMaxRow) {
+      const unsigned grid = norm_grid(ctas, plan.period);
+      sum.ctas = static_cast<int>(grid);
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
         auto go = [&](auto n, auto s) {
@@ -215,15 +224,15 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
           if (q.shared) rc = norm_launch<norm_row_backward_kernel<T, N, S, true>>(grid, threads, plan.smem, stream, q, plan.ring);
           else rc = norm_launch<norm_row_backward_kernel<T, N, S, false>>(grid, threads, plan.smem, stream, q, plan.ring);
         };
-        auto staged = [&](auto n) { plan.staged ? go(n, std::true_type{}) : go(n, std::false_type{}); };
-        if (norm_elems(dim) == 8) staged(std::integral_constant<int, 8>{}); else staged(std::integral_constant<int, 16>{});
+        auto edged = [&](auto n) { plan.edges ? go(n, std::true_type{}) : go(n, std::false_type{}); };
+        if (norm_elems(dim) == 8) edged(std::integral_constant<int, 8>{}); else edged(std::integral_constant<int, 16>{});
       });
     } else {
       with_type(dtype, [&](auto t) {
         const auto kernel = norm_any_backward_kernel<decltype(t)>;
         const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ADAPT_NORM_MAX_DIM * 4);
         if (err != cudaSuccess) rc = cuda_fail(err, "block norm, backward");
-        else kernel<<<grid, kNormThreads, q.dim * 4, stream>>>(q);
+        else kernel<<<static_cast<unsigned>(ctas), kNormThreads, q.dim * 4, stream>>>(q);
       });
     }
     if (rc != ADAPT_OK) return rc;
@@ -231,7 +240,16 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   }
   if (sums) {
     LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM_BACKWARD, stream);
-    norm_columns_kernel<<<dim3(static_cast<unsigned>((q.dim + 31) / 32), 3), 32 * kNormColumnWarps, 0, stream>>>(sum);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((q.dim + 31) / 32), 3);
+    cfg.blockDim = dim3(32 * kNormColumnWarps);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its launch hides behind the rows
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ADAPT_CUDA(cudaLaunchKernelEx(&cfg, norm_columns_kernel, sum));
     ADAPT_LAUNCH_OK("block norm, sums over rows");
   }
   return ADAPT_OK;

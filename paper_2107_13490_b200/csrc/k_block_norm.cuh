@@ -202,19 +202,62 @@ __global__ __launch_bounds__(kNormThreads) void norm_any_backward_kernel(NormPar
 
 // ---- rows held in registers ------------------------------------------------------------------------------
 //
-// A CTA walks over rows, a row at a time; a thread holds kElems elements of it.  Where all rows are 16-byte
-// aligned (kStaged) they come through a ring of stages in shared memory that bulk copies fill rows ahead, so that
-// loads are under way while the sums of a row meet; others are read where they lie, element by element.
+// A CTA walks over rows, a row at a time; a thread holds kElems elements of it, in chunks of 16 bytes.  The rows come
+// through a ring of stages in shared memory that bulk copies fill rows ahead, so that loads are under way while the
+// sums of a row meet.  Arithmetic is on pairs of elements: issue slots are the next bound behind HBM.
 //
-// dim 4096, bf16: 256 threads of 16 elements, two CTAs of two stages an SM for the backward pass.
+// Rows that do not begin on 16-byte boundaries (an odd dim) are copied with the aligned blocks around them.  All tensors
+// have to lie alike (kEdges): then chunks are cut at those boundaries, the first and the last hold fewer
+// elements, and a CTA takes rows that lie alike too, so that a thread keeps its columns.
 
 constexpr int kNormMaxThreads = 512;
 constexpr int kNormMaxStages = 4;
 
 struct NormRing {
   int streams, stages;       // rows of a stage, stages
+  int stage_row;             // bytes of a row in a stage
   int slot[5];               // place of block, residual, gate, d_y, d_normed in a stage, -1: none
 };
+
+__device__ __forceinline__ f32x2 both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float fast_exp2(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float fast_inverse(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+
+// g(gate) of a pair: 1 / (1 + e^-v), to 2^-22 and |v| steps of the exponent's argument; 0 below 2^-126.
+__device__ __forceinline__ f32x2 gate_open(f32x2 v) {
+  const float2 e = unpack2(mul2(v, both(-kLog2E)));
+  const float2 d = unpack2(add2(pack2(fast_exp2(e.x), fast_exp2(e.y)), both(1.0f)));
+  return pack2(fast_inverse(d.x), fast_inverse(d.y));
+}
+
+// The gate of the backward pass's first phase, kept in one number for the second: the smaller of g and 1 - g (the
+// other is 1 minus it, to a rounding), with the sign that says which.  So g (1 - g) keeps its relative precision
+// where the gate is far open or closed.
+__device__ __forceinline__ f32x2 gate_kept(f32x2 v) {
+  const float2 f = unpack2(v);
+  const float2 e = unpack2(mul2(pack2(fabsf(f.x), fabsf(f.y)), both(-kLog2E)));
+  const f32x2 t = pack2(fast_exp2(e.x), fast_exp2(e.y));
+  const float2 d = unpack2(add2(t, both(1.0f)));
+  const float2 c = unpack2(mul2(t, pack2(fast_inverse(d.x), fast_inverse(d.y))));
+  return pack2(copysignf(c.x, f.x), copysignf(c.y, f.y));
+}
+struct GatePair { f32x2 open, slope; };
+__device__ __forceinline__ GatePair gate_again(f32x2 kept) {
+  const float2 k = unpack2(kept);
+  const f32x2 least = pack2(fabsf(k.x), fabsf(k.y));
+  const f32x2 most = fma2(least, both(-1.0f), both(1.0f));
+  const float2 l = unpack2(least), m = unpack2(most);
+  return {pack2(signbit(k.x) ? l.x : m.x, signbit(k.y) ? l.y : m.y), mul2(least, most)};
+}
 
 // Sums over a CTA, in one of two sets of places in turn, so that one barrier each is enough.
 struct CtaSums {
@@ -236,312 +279,387 @@ struct CtaSums {
   }
 };
 
-// The rows of a CTA in order, read ahead into the ring by its first thread.
-template <typename T, bool kStaged>
+// The rows of a CTA in order, read ahead into the ring by its first thread, and the columns of a thread.
+template <typename T, int kElems, bool kEdges>
 struct NormRows {
+  static constexpr int V = 16 / sizeof(T), P = V / 2, kChunks = kElems / V;
   const NormParams& q;
   const NormRing& ring;
   unsigned stages, bars;     // addresses
-  int row_bytes;
   unsigned use;
+  int skip;                  // elements between a 16-byte boundary and the rows' first element
+  unsigned in;               // which of the thread's elements are elements of the row (kEdges)
   __device__ __forceinline__ NormRows(const NormParams& q_, const NormRing& r, unsigned char* smem, unsigned long long* b)
-      : q(q_), ring(r), stages(shared_address(smem)), bars(shared_address(b)), row_bytes(q_.dim * static_cast<int>(sizeof(T))), use(0) {
-    if constexpr (kStaged) {
-      if (threadIdx.x == 0) {
-        for (int s = 0; s < ring.stages; ++s) barrier_init(bars + 8 * s, 1);
-        barrier_init_fence();
-        for (int s = 0; s < ring.stages; ++s) fill(s, static_cast<long long>(blockIdx.x) + static_cast<long long>(s) * gridDim.x);
+      : q(q_), ring(r), stages(shared_address(smem)), bars(shared_address(b)), use(0), skip(0), in(~0u) {
+    if constexpr (kEdges) {
+      skip = static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + blockIdx.x * q.ld_block) & 15u) / sizeof(T));
+      in = 0;
+#pragma unroll
+      for (int j = 0; j < kElems; ++j) {
+        const int c = column(j / V) + j % V;
+        in |= (c >= 0 && c < q.dim ? 1u : 0u) << j;
       }
-      __syncthreads();
     }
+    if (threadIdx.x == 0) {
+      for (int s = 0; s < ring.stages; ++s) barrier_init(bars + 8 * s, 1);
+      barrier_init_fence();
+      for (int s = 0; s < ring.stages; ++s) fill(s, static_cast<long long>(blockIdx.x) + static_cast<long long>(s) * gridDim.x);
+    }
+    __syncthreads();
   }
+  __device__ __forceinline__ int column(int i) const { return (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V - skip; }
+  // Whether chunk i has an element of the row, and whether all of its elements are.
+  __device__ __forceinline__ bool any(int i) const { return column(i) < q.dim; }
+  __device__ __forceinline__ bool whole(int i) const { return !kEdges || ((in >> (i * V)) & ((1u << V) - 1)) == (1u << V) - 1; }
+  __device__ __forceinline__ bool has(int j) const { return !kEdges || (in >> j & 1); }
+
   __device__ __forceinline__ void fill(int s, long long r) const {
     if (r >= q.rows) return;
-    barrier_expect_bytes(bars + 8 * s, ring.streams * row_bytes);
+    const unsigned bytes = kEdges ? ((skip + q.dim) * static_cast<int>(sizeof(T)) + 15) & ~15 : q.dim * static_cast<int>(sizeof(T));
+    barrier_expect_bytes(bars + 8 * s, ring.streams * bytes);
     const void* from[5] = {q.block, q.residual, q.gate, q.d_y, q.d_normed};
     const long long ld[5] = {q.ld_block, q.ld_residual, q.ld_gate, q.ld_d_y, q.ld_d_normed};
 #pragma unroll
     for (int i = 0; i < 5; ++i)
       if (ring.slot[i] >= 0)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     :: "r"(stages + (s * ring.streams + ring.slot[i]) * row_bytes), "l"(static_cast<const T*>(from[i]) + r * ld[i]), "r"(row_bytes),
-                        "r"(bars + 8 * s) : "memory");
+                     :: "r"(stages + (s * ring.streams + ring.slot[i]) * ring.stage_row), "l"(static_cast<const T*>(from[i]) + r * ld[i] - skip),
+                        "r"(bytes), "r"(bars + 8 * s) : "memory");
   }
   // Waits for the row's data; 0, or NaN where they never came.
   __device__ __forceinline__ float ready() const {
-    if constexpr (kStaged)
-      if (!barrier_wait(bars + 8 * (use % ring.stages), (use / ring.stages) & 1)) return __int_as_float(0x7FC00000);
-    return 0.0f;
+    return barrier_wait(bars + 8 * (use % ring.stages), (use / ring.stages) & 1) ? 0.0f : __int_as_float(0x7FC00000);
   }
   // Called when every thread has read what it needs of the row `r`.
   __device__ __forceinline__ void release(long long r) {
-    if constexpr (kStaged) {
-      if (threadIdx.x == 0) fill(use % ring.stages, r + static_cast<long long>(ring.stages) * gridDim.x);
-      ++use;
+    if (threadIdx.x == 0) fill(use % ring.stages, r + static_cast<long long>(ring.stages) * gridDim.x);
+    ++use;
+  }
+  // Chunk i of stream kStream; 0 for what is not in the row.
+  template <int kStream>
+  __device__ __forceinline__ void read(int i, f32x2 (&f)[P]) const {
+    uint4 raw;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w)
+                 : "r"(stages + ((use % ring.stages) * ring.streams + ring.slot[kStream]) * ring.stage_row + (i * blockDim.x + threadIdx.x) * 16));
+    float v[V];
+    unpack16<T>(raw, v);
+    if (kEdges && !whole(i)) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = has(i * V + k) ? v[k] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < P; ++k) f[k] = pack2(v[2 * k], v[2 * k + 1]);
+  }
+  __device__ __forceinline__ void weights(const float* w, int i, f32x2 (&f)[P]) const {
+    const int c = column(i);
+    if constexpr (kEdges) {
+#pragma unroll
+      for (int k = 0; k < P; ++k)
+        f[k] = pack2(has(i * V + 2 * k) ? __ldg(w + c + 2 * k) : 0.0f, has(i * V + 2 * k + 1) ? __ldg(w + c + 2 * k + 1) : 0.0f);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; k += 4) {
+        const float4 t = __ldg(reinterpret_cast<const float4*>(w + c + k));
+        f[k / 2] = pack2(t.x, t.y);
+        f[k / 2 + 1] = pack2(t.z, t.w);
+      }
     }
   }
-  // Elements c .. c + V - 1 of stream kStream of row r, which has to be there.
-  template <int kStream, int V>
-  __device__ __forceinline__ void read(long long r, int c, float (&f)[V]) const {
-    if constexpr (kStaged) {
-      uint4 raw;
-      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w)
-                   : "r"(stages + ((use % ring.stages) * ring.streams + ring.slot[kStream]) * row_bytes + c * static_cast<int>(sizeof(T))));
-      unpack16<T>(raw, f);
+  __device__ __forceinline__ void write(void* to, long long at, int i, const f32x2 (&f)[P]) const {
+    float v[V];
+#pragma unroll
+    for (int k = 0; k < P; ++k) { const float2 t = unpack2(f[k]); v[2 * k] = t.x; v[2 * k + 1] = t.y; }
+    T* p = static_cast<T*>(to) + at + column(i);
+    if (whole(i)) {
+      __stcs(reinterpret_cast<uint4*>(p), pack16<T>(v));
     } else {
-      const void* from = kStream == 0 ? q.block : kStream == 1 ? q.residual : kStream == 2 ? q.gate : kStream == 3 ? q.d_y : q.d_normed;
-      const long long ld = kStream == 0 ? q.ld_block : kStream == 1 ? q.ld_residual : kStream == 2 ? q.ld_gate : kStream == 3 ? q.ld_d_y : q.ld_d_normed;
-      f[0] = to_float(static_cast<const T*>(from)[r * ld + c]);
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (has(i * V + k)) p[k] = from_float<T>(v[k]);
+    }
+  }
+  // A column's sum over the rows.
+  __device__ __forceinline__ void write_sums(float* to, int i, const f32x2* f) const {
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const float2 t = unpack2(f[k]);
+      float* p = to + column(i) + 2 * k;
+      if (has(i * V + 2 * k)) p[0] = t.x;
+      if (has(i * V + 2 * k + 1)) p[1] = t.y;
     }
   }
 };
 
-template <int V>
-__device__ __forceinline__ void read_weights(const float* w, int c, float (&f)[V]) {
-  if constexpr (V == 1) {
-    f[0] = __ldg(w + c);
-  } else {
+template <int N>
+__device__ __forceinline__ float pairs_sum(const f32x2 (&v)[N]) {
+  f32x2 s = v[0];
 #pragma unroll
-    for (int k = 0; k < V; k += 4) {
-      const float4 t = __ldg(reinterpret_cast<const float4*>(w + c + k));
-      f[k] = t.x; f[k + 1] = t.y; f[k + 2] = t.z; f[k + 3] = t.w;
-    }
-  }
-}
-template <typename T, int V>
-__device__ __forceinline__ void write_part(T* p, const float (&f)[V]) {
-  if constexpr (V == 1) *p = from_float<T>(f[0]);
-  else __stcs(reinterpret_cast<uint4*>(p), pack16<T>(f));
+  for (int k = 1; k < N; ++k) s = add2(s, v[k]);
+  const float2 t = unpack2(s);
+  return t.x + t.y;
 }
 
-template <typename T, bool kStaged>
-__host__ __device__ constexpr int norm_unit() { return kStaged ? 16 / static_cast<int>(sizeof(T)) : 1; }
-
-template <typename T, int kElems, bool kStaged>
+template <typename T, int kElems, bool kEdges>
 __global__ __launch_bounds__(kNormMaxThreads, kElems <= 16 ? 2 : 1) void norm_row_kernel(const NormParams q, const NormRing ring) {
-  constexpr int V = norm_unit<T, kStaged>(), kChunks = kElems / V;
+  typedef NormRows<T, kElems, kEdges> Rows;
+  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kElems / 2;
   extern __shared__ __align__(128) unsigned char norm_smem[];
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
   __shared__ float2 places[2][kNormMaxThreads / 32];
-  NormRows<T, kStaged> rows(q, ring, norm_smem, bars);
+  Rows rows(q, ring, norm_smem, bars);
   CtaSums sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
-  auto column = [&](int i) { return (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V; };
-  // mean and 1 / deviation; the deviation around the mean, in a second sum
-  auto statistics = [&](const float (&v)[kElems], int kind) {
-    float mean = 0.0f, s = 0.0f;
+  // mean and 1 / deviation; the deviation around the mean, in a second sum.  Leaves v - mean.
+  auto statistics = [&](f32x2 (&v)[kPairs], int kind) {
+    float mean = 0.0f;
     if (kind == kNormLayer) {
+      mean = sums(pairs_sum(v), 0.0f).x * inv;   // (0 beyond the row)
+      const f32x2 less = both(-mean);
 #pragma unroll
-      for (int j = 0; j < kElems; ++j) s += v[j];   // (0 beyond the row)
-      mean = sums(s, 0.0f).x * inv;
-      s = 0.0f;
+      for (int i = 0; i < kChunks; ++i) {
+        if (!rows.any(i)) break;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          v[i * P + k] = add2(v[i * P + k], less);
+          if (kEdges && !rows.whole(i)) {
+            const float2 t = unpack2(v[i * P + k]);
+            v[i * P + k] = pack2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
+          }
+        }
+      }
     }
+    f32x2 s = both(0.0f);
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-      if (column(i) >= q.dim) break;
-#pragma unroll
-      for (int k = 0; k < V; ++k) { const float d = v[i * V + k] - mean; s = fmaf(d, d, s); }
-    }
-    return make_float2(mean, rsqrtf(fmaf(sums(s, 0.0f).x, inv, q.eps)));
+    for (int k = 0; k < kPairs; ++k) s = fma2(v[k], v[k], s);
+    const float2 t = unpack2(s);
+    return make_float2(mean, rsqrtf(fmaf(sums(t.x + t.y, 0.0f).x, inv, q.eps)));
   };
   for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
     const float poison = rows.ready();
-    float v[kElems];
+    f32x2 v[kPairs];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      float f[V] = {};
-      const int c = column(i);
-      if (c < q.dim) rows.template read<0>(r, c, f);
+      f32x2 f[P];
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[i * V + k] = f[k];
+      for (int k = 0; k < P; ++k) f[k] = both(0.0f);
+      if (rows.any(i)) rows.template read<0>(i, f);
+#pragma unroll
+      for (int k = 0; k < P; ++k) v[i * P + k] = f[k];
     }
-    v[0] += poison;
+    v[0] = add2(v[0], both(poison));
     float2 a = make_float2(0.0f, 1.0f), b = a;
     if (q.after != kNormNone) a = statistics(v, q.after);
+    const f32x2 factor = both(a.y);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      const int c = column(i);
-      if (c >= q.dim) break;
-      float g[V], w[V];
+      if (!rows.any(i)) break;
+      f32x2 g[P];
       if (q.after != kNormNone) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[i * V + k] = (v[i * V + k] - a.x) * a.y;
-        if (q.weight_after) {
-          read_weights<V>(q.weight_after, c, w);
+        for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], factor);
+      }
+      if (q.weight_after) {
+        rows.weights(q.weight_after, i, g);
 #pragma unroll
-          for (int k = 0; k < V; ++k) v[i * V + k] *= w[k];
-        }
+        for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], g[k]);
       }
       if (q.gate) {
-        if (q.shared) read_weights<V>(static_cast<const float*>(q.gate), c, g); else rows.template read<2>(r, c, g);
+        if (q.shared) rows.weights(static_cast<const float*>(q.gate), i, g); else rows.template read<2>(i, g);
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[i * V + k] *= norm_gate(g[k], q.sigmoid).open;
+        for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], q.sigmoid ? gate_open(g[k]) : g[k]);
       }
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[i * V + k] *= q.scale;
+      for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], both(q.scale));
       if (q.residual) {
-        rows.template read<1>(r, c, g);
+        rows.template read<1>(i, g);
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[i * V + k] = fmaf(g[k], q.residual_scale, v[i * V + k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = fma2(g[k], both(q.residual_scale), v[i * P + k]);
+      }
+      if (q.y) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) g[k] = v[i * P + k];
+        rows.write(q.y, r * q.ld_y, i, g);
       }
     }
     if (q.before != kNormNone) b = statistics(v, q.before); else __syncthreads();
     rows.release(r);
+    if (q.normed) {
+      const f32x2 by = both(b.y);
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-      const int c = column(i);
-      if (c >= q.dim) break;
-      float f[V], w[V];
-      if (q.y) {
+      for (int i = 0; i < kChunks; ++i) {
+        if (!rows.any(i)) break;
+        f32x2 f[P], w[P];
 #pragma unroll
-        for (int k = 0; k < V; ++k) f[k] = v[i * V + k];
-        write_part<T, V>(static_cast<T*>(q.y) + r * q.ld_y + c, f);
-      }
-      if (q.normed) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) f[k] = (v[i * V + k] - b.x) * b.y;
+        for (int k = 0; k < P; ++k) f[k] = mul2(v[i * P + k], by);
         if (q.weight_before) {
-          read_weights<V>(q.weight_before, c, w);
+          rows.weights(q.weight_before, i, w);
 #pragma unroll
-          for (int k = 0; k < V; ++k) f[k] *= w[k];
+          for (int k = 0; k < P; ++k) f[k] = mul2(f[k], w[k]);
         }
-        write_part<T, V>(static_cast<T*>(q.normed) + r * q.ld_normed + c, f);
+        rows.write(q.normed, r * q.ld_normed, i, f);
       }
     }
     if (q.stats && threadIdx.x == 0) reinterpret_cast<float4*>(q.stats)[r] = make_float4(a.x, a.y, b.x, b.y);
   }
 }
 
-// The gate of the first phase kept in one number for the second: the smaller of g and 1 - g (the other is 1 minus it,
-// to a rounding), with the sign that says which.
-__device__ __forceinline__ float gate_kept(float v, bool sigmoid) {
-  if (!sigmoid) return v;
-  const float t = __expf(-fabsf(v));
-  return copysignf(__fdividef(t, 1.0f + t), v);
-}
-__device__ __forceinline__ Gate gate_again(float kept, bool sigmoid) {
-  if (!sigmoid) return {kept, 1.0f};
-  const float least = fabsf(kept), most = 1.0f - least;
-  return {signbit(kept) ? least : most, least * most};
-}
-
-template <typename T, int kElems, bool kStaged, bool kSharedGate>
+template <typename T, int kElems, bool kEdges, bool kSharedGate>
 __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(const NormParams q, const NormRing ring) {
-  constexpr int V = norm_unit<T, kStaged>(), kChunks = kElems / V;
+  typedef NormRows<T, kElems, kEdges> Rows;
+  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kElems / 2;
   extern __shared__ __align__(128) unsigned char norm_smem[];
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
   __shared__ float2 places[2][kNormMaxThreads / 32];
-  NormRows<T, kStaged> rows(q, ring, norm_smem, bars);
+  Rows rows(q, ring, norm_smem, bars);
   CtaSums sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
-  auto column = [&](int i) { return (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V; };
-  float of_after[kElems] = {}, of_before[kElems] = {}, of_gate[kSharedGate ? kElems : 1] = {};   // sums over rows
+  f32x2 of_after[kPairs], of_before[kPairs], of_gate[kSharedGate ? kPairs : 1];   // sums over rows
+#pragma unroll
+  for (int k = 0; k < kPairs; ++k) { of_after[k] = of_before[k] = both(0.0f); of_gate[kSharedGate ? k : 0] = both(0.0f); }
   for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
     const float4 st = __ldg(reinterpret_cast<const float4*>(q.stats_in) + r);
     const float poison = rows.ready();
-    float one[kElems], two[kElems];   // norm_before(y) and the gate; then the gradient of norm_after's output and the output
-    auto block_hat = [&](int c, float (&hat)[V], float (&value)[V]) {
-      rows.template read<0>(r, c, hat);
+    f32x2 one[kPairs], two[kPairs];   // norm_before(y) and the gate; then the gradient of norm_after's output and the output
+    auto block_hat = [&](int i, f32x2 (&hat)[P], f32x2 (&value)[P]) {
+      rows.template read<0>(i, hat);
+      if (q.after == kNormLayer) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) hat[k] = add2(hat[k], both(-st.x));
+      }
       if (q.after != kNormNone) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) hat[k] = (hat[k] - st.x) * st.y;
+        for (int k = 0; k < P; ++k) hat[k] = mul2(hat[k], both(st.y));
       }
-#pragma unroll
-      for (int k = 0; k < V; ++k) value[k] = hat[k];
       if (q.weight_after) {
-        float w[V];
-        read_weights<V>(q.weight_after, c, w);
+        f32x2 w[P];
+        rows.weights(q.weight_after, i, w);
 #pragma unroll
-        for (int k = 0; k < V; ++k) value[k] *= w[k];
+        for (int k = 0; k < P; ++k) value[k] = mul2(hat[k], w[k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < P; ++k) value[k] = hat[k];
       }
     };
-    auto keep_gate = [&](int i, int c) {
-      float g[V];
-      if (kSharedGate) read_weights<V>(static_cast<const float*>(q.gate), c, g);
-      else if (q.gate) rows.template read<2>(r, c, g);
+    auto keep_gate = [&](int i) {
+      f32x2 g[P];
+      if (kSharedGate) rows.weights(static_cast<const float*>(q.gate), i, g);
+      else if (q.gate) rows.template read<2>(i, g);
 #pragma unroll
-      for (int k = 0; k < V; ++k) two[i * V + k] = q.gate ? gate_kept(g[k], q.sigmoid) : 1.0f;
+      for (int k = 0; k < P; ++k) two[i * P + k] = !q.gate ? both(1.0f) : q.sigmoid ? gate_kept(g[k]) : g[k];
+    };
+    auto gate_of = [&](f32x2 kept) -> GatePair {
+      if (q.sigmoid) return gate_again(kept);
+      return {kept, both(1.0f)};
     };
     float2 m = make_float2(0.0f, 0.0f);
     if (q.d_normed) {
-      float sh = 0.0f, s = poison;
+      f32x2 sh = both(0.0f), s = both(poison);
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
-        const int c = column(i);
-        if (c >= q.dim) break;
-        float hat[V], value[V], f[V];
-        block_hat(c, hat, value);
-        keep_gate(i, c);
+        if (!rows.any(i)) break;
+        f32x2 hat[P], y[P], f[P], w[P];
+        block_hat(i, hat, y);
+        keep_gate(i);
+        if (q.gate) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) value[k] *= gate_again(two[i * V + k], q.sigmoid).open * q.scale;
-        if (q.residual) {
-          rows.template read<1>(r, c, f);
-#pragma unroll
-          for (int k = 0; k < V; ++k) value[k] = fmaf(f[k], q.residual_scale, value[k]);
+          for (int k = 0; k < P; ++k) y[k] = mul2(y[k], gate_of(two[i * P + k]).open);
         }
-        rows.template read<4>(r, c, f);
-        float w[V];
-        if (q.weight_before) read_weights<V>(q.weight_before, c, w);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const float y_hat = (value[k] - st.z) * st.w, d = q.weight_before ? f[k] * w[k] : f[k];
-          one[i * V + k] = y_hat;
-          of_before[i * V + k] = fmaf(f[k], y_hat, of_before[i * V + k]);
-          sh = fmaf(d, y_hat, sh);
-          s += d;
+        for (int k = 0; k < P; ++k) y[k] = mul2(y[k], both(q.scale));
+        if (q.residual) {
+          rows.template read<1>(i, f);
+#pragma unroll
+          for (int k = 0; k < P; ++k) y[k] = fma2(f[k], both(q.residual_scale), y[k]);
+        }
+        if (q.before == kNormLayer) {
+#pragma unroll
+          for (int k = 0; k < P; ++k) y[k] = add2(y[k], both(-st.z));
+        }
+        rows.template read<4>(i, f);   // (0 beyond the row, so that nothing there counts)
+        if (q.weight_before) rows.weights(q.weight_before, i, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          const f32x2 y_hat = mul2(y[k], both(st.w));
+          one[i * P + k] = y_hat;
+          of_before[i * P + k] = fma2(f[k], y_hat, of_before[i * P + k]);
+          if (q.weight_before) f[k] = mul2(f[k], w[k]);
+          sh = fma2(f[k], y_hat, sh);
+          s = add2(s, f[k]);
         }
       }
-      m = sums(sh, s);
+      const float2 h = unpack2(sh), t = unpack2(s);
+      m = sums(h.x + h.y, t.x + t.y);
       m.x *= inv;
       m.y = q.before == kNormLayer ? m.y * inv : poison;
     }
-    float sh = 0.0f, s = poison;
+    f32x2 sh = both(0.0f), s = both(poison);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      const int c = column(i);
-      if (c >= q.dim) break;
-      float hat[V], value[V], d[V] = {}, f[V];
-      block_hat(c, hat, value);
-      if (!q.d_normed) keep_gate(i, c);
-      if (q.d_y) rows.template read<3>(r, c, d);
-      if (q.d_normed) {
-        float w[V];
-        rows.template read<4>(r, c, f);
-        if (q.weight_before) read_weights<V>(q.weight_before, c, w);
+      if (!rows.any(i)) break;
+      f32x2 hat[P], value[P], d[P], f[P], w[P];
+      block_hat(i, hat, value);
+      if (!q.d_normed) keep_gate(i);
+      if (q.d_y) {
+        rows.template read<3>(i, d);
+      } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-          d[k] = fmaf(fmaf(-one[i * V + k], m.x, q.weight_before ? f[k] * w[k] : f[k]) - m.y, st.w, d[k]);
+        for (int k = 0; k < P; ++k) d[k] = both(0.0f);
+      }
+      if (q.d_normed) {
+        rows.template read<4>(i, f);
+        if (q.weight_before) {
+          rows.weights(q.weight_before, i, w);
+#pragma unroll
+          for (int k = 0; k < P; ++k) f[k] = mul2(f[k], w[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          f[k] = fma2(one[i * P + k], both(-m.x), f[k]);
+          if (q.before == kNormLayer) f[k] = add2(f[k], both(-m.y));
+          d[k] = fma2(f[k], both(st.w), d[k]);
+        }
       }
       if (q.d_residual) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) f[k] = d[k] * q.residual_scale;
-        write_part<T, V>(static_cast<T*>(q.d_residual) + r * q.ld_d_residual + c, f);
+        for (int k = 0; k < P; ++k) f[k] = mul2(d[k], both(q.residual_scale));
+        rows.write(q.d_residual, r * q.ld_d_residual, i, f);
       }
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const Gate gate = gate_again(two[i * V + k], q.sigmoid);
-        d[k] *= q.scale;
-        f[k] = d[k] * value[k] * gate.slope;
-        d[k] *= gate.open;
-        if (kSharedGate) of_gate[kSharedGate ? i * V + k : 0] += f[k];
+      for (int k = 0; k < P; ++k) d[k] = mul2(d[k], both(q.scale));
+      if (q.gate) {
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          const GatePair g = gate_of(two[i * P + k]);
+          f[k] = mul2(d[k], value[k]);
+          if (q.sigmoid) f[k] = mul2(f[k], g.slope);
+          d[k] = mul2(d[k], g.open);
+          if (kSharedGate) of_gate[kSharedGate ? i * P + k : 0] = add2(of_gate[kSharedGate ? i * P + k : 0], f[k]);
+        }
+        if (!kSharedGate && q.d_gate) rows.write(q.d_gate, r * q.ld_d_gate, i, f);
       }
-      if (!kSharedGate && q.d_gate) write_part<T, V>(static_cast<T*>(q.d_gate) + r * q.ld_d_gate + c, f);
       if (q.after != kNormNone) {
-        float w[V];
-        if (q.weight_after) read_weights<V>(q.weight_after, c, w);
+        if (kEdges && !rows.whole(i)) {   // what is beyond the row does not count
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-          of_after[i * V + k] = fmaf(d[k], hat[k], of_after[i * V + k]);
-          if (q.weight_after) d[k] *= w[k];
-          sh = fmaf(d[k], hat[k], sh);
-          s += d[k];
+          for (int k = 0; k < P; ++k) {
+            const float2 t = unpack2(d[k]);
+            d[k] = pack2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
+          }
+        }
+        if (q.weight_after) rows.weights(q.weight_after, i, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          of_after[i * P + k] = fma2(d[k], hat[k], of_after[i * P + k]);
+          if (q.weight_after) d[k] = mul2(d[k], w[k]);
+          sh = fma2(d[k], hat[k], sh);
+          s = add2(s, d[k]);
         }
       }
 #pragma unroll
-      for (int k = 0; k < V; ++k) { one[i * V + k] = d[k]; two[i * V + k] = hat[k]; }
+      for (int k = 0; k < P; ++k) { one[i * P + k] = d[k]; two[i * P + k] = hat[k]; }
     }
     if (q.after != kNormNone) {
-      m = sums(sh, s);
+      const float2 h = unpack2(sh), t = unpack2(s);
+      m = sums(h.x + h.y, t.x + t.y);
       m.x *= inv;
       m.y = q.after == kNormLayer ? m.y * inv : poison;
     } else {
@@ -551,13 +669,14 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
     if (!q.d_block) continue;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      const int c = column(i);
-      if (c >= q.dim) break;
-      float f[V];
+      if (!rows.any(i)) break;
+      f32x2 f[P];
 #pragma unroll
-      for (int k = 0; k < V; ++k)
-        f[k] = q.after != kNormNone ? (fmaf(-two[i * V + k], m.x, one[i * V + k]) - m.y) * st.y : one[i * V + k];
-      write_part<T, V>(static_cast<T*>(q.d_block) + r * q.ld_d_block + c, f);
+      for (int k = 0; k < P; ++k) {
+        f[k] = one[i * P + k];
+        if (q.after != kNormNone) f[k] = mul2(add2(fma2(two[i * P + k], both(-m.x), f[k]), both(-m.y)), both(st.y));
+      }
+      rows.write(q.d_block, r * q.ld_d_block, i, f);
     }
   }
   if (!q.partial) return;
@@ -565,38 +684,35 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
   float* mine = q.partial + static_cast<long long>(blockIdx.x) * q.dim;
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
-    const int c = column(i);
-    if (c >= q.dim) break;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      if (kSharedGate) mine[c + k] = of_gate[kSharedGate ? i * V + k : 0];
-      mine[plane + c + k] = of_after[i * V + k];
-      mine[2 * plane + c + k] = of_before[i * V + k];
-    }
+    if (!rows.any(i)) break;
+    if (kSharedGate) rows.write_sums(mine, i, of_gate + (kSharedGate ? i * P : 0));
+    rows.write_sums(mine + plane, i, of_after + i * P);
+    rows.write_sums(mine + 2 * plane, i, of_before + i * P);
   }
 }
 
-// Adds up the CTAs' sums: 32 columns a CTA, which its warps take in turn.
+// Adds up the CTAs' sums: 32 columns a CTA, the CTAs dealt to its warps.
 struct NormColumns { const float* partial; float* out[3]; int ctas, dim; };
-constexpr int kNormColumnWarps = 8;
+constexpr int kNormColumnWarps = 32;
 
 __global__ __launch_bounds__(32 * kNormColumnWarps) void norm_columns_kernel(NormColumns q) {
-  __shared__ float part[kNormColumnWarps][32];
-  const int plane = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+  __shared__ float part[kNormColumnWarps][33];
+  const int plane = blockIdx.y, lane = threadIdx.x & 31, c = blockIdx.x * 32 + lane, warp = threadIdx.x >> 5;
   float* out = q.out[plane];
   if (!out) return;
+  wait_for_previous_kernel();
   float s = 0.0f;
   if (c < q.dim) {
     const float* from = q.partial + static_cast<long long>(plane) * q.ctas * q.dim + c;
-    for (int i = warp; i < q.ctas; i += kNormColumnWarps) s += from[static_cast<long long>(i) * q.dim];
+#pragma unroll 8
+    for (int i = warp; i < q.ctas; i += kNormColumnWarps) s += __ldcg(from + static_cast<long long>(i) * q.dim);
   }
-  part[warp][threadIdx.x & 31] = s;
+  part[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && c < q.dim) {
+  s = part[lane][warp];   // warp w: column w of the 32
 #pragma unroll
-    for (int w = 1; w < kNormColumnWarps; ++w) s += part[w][threadIdx.x & 31];
-    out[c] = s;
-  }
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+  if (lane == 0 && blockIdx.x * 32 + warp < q.dim) out[blockIdx.x * 32 + warp] = s;
 }
 
 }  // namespace adapt
