@@ -22,7 +22,7 @@ constexpr int kNormMaxRow = 16 * kNormMaxThreads;          // elements of a row 
 constexpr int kNormMaxRowForward = 32 * kNormMaxThreads;   // and forward
 
 // Elements of a thread and threads of a CTA for a row, and CTAs of an SM.  Backward: 128 registers a thread.
-int norm_elems(int64_t dim) { return dim <= 2048 ? 8 : dim <= kNormMaxRow ? 16 : 32; }
+int norm_elems(int64_t dim) { return dim <= kNormMaxRow ? 16 : 32; }
 int norm_threads(int64_t dim) {   // (with room for up to 7 elements between a boundary and an odd row)
   const int e = norm_elems(dim);
   return std::min<int>(kNormMaxThreads, static_cast<int>((dim + (dim % 8 ? 7 : 0) + 32 * e - 1) / (32 * e)) * 32);
@@ -48,7 +48,7 @@ struct NormPlan {
     int i = 0;
     for (const auto& p : in) {
       staged = staged && alike(p);
-      ring.slot[i++] = p.first ? ring.streams++ : -1;
+      ring.place[i++] = p.first ? ring.streams++ : -1;
     }
     for (const auto& p : out) staged = staged && alike(p);
     edges = first != 0 || by != 0 || q.dim * e % 16 != 0;
@@ -57,6 +57,7 @@ struct NormPlan {
     while (period * by % 16) period *= 2;
     ring.stage_row = edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
     if (edges && q.dim + 16 / e - 1 > elems * threads) staged = false;   // the elements before a boundary take room too
+    for (int& p : ring.place) p = p < 0 ? -1 : p * ring.stage_row;
     const int stage = ring.streams * ring.stage_row;
     ring.stages = std::min(kNormMaxStages, std::max(200 * 1024 / per_sm / stage, 220 * 1024 / stage > 0 ? 1 : 0));
     staged = staged && ring.stages > 0;
@@ -141,8 +142,7 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
           if (plan.edges) rc = norm_launch<norm_row_kernel<T, N, true>>(grid, threads, plan.smem, stream, q, plan.ring);
           else rc = norm_launch<norm_row_kernel<T, N, false>>(grid, threads, plan.smem, stream, q, plan.ring);
         };
-        if (elems == 8) go(std::integral_constant<int, 8>{});
-        else if (elems == 16) go(std::integral_constant<int, 16>{});
+        if (elems == 16) go(std::integral_constant<int, 16>{});
         else go(std::integral_constant<int, 32>{});
       });
       return rc;
@@ -225,7 +225,7 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
           else rc = norm_launch<norm_row_backward_kernel<T, N, S, false>>(grid, threads, plan.smem, stream, q, plan.ring);
         };
         auto edged = [&](auto n) { plan.edges ? go(n, std::true_type{}) : go(n, std::false_type{}); };
-        if (norm_elems(dim) == 8) edged(std::integral_constant<int, 8>{}); else edged(std::integral_constant<int, 16>{});
+        edged(std::integral_constant<int, 16>{});
       });
     } else {
       with_type(dtype, [&](auto t) {

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_any_backward_kernel(NormPar
 //
 // A CTA walks over rows, a row at a time; a thread holds kElems elements of it, in chunks of 16 bytes.  The rows come
 // through a ring of stages in shared memory that bulk copies fill rows ahead, so that loads are under way while the
-// sums of a row meet.  Arithmetic is on pairs of elements: issue slots are the next bound behind HBM.
+// sums of a row meet.
 //
 // Rows that do not begin on 16-byte boundaries (an odd dim) are copied with the aligned blocks around them.  All tensors
 // have to lie alike (kEdges): then chunks are cut at those boundaries, the first and the last hold fewer
@@ -216,10 +216,16 @@ constexpr int kNormMaxStages = 4;
 struct NormRing {
   int streams, stages;       // rows of a stage, stages
   int stage_row;             // bytes of a row in a stage
-  int slot[5];               // place of block, residual, gate, d_y, d_normed in a stage, -1: none
+  int place[5];              // bytes into a stage of block, residual, gate, d_y, d_normed, -1: none
 };
 
-__device__ __forceinline__ f32x2 both(float v) { return pack2(v, v); }
+// Two elements.  (The packed fp32 instructions were tried: their operands have to lie in pairs of registers, and the
+// moves that make such pairs of constants and unpacked elements were more than what they save.)
+typedef float2 Two;
+__device__ __forceinline__ Two both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ Two sum(Two a, Two b) { return make_float2(a.x + b.x, a.y + b.y); }
+__device__ __forceinline__ Two times(Two a, Two b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ Two times_plus(Two a, Two b, Two c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
 __device__ __forceinline__ float fast_exp2(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -233,50 +239,64 @@ __device__ __forceinline__ float fast_inverse(float v) {
 constexpr float kLog2E = 1.4426950408889634f;
 
 // g(gate) of a pair: 1 / (1 + e^-v), to 2^-22 and |v| steps of the exponent's argument; 0 below 2^-126.
-__device__ __forceinline__ f32x2 gate_open(f32x2 v) {
-  const float2 e = unpack2(mul2(v, both(-kLog2E)));
-  const float2 d = unpack2(add2(pack2(fast_exp2(e.x), fast_exp2(e.y)), both(1.0f)));
-  return pack2(fast_inverse(d.x), fast_inverse(d.y));
+__device__ __forceinline__ Two gate_open(Two v) {
+  const float2 e = times(v, both(-kLog2E));
+  const float2 d = sum(make_float2(fast_exp2(e.x), fast_exp2(e.y)), both(1.0f));
+  return make_float2(fast_inverse(d.x), fast_inverse(d.y));
 }
 
 // The gate of the backward pass's first phase, kept in one number for the second: the smaller of g and 1 - g (the
 // other is 1 minus it, to a rounding), with the sign that says which.  So g (1 - g) keeps its relative precision
 // where the gate is far open or closed.
-__device__ __forceinline__ f32x2 gate_kept(f32x2 v) {
-  const float2 f = unpack2(v);
-  const float2 e = unpack2(mul2(pack2(fabsf(f.x), fabsf(f.y)), both(-kLog2E)));
-  const f32x2 t = pack2(fast_exp2(e.x), fast_exp2(e.y));
-  const float2 d = unpack2(add2(t, both(1.0f)));
-  const float2 c = unpack2(mul2(t, pack2(fast_inverse(d.x), fast_inverse(d.y))));
-  return pack2(copysignf(c.x, f.x), copysignf(c.y, f.y));
+__device__ __forceinline__ Two gate_kept(Two v) {
+  const float2 f = v;
+  const float2 e = times(make_float2(fabsf(f.x), fabsf(f.y)), both(-kLog2E));
+  const Two t = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+  const float2 d = sum(t, both(1.0f));
+  const float2 c = times(t, make_float2(fast_inverse(d.x), fast_inverse(d.y)));
+  return make_float2(copysignf(c.x, f.x), copysignf(c.y, f.y));
 }
-struct GatePair { f32x2 open, slope; };
-__device__ __forceinline__ GatePair gate_again(f32x2 kept) {
-  const float2 k = unpack2(kept);
-  const f32x2 least = pack2(fabsf(k.x), fabsf(k.y));
-  const f32x2 most = fma2(least, both(-1.0f), both(1.0f));
-  const float2 l = unpack2(least), m = unpack2(most);
-  return {pack2(signbit(k.x) ? l.x : m.x, signbit(k.y) ? l.y : m.y), mul2(least, most)};
+struct GatePair { Two open, slope; };
+__device__ __forceinline__ GatePair gate_again(Two kept) {
+  const float2 k = kept;
+  const Two least = make_float2(fabsf(k.x), fabsf(k.y));
+  const Two most = times_plus(least, both(-1.0f), both(1.0f));
+  const float2 l = least, m = most;
+  return {make_float2(signbit(k.x) ? l.x : m.x, signbit(k.y) ? l.y : m.y), times(least, most)};
 }
 
 // Sums over a CTA, in one of two sets of places in turn, so that one barrier each is enough.
 struct CtaSums {
   float2 (*places)[kNormMaxThreads / 32];
   int turn;
-  __device__ __forceinline__ float2 operator()(float a, float b) {
+  template <bool kTwo>
+  __device__ __forceinline__ float2 over_warp(float a, float b, int from) const {
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
+      if (d > from) continue;
       a += __shfl_xor_sync(~0u, a, d);
-      b += __shfl_xor_sync(~0u, b, d);
+      if (kTwo) b += __shfl_xor_sync(~0u, b, d);
     }
-    if (blockDim.x == 32) { __syncwarp(); return make_float2(a, b); }
-    if ((threadIdx.x & 31) == 0) places[turn][threadIdx.x >> 5] = make_float2(a, b);
+    return make_float2(a, b);
+  }
+  template <bool kTwo>
+  __device__ __forceinline__ float2 meet(float a, float b) {
+    float2 s = over_warp<kTwo>(a, b, 16);
+    if (blockDim.x == 32) { __syncwarp(); return s; }
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) places[turn][threadIdx.x >> 5] = s;
     __syncthreads();
-    float2 s = places[turn][0];
-    for (unsigned w = 1; w < blockDim.x / 32; ++w) { const float2 p = places[turn][w]; s.x += p.x; s.y += p.y; }
+    s = lane < static_cast<int>(blockDim.x >> 5) ? places[turn][lane] : make_float2(0.0f, 0.0f);
     turn ^= 1;
+    static_assert(kNormMaxThreads / 32 <= 16, "half a warp holds the sums of all warps");
+    s = over_warp<kTwo>(s.x, s.y, 8);
+    // (both halves of the warp have to hold the sum)
+    s.x = __shfl_sync(~0u, s.x, 0);
+    if (kTwo) s.y = __shfl_sync(~0u, s.y, 0);
     return s;
   }
+  __device__ __forceinline__ float one(float a) { return meet<false>(a, 0.0f).x; }
+  __device__ __forceinline__ float2 two(float a, float b) { return meet<true>(a, b); }
 };
 
 // The rows of a CTA in order, read ahead into the ring by its first thread, and the columns of a thread.
@@ -286,11 +306,11 @@ struct NormRows {
   const NormParams& q;
   const NormRing& ring;
   unsigned stages, bars;     // addresses
-  unsigned use;
+  unsigned stage, parity, at;   // the stage of the row at hand, the barrier's phase, this thread's place in the stage
   int skip;                  // elements between a 16-byte boundary and the rows' first element
   unsigned in;               // which of the thread's elements are elements of the row (kEdges)
   __device__ __forceinline__ NormRows(const NormParams& q_, const NormRing& r, unsigned char* smem, unsigned long long* b)
-      : q(q_), ring(r), stages(shared_address(smem)), bars(shared_address(b)), use(0), skip(0), in(~0u) {
+      : q(q_), ring(r), stages(shared_address(smem)), bars(shared_address(b)), stage(0), parity(0), at(shared_address(smem) + threadIdx.x * 16), skip(0), in(~0u) {
     if constexpr (kEdges) {
       skip = static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + blockIdx.x * q.ld_block) & 15u) / sizeof(T));
       in = 0;
@@ -321,26 +341,27 @@ struct NormRows {
     const long long ld[5] = {q.ld_block, q.ld_residual, q.ld_gate, q.ld_d_y, q.ld_d_normed};
 #pragma unroll
     for (int i = 0; i < 5; ++i)
-      if (ring.slot[i] >= 0)
+      if (ring.place[i] >= 0)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     :: "r"(stages + (s * ring.streams + ring.slot[i]) * ring.stage_row), "l"(static_cast<const T*>(from[i]) + r * ld[i] - skip),
+                     :: "r"(stages + s * ring.streams * ring.stage_row + ring.place[i]), "l"(static_cast<const T*>(from[i]) + r * ld[i] - skip),
                         "r"(bytes), "r"(bars + 8 * s) : "memory");
   }
   // Waits for the row's data; 0, or NaN where they never came.
   __device__ __forceinline__ float ready() const {
-    return barrier_wait(bars + 8 * (use % ring.stages), (use / ring.stages) & 1) ? 0.0f : __int_as_float(0x7FC00000);
+    return barrier_wait(bars + 8 * stage, parity) ? 0.0f : __int_as_float(0x7FC00000);
   }
   // Called when every thread has read what it needs of the row `r`.
   __device__ __forceinline__ void release(long long r) {
-    if (threadIdx.x == 0) fill(use % ring.stages, r + static_cast<long long>(ring.stages) * gridDim.x);
-    ++use;
+    if (threadIdx.x == 0) fill(stage, r + static_cast<long long>(ring.stages) * gridDim.x);
+    at += ring.streams * ring.stage_row;
+    if (++stage == static_cast<unsigned>(ring.stages)) { stage = 0; parity ^= 1; at = stages + threadIdx.x * 16; }
   }
   // Chunk i of stream kStream; 0 for what is not in the row.
   template <int kStream>
-  __device__ __forceinline__ void read(int i, f32x2 (&f)[P]) const {
+  __device__ __forceinline__ void read(int i, Two (&f)[P]) const {
     uint4 raw;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w)
-                 : "r"(stages + ((use % ring.stages) * ring.streams + ring.slot[kStream]) * ring.stage_row + (i * blockDim.x + threadIdx.x) * 16));
+                 : "r"(at + ring.place[kStream] + i * blockDim.x * 16));
     float v[V];
     unpack16<T>(raw, v);
     if (kEdges && !whole(i)) {
@@ -348,27 +369,27 @@ struct NormRows {
       for (int k = 0; k < V; ++k) v[k] = has(i * V + k) ? v[k] : 0.0f;
     }
 #pragma unroll
-    for (int k = 0; k < P; ++k) f[k] = pack2(v[2 * k], v[2 * k + 1]);
+    for (int k = 0; k < P; ++k) f[k] = make_float2(v[2 * k], v[2 * k + 1]);
   }
-  __device__ __forceinline__ void weights(const float* w, int i, f32x2 (&f)[P]) const {
+  __device__ __forceinline__ void weights(const float* w, int i, Two (&f)[P]) const {
     const int c = column(i);
     if constexpr (kEdges) {
 #pragma unroll
       for (int k = 0; k < P; ++k)
-        f[k] = pack2(has(i * V + 2 * k) ? __ldg(w + c + 2 * k) : 0.0f, has(i * V + 2 * k + 1) ? __ldg(w + c + 2 * k + 1) : 0.0f);
+        f[k] = make_float2(has(i * V + 2 * k) ? __ldg(w + c + 2 * k) : 0.0f, has(i * V + 2 * k + 1) ? __ldg(w + c + 2 * k + 1) : 0.0f);
     } else {
 #pragma unroll
       for (int k = 0; k < V; k += 4) {
         const float4 t = __ldg(reinterpret_cast<const float4*>(w + c + k));
-        f[k / 2] = pack2(t.x, t.y);
-        f[k / 2 + 1] = pack2(t.z, t.w);
+        f[k / 2] = make_float2(t.x, t.y);
+        f[k / 2 + 1] = make_float2(t.z, t.w);
       }
     }
   }
-  __device__ __forceinline__ void write(void* to, long long at, int i, const f32x2 (&f)[P]) const {
+  __device__ __forceinline__ void write(void* to, long long at, int i, const Two (&f)[P]) const {
     float v[V];
 #pragma unroll
-    for (int k = 0; k < P; ++k) { const float2 t = unpack2(f[k]); v[2 * k] = t.x; v[2 * k + 1] = t.y; }
+    for (int k = 0; k < P; ++k) { const float2 t = f[k]; v[2 * k] = t.x; v[2 * k + 1] = t.y; }
     T* p = static_cast<T*>(to) + at + column(i);
     if (whole(i)) {
       __stcs(reinterpret_cast<uint4*>(p), pack16<T>(v));
@@ -379,10 +400,10 @@ struct NormRows {
     }
   }
   // A column's sum over the rows.
-  __device__ __forceinline__ void write_sums(float* to, int i, const f32x2* f) const {
+  __device__ __forceinline__ void write_sums(float* to, int i, const Two* f) const {
 #pragma unroll
     for (int k = 0; k < P; ++k) {
-      const float2 t = unpack2(f[k]);
+      const float2 t = f[k];
       float* p = to + column(i) + 2 * k;
       if (has(i * V + 2 * k)) p[0] = t.x;
       if (has(i * V + 2 * k + 1)) p[1] = t.y;
@@ -391,11 +412,11 @@ struct NormRows {
 };
 
 template <int N>
-__device__ __forceinline__ float pairs_sum(const f32x2 (&v)[N]) {
-  f32x2 s = v[0];
+__device__ __forceinline__ float pairs_sum(const Two (&v)[N]) {
+  Two s = v[0];
 #pragma unroll
-  for (int k = 1; k < N; ++k) s = add2(s, v[k]);
-  const float2 t = unpack2(s);
+  for (int k = 1; k < N; ++k) s = sum(s, v[k]);
+  const float2 t = s;
   return t.x + t.y;
 }
 
@@ -410,70 +431,70 @@ __global__ __launch_bounds__(kNormMaxThreads, kElems <= 16 ? 2 : 1) void norm_ro
   CtaSums sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
   // mean and 1 / deviation; the deviation around the mean, in a second sum.  Leaves v - mean.
-  auto statistics = [&](f32x2 (&v)[kPairs], int kind) {
+  auto statistics = [&](Two (&v)[kPairs], int kind) {
     float mean = 0.0f;
     if (kind == kNormLayer) {
-      mean = sums(pairs_sum(v), 0.0f).x * inv;   // (0 beyond the row)
-      const f32x2 less = both(-mean);
+      mean = sums.one(pairs_sum(v)) * inv;   // (0 beyond the row)
+      const Two less = both(-mean);
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          v[i * P + k] = add2(v[i * P + k], less);
+          v[i * P + k] = sum(v[i * P + k], less);
           if (kEdges && !rows.whole(i)) {
-            const float2 t = unpack2(v[i * P + k]);
-            v[i * P + k] = pack2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
+            const float2 t = v[i * P + k];
+            v[i * P + k] = make_float2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
           }
         }
       }
     }
-    f32x2 s = both(0.0f);
+    Two s = both(0.0f);
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) s = fma2(v[k], v[k], s);
-    const float2 t = unpack2(s);
-    return make_float2(mean, rsqrtf(fmaf(sums(t.x + t.y, 0.0f).x, inv, q.eps)));
+    for (int k = 0; k < kPairs; ++k) s = times_plus(v[k], v[k], s);
+    const float2 t = s;
+    return make_float2(mean, rsqrtf(fmaf(sums.one(t.x + t.y), inv, q.eps)));
   };
   for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
     const float poison = rows.ready();
-    f32x2 v[kPairs];
+    Two v[kPairs];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      f32x2 f[P];
+      Two f[P];
 #pragma unroll
       for (int k = 0; k < P; ++k) f[k] = both(0.0f);
       if (rows.any(i)) rows.template read<0>(i, f);
 #pragma unroll
       for (int k = 0; k < P; ++k) v[i * P + k] = f[k];
     }
-    v[0] = add2(v[0], both(poison));
+    v[0] = sum(v[0], both(poison));
     float2 a = make_float2(0.0f, 1.0f), b = a;
     if (q.after != kNormNone) a = statistics(v, q.after);
-    const f32x2 factor = both(a.y);
+    const Two factor = both(a.y);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
-      f32x2 g[P];
+      Two g[P];
       if (q.after != kNormNone) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], factor);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], factor);
       }
       if (q.weight_after) {
         rows.weights(q.weight_after, i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], g[k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], g[k]);
       }
       if (q.gate) {
         if (q.shared) rows.weights(static_cast<const float*>(q.gate), i, g); else rows.template read<2>(i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], q.sigmoid ? gate_open(g[k]) : g[k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], q.sigmoid ? gate_open(g[k]) : g[k]);
       }
 #pragma unroll
-      for (int k = 0; k < P; ++k) v[i * P + k] = mul2(v[i * P + k], both(q.scale));
+      for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], both(q.scale));
       if (q.residual) {
         rows.template read<1>(i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = fma2(g[k], both(q.residual_scale), v[i * P + k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times_plus(g[k], both(q.residual_scale), v[i * P + k]);
       }
       if (q.y) {
 #pragma unroll
@@ -484,17 +505,17 @@ __global__ __launch_bounds__(kNormMaxThreads, kElems <= 16 ? 2 : 1) void norm_ro
     if (q.before != kNormNone) b = statistics(v, q.before); else __syncthreads();
     rows.release(r);
     if (q.normed) {
-      const f32x2 by = both(b.y);
+      const Two by = both(b.y);
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
-        f32x2 f[P], w[P];
+        Two f[P], w[P];
 #pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = mul2(v[i * P + k], by);
+        for (int k = 0; k < P; ++k) f[k] = times(v[i * P + k], by);
         if (q.weight_before) {
           rows.weights(q.weight_before, i, w);
 #pragma unroll
-          for (int k = 0; k < P; ++k) f[k] = mul2(f[k], w[k]);
+          for (int k = 0; k < P; ++k) f[k] = times(f[k], w[k]);
         }
         rows.write(q.normed, r * q.ld_normed, i, f);
       }
@@ -513,90 +534,93 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
   Rows rows(q, ring, norm_smem, bars);
   CtaSums sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
-  f32x2 of_after[kPairs], of_before[kPairs], of_gate[kSharedGate ? kPairs : 1];   // sums over rows
+  Two of_after[kPairs], of_before[kPairs], of_gate[kSharedGate ? kPairs : 1];   // sums over rows
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) { of_after[k] = of_before[k] = both(0.0f); of_gate[kSharedGate ? k : 0] = both(0.0f); }
+  const float4* statistics = reinterpret_cast<const float4*>(q.stats_in);
+  float4 next = blockIdx.x < static_cast<unsigned>(q.rows) ? __ldg(statistics + blockIdx.x) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
-    const float4 st = __ldg(reinterpret_cast<const float4*>(q.stats_in) + r);
+    const float4 st = next;
+    if (r + gridDim.x < q.rows) next = __ldg(statistics + r + gridDim.x);
     const float poison = rows.ready();
-    f32x2 one[kPairs], two[kPairs];   // norm_before(y) and the gate; then the gradient of norm_after's output and the output
-    auto block_hat = [&](int i, f32x2 (&hat)[P], f32x2 (&value)[P]) {
+    Two one[kPairs], two[kPairs];   // norm_before(y) and the gate; then the gradient of norm_after's output and the output
+    auto block_hat = [&](int i, Two (&hat)[P], Two (&value)[P]) {
       rows.template read<0>(i, hat);
       if (q.after == kNormLayer) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) hat[k] = add2(hat[k], both(-st.x));
+        for (int k = 0; k < P; ++k) hat[k] = sum(hat[k], both(-st.x));
       }
       if (q.after != kNormNone) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) hat[k] = mul2(hat[k], both(st.y));
+        for (int k = 0; k < P; ++k) hat[k] = times(hat[k], both(st.y));
       }
       if (q.weight_after) {
-        f32x2 w[P];
+        Two w[P];
         rows.weights(q.weight_after, i, w);
 #pragma unroll
-        for (int k = 0; k < P; ++k) value[k] = mul2(hat[k], w[k]);
+        for (int k = 0; k < P; ++k) value[k] = times(hat[k], w[k]);
       } else {
 #pragma unroll
         for (int k = 0; k < P; ++k) value[k] = hat[k];
       }
     };
     auto keep_gate = [&](int i) {
-      f32x2 g[P];
+      Two g[P];
       if (kSharedGate) rows.weights(static_cast<const float*>(q.gate), i, g);
       else if (q.gate) rows.template read<2>(i, g);
 #pragma unroll
       for (int k = 0; k < P; ++k) two[i * P + k] = !q.gate ? both(1.0f) : q.sigmoid ? gate_kept(g[k]) : g[k];
     };
-    auto gate_of = [&](f32x2 kept) -> GatePair {
+    auto gate_of = [&](Two kept) -> GatePair {
       if (q.sigmoid) return gate_again(kept);
       return {kept, both(1.0f)};
     };
     float2 m = make_float2(0.0f, 0.0f);
     if (q.d_normed) {
-      f32x2 sh = both(0.0f), s = both(poison);
+      Two sh = both(0.0f), s = both(poison);
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
-        f32x2 hat[P], y[P], f[P], w[P];
+        Two hat[P], y[P], f[P], w[P];
         block_hat(i, hat, y);
         keep_gate(i);
         if (q.gate) {
 #pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = mul2(y[k], gate_of(two[i * P + k]).open);
+          for (int k = 0; k < P; ++k) y[k] = times(y[k], gate_of(two[i * P + k]).open);
         }
 #pragma unroll
-        for (int k = 0; k < P; ++k) y[k] = mul2(y[k], both(q.scale));
+        for (int k = 0; k < P; ++k) y[k] = times(y[k], both(q.scale));
         if (q.residual) {
           rows.template read<1>(i, f);
 #pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = fma2(f[k], both(q.residual_scale), y[k]);
+          for (int k = 0; k < P; ++k) y[k] = times_plus(f[k], both(q.residual_scale), y[k]);
         }
         if (q.before == kNormLayer) {
 #pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = add2(y[k], both(-st.z));
+          for (int k = 0; k < P; ++k) y[k] = sum(y[k], both(-st.z));
         }
         rows.template read<4>(i, f);   // (0 beyond the row, so that nothing there counts)
         if (q.weight_before) rows.weights(q.weight_before, i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          const f32x2 y_hat = mul2(y[k], both(st.w));
+          const Two y_hat = times(y[k], both(st.w));
           one[i * P + k] = y_hat;
-          of_before[i * P + k] = fma2(f[k], y_hat, of_before[i * P + k]);
-          if (q.weight_before) f[k] = mul2(f[k], w[k]);
-          sh = fma2(f[k], y_hat, sh);
-          s = add2(s, f[k]);
+          of_before[i * P + k] = times_plus(f[k], y_hat, of_before[i * P + k]);
+          if (q.weight_before) f[k] = times(f[k], w[k]);
+          sh = times_plus(f[k], y_hat, sh);
+          s = sum(s, f[k]);
         }
       }
-      const float2 h = unpack2(sh), t = unpack2(s);
-      m = sums(h.x + h.y, t.x + t.y);
+      const float2 h = sh, t = s;
+      m = sums.two(h.x + h.y, t.x + t.y);
       m.x *= inv;
       m.y = q.before == kNormLayer ? m.y * inv : poison;
     }
-    f32x2 sh = both(0.0f), s = both(poison);
+    Two sh = both(0.0f), s = both(poison);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
-      f32x2 hat[P], value[P], d[P], f[P], w[P];
+      Two hat[P], value[P], d[P], f[P], w[P];
       block_hat(i, hat, value);
       if (!q.d_normed) keep_gate(i);
       if (q.d_y) {
@@ -610,30 +634,30 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
         if (q.weight_before) {
           rows.weights(q.weight_before, i, w);
 #pragma unroll
-          for (int k = 0; k < P; ++k) f[k] = mul2(f[k], w[k]);
+          for (int k = 0; k < P; ++k) f[k] = times(f[k], w[k]);
         }
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          f[k] = fma2(one[i * P + k], both(-m.x), f[k]);
-          if (q.before == kNormLayer) f[k] = add2(f[k], both(-m.y));
-          d[k] = fma2(f[k], both(st.w), d[k]);
+          f[k] = times_plus(one[i * P + k], both(-m.x), f[k]);
+          if (q.before == kNormLayer) f[k] = sum(f[k], both(-m.y));
+          d[k] = times_plus(f[k], both(st.w), d[k]);
         }
       }
       if (q.d_residual) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = mul2(d[k], both(q.residual_scale));
+        for (int k = 0; k < P; ++k) f[k] = times(d[k], both(q.residual_scale));
         rows.write(q.d_residual, r * q.ld_d_residual, i, f);
       }
 #pragma unroll
-      for (int k = 0; k < P; ++k) d[k] = mul2(d[k], both(q.scale));
+      for (int k = 0; k < P; ++k) d[k] = times(d[k], both(q.scale));
       if (q.gate) {
 #pragma unroll
         for (int k = 0; k < P; ++k) {
           const GatePair g = gate_of(two[i * P + k]);
-          f[k] = mul2(d[k], value[k]);
-          if (q.sigmoid) f[k] = mul2(f[k], g.slope);
-          d[k] = mul2(d[k], g.open);
-          if (kSharedGate) of_gate[kSharedGate ? i * P + k : 0] = add2(of_gate[kSharedGate ? i * P + k : 0], f[k]);
+          f[k] = times(d[k], value[k]);
+          if (q.sigmoid) f[k] = times(f[k], g.slope);
+          d[k] = times(d[k], g.open);
+          if (kSharedGate) of_gate[kSharedGate ? i * P + k : 0] = sum(of_gate[kSharedGate ? i * P + k : 0], f[k]);
         }
         if (!kSharedGate && q.d_gate) rows.write(q.d_gate, r * q.ld_d_gate, i, f);
       }
@@ -641,25 +665,25 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
         if (kEdges && !rows.whole(i)) {   // what is beyond the row does not count
 #pragma unroll
           for (int k = 0; k < P; ++k) {
-            const float2 t = unpack2(d[k]);
-            d[k] = pack2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
+            const float2 t = d[k];
+            d[k] = make_float2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
           }
         }
         if (q.weight_after) rows.weights(q.weight_after, i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          of_after[i * P + k] = fma2(d[k], hat[k], of_after[i * P + k]);
-          if (q.weight_after) d[k] = mul2(d[k], w[k]);
-          sh = fma2(d[k], hat[k], sh);
-          s = add2(s, d[k]);
+          of_after[i * P + k] = times_plus(d[k], hat[k], of_after[i * P + k]);
+          if (q.weight_after) d[k] = times(d[k], w[k]);
+          sh = times_plus(d[k], hat[k], sh);
+          s = sum(s, d[k]);
         }
       }
 #pragma unroll
       for (int k = 0; k < P; ++k) { one[i * P + k] = d[k]; two[i * P + k] = hat[k]; }
     }
     if (q.after != kNormNone) {
-      const float2 h = unpack2(sh), t = unpack2(s);
-      m = sums(h.x + h.y, t.x + t.y);
+      const float2 h = sh, t = s;
+      m = sums.two(h.x + h.y, t.x + t.y);
       m.x *= inv;
       m.y = q.after == kNormLayer ? m.y * inv : poison;
     } else {
@@ -670,11 +694,11 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
-      f32x2 f[P];
+      Two f[P];
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         f[k] = one[i * P + k];
-        if (q.after != kNormNone) f[k] = mul2(add2(fma2(two[i * P + k], both(-m.x), f[k]), both(-m.y)), both(st.y));
+        if (q.after != kNormNone) f[k] = times(sum(times_plus(two[i * P + k], both(-m.x), f[k]), both(-m.y)), both(st.y));
       }
       rows.write(q.d_block, r * q.ld_d_block, i, f);
     }

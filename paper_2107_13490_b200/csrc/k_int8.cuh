@@ -224,7 +224,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kWideThreads, 1) void int
     bool ok = true;
     for (int i = pair; i < tiles && ok; i += pairs, ++turn) {
       const unsigned buffer = turn & 1;
-      ok = barrier_wait(open + 8 * buffer, ((turn >> 1) & 1) ^ 1);
+      ok = barrier_wait<true>(open + 8 * buffer, ((turn >> 1) & 1) ^ 1);
       if (!ok) break;
       tensor_fence_after();
       for (int b = 0; b < blocks; ++b, ++use) {
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
                    :: "r"(peer_address(received + in_slot * slot, to_rank)), "r"(aligned + out_slot * slot), "r"(slot),
                       "r"(peer_address(exchange, to_rank)) : "memory");
     }
-    bool good = ok && barrier_wait(exchange, 0);
+    bool good = ok && barrier_wait<true>(exchange, 0);
     for (int c = 0; c < share && first + c < count; c += 4) {
       int sum[4];
       tensor_read4(mine + first + c, sum);

@@ -28,11 +28,18 @@ __device__ __forceinline__ void barrier_expect_bytes(unsigned bar, unsigned byte
 __device__ __forceinline__ void barrier_arrive_cluster(unsigned bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
+// Waits for a phase that this CTA's threads and copies into it complete; kCluster: threads of other CTAs too (an
+// acquire of that scope also drops what the L1 cache holds).
+template <bool kCluster = false>
 __device__ __forceinline__ bool barrier_wait(unsigned bar, unsigned parity) {
   for (unsigned i = 0; i < kWaitTries; ++i) {
     unsigned done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                 "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if constexpr (kCluster)
+      asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                   "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+      asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                   "selp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     if (done) return true;
   }
   return false;
