@@ -18,16 +18,13 @@ static_assert(ADAPT_NORM_NONE == kNormNone && ADAPT_NORM_RMS == kNormRms && ADAP
 namespace {
 
 constexpr int kSms = 148;   // of a B200
-constexpr int kNormMaxRow = 16 * kNormMaxThreads;          // elements of a row in a CTA's registers, backward
-constexpr int kNormMaxRowForward = 32 * kNormMaxThreads;   // and forward
+constexpr int kNormMaxRow = kNormElems * kNormBackwardThreads;   // elements of a row in a CTA's registers, backward
+constexpr int kNormMaxRowForward = kNormElems * kNormMaxThreads;   // and forward
 
-// Elements of a thread and threads of a CTA for a row, and CTAs of an SM.  Backward: 128 registers a thread.
-int norm_elems(int64_t dim) { return dim <= kNormMaxRow ? 16 : 32; }
-int norm_threads(int64_t dim) {   // (with room for up to 7 elements between a boundary and an odd row)
-  const int e = norm_elems(dim);
-  return std::min<int>(kNormMaxThreads, static_cast<int>((dim + (dim % 8 ? 7 : 0) + 32 * e - 1) / (32 * e)) * 32);
-}
-int norm_per_sm(int64_t dim) { return std::max(1, std::min(8, kNormMaxThreads / norm_threads(dim))); }
+// Threads of a CTA for a row (with room for up to 7 elements between a boundary and an odd row), and CTAs of an SM:
+// 128 registers a thread backward, 64 forward.
+int norm_threads(int64_t dim) { return static_cast<int>((dim + (dim % 8 ? 7 : 0) + 32 * kNormElems - 1) / (32 * kNormElems)) * 32; }
+int norm_per_sm(int64_t dim) { return std::max(1, std::min(8, 512 / norm_threads(dim))); }
 
 // CTAs of a backward pass, each with sums of its own over its rows.
 int64_t norm_ctas(int64_t rows, int64_t dim) { return std::min<int64_t>(rows, kSms * norm_per_sm(dim)); }
@@ -39,7 +36,7 @@ struct NormPlan {
   NormRing ring = {};
   int smem = 0, period = 1;   // rows whose numbers differ by a multiple of the period lie alike
   bool staged = true, edges = false;
-  NormPlan(const NormParams& q, int e, int per_sm, int elems, int threads, std::initializer_list<std::pair<const void*, long long>> in,
+  NormPlan(const NormParams& q, int e, int per_sm, int threads, std::initializer_list<std::pair<const void*, long long>> in,
            std::initializer_list<std::pair<const void*, long long>> out) {
     auto phase = [](const void* p) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 15u); };
     auto step = [&](long long ld) { return q.rows == 1 ? 0u : static_cast<unsigned>(ld * e & 15); };
@@ -56,7 +53,7 @@ struct NormPlan {
       edges = edges || misaligned(p, 16);
     while (period * by % 16) period *= 2;
     ring.stage_row = edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
-    if (edges && q.dim + 16 / e - 1 > elems * threads) staged = false;   // the elements before a boundary take room too
+    if (edges && q.dim + 16 / e - 1 > kNormElems * threads) staged = false;   // the elements before a boundary take room too
     for (int& p : ring.place) p = p < 0 ? -1 : p * ring.stage_row;
     const int stage = ring.streams * ring.stage_row;
     ring.stages = std::min(kNormMaxStages, std::max(200 * 1024 / per_sm / stage, 220 * 1024 / stage > 0 ? 1 : 0));
@@ -64,6 +61,23 @@ struct NormPlan {
     smem = ring.stages * stage;
   }
 };
+
+// Calls f with what a kernel is made for.
+template <typename F>
+void with_form(const NormParams& q, bool edges, F f) {
+  auto gates = [&](auto e, auto a, auto b) {
+    if (!q.gate) f(e, a, b, std::integral_constant<int, kGateNone>{});
+    else if (q.shared) f(e, a, b, std::integral_constant<int, kGateForAll>{});
+    else if (q.sigmoid) f(e, a, b, std::integral_constant<int, kGateEachSigmoid>{});
+    else f(e, a, b, std::integral_constant<int, kGateEach>{});
+  };
+  auto norms = [&](auto e) {
+    if (q.after == kNormNone) gates(e, std::false_type{}, std::true_type{});
+    else if (q.before == kNormNone) gates(e, std::true_type{}, std::false_type{});
+    else gates(e, std::true_type{}, std::true_type{});
+  };
+  if (edges) norms(std::true_type{}); else norms(std::false_type{});
+}
 
 // Launches a kernel that may need more shared memory than a kernel has by itself.
 template <auto kKernel>
@@ -129,21 +143,19 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   int rc = ADAPT_OK;
   LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM, stream);
-  if (dim <= kNormMaxRowForward) {
-    const int elems = norm_elems(dim), threads = norm_threads(dim), per_sm = std::max(1, std::min(16, (elems <= 16 ? 1024 : 512) / threads));
-    const NormPlan plan(q, e, per_sm, elems, threads, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
+  const bool known = q.before == kNormNone ? !normed : normed != nullptr;   // (a norm whose output is not wanted: its statistics may be)
+  if (dim <= kNormMaxRowForward && norm_threads(dim) <= kNormMaxThreads && known && (q.after != kNormNone || q.before != kNormNone)) {
+    const int threads = norm_threads(dim), per_sm = std::max(1, std::min(16, 1024 / threads));
+    const NormPlan plan(q, e, per_sm, threads, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
                         {nullptr, 0}, {nullptr, 0}}, {{y, q.ld_y}, {normed, q.ld_normed}});
     if (plan.staged) {
       const unsigned grid = norm_grid(std::min<int64_t>(rows, kSms * per_sm), plan.period);
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        auto go = [&](auto n) {
-          constexpr int N = decltype(n)::value;
-          if (plan.edges) rc = norm_launch<norm_row_kernel<T, N, true>>(grid, threads, plan.smem, stream, q, plan.ring);
-          else rc = norm_launch<norm_row_kernel<T, N, false>>(grid, threads, plan.smem, stream, q, plan.ring);
-        };
-        if (elems == 16) go(std::integral_constant<int, 16>{});
-        else go(std::integral_constant<int, 32>{});
+        with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
+          rc = norm_launch<norm_row_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
+              grid, threads, plan.smem, stream, q, plan.ring);
+        });
       });
       return rc;
     }
@@ -210,22 +222,19 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   {
     LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM_BACKWARD, stream);
     const int threads = norm_threads(dim);
-    const NormPlan plan(q, e, norm_per_sm(dim), norm_elems(dim), threads, {{block, q.ld_block}, {residual, q.ld_residual},
+    const NormPlan plan(q, e, norm_per_sm(dim), threads, {{block, q.ld_block}, {residual, q.ld_residual},
                         {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
                         {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
-    if (plan.staged && dim <= kNormMaxRow) {
+    if (plan.staged && threads <= kNormBackwardThreads && (q.after != kNormNone || d_normed)) {
       const unsigned grid = norm_grid(ctas, plan.period);
       sum.ctas = static_cast<int>(grid);
+      if (!d_normed) q.before = kNormNone;   // (its gradient is not given)
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
-        auto go = [&](auto n, auto s) {
-          constexpr int N = decltype(n)::value;
-          constexpr bool S = decltype(s)::value;
-          if (q.shared) rc = norm_launch<norm_row_backward_kernel<T, N, S, true>>(grid, threads, plan.smem, stream, q, plan.ring);
-          else rc = norm_launch<norm_row_backward_kernel<T, N, S, false>>(grid, threads, plan.smem, stream, q, plan.ring);
-        };
-        auto edged = [&](auto n) { plan.edges ? go(n, std::true_type{}) : go(n, std::false_type{}); };
-        edged(std::integral_constant<int, 16>{});
+        with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
+          rc = norm_launch<norm_row_backward_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
+              grid, threads, plan.smem, stream, q, plan.ring);
+        });
       });
     } else {
       with_type(dtype, [&](auto t) {

@@ -210,7 +210,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_any_backward_kernel(NormPar
 // have to lie alike (kEdges): then chunks are cut at those boundaries, the first and the last hold fewer
 // elements, and a CTA takes rows that lie alike too, so that a thread keeps its columns.
 
-constexpr int kNormMaxThreads = 512;
+constexpr int kNormElems = 16;             // elements of a thread
+constexpr int kNormMaxThreads = 1024;      // of a CTA, forward
+constexpr int kNormBackwardThreads = 512;  // and backward
 constexpr int kNormMaxStages = 4;
 
 struct NormRing {
@@ -266,14 +268,14 @@ __device__ __forceinline__ GatePair gate_again(Two kept) {
 }
 
 // Sums over a CTA, in one of two sets of places in turn, so that one barrier each is enough.
+template <int kThreads>
 struct CtaSums {
-  float2 (*places)[kNormMaxThreads / 32];
+  float2 (*places)[kThreads / 32];
   int turn;
   template <bool kTwo>
-  __device__ __forceinline__ float2 over_warp(float a, float b, int from) const {
+  __device__ __forceinline__ float2 over_warp(float a, float b) const {
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
-      if (d > from) continue;
       a += __shfl_xor_sync(~0u, a, d);
       if (kTwo) b += __shfl_xor_sync(~0u, b, d);
     }
@@ -281,19 +283,14 @@ struct CtaSums {
   }
   template <bool kTwo>
   __device__ __forceinline__ float2 meet(float a, float b) {
-    float2 s = over_warp<kTwo>(a, b, 16);
+    float2 s = over_warp<kTwo>(a, b);
     if (blockDim.x == 32) { __syncwarp(); return s; }
     const int lane = threadIdx.x & 31;
     if (lane == 0) places[turn][threadIdx.x >> 5] = s;
     __syncthreads();
     s = lane < static_cast<int>(blockDim.x >> 5) ? places[turn][lane] : make_float2(0.0f, 0.0f);
     turn ^= 1;
-    static_assert(kNormMaxThreads / 32 <= 16, "half a warp holds the sums of all warps");
-    s = over_warp<kTwo>(s.x, s.y, 8);
-    // (both halves of the warp have to hold the sum)
-    s.x = __shfl_sync(~0u, s.x, 0);
-    if (kTwo) s.y = __shfl_sync(~0u, s.y, 0);
-    return s;
+    return over_warp<kTwo>(s.x, s.y);
   }
   __device__ __forceinline__ float one(float a) { return meet<false>(a, 0.0f).x; }
   __device__ __forceinline__ float2 two(float a, float b) { return meet<true>(a, b); }
@@ -331,6 +328,18 @@ struct NormRows {
   // Whether chunk i has an element of the row, and whether all of its elements are.
   __device__ __forceinline__ bool any(int i) const { return column(i) < q.dim; }
   __device__ __forceinline__ bool whole(int i) const { return !kEdges || ((in >> (i * V)) & ((1u << V) - 1)) == (1u << V) - 1; }
+  __device__ __forceinline__ bool inside(int j) const { return kEdges ? (in >> j & 1) : any(j / V); }
+  // Sets chunk i of a thread's elements, or a chunk by itself, to 0 beyond the row.
+  template <int N>
+  __device__ __forceinline__ void blank(int i, Two (&v)[N]) const {
+    if (whole(i)) return;
+    const int first = N == P ? 0 : i * P;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      if (!has(i * V + 2 * k)) v[first + k].x = 0.0f;
+      if (!has(i * V + 2 * k + 1)) v[first + k].y = 0.0f;
+    }
+  }
   __device__ __forceinline__ bool has(int j) const { return !kEdges || (in >> j & 1); }
 
   __device__ __forceinline__ void fill(int s, long long r) const {
@@ -371,8 +380,14 @@ struct NormRows {
 #pragma unroll
     for (int k = 0; k < P; ++k) f[k] = make_float2(v[2 * k], v[2 * k + 1]);
   }
+  // (no weights: 1)
   __device__ __forceinline__ void weights(const float* w, int i, Two (&f)[P]) const {
     const int c = column(i);
+    if (!w) {
+#pragma unroll
+      for (int k = 0; k < P; ++k) f[k] = both(1.0f);
+      return;
+    }
     if constexpr (kEdges) {
 #pragma unroll
       for (int k = 0; k < P; ++k)
@@ -411,49 +426,37 @@ struct NormRows {
   }
 };
 
-template <int N>
-__device__ __forceinline__ float pairs_sum(const Two (&v)[N]) {
-  Two s = v[0];
-#pragma unroll
-  for (int k = 1; k < N; ++k) s = sum(s, v[k]);
-  const float2 t = s;
-  return t.x + t.y;
-}
+// What a kernel is made for, so that nothing is decided element by element.
+constexpr int kGateNone = 0, kGateEach = 1, kGateEachSigmoid = 2, kGateForAll = 3;
 
-template <typename T, int kElems, bool kEdges>
-__global__ __launch_bounds__(kNormMaxThreads, kElems <= 16 ? 2 : 1) void norm_row_kernel(const NormParams q, const NormRing ring) {
-  typedef NormRows<T, kElems, kEdges> Rows;
-  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kElems / 2;
+template <typename T, bool kEdges, bool kAfter, bool kBefore, int kGate>
+__global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const NormParams q, const NormRing ring) {
+  typedef NormRows<T, kNormElems, kEdges> Rows;
+  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kNormElems / 2;
   extern __shared__ __align__(128) unsigned char norm_smem[];
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
   __shared__ float2 places[2][kNormMaxThreads / 32];
   Rows rows(q, ring, norm_smem, bars);
-  CtaSums sums{places, 0};
+  CtaSums<kNormMaxThreads> sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
-  // mean and 1 / deviation; the deviation around the mean, in a second sum.  Leaves v - mean.
-  auto statistics = [&](Two (&v)[kPairs], int kind) {
-    float mean = 0.0f;
+  // mean and 1 / deviation; the deviation around the mean, in a second sum
+  auto statistics = [&](const Two (&v)[kPairs], int kind) {
+    float mean = 0.0f, s = 0.0f;
     if (kind == kNormLayer) {
-      mean = sums.one(pairs_sum(v)) * inv;   // (0 beyond the row)
-      const Two less = both(-mean);
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i) {
-        if (!rows.any(i)) break;
+      for (int k = 0; k < kPairs; ++k) s += v[k].x + v[k].y;   // (0 beyond the row)
+      mean = sums.one(s) * inv;
+      s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-          v[i * P + k] = sum(v[i * P + k], less);
-          if (kEdges && !rows.whole(i)) {
-            const float2 t = v[i * P + k];
-            v[i * P + k] = make_float2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
-          }
-        }
+      for (int j = 0; j < kNormElems; ++j) {
+        const float d = (j & 1 ? v[j / 2].y : v[j / 2].x) - mean;
+        if (rows.inside(j)) s = fmaf(d, d, s);
       }
-    }
-    Two s = both(0.0f);
+    } else {
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) s = times_plus(v[k], v[k], s);
-    const float2 t = s;
-    return make_float2(mean, rsqrtf(fmaf(sums.one(t.x + t.y), inv, q.eps)));
+      for (int k = 0; k < kPairs; ++k) { s = fmaf(v[k].x, v[k].x, s); s = fmaf(v[k].y, v[k].y, s); }
+    }
+    return make_float2(mean, rsqrtf(fmaf(sums.one(s), inv, q.eps)));
   };
   for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
     const float poison = rows.ready();
@@ -467,56 +470,50 @@ __global__ __launch_bounds__(kNormMaxThreads, kElems <= 16 ? 2 : 1) void norm_ro
 #pragma unroll
       for (int k = 0; k < P; ++k) v[i * P + k] = f[k];
     }
-    v[0] = sum(v[0], both(poison));
+    v[0].x += poison;
     float2 a = make_float2(0.0f, 1.0f), b = a;
-    if (q.after != kNormNone) a = statistics(v, q.after);
-    const Two factor = both(a.y);
+    if (kAfter) a = statistics(v, q.after);
+    const Two r_a = both(a.y), mean_a = both(-a.x * a.y), scale = both(q.scale), residual_scale = both(q.residual_scale);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
       Two g[P];
-      if (q.after != kNormNone) {
-#pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], factor);
-      }
-      if (q.weight_after) {
+      if (kAfter) {
         rows.weights(q.weight_after, i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], g[k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times(times_plus(v[i * P + k], r_a, mean_a), g[k]);
       }
-      if (q.gate) {
-        if (q.shared) rows.weights(static_cast<const float*>(q.gate), i, g); else rows.template read<2>(i, g);
+      if (kGate == kGateForAll) rows.weights(static_cast<const float*>(q.gate), i, g);
+      else if (kGate != kGateNone) rows.template read<2>(i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], q.sigmoid ? gate_open(g[k]) : g[k]);
+      for (int k = 0; k < P; ++k) {
+        if (kGate == kGateEachSigmoid || (kGate == kGateForAll && q.sigmoid)) g[k] = gate_open(g[k]);
+        if (kGate != kGateNone) v[i * P + k] = times(v[i * P + k], g[k]);
+        v[i * P + k] = times(v[i * P + k], scale);
       }
-#pragma unroll
-      for (int k = 0; k < P; ++k) v[i * P + k] = times(v[i * P + k], both(q.scale));
       if (q.residual) {
         rows.template read<1>(i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = times_plus(g[k], both(q.residual_scale), v[i * P + k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times_plus(g[k], residual_scale, v[i * P + k]);
       }
+      if (kEdges) rows.blank(i, v);
       if (q.y) {
 #pragma unroll
         for (int k = 0; k < P; ++k) g[k] = v[i * P + k];
         rows.write(q.y, r * q.ld_y, i, g);
       }
     }
-    if (q.before != kNormNone) b = statistics(v, q.before); else __syncthreads();
+    if (kBefore) b = statistics(v, q.before); else __syncthreads();
     rows.release(r);
-    if (q.normed) {
-      const Two by = both(b.y);
+    if (kBefore) {
+      const Two r_b = both(b.y), mean_b = both(-b.x * b.y);
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
         Two f[P], w[P];
+        rows.weights(q.weight_before, i, w);
 #pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = times(v[i * P + k], by);
-        if (q.weight_before) {
-          rows.weights(q.weight_before, i, w);
-#pragma unroll
-          for (int k = 0; k < P; ++k) f[k] = times(f[k], w[k]);
-        }
+        for (int k = 0; k < P; ++k) f[k] = times(times_plus(v[i * P + k], r_b, mean_b), w[k]);
         rows.write(q.normed, r * q.ld_normed, i, f);
       }
     }
@@ -524,166 +521,145 @@ __global__ __launch_bounds__(kNormMaxThreads, kElems <= 16 ? 2 : 1) void norm_ro
   }
 }
 
-template <typename T, int kElems, bool kEdges, bool kSharedGate>
-__global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(const NormParams q, const NormRing ring) {
-  typedef NormRows<T, kElems, kEdges> Rows;
-  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kElems / 2;
+template <typename T, bool kEdges, bool kAfter, bool kBefore, int kGate>
+__global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_kernel(const NormParams q, const NormRing ring) {
+  typedef NormRows<T, kNormElems, kEdges> Rows;
+  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kNormElems / 2;
+  constexpr bool kForAll = kGate == kGateForAll;
   extern __shared__ __align__(128) unsigned char norm_smem[];
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
-  __shared__ float2 places[2][kNormMaxThreads / 32];
+  __shared__ float2 places[2][kNormBackwardThreads / 32];
   Rows rows(q, ring, norm_smem, bars);
-  CtaSums sums{places, 0};
+  CtaSums<kNormBackwardThreads> sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
-  Two of_after[kPairs], of_before[kPairs], of_gate[kSharedGate ? kPairs : 1];   // sums over rows
+  const Two scale = both(q.scale), residual_scale = both(q.residual_scale);
+  Two of_after[kAfter ? kPairs : 1], of_before[kBefore ? kPairs : 1], of_gate[kForAll ? kPairs : 1];   // sums over rows
 #pragma unroll
-  for (int k = 0; k < kPairs; ++k) { of_after[k] = of_before[k] = both(0.0f); of_gate[kSharedGate ? k : 0] = both(0.0f); }
+  for (int k = 0; k < kPairs; ++k) of_after[kAfter ? k : 0] = of_before[kBefore ? k : 0] = of_gate[kForAll ? k : 0] = both(0.0f);
   const float4* statistics = reinterpret_cast<const float4*>(q.stats_in);
   float4 next = blockIdx.x < static_cast<unsigned>(q.rows) ? __ldg(statistics + blockIdx.x) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
     const float4 st = next;
     if (r + gridDim.x < q.rows) next = __ldg(statistics + r + gridDim.x);
     const float poison = rows.ready();
-    Two one[kPairs], two[kPairs];   // norm_before(y) and the gate; then the gradient of norm_after's output and the output
+    const Two r_a = both(st.y), mean_a = both(-st.x * st.y), r_b = both(st.w), mean_b = both(-st.z * st.w);
+    // norm_before(y) and the gate; then the gradient of norm_after's output, and that output
+    Two one[kPairs], two[kPairs];
     auto block_hat = [&](int i, Two (&hat)[P], Two (&value)[P]) {
       rows.template read<0>(i, hat);
-      if (q.after == kNormLayer) {
-#pragma unroll
-        for (int k = 0; k < P; ++k) hat[k] = sum(hat[k], both(-st.x));
-      }
-      if (q.after != kNormNone) {
-#pragma unroll
-        for (int k = 0; k < P; ++k) hat[k] = times(hat[k], both(st.y));
-      }
-      if (q.weight_after) {
+      if (kAfter) {
         Two w[P];
         rows.weights(q.weight_after, i, w);
 #pragma unroll
-        for (int k = 0; k < P; ++k) value[k] = times(hat[k], w[k]);
+        for (int k = 0; k < P; ++k) {
+          hat[k] = times_plus(hat[k], r_a, mean_a);
+          value[k] = times(hat[k], w[k]);
+        }
       } else {
 #pragma unroll
         for (int k = 0; k < P; ++k) value[k] = hat[k];
       }
     };
     auto keep_gate = [&](int i) {
+      if (kGate == kGateNone) return;
       Two g[P];
-      if (kSharedGate) rows.weights(static_cast<const float*>(q.gate), i, g);
-      else if (q.gate) rows.template read<2>(i, g);
+      if (kForAll) rows.weights(static_cast<const float*>(q.gate), i, g); else rows.template read<2>(i, g);
 #pragma unroll
-      for (int k = 0; k < P; ++k) two[i * P + k] = !q.gate ? both(1.0f) : q.sigmoid ? gate_kept(g[k]) : g[k];
+      for (int k = 0; k < P; ++k) two[i * P + k] = kGate == kGateEachSigmoid || (kForAll && q.sigmoid) ? gate_kept(g[k]) : g[k];
     };
     auto gate_of = [&](Two kept) -> GatePair {
-      if (q.sigmoid) return gate_again(kept);
+      if (kGate == kGateEachSigmoid || (kForAll && q.sigmoid)) return gate_again(kept);
       return {kept, both(1.0f)};
     };
     float2 m = make_float2(0.0f, 0.0f);
-    if (q.d_normed) {
-      Two sh = both(0.0f), s = both(poison);
+    if (kBefore) {
+      float sh = 0.0f, s = poison;
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
         Two hat[P], y[P], f[P], w[P];
         block_hat(i, hat, y);
         keep_gate(i);
-        if (q.gate) {
 #pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = times(y[k], gate_of(two[i * P + k]).open);
+        for (int k = 0; k < P; ++k) {
+          if (kGate != kGateNone) y[k] = times(y[k], gate_of(two[i * P + k]).open);
+          y[k] = times(y[k], scale);
         }
-#pragma unroll
-        for (int k = 0; k < P; ++k) y[k] = times(y[k], both(q.scale));
         if (q.residual) {
           rows.template read<1>(i, f);
 #pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = times_plus(f[k], both(q.residual_scale), y[k]);
-        }
-        if (q.before == kNormLayer) {
-#pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = sum(y[k], both(-st.z));
+          for (int k = 0; k < P; ++k) y[k] = times_plus(f[k], residual_scale, y[k]);
         }
         rows.template read<4>(i, f);   // (0 beyond the row, so that nothing there counts)
-        if (q.weight_before) rows.weights(q.weight_before, i, w);
+        rows.weights(q.weight_before, i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          const Two y_hat = times(y[k], both(st.w));
+          const Two y_hat = times_plus(y[k], r_b, mean_b);
           one[i * P + k] = y_hat;
-          of_before[i * P + k] = times_plus(f[k], y_hat, of_before[i * P + k]);
-          if (q.weight_before) f[k] = times(f[k], w[k]);
-          sh = times_plus(f[k], y_hat, sh);
-          s = sum(s, f[k]);
+          of_before[kBefore ? i * P + k : 0] = times_plus(f[k], y_hat, of_before[kBefore ? i * P + k : 0]);
+          const Two d = times(f[k], w[k]);
+          sh = fmaf(d.x, y_hat.x, sh); sh = fmaf(d.y, y_hat.y, sh);
+          s += d.x + d.y;
         }
       }
-      const float2 h = sh, t = s;
-      m = sums.two(h.x + h.y, t.x + t.y);
+      m = sums.two(sh, s);
       m.x *= inv;
       m.y = q.before == kNormLayer ? m.y * inv : poison;
     }
-    Two sh = both(0.0f), s = both(poison);
+    float sh = 0.0f, s = poison;
+    const Two less_x = both(-m.x), less_y = both(-m.y);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
       Two hat[P], value[P], d[P], f[P], w[P];
       block_hat(i, hat, value);
-      if (!q.d_normed) keep_gate(i);
+      if (!kBefore) keep_gate(i);
       if (q.d_y) {
         rows.template read<3>(i, d);
       } else {
 #pragma unroll
         for (int k = 0; k < P; ++k) d[k] = both(0.0f);
       }
-      if (q.d_normed) {
+      if (kBefore) {
         rows.template read<4>(i, f);
-        if (q.weight_before) {
-          rows.weights(q.weight_before, i, w);
+        rows.weights(q.weight_before, i, w);
 #pragma unroll
-          for (int k = 0; k < P; ++k) f[k] = times(f[k], w[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-          f[k] = times_plus(one[i * P + k], both(-m.x), f[k]);
-          if (q.before == kNormLayer) f[k] = sum(f[k], both(-m.y));
-          d[k] = times_plus(f[k], both(st.w), d[k]);
-        }
+        for (int k = 0; k < P; ++k) d[k] = times_plus(times_plus(one[i * P + k], less_x, times_plus(f[k], w[k], less_y)), r_b, d[k]);
       }
+      if (kEdges) rows.blank(i, d);
       if (q.d_residual) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = times(d[k], both(q.residual_scale));
+        for (int k = 0; k < P; ++k) f[k] = times(d[k], residual_scale);
         rows.write(q.d_residual, r * q.ld_d_residual, i, f);
       }
 #pragma unroll
-      for (int k = 0; k < P; ++k) d[k] = times(d[k], both(q.scale));
-      if (q.gate) {
+      for (int k = 0; k < P; ++k) d[k] = times(d[k], scale);
+      if (kGate != kGateNone) {
 #pragma unroll
         for (int k = 0; k < P; ++k) {
           const GatePair g = gate_of(two[i * P + k]);
-          f[k] = times(d[k], value[k]);
-          if (q.sigmoid) f[k] = times(f[k], g.slope);
+          f[k] = times(times(d[k], value[k]), g.slope);
           d[k] = times(d[k], g.open);
-          if (kSharedGate) of_gate[kSharedGate ? i * P + k : 0] = sum(of_gate[kSharedGate ? i * P + k : 0], f[k]);
+          if (kForAll) of_gate[kForAll ? i * P + k : 0] = sum(of_gate[kForAll ? i * P + k : 0], f[k]);
         }
-        if (!kSharedGate && q.d_gate) rows.write(q.d_gate, r * q.ld_d_gate, i, f);
+        if (!kForAll && q.d_gate) rows.write(q.d_gate, r * q.ld_d_gate, i, f);
       }
-      if (q.after != kNormNone) {
-        if (kEdges && !rows.whole(i)) {   // what is beyond the row does not count
-#pragma unroll
-          for (int k = 0; k < P; ++k) {
-            const float2 t = d[k];
-            d[k] = make_float2(rows.has((i * P + k) * 2) ? t.x : 0.0f, rows.has((i * P + k) * 2 + 1) ? t.y : 0.0f);
-          }
-        }
-        if (q.weight_after) rows.weights(q.weight_after, i, w);
+      if (kAfter) {
+        rows.weights(q.weight_after, i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          of_after[i * P + k] = times_plus(d[k], hat[k], of_after[i * P + k]);
-          if (q.weight_after) d[k] = times(d[k], w[k]);
-          sh = times_plus(d[k], hat[k], sh);
-          s = sum(s, d[k]);
+          of_after[kAfter ? i * P + k : 0] = times_plus(d[k], hat[k], of_after[kAfter ? i * P + k : 0]);
+          d[k] = times(d[k], w[k]);
+          sh = fmaf(d[k].x, hat[k].x, sh); sh = fmaf(d[k].y, hat[k].y, sh);
+          s += d[k].x + d[k].y;
+          two[i * P + k] = hat[k];
         }
       }
 #pragma unroll
-      for (int k = 0; k < P; ++k) { one[i * P + k] = d[k]; two[i * P + k] = hat[k]; }
+      for (int k = 0; k < P; ++k) one[i * P + k] = d[k];
     }
-    if (q.after != kNormNone) {
-      const float2 h = sh, t = s;
-      m = sums.two(h.x + h.y, t.x + t.y);
+    if (kAfter) {
+      m = sums.two(sh, s);
       m.x *= inv;
       m.y = q.after == kNormLayer ? m.y * inv : poison;
     } else {
@@ -691,15 +667,14 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
     }
     rows.release(r);
     if (!q.d_block) continue;
+    const Two by_x = both(-m.x * st.y), by_y = both(-m.y * st.y);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
       Two f[P];
 #pragma unroll
-      for (int k = 0; k < P; ++k) {
-        f[k] = one[i * P + k];
-        if (q.after != kNormNone) f[k] = times(sum(times_plus(two[i * P + k], both(-m.x), f[k]), both(-m.y)), both(st.y));
-      }
+      for (int k = 0; k < P; ++k)
+        f[k] = kAfter ? times_plus(two[i * P + k], by_x, times_plus(one[i * P + k], r_a, by_y)) : one[i * P + k];
       rows.write(q.d_block, r * q.ld_d_block, i, f);
     }
   }
@@ -709,9 +684,9 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_backward_kernel(c
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     if (!rows.any(i)) break;
-    if (kSharedGate) rows.write_sums(mine, i, of_gate + (kSharedGate ? i * P : 0));
-    rows.write_sums(mine + plane, i, of_after + i * P);
-    rows.write_sums(mine + 2 * plane, i, of_before + i * P);
+    if (kForAll) rows.write_sums(mine, i, of_gate + (kForAll ? i * P : 0));
+    if (kAfter) rows.write_sums(mine + plane, i, of_after + (kAfter ? i * P : 0));
+    if (kBefore) rows.write_sums(mine + 2 * plane, i, of_before + (kBefore ? i * P : 0));
   }
 }
 
