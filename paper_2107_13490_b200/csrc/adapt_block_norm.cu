@@ -18,8 +18,6 @@ static_assert(ADAPT_NORM_NONE == kNormNone && ADAPT_NORM_RMS == kNormRms && ADAP
 namespace {
 
 constexpr int kSms = 148;   // of a B200
-constexpr int kNormMaxRow = kNormElems * kNormBackwardThreads;   // elements of a row in a CTA's registers, backward
-constexpr int kNormMaxRowForward = kNormElems * kNormMaxThreads;   // and forward
 
 // Threads of a CTA for a row (with room for up to 7 elements between a boundary and an odd row), and CTAs of an SM:
 // 128 registers a thread backward, 64 forward.
@@ -144,7 +142,7 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
   int rc = ADAPT_OK;
   LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM, stream);
   const bool known = q.before == kNormNone ? !normed : normed != nullptr;   // (a norm whose output is not wanted: its statistics may be)
-  if (dim <= kNormMaxRowForward && norm_threads(dim) <= kNormMaxThreads && known && (q.after != kNormNone || q.before != kNormNone)) {
+  if (norm_threads(dim) <= kNormMaxThreads && known && (q.after != kNormNone || q.before != kNormNone)) {
     const int threads = norm_threads(dim), per_sm = std::max(1, std::min(16, 1024 / threads));
     const NormPlan plan(q, e, per_sm, threads, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
                         {nullptr, 0}, {nullptr, 0}}, {{y, q.ld_y}, {normed, q.ld_normed}});

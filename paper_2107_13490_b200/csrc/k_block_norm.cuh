@@ -221,13 +221,18 @@ struct NormRing {
   int place[5];              // bytes into a stage of block, residual, gate, d_y, d_normed, -1: none
 };
 
-// Two elements.  (The packed fp32 instructions were tried: their operands have to lie in pairs of registers, and the
-// moves that make such pairs of constants and unpacked elements were more than what they save.)
+// Two elements.  What multiplies or adds elements with elements takes both in one packed instruction; a factor for all
+// would have to be held in a pair of registers, so that is done one by one.
 typedef float2 Two;
 __device__ __forceinline__ Two both(float v) { return make_float2(v, v); }
-__device__ __forceinline__ Two sum(Two a, Two b) { return make_float2(a.x + b.x, a.y + b.y); }
-__device__ __forceinline__ Two times(Two a, Two b) { return make_float2(a.x * b.x, a.y * b.y); }
-__device__ __forceinline__ Two times_plus(Two a, Two b, Two c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+__device__ __forceinline__ f32x2 packed(Two a) { return pack2(a.x, a.y); }
+__device__ __forceinline__ Two sum(Two a, Two b) { return unpack2(add2(packed(a), packed(b))); }
+__device__ __forceinline__ Two times(Two a, Two b) { return unpack2(mul2(packed(a), packed(b))); }
+__device__ __forceinline__ Two times_plus(Two a, Two b, Two c) { return unpack2(fma2(packed(a), packed(b), packed(c))); }
+__device__ __forceinline__ Two times(Two a, float b) { return make_float2(a.x * b, a.y * b); }
+__device__ __forceinline__ Two times_plus(Two a, float b, float c) { return make_float2(fmaf(a.x, b, c), fmaf(a.y, b, c)); }
+__device__ __forceinline__ Two times_plus(Two a, float b, Two c) { return make_float2(fmaf(a.x, b, c.x), fmaf(a.y, b, c.y)); }
+__device__ __forceinline__ Two times_plus(Two a, Two b, float c) { return make_float2(fmaf(a.x, b.x, c), fmaf(a.y, b.y, c)); }
 __device__ __forceinline__ float fast_exp2(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -242,30 +247,23 @@ constexpr float kLog2E = 1.4426950408889634f;
 
 // g(gate) of a pair: 1 / (1 + e^-v), to 2^-22 and |v| steps of the exponent's argument; 0 below 2^-126.
 __device__ __forceinline__ Two gate_open(Two v) {
-  const float2 e = times(v, both(-kLog2E));
-  const float2 d = sum(make_float2(fast_exp2(e.x), fast_exp2(e.y)), both(1.0f));
-  return make_float2(fast_inverse(d.x), fast_inverse(d.y));
+  const Two e = times(v, -kLog2E);
+  return make_float2(fast_inverse(1.0f + fast_exp2(e.x)), fast_inverse(1.0f + fast_exp2(e.y)));
 }
 
 // The gate of the backward pass's first phase, kept in one number for the second: the smaller of g and 1 - g (the
 // other is 1 minus it, to a rounding), with the sign that says which.  So g (1 - g) keeps its relative precision
 // where the gate is far open or closed.
-__device__ __forceinline__ Two gate_kept(Two v) {
-  const float2 f = v;
-  const float2 e = times(make_float2(fabsf(f.x), fabsf(f.y)), both(-kLog2E));
-  const Two t = make_float2(fast_exp2(e.x), fast_exp2(e.y));
-  const float2 d = sum(t, both(1.0f));
-  const float2 c = times(t, make_float2(fast_inverse(d.x), fast_inverse(d.y)));
-  return make_float2(copysignf(c.x, f.x), copysignf(c.y, f.y));
+__device__ __forceinline__ float gate_kept(float v) {
+  const float t = fast_exp2(fabsf(v) * -kLog2E);
+  return copysignf(t * fast_inverse(1.0f + t), v);
 }
-struct GatePair { Two open, slope; };
-__device__ __forceinline__ GatePair gate_again(Two kept) {
-  const float2 k = kept;
-  const Two least = make_float2(fabsf(k.x), fabsf(k.y));
-  const Two most = times_plus(least, both(-1.0f), both(1.0f));
-  const float2 l = least, m = most;
-  return {make_float2(signbit(k.x) ? l.x : m.x, signbit(k.y) ? l.y : m.y), times(least, most)};
+__device__ __forceinline__ Two gate_kept(Two v) { return make_float2(gate_kept(v.x), gate_kept(v.y)); }
+__device__ __forceinline__ Two kept_open(Two k) {
+  const Two most = make_float2(1.0f - fabsf(k.x), 1.0f - fabsf(k.y));
+  return make_float2(signbit(k.x) ? fabsf(k.x) : most.x, signbit(k.y) ? fabsf(k.y) : most.y);
 }
+__device__ __forceinline__ Two kept_slope(Two k) { return make_float2(fmaf(-fabsf(k.x), fabsf(k.x), fabsf(k.x)), fmaf(-fabsf(k.y), fabsf(k.y), fabsf(k.y))); }
 
 // Sums over a CTA, in one of two sets of places in turn, so that one barrier each is enough.
 template <int kThreads>
@@ -302,12 +300,14 @@ struct NormRows {
   static constexpr int V = 16 / sizeof(T), P = V / 2, kChunks = kElems / V;
   const NormParams& q;
   const NormRing& ring;
-  unsigned stages, bars;     // addresses
-  unsigned stage, parity, at;   // the stage of the row at hand, the barrier's phase, this thread's place in the stage
+  unsigned char* stages;
+  unsigned bars;             // an address
+  unsigned stage, parity;    // the stage of the row at hand, its barrier's phase
+  const unsigned char* at;   // this thread's place in the stage
   int skip;                  // elements between a 16-byte boundary and the rows' first element
   unsigned in;               // which of the thread's elements are elements of the row (kEdges)
   __device__ __forceinline__ NormRows(const NormParams& q_, const NormRing& r, unsigned char* smem, unsigned long long* b)
-      : q(q_), ring(r), stages(shared_address(smem)), bars(shared_address(b)), stage(0), parity(0), at(shared_address(smem) + threadIdx.x * 16), skip(0), in(~0u) {
+      : q(q_), ring(r), stages(smem), bars(shared_address(b)), stage(0), parity(0), at(smem + threadIdx.x * 16), skip(0), in(~0u) {
     if constexpr (kEdges) {
       skip = static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + blockIdx.x * q.ld_block) & 15u) / sizeof(T));
       in = 0;
@@ -352,7 +352,7 @@ struct NormRows {
     for (int i = 0; i < 5; ++i)
       if (ring.place[i] >= 0)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     :: "r"(stages + s * ring.streams * ring.stage_row + ring.place[i]), "l"(static_cast<const T*>(from[i]) + r * ld[i] - skip),
+                     :: "r"(shared_address(stages) + s * ring.streams * ring.stage_row + ring.place[i]), "l"(static_cast<const T*>(from[i]) + r * ld[i] - skip),
                         "r"(bytes), "r"(bars + 8 * s) : "memory");
   }
   // Waits for the row's data; 0, or NaN where they never came.
@@ -368,9 +368,7 @@ struct NormRows {
   // Chunk i of stream kStream; 0 for what is not in the row.
   template <int kStream>
   __device__ __forceinline__ void read(int i, Two (&f)[P]) const {
-    uint4 raw;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w)
-                 : "r"(at + ring.place[kStream] + i * blockDim.x * 16));
+    const uint4 raw = *reinterpret_cast<const uint4*>(at + ring.place[kStream] + i * blockDim.x * 16);
     float v[V];
     unpack16<T>(raw, v);
     if (kEdges && !whole(i)) {
@@ -453,8 +451,10 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
         if (rows.inside(j)) s = fmaf(d, d, s);
       }
     } else {
+      Two t = both(0.0f);
 #pragma unroll
-      for (int k = 0; k < kPairs; ++k) { s = fmaf(v[k].x, v[k].x, s); s = fmaf(v[k].y, v[k].y, s); }
+      for (int k = 0; k < kPairs; ++k) t = times_plus(v[k], v[k], t);
+      s = t.x + t.y;
     }
     return make_float2(mean, rsqrtf(fmaf(sums.one(s), inv, q.eps)));
   };
@@ -473,15 +473,17 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
     v[0].x += poison;
     float2 a = make_float2(0.0f, 1.0f), b = a;
     if (kAfter) a = statistics(v, q.after);
-    const Two r_a = both(a.y), mean_a = both(-a.x * a.y), scale = both(q.scale), residual_scale = both(q.residual_scale);
+    // (where there is a norm, its factor takes the scale along)
+    const float r_a = a.y * q.scale, mean_a = -a.x * r_a;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
       Two g[P];
-      if (kAfter) {
-        rows.weights(q.weight_after, i, g);
+      if (kAfter) rows.weights(q.weight_after, i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = times(times_plus(v[i * P + k], r_a, mean_a), g[k]);
+      for (int k = 0; k < P; ++k) {
+        if (kAfter) v[i * P + k] = times(times_plus(v[i * P + k], r_a, mean_a), g[k]);
+        else v[i * P + k] = times(v[i * P + k], q.scale);
       }
       if (kGate == kGateForAll) rows.weights(static_cast<const float*>(q.gate), i, g);
       else if (kGate != kGateNone) rows.template read<2>(i, g);
@@ -489,12 +491,11 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
       for (int k = 0; k < P; ++k) {
         if (kGate == kGateEachSigmoid || (kGate == kGateForAll && q.sigmoid)) g[k] = gate_open(g[k]);
         if (kGate != kGateNone) v[i * P + k] = times(v[i * P + k], g[k]);
-        v[i * P + k] = times(v[i * P + k], scale);
       }
       if (q.residual) {
         rows.template read<1>(i, g);
 #pragma unroll
-        for (int k = 0; k < P; ++k) v[i * P + k] = times_plus(g[k], residual_scale, v[i * P + k]);
+        for (int k = 0; k < P; ++k) v[i * P + k] = times_plus(g[k], q.residual_scale, v[i * P + k]);
       }
       if (kEdges) rows.blank(i, v);
       if (q.y) {
@@ -506,14 +507,14 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
     if (kBefore) b = statistics(v, q.before); else __syncthreads();
     rows.release(r);
     if (kBefore) {
-      const Two r_b = both(b.y), mean_b = both(-b.x * b.y);
+      const float mean_b = -b.x * b.y;
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
         Two f[P], w[P];
         rows.weights(q.weight_before, i, w);
 #pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = times(times_plus(v[i * P + k], r_b, mean_b), w[k]);
+        for (int k = 0; k < P; ++k) f[k] = times(times_plus(v[i * P + k], b.y, mean_b), w[k]);
         rows.write(q.normed, r * q.ld_normed, i, f);
       }
     }
@@ -532,7 +533,6 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
   Rows rows(q, ring, norm_smem, bars);
   CtaSums<kNormBackwardThreads> sums{places, 0};
   const float inv = 1.0f / static_cast<float>(q.dim);
-  const Two scale = both(q.scale), residual_scale = both(q.residual_scale);
   Two of_after[kAfter ? kPairs : 1], of_before[kBefore ? kPairs : 1], of_gate[kForAll ? kPairs : 1];   // sums over rows
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) of_after[kAfter ? k : 0] = of_before[kBefore ? k : 0] = of_gate[kForAll ? k : 0] = both(0.0f);
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
     const float4 st = next;
     if (r + gridDim.x < q.rows) next = __ldg(statistics + r + gridDim.x);
     const float poison = rows.ready();
-    const Two r_a = both(st.y), mean_a = both(-st.x * st.y), r_b = both(st.w), mean_b = both(-st.z * st.w);
+    const float mean_a = -st.x * st.y, mean_b = -st.z * st.w, scale_b = q.scale * st.w, residual_b = q.residual_scale * st.w;
     // norm_before(y) and the gate; then the gradient of norm_after's output, and that output
     Two one[kPairs], two[kPairs];
     auto block_hat = [&](int i, Two (&hat)[P], Two (&value)[P]) {
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
         rows.weights(q.weight_after, i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          hat[k] = times_plus(hat[k], r_a, mean_a);
+          hat[k] = times_plus(hat[k], st.y, mean_a);
           value[k] = times(hat[k], w[k]);
         }
       } else {
@@ -567,47 +567,42 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
 #pragma unroll
       for (int k = 0; k < P; ++k) two[i * P + k] = kGate == kGateEachSigmoid || (kForAll && q.sigmoid) ? gate_kept(g[k]) : g[k];
     };
-    auto gate_of = [&](Two kept) -> GatePair {
-      if (kGate == kGateEachSigmoid || (kForAll && q.sigmoid)) return gate_again(kept);
-      return {kept, both(1.0f)};
-    };
+    auto opened = [&](Two kept) { return kGate == kGateEachSigmoid || (kForAll && q.sigmoid) ? kept_open(kept) : kept; };
     float2 m = make_float2(0.0f, 0.0f);
     if (kBefore) {
-      float sh = 0.0f, s = poison;
+      Two sh = both(0.0f), s = sh;
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
-        Two hat[P], y[P], f[P], w[P];
+        Two hat[P], y[P], f[P], w[P], base[P];
         block_hat(i, hat, y);
         keep_gate(i);
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-          if (kGate != kGateNone) y[k] = times(y[k], gate_of(two[i * P + k]).open);
-          y[k] = times(y[k], scale);
-        }
         if (q.residual) {
           rows.template read<1>(i, f);
 #pragma unroll
-          for (int k = 0; k < P; ++k) y[k] = times_plus(f[k], residual_scale, y[k]);
+          for (int k = 0; k < P; ++k) base[k] = times_plus(f[k], residual_b, mean_b);
+        } else {
+#pragma unroll
+          for (int k = 0; k < P; ++k) base[k] = both(mean_b);
         }
         rows.template read<4>(i, f);   // (0 beyond the row, so that nothing there counts)
         rows.weights(q.weight_before, i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          const Two y_hat = times_plus(y[k], r_b, mean_b);
+          if (kGate != kGateNone) y[k] = times(y[k], opened(two[i * P + k]));
+          const Two y_hat = times_plus(y[k], scale_b, base[k]);
           one[i * P + k] = y_hat;
           of_before[kBefore ? i * P + k : 0] = times_plus(f[k], y_hat, of_before[kBefore ? i * P + k : 0]);
           const Two d = times(f[k], w[k]);
-          sh = fmaf(d.x, y_hat.x, sh); sh = fmaf(d.y, y_hat.y, sh);
-          s += d.x + d.y;
+          sh = times_plus(d, y_hat, sh);
+          s = sum(s, d);
         }
       }
-      m = sums.two(sh, s);
+      m = sums.two(sh.x + sh.y, s.x + s.y + poison);
       m.x *= inv;
       m.y = q.before == kNormLayer ? m.y * inv : poison;
     }
-    float sh = 0.0f, s = poison;
-    const Two less_x = both(-m.x), less_y = both(-m.y);
+    Two sh = both(0.0f), s = sh;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
@@ -624,22 +619,22 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
         rows.template read<4>(i, f);
         rows.weights(q.weight_before, i, w);
 #pragma unroll
-        for (int k = 0; k < P; ++k) d[k] = times_plus(times_plus(one[i * P + k], less_x, times_plus(f[k], w[k], less_y)), r_b, d[k]);
+        for (int k = 0; k < P; ++k) d[k] = times_plus(times_plus(one[i * P + k], -m.x, times_plus(f[k], w[k], -m.y)), st.w, d[k]);
       }
       if (kEdges) rows.blank(i, d);
       if (q.d_residual) {
 #pragma unroll
-        for (int k = 0; k < P; ++k) f[k] = times(d[k], residual_scale);
+        for (int k = 0; k < P; ++k) f[k] = times(d[k], q.residual_scale);
         rows.write(q.d_residual, r * q.ld_d_residual, i, f);
       }
 #pragma unroll
-      for (int k = 0; k < P; ++k) d[k] = times(d[k], scale);
+      for (int k = 0; k < P; ++k) d[k] = times(d[k], q.scale);
       if (kGate != kGateNone) {
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-          const GatePair g = gate_of(two[i * P + k]);
-          f[k] = times(times(d[k], value[k]), g.slope);
-          d[k] = times(d[k], g.open);
+          f[k] = times(d[k], value[k]);
+          if (kGate == kGateEachSigmoid || (kForAll && q.sigmoid)) f[k] = times(f[k], kept_slope(two[i * P + k]));
+          d[k] = times(d[k], opened(two[i * P + k]));
           if (kForAll) of_gate[kForAll ? i * P + k : 0] = sum(of_gate[kForAll ? i * P + k : 0], f[k]);
         }
         if (!kForAll && q.d_gate) rows.write(q.d_gate, r * q.ld_d_gate, i, f);
@@ -650,8 +645,8 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
         for (int k = 0; k < P; ++k) {
           of_after[kAfter ? i * P + k : 0] = times_plus(d[k], hat[k], of_after[kAfter ? i * P + k : 0]);
           d[k] = times(d[k], w[k]);
-          sh = fmaf(d[k].x, hat[k].x, sh); sh = fmaf(d[k].y, hat[k].y, sh);
-          s += d[k].x + d[k].y;
+          sh = times_plus(d[k], hat[k], sh);
+          s = sum(s, d[k]);
           two[i * P + k] = hat[k];
         }
       }
@@ -659,7 +654,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
       for (int k = 0; k < P; ++k) one[i * P + k] = d[k];
     }
     if (kAfter) {
-      m = sums.two(sh, s);
+      m = sums.two(sh.x + sh.y, s.x + s.y + poison);
       m.x *= inv;
       m.y = q.after == kNormLayer ? m.y * inv : poison;
     } else {
@@ -667,14 +662,14 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
     }
     rows.release(r);
     if (!q.d_block) continue;
-    const Two by_x = both(-m.x * st.y), by_y = both(-m.y * st.y);
+    const float by_x = -m.x * st.y, by_y = -m.y * st.y;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
       Two f[P];
 #pragma unroll
       for (int k = 0; k < P; ++k)
-        f[k] = kAfter ? times_plus(two[i * P + k], by_x, times_plus(one[i * P + k], r_a, by_y)) : one[i * P + k];
+        f[k] = kAfter ? times_plus(two[i * P + k], by_x, times_plus(one[i * P + k], st.y, by_y)) : one[i * P + k];
       rows.write(q.d_block, r * q.ld_d_block, i, f);
     }
   }
