@@ -53,10 +53,18 @@ struct NormPlan {
     ring.stage_row = edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
     if (edges && q.dim + 16 / e - 1 > kNormElems * threads) staged = false;   // the elements before a boundary take room too
     for (int& p : ring.place) p = p < 0 ? -1 : p * ring.stage_row;
-    const int stage = ring.streams * ring.stage_row;
-    ring.stages = std::min(kNormMaxStages, std::max(200 * 1024 / per_sm / stage, 220 * 1024 / stage > 0 ? 1 : 0));
+    const int stage = ring.streams * ring.stage_row, copy = edges ? kNormElems * threads * 4 : 0;
+    const bool used[3] = {q.after != kNormNone, q.before != kNormNone, q.shared};
+    int copies = 0;
+    for (bool u : used) copies += u ? copy : 0;
+    ring.stages = std::min(kNormMaxStages, std::max((200 * 1024 / per_sm - copies) / stage, (220 * 1024 - copies) / stage > 0 ? 1 : 0));
     staged = staged && ring.stages > 0;
     smem = ring.stages * stage;
+    smem = (smem + 15) / 16 * 16;
+    for (int w = 0; w < 3; ++w) {
+      ring.weights[w] = used[w] && edges ? smem : -1;
+      if (used[w]) smem += copy;
+    }
   }
 };
 

@@ -219,6 +219,7 @@ struct NormRing {
   int streams, stages;       // rows of a stage, stages
   int stage_row;             // bytes of a row in a stage
   int place[5];              // bytes into a stage of block, residual, gate, d_y, d_normed, -1: none
+  int weights[3];            // (kEdges) bytes into shared memory of the copies of weight_after, weight_before and a shared gate
 };
 
 // Two elements.  What multiplies or adds elements with elements takes both in one packed instruction; a factor for all
@@ -317,6 +318,16 @@ struct NormRows {
         in |= (c >= 0 && c < q.dim ? 1u : 0u) << j;
       }
     }
+    if constexpr (kEdges) {   // weights beside their columns, so that they are read in 16 bytes too
+      const float* from[3] = {q.weight_after, q.weight_before, q.shared ? static_cast<const float*>(q.gate) : nullptr};
+      const int width = kChunks * static_cast<int>(blockDim.x) * V;
+#pragma unroll
+      for (int w = 0; w < 3; ++w)
+        if (ring.weights[w] >= 0)
+          for (int c = threadIdx.x; c < width; c += blockDim.x)
+            reinterpret_cast<float*>(smem + ring.weights[w])[c] =
+                c - skip < 0 || c - skip >= q.dim ? 0.0f : from[w] ? __ldg(from[w] + c - skip) : 1.0f;
+    }
     if (threadIdx.x == 0) {
       for (int s = 0; s < ring.stages; ++s) barrier_init(bars + 8 * s, 1);
       barrier_init_fence();
@@ -378,25 +389,25 @@ struct NormRows {
 #pragma unroll
     for (int k = 0; k < P; ++k) f[k] = make_float2(v[2 * k], v[2 * k + 1]);
   }
-  // (no weights: 1)
-  __device__ __forceinline__ void weights(const float* w, int i, Two (&f)[P]) const {
-    const int c = column(i);
-    if (!w) {
+  // Weights kWhich: after, before, a shared gate (none: 1).
+  template <int kWhich>
+  __device__ __forceinline__ void weights(int i, Two (&f)[P]) const {
+    const float* w = kWhich == 0 ? q.weight_after : kWhich == 1 ? q.weight_before : static_cast<const float*>(q.gate);
+    const float4* from;
+    if constexpr (kEdges) {
+      from = reinterpret_cast<const float4*>(stages + ring.weights[kWhich]) + (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * (V / 4);
+    } else if (!w) {
 #pragma unroll
       for (int k = 0; k < P; ++k) f[k] = both(1.0f);
       return;
-    }
-    if constexpr (kEdges) {
-#pragma unroll
-      for (int k = 0; k < P; ++k)
-        f[k] = make_float2(has(i * V + 2 * k) ? __ldg(w + c + 2 * k) : 0.0f, has(i * V + 2 * k + 1) ? __ldg(w + c + 2 * k + 1) : 0.0f);
     } else {
+      from = reinterpret_cast<const float4*>(w + column(i));
+    }
 #pragma unroll
-      for (int k = 0; k < V; k += 4) {
-        const float4 t = __ldg(reinterpret_cast<const float4*>(w + c + k));
-        f[k / 2] = make_float2(t.x, t.y);
-        f[k / 2 + 1] = make_float2(t.z, t.w);
-      }
+    for (int k = 0; k < V / 4; ++k) {
+      const float4 t = kEdges ? from[k] : __ldg(from + k);
+      f[2 * k] = make_float2(t.x, t.y);
+      f[2 * k + 1] = make_float2(t.z, t.w);
     }
   }
   __device__ __forceinline__ void write(void* to, long long at, int i, const Two (&f)[P]) const {
@@ -479,13 +490,13 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
     for (int i = 0; i < kChunks; ++i) {
       if (!rows.any(i)) break;
       Two g[P];
-      if (kAfter) rows.weights(q.weight_after, i, g);
+      if (kAfter) rows.template weights<0>(i, g);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         if (kAfter) v[i * P + k] = times(times_plus(v[i * P + k], r_a, mean_a), g[k]);
         else v[i * P + k] = times(v[i * P + k], q.scale);
       }
-      if (kGate == kGateForAll) rows.weights(static_cast<const float*>(q.gate), i, g);
+      if (kGate == kGateForAll) rows.template weights<2>(i, g);
       else if (kGate != kGateNone) rows.template read<2>(i, g);
 #pragma unroll
       for (int k = 0; k < P; ++k) {
@@ -512,7 +523,7 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
       for (int i = 0; i < kChunks; ++i) {
         if (!rows.any(i)) break;
         Two f[P], w[P];
-        rows.weights(q.weight_before, i, w);
+        rows.template weights<1>(i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) f[k] = times(times_plus(v[i * P + k], b.y, mean_b), w[k]);
         rows.write(q.normed, r * q.ld_normed, i, f);
@@ -549,7 +560,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
       rows.template read<0>(i, hat);
       if (kAfter) {
         Two w[P];
-        rows.weights(q.weight_after, i, w);
+        rows.template weights<0>(i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
           hat[k] = times_plus(hat[k], st.y, mean_a);
@@ -563,7 +574,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
     auto keep_gate = [&](int i) {
       if (kGate == kGateNone) return;
       Two g[P];
-      if (kForAll) rows.weights(static_cast<const float*>(q.gate), i, g); else rows.template read<2>(i, g);
+      if (kForAll) rows.template weights<2>(i, g); else rows.template read<2>(i, g);
 #pragma unroll
       for (int k = 0; k < P; ++k) two[i * P + k] = kGate == kGateEachSigmoid || (kForAll && q.sigmoid) ? gate_kept(g[k]) : g[k];
     };
@@ -586,7 +597,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
           for (int k = 0; k < P; ++k) base[k] = both(mean_b);
         }
         rows.template read<4>(i, f);   // (0 beyond the row, so that nothing there counts)
-        rows.weights(q.weight_before, i, w);
+        rows.template weights<1>(i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
           if (kGate != kGateNone) y[k] = times(y[k], opened(two[i * P + k]));
@@ -617,7 +628,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
       }
       if (kBefore) {
         rows.template read<4>(i, f);
-        rows.weights(q.weight_before, i, w);
+        rows.template weights<1>(i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) d[k] = times_plus(times_plus(one[i * P + k], -m.x, times_plus(f[k], w[k], -m.y)), st.w, d[k]);
       }
@@ -640,7 +651,7 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
         if (!kForAll && q.d_gate) rows.write(q.d_gate, r * q.ld_d_gate, i, f);
       }
       if (kAfter) {
-        rows.weights(q.weight_after, i, w);
+        rows.template weights<0>(i, w);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
           of_after[kAfter ? i * P + k : 0] = times_plus(d[k], hat[k], of_after[kAfter ? i * P + k : 0]);
