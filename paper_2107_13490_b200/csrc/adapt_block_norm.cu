@@ -19,13 +19,27 @@ namespace {
 
 constexpr int kSms = 148;   // of a B200
 
-// Threads of a CTA for a row (with room for up to 7 elements between a boundary and an odd row), and CTAs of an SM:
-// 128 registers a thread backward, 64 forward.
-int norm_threads(int64_t dim) { return static_cast<int>((dim + (dim % 8 ? 7 : 0) + 32 * kNormElems - 1) / (32 * kNormElems)) * 32; }
-int norm_per_sm(int64_t dim) { return std::max(1, std::min(8, 512 / norm_threads(dim))); }
+// How a row is held: by CTAs of so many threads, `parts` of them, `per_sm` on an SM.  (There is room for up to 7 elements
+// between a boundary and an odd row.)  128 registers a thread backward, 64 forward.
+struct NormShape {
+  int parts = 1, threads, per_sm;
+  NormShape(int64_t dim, int most, int of_sm, int ctas) {
+    const int64_t room = dim + (dim % 8 ? 7 : 0);
+    while (room > static_cast<int64_t>(kNormElems) * most * parts) parts *= 2;
+    const int64_t unit = 32ll * kNormElems * parts;
+    threads = static_cast<int>((room + unit - 1) / unit) * 32;
+    per_sm = std::max(1, std::min(ctas, of_sm / threads));
+  }
+};
+NormShape norm_forward(int64_t dim) { return NormShape(dim, kNormMaxThreads, 1024, 16); }
+NormShape norm_backward(int64_t dim) { return NormShape(dim, kNormBackwardThreads, 512, 8); }
+static_assert(ADAPT_NORM_MAX_DIM <= kNormElems * kNormBackwardThreads * kNormMaxParts, "a cluster holds the longest row");
 
-// CTAs of a backward pass, each with sums of its own over its rows.
-int64_t norm_ctas(int64_t rows, int64_t dim) { return std::min<int64_t>(rows, kSms * norm_per_sm(dim)); }
+// CTAs (or clusters) of a backward pass, each with sums of its own over its rows.
+int64_t norm_ctas(int64_t rows, int64_t dim) {
+  const NormShape shape = norm_backward(dim);
+  return std::min<int64_t>(rows, kSms * shape.per_sm / shape.parts);
+}
 // A multiple of the period, so that a CTA's rows lie alike; the CTAs that has more have no rows, and sums of 0.
 unsigned norm_grid(int64_t ctas, int period) { return static_cast<unsigned>((ctas + period - 1) / period * period); }
 
@@ -34,7 +48,7 @@ struct NormPlan {
   NormRing ring = {};
   int smem = 0, period = 1;   // rows whose numbers differ by a multiple of the period lie alike
   bool staged = true, edges = false;
-  NormPlan(const NormParams& q, int e, int per_sm, int threads, std::initializer_list<std::pair<const void*, long long>> in,
+  NormPlan(const NormParams& q, int e, const NormShape& shape, std::initializer_list<std::pair<const void*, long long>> in,
            std::initializer_list<std::pair<const void*, long long>> out) {
     auto phase = [](const void* p) { return static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) & 15u); };
     auto step = [&](long long ld) { return q.rows == 1 ? 0u : static_cast<unsigned>(ld * e & 15); };
@@ -50,10 +64,12 @@ struct NormPlan {
     for (const void* p : {static_cast<const void*>(q.weight_after), static_cast<const void*>(q.weight_before), q.shared ? q.gate : nullptr})
       edges = edges || misaligned(p, 16);
     while (period * by % 16) period *= 2;
-    ring.stage_row = edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
-    if (edges && q.dim + 16 / e - 1 > kNormElems * threads) staged = false;   // the elements before a boundary take room too
+    ring.parts = shape.parts;
+    const int width = kNormElems * shape.threads, per_sm = shape.per_sm;   // elements of a part
+    if (edges && q.dim + 16 / e - 1 > width * shape.parts) staged = false;   // the elements before a boundary take room too
+    ring.stage_row = shape.parts > 1 ? width * e : edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
     for (int& p : ring.place) p = p < 0 ? -1 : p * ring.stage_row;
-    const int stage = ring.streams * ring.stage_row, copy = edges ? kNormElems * threads * 4 : 0;
+    const int stage = ring.streams * ring.stage_row, copy = edges ? width * 4 : 0;
     const bool used[3] = {q.after != kNormNone, q.before != kNormNone, q.shared};
     int copies = 0;
     for (bool u : used) copies += u ? copy : 0;
@@ -87,7 +103,7 @@ void with_form(const NormParams& q, bool edges, F f) {
 
 // Launches a kernel that may need more shared memory than a kernel has by itself.
 template <auto kKernel>
-int norm_launch(unsigned grid, int threads, int smem, cudaStream_t stream, const NormParams& q, const NormRing& ring) {
+int norm_launch(unsigned groups, const NormShape& shape, int smem, cudaStream_t stream, const NormParams& q, const NormRing& ring) {
   static std::atomic<uint64_t> ready{0};   // devices that know
   int device = 0;
   ADAPT_CUDA(cudaGetDevice(&device));
@@ -96,8 +112,17 @@ int norm_launch(unsigned grid, int threads, int smem, cudaStream_t stream, const
     ADAPT_CUDA(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
     ready.fetch_or(bit);
   }
-  kKernel<<<grid, threads, smem, stream>>>(q, ring);
-  ADAPT_LAUNCH_OK("block norm");
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(groups * shape.parts);
+  cfg.blockDim = dim3(shape.threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = shape.parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = shape.parts > 1 ? 1 : 0;
+  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kKernel, q, ring));
   return ADAPT_OK;
 }
 
@@ -150,17 +175,17 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
   int rc = ADAPT_OK;
   LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM, stream);
   const bool known = q.before == kNormNone ? !normed : normed != nullptr;   // (a norm whose output is not wanted: its statistics may be)
-  if (norm_threads(dim) <= kNormMaxThreads && known && (q.after != kNormNone || q.before != kNormNone)) {
-    const int threads = norm_threads(dim), per_sm = std::max(1, std::min(16, 1024 / threads));
-    const NormPlan plan(q, e, per_sm, threads, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
+  if (known && (q.after != kNormNone || q.before != kNormNone)) {
+    const NormShape shape = norm_forward(dim);
+    const NormPlan plan(q, e, shape, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
                         {nullptr, 0}, {nullptr, 0}}, {{y, q.ld_y}, {normed, q.ld_normed}});
     if (plan.staged) {
-      const unsigned grid = norm_grid(std::min<int64_t>(rows, kSms * per_sm), plan.period);
+      const unsigned grid = norm_grid(std::min<int64_t>(rows, kSms * shape.per_sm / shape.parts), plan.period);
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
         with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
           rc = norm_launch<norm_row_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
-              grid, threads, plan.smem, stream, q, plan.ring);
+              grid, shape, plan.smem, stream, q, plan.ring);
         });
       });
       return rc;
@@ -227,11 +252,11 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   int rc = ADAPT_OK;
   {
     LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM_BACKWARD, stream);
-    const int threads = norm_threads(dim);
-    const NormPlan plan(q, e, norm_per_sm(dim), threads, {{block, q.ld_block}, {residual, q.ld_residual},
+    const NormShape shape = norm_backward(dim);
+    const NormPlan plan(q, e, shape, {{block, q.ld_block}, {residual, q.ld_residual},
                         {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
                         {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
-    if (plan.staged && threads <= kNormBackwardThreads && (q.after != kNormNone || d_normed)) {
+    if (plan.staged && (q.after != kNormNone || d_normed)) {
       const unsigned grid = norm_grid(ctas, plan.period);
       sum.ctas = static_cast<int>(grid);
       if (!d_normed) q.before = kNormNone;   // (its gradient is not given)
@@ -239,7 +264,7 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
         using T = decltype(t);
         with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
           rc = norm_launch<norm_row_backward_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
-              grid, threads, plan.smem, stream, q, plan.ring);
+              grid, shape, plan.smem, stream, q, plan.ring);
         });
       });
     } else {

@@ -209,6 +209,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_any_backward_kernel(NormPar
 // Rows that do not begin on 16-byte boundaries (an odd dim) are copied with the aligned blocks around them.  All tensors
 // have to lie alike (kEdges): then chunks are cut at those boundaries, the first and the last hold fewer
 // elements, and a CTA takes rows that lie alike too, so that a thread keeps its columns.
+//
+// Rows that one CTA cannot hold are shared by the CTAs of a cluster, which add up their sums through shared memory.
 
 constexpr int kNormElems = 16;             // elements of a thread
 constexpr int kNormMaxThreads = 1024;      // of a CTA, forward
@@ -218,6 +220,7 @@ constexpr int kNormMaxStages = 4;
 struct NormRing {
   int streams, stages;       // rows of a stage, stages
   int stage_row;             // bytes of a row in a stage
+  int parts;                 // CTAs of a cluster that share a row
   int place[5];              // bytes into a stage of block, residual, gate, d_y, d_normed, -1: none
   int weights[3];            // (kEdges) bytes into shared memory of the copies of weight_after, weight_before and a shared gate
 };
@@ -267,10 +270,13 @@ __device__ __forceinline__ Two kept_open(Two k) {
 __device__ __forceinline__ Two kept_slope(Two k) { return make_float2(fmaf(-fabsf(k.x), fabsf(k.x), fabsf(k.x)), fmaf(-fabsf(k.y), fabsf(k.y), fabsf(k.y))); }
 
 // Sums over a CTA, in one of two sets of places in turn, so that one barrier each is enough.
+constexpr int kNormMaxParts = 4;
+
 template <int kThreads>
 struct CtaSums {
   float2 (*places)[kThreads / 32];
-  int turn;
+  float2 (*parts)[kNormMaxParts];   // a sum of each CTA of the cluster
+  int turn, part, count;
   template <bool kTwo>
   __device__ __forceinline__ float2 over_warp(float a, float b) const {
 #pragma unroll
@@ -283,13 +289,22 @@ struct CtaSums {
   template <bool kTwo>
   __device__ __forceinline__ float2 meet(float a, float b) {
     float2 s = over_warp<kTwo>(a, b);
-    if (blockDim.x == 32) { __syncwarp(); return s; }
+    if (blockDim.x == 32) { __syncwarp(); return s; }   // (rows so short are not shared)
     const int lane = threadIdx.x & 31;
     if (lane == 0) places[turn][threadIdx.x >> 5] = s;
     __syncthreads();
     s = lane < static_cast<int>(blockDim.x >> 5) ? places[turn][lane] : make_float2(0.0f, 0.0f);
+    s = over_warp<kTwo>(s.x, s.y);
+    if (count > 1) {
+      if (threadIdx.x < static_cast<unsigned>(count))
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(peer_address(shared_address(&parts[turn][part]), threadIdx.x)), "f"(s.x), "f"(s.y)
+                     : "memory");
+      meet_cluster();
+      s = make_float2(0.0f, 0.0f);
+      for (int p = 0; p < count; ++p) { const float2 t = parts[turn][p]; s.x += t.x; s.y += t.y; }
+    }
     turn ^= 1;
-    return over_warp<kTwo>(s.x, s.y);
+    return s;
   }
   __device__ __forceinline__ float one(float a) { return meet<false>(a, 0.0f).x; }
   __device__ __forceinline__ float2 two(float a, float b) { return meet<true>(a, b); }
@@ -305,12 +320,21 @@ struct NormRows {
   unsigned bars;             // an address
   unsigned stage, parity;    // the stage of the row at hand, its barrier's phase
   const unsigned char* at;   // this thread's place in the stage
+  int part;                  // of the row, for this CTA
+  long long group;           // clusters take the rows in turn
+  long long groups;
   int skip;                  // elements between a 16-byte boundary and the rows' first element
   unsigned in;               // which of the thread's elements are elements of the row (kEdges)
   __device__ __forceinline__ NormRows(const NormParams& q_, const NormRing& r, unsigned char* smem, unsigned long long* b)
-      : q(q_), ring(r), stages(smem), bars(shared_address(b)), stage(0), parity(0), at(smem + threadIdx.x * 16), skip(0), in(~0u) {
+      : q(q_), ring(r), stages(smem), bars(shared_address(b)), stage(0), parity(0), at(smem + threadIdx.x * 16), part(0),
+        group(blockIdx.x), groups(gridDim.x), skip(0), in(~0u) {
+    if (ring.parts > 1) {
+      part = cta_in_cluster();
+      group = blockIdx.x / ring.parts;
+      groups = gridDim.x / ring.parts;
+    }
     if constexpr (kEdges) {
-      skip = static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + blockIdx.x * q.ld_block) & 15u) / sizeof(T));
+      skip = static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + group * q.ld_block) & 15u) / sizeof(T));
       in = 0;
 #pragma unroll
       for (int j = 0; j < kElems; ++j) {
@@ -326,16 +350,17 @@ struct NormRows {
         if (ring.weights[w] >= 0)
           for (int c = threadIdx.x; c < width; c += blockDim.x)
             reinterpret_cast<float*>(smem + ring.weights[w])[c] =
-                c - skip < 0 || c - skip >= q.dim ? 0.0f : from[w] ? __ldg(from[w] + c - skip) : 1.0f;
+                first() + c < 0 || first() + c >= q.dim ? 0.0f : from[w] ? __ldg(from[w] + first() + c) : 1.0f;
     }
     if (threadIdx.x == 0) {
       for (int s = 0; s < ring.stages; ++s) barrier_init(bars + 8 * s, 1);
       barrier_init_fence();
-      for (int s = 0; s < ring.stages; ++s) fill(s, static_cast<long long>(blockIdx.x) + static_cast<long long>(s) * gridDim.x);
+      for (int s = 0; s < ring.stages; ++s) fill(s, group + s * groups);
     }
-    __syncthreads();
+    if (ring.parts > 1) meet_cluster(); else __syncthreads();
   }
-  __device__ __forceinline__ int column(int i) const { return (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V - skip; }
+  __device__ __forceinline__ int first() const { return part * kElems * static_cast<int>(blockDim.x) - skip; }   // column of the CTA
+  __device__ __forceinline__ int column(int i) const { return first() + (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V; }
   // Whether chunk i has an element of the row, and whether all of its elements are.
   __device__ __forceinline__ bool any(int i) const { return column(i) < q.dim; }
   __device__ __forceinline__ bool whole(int i) const { return !kEdges || ((in >> (i * V)) & ((1u << V) - 1)) == (1u << V) - 1; }
@@ -355,7 +380,9 @@ struct NormRows {
 
   __device__ __forceinline__ void fill(int s, long long r) const {
     if (r >= q.rows) return;
-    const unsigned bytes = kEdges ? ((skip + q.dim) * static_cast<int>(sizeof(T)) + 15) & ~15 : q.dim * static_cast<int>(sizeof(T));
+    const int from_column = first(), columns = min(q.dim - from_column, kElems * static_cast<int>(blockDim.x));
+    if (columns <= 0) { barrier_expect_bytes(bars + 8 * s, 0); return; }
+    const unsigned bytes = (columns * static_cast<int>(sizeof(T)) + 15) & ~15;
     barrier_expect_bytes(bars + 8 * s, ring.streams * bytes);
     const void* from[5] = {q.block, q.residual, q.gate, q.d_y, q.d_normed};
     const long long ld[5] = {q.ld_block, q.ld_residual, q.ld_gate, q.ld_d_y, q.ld_d_normed};
@@ -363,7 +390,7 @@ struct NormRows {
     for (int i = 0; i < 5; ++i)
       if (ring.place[i] >= 0)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     :: "r"(shared_address(stages) + s * ring.streams * ring.stage_row + ring.place[i]), "l"(static_cast<const T*>(from[i]) + r * ld[i] - skip),
+                     :: "r"(shared_address(stages) + s * ring.streams * ring.stage_row + ring.place[i]), "l"(static_cast<const T*>(from[i]) + r * ld[i] + from_column),
                         "r"(bytes), "r"(bars + 8 * s) : "memory");
   }
   // Waits for the row's data; 0, or NaN where they never came.
@@ -372,7 +399,7 @@ struct NormRows {
   }
   // Called when every thread has read what it needs of the row `r`.
   __device__ __forceinline__ void release(long long r) {
-    if (threadIdx.x == 0) fill(stage, r + static_cast<long long>(ring.stages) * gridDim.x);
+    if (threadIdx.x == 0) fill(stage, r + ring.stages * groups);
     at += ring.streams * ring.stage_row;
     if (++stage == static_cast<unsigned>(ring.stages)) { stage = 0; parity ^= 1; at = stages + threadIdx.x * 16; }
   }
@@ -446,7 +473,8 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
   __shared__ float2 places[2][kNormMaxThreads / 32];
   Rows rows(q, ring, norm_smem, bars);
-  CtaSums<kNormMaxThreads> sums{places, 0};
+  __shared__ float2 parts[2][kNormMaxParts];
+  CtaSums<kNormMaxThreads> sums{places, parts, 0, rows.part, ring.parts};
   const float inv = 1.0f / static_cast<float>(q.dim);
   // mean and 1 / deviation; the deviation around the mean, in a second sum
   auto statistics = [&](const Two (&v)[kPairs], int kind) {
@@ -469,7 +497,7 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
     }
     return make_float2(mean, rsqrtf(fmaf(sums.one(s), inv, q.eps)));
   };
-  for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
+  for (long long r = rows.group; r < q.rows; r += rows.groups) {
     const float poison = rows.ready();
     Two v[kPairs];
 #pragma unroll
@@ -529,7 +557,7 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
         rows.write(q.normed, r * q.ld_normed, i, f);
       }
     }
-    if (q.stats && threadIdx.x == 0) reinterpret_cast<float4*>(q.stats)[r] = make_float4(a.x, a.y, b.x, b.y);
+    if (q.stats && threadIdx.x == 0 && rows.part == 0) reinterpret_cast<float4*>(q.stats)[r] = make_float4(a.x, a.y, b.x, b.y);
   }
 }
 
@@ -542,16 +570,17 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
   __shared__ float2 places[2][kNormBackwardThreads / 32];
   Rows rows(q, ring, norm_smem, bars);
-  CtaSums<kNormBackwardThreads> sums{places, 0};
+  __shared__ float2 parts[2][kNormMaxParts];
+  CtaSums<kNormBackwardThreads> sums{places, parts, 0, rows.part, ring.parts};
   const float inv = 1.0f / static_cast<float>(q.dim);
   Two of_after[kAfter ? kPairs : 1], of_before[kBefore ? kPairs : 1], of_gate[kForAll ? kPairs : 1];   // sums over rows
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) of_after[kAfter ? k : 0] = of_before[kBefore ? k : 0] = of_gate[kForAll ? k : 0] = both(0.0f);
   const float4* statistics = reinterpret_cast<const float4*>(q.stats_in);
-  float4 next = blockIdx.x < static_cast<unsigned>(q.rows) ? __ldg(statistics + blockIdx.x) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (long long r = blockIdx.x; r < q.rows; r += gridDim.x) {
+  float4 next = rows.group < q.rows ? __ldg(statistics + rows.group) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (long long r = rows.group; r < q.rows; r += rows.groups) {
     const float4 st = next;
-    if (r + gridDim.x < q.rows) next = __ldg(statistics + r + gridDim.x);
+    if (r + rows.groups < q.rows) next = __ldg(statistics + r + rows.groups);
     const float poison = rows.ready();
     const float mean_a = -st.x * st.y, mean_b = -st.z * st.w, scale_b = q.scale * st.w, residual_b = q.residual_scale * st.w;
     // norm_before(y) and the gate; then the gradient of norm_after's output, and that output
@@ -685,8 +714,8 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
     }
   }
   if (!q.partial) return;
-  const long long plane = static_cast<long long>(gridDim.x) * q.dim;
-  float* mine = q.partial + static_cast<long long>(blockIdx.x) * q.dim;
+  const long long plane = rows.groups * q.dim;
+  float* mine = q.partial + rows.group * q.dim;
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     if (!rows.any(i)) break;
