@@ -1,6 +1,7 @@
 // C-ABI entry points of the token embedding and its gradient.  Declarations and argument contracts live in
 // adapt.h.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -11,27 +12,70 @@ using namespace adapt;
 
 namespace {
 
+constexpr int kSms = 148;   // of a B200
+
 bool in_int(int64_t v, int64_t least) { return v >= least && v <= 0x7FFFFFFF; }
 
-// Places of a piece: its sums go to memory and back in fp32 (4 / piece of the bytes of dy in 16 bits), and a
-// token's pieces are joined one after the other.
-int embed_piece(int64_t n) {
-  int piece = 32;
-  while (piece < 1024 && n > 256ll * piece) piece *= 2;
-  return piece;
-}
+// Sorted places of a block: two rows of sums in fp32 at most go to memory and back for the block's rows of dy, and a
+// thousand blocks or so keep the device busy.
+int embed_block(int64_t n) { return n <= (1 << 15) ? 32 : n <= (1 << 17) ? 64 : 128; }
 
 struct EmbedLayout {
-  size_t keys[2], places[2], present, partial, bytes;
-  EmbedLayout(int64_t n, int64_t dim, int64_t vocab) {
+  size_t keys[2], places[2], partial, bytes;
+  EmbedLayout(int64_t n, int64_t dim) {
     size_t at = 0;
     auto take = [&](size_t b) { const size_t here = at; at = align_up(at + b, 256); return here; };
     for (int i = 0; i < 2; ++i) { keys[i] = take(4 * n); places[i] = take(4 * n); }
-    present = take((vocab + 31) / 32 * 4);
-    partial = take((n / embed_piece(n) + 1) * dim * 4);
+    partial = take((n + embed_block(n) - 1) / embed_block(n) * 2 * dim * 4);
     bytes = at;
   }
 };
+
+// Clusters of `parts` CTAs of the sort that the device holds at once.
+template <typename G>
+int sort_clusters(int parts, int* out) {
+  static std::atomic<int> known[64][5];   // by device and the logarithm of parts
+  int device = 0, log = 0;
+  ADAPT_CUDA(cudaGetDevice(&device));
+  while ((1 << log) < parts) ++log;
+  std::atomic<int>& slot = known[device & 63][log];
+  int n = slot.load();
+  if (!n) {
+    const auto kernel = embed_sort_kernel<G>;
+    ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem));
+    ADAPT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(parts);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = kSortSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ADAPT_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+    n = std::max(1, std::min(n, kSms / parts));
+    slot.store(n);
+  }
+  *out = n;
+  return ADAPT_OK;
+}
+
+// Launches a kernel behind another one of the same call, which it waits for by itself.
+template <typename... A, typename... B>
+cudaError_t launch_behind(void (*kernel)(A...), unsigned grid, int threads, int smem, cudaStream_t stream, B... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 }  // namespace
 
@@ -70,7 +114,7 @@ int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_ta
 
 size_t adapt_embedding_workspace_bytes(int64_t n, int64_t dim, int64_t vocab) {
   if (!in_int(vocab, 1) || !in_int(dim, 1) || !in_int(n, 1)) return 0;
-  return EmbedLayout(n, dim, vocab).bytes;
+  return EmbedLayout(n, dim).bytes;
 }
 
 int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_dy, int dtype, const int64_t* ids,
@@ -84,7 +128,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
   if (n > 0 && (!dy || !ids || misaligned(dy, e) || misaligned(ids, 8) || (n > 1 && ld_dy < dim))) return ADAPT_ERR_INVALID_ARG;
   if (n == 1) ld_dy = dim;
   if (vocab == 1) ld_grad = dim;
-  const EmbedLayout lay(n, dim, vocab);
+  const EmbedLayout lay(n, dim);
   if (n > 0) {
     if (!workspace || misaligned(workspace, 256)) return ADAPT_ERR_INVALID_ARG;
     if (workspace_bytes < lay.bytes) return ADAPT_ERR_WORKSPACE;
@@ -98,62 +142,68 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
     q.keys[i] = reinterpret_cast<unsigned*>(ws + lay.keys[i]);
     q.places[i] = reinterpret_cast<unsigned*>(ws + lay.places[i]);
   }
-  q.present = reinterpret_cast<unsigned*>(ws + lay.present);
   q.partial = reinterpret_cast<float*>(ws + lay.partial);
   int bits = 1;
   while (bits < 32 && (vocab >> bits)) ++bits;
-  q.passes = (bits + kSortWidth - 1) / kSortWidth;
-  q.width = (bits + q.passes - 1) / q.passes;
-  q.piece = embed_piece(n);
-  q.chunk = q.piece / 2;
+  q.passes = n <= kSortFew ? 0 : (bits + kSortWidth - 1) / kSortWidth;
+  q.width = q.passes ? (bits + q.passes - 1) / q.passes : 0;
+  q.block = embed_block(n);
   const int wide = 16 / e;
   const bool vec = dim % wide == 0 && !misaligned(dy, 16) && !misaligned(dtable, 16) && (n <= 1 || ld_dy % wide == 0) &&
                    (vocab == 1 || ld_grad % wide == 0);
-  const int64_t columns = kEmbedThreads * (vec ? wide : 4);
-  q.slices = static_cast<int>((dim + columns - 1) / columns);
-  q.token_ctas = static_cast<int>((n + q.chunk - 1) / q.chunk);
-  const int64_t zero_ctas = accumulate ? 0 : std::min<int64_t>(vocab, 148 * 8);
-  const int64_t grid = (q.token_ctas + zero_ctas) * q.slices, joins = (n + q.piece - 1) / q.piece * q.slices;
-  if (grid > 0x7FFFFFFF || joins > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
+  const int64_t columns = vec ? wide : 4, parts_of_row = (dim + columns - 1) / columns;   // of a thread
+  q.lanes = 8;
+  while (q.lanes < kEmbedThreads && q.lanes < parts_of_row) q.lanes *= 2;
+  q.slices = static_cast<int>((parts_of_row + q.lanes - 1) / q.lanes);
+  const int teams = kEmbedThreads / q.lanes;
+  const int64_t blocks = (n + q.block - 1) / q.block, sums = (blocks + teams - 1) / teams * q.slices,
+                joins = blocks * ((dim + kJoinColumns - 1) / kJoinColumns);
+  if (sums > 0x7FFFFFFF || joins > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
-  if (n > 0) {
-    int parts = 1;
-    while (parts < kSortMaxCluster && n > 1024ll * parts) parts *= 2;
-    LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(parts);
-    cfg.blockDim = dim3(kSortThreads);
-    cfg.dynamicSmemBytes = kSortSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    ADAPT_CUDA(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem));
-    if (parts > 8) ADAPT_CUDA(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    ADAPT_CUDA(cudaLaunchKernelEx(&cfg, embed_sort_kernel, q));
-  }
+  int rc = ADAPT_OK;
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
     auto go = [&](auto g) {
       using G = decltype(g);
       constexpr int V = 16 / sizeof(T);
+      int parts = 1, clusters = 1;
+      while (q.passes && parts < kSortMaxCluster && n > 1024ll * parts) parts *= 2;
+      if ((rc = sort_clusters<G>(parts, &clusters)) != ADAPT_OK) return;
+      // one that sorts, and as many for the rows of tokens that do not occur as there are 64 KB of them for each
+      const int64_t bytes = accumulate ? 0 : vocab * dim * eg;
+      clusters = accumulate ? 1 : std::max(2, std::min<int>(clusters, static_cast<int>(std::min<int64_t>(1000, bytes / (65536ll * parts) + 2))));
       {
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
-        if (vec) embed_sum_kernel<T, G, V, 1><<<static_cast<unsigned>(grid), kEmbedThreads, 0, stream>>>(q);
-        else embed_sum_kernel<T, G, 1, 4><<<static_cast<unsigned>(grid), kEmbedThreads, 0, stream>>>(q);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(parts * clusters);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = kSortSmem;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        const cudaError_t err = cudaLaunchKernelEx(&cfg, embed_sort_kernel<G>, static_cast<const EmbedGradParams>(q));
+        if (err != cudaSuccess) { rc = cuda_fail(err, "sort of tokens"); return; }
       }
-      if (n >= 2 * q.piece) {
+      if (n == 0) return;
+      const int smem = (2 * teams * q.block + 2) * 4;
+      {
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
-        if (vec) embed_join_kernel<T, G, V, 1><<<static_cast<unsigned>(joins), kEmbedThreads, 0, stream>>>(q);
-        else embed_join_kernel<T, G, 1, 4><<<static_cast<unsigned>(joins), kEmbedThreads, 0, stream>>>(q);
+        const cudaError_t err = vec ? launch_behind(embed_sum_kernel<T, G, V, 1>, static_cast<unsigned>(sums), kEmbedThreads, smem, stream, q)
+                                    : launch_behind(embed_sum_kernel<T, G, 1, 4>, static_cast<unsigned>(sums), kEmbedThreads, smem, stream, q);
+        if (err != cudaSuccess) { rc = cuda_fail(err, "token embedding, backward"); return; }
+      }
+      if (blocks > 1) {
+        LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
+        const cudaError_t err = launch_behind(embed_join_kernel<G>, static_cast<unsigned>(joins), 32 * kJoinWarps, 0, stream, q);
+        if (err != cudaSuccess) rc = cuda_fail(err, "token embedding, joined sums");
       }
     };
     if (grad_dtype == dtype) go(T{}); else go(float{});
   });
-  ADAPT_LAUNCH_OK("token embedding, backward");
-  return ADAPT_OK;
+  return rc;
 }
 
 }  // extern "C"

@@ -2,20 +2,21 @@
 //
 //   out[i] = scale * table[ids[i]],     dtable[v] = scale * sum_{i : ids[i] = v} dy[i]
 //
-// Both move rows and compute almost nothing: HBM bounds them, and for few tokens the launch.
+// Both move rows and compute almost nothing: HBM bounds them, and for few tokens the launches.
 //
-// The gradient sorts the tokens (stable, so that a token's occurrences stay in order) in one launch of a
-// single cluster, whose CTAs exchange their digit counts through shared memory; the sums then run
-// over the sorted places.  A token's occurrences are cut into pieces of kPiece places (a whole number of them, the
-// last one takes the rest), so that frequent tokens are summed by many CTAs; the sums of such pieces
-// meet in a second launch, in the order of the pieces.  So every sum has one order, whatever the
-// timing, and no row of dy is read twice.
+// The gradient takes three launches.  The first sorts the tokens (stable, so that a token's occurrences stay in order) in
+// one cluster, whose CTAs exchange their digit counts through shared memory, while the other clusters write the rows of
+// tokens that do not occur, most of the table as a rule.  The second sums over blocks of the sorted places, one
+// block a team of threads, so that frequent tokens are summed by many; where a token goes on beyond a block's end,
+// its sums so far are left in memory, and the third launch joins them in the order of the blocks.  So every sum has one
+// order, whatever the timing, and no row of dy is read twice.
 #pragma once
 
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 #include "k_elem.cuh"
+#include "tensor_core.cuh"
 
 namespace adapt {
 
@@ -94,80 +95,94 @@ struct EmbedGradParams {
   bool accumulate;
   unsigned* keys[2];     // [n] tokens (vocab: none)
   unsigned* places[2];   // [n] their places
-  unsigned* present;     // [ceil(vocab / 32)] bits: the token occurs
-  float* partial;        // [n / piece + 1][dim] sums of pieces
-  int width, passes;     // digits of the sort
-  int piece;             // places of a piece
-  int chunk;             // sorted places of a CTA
-  int slices;            // CTAs side by side that share a row's columns
-  int token_ctas;        // CTAs that sum; the others write the rows of tokens that do not occur
+  float* partial;        // [blocks][2][dim] sums of a block's first token, which began in front, and of its last, which goes on
+  int width, passes;     // digits of the sort (passes 0: by comparisons)
+  int block;             // sorted places of a block
+  int lanes;             // threads of a team
+  int slices;            // teams side by side that share a row's columns
 };
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortWidth = 9;       // bits of a digit at most: two digits up to 262142 tokens
 constexpr int kSortMaxCluster = 16;
-constexpr int kSortSmem = (kSortWarps + 1) * (1 << kSortWidth) * 4;
+constexpr int kSortFew = 1024;      // places that are sorted by comparisons
+constexpr int kSortSmem = (kSortWarps + 2) * (1 << kSortWidth) * 4;
+constexpr int kAbsentRows = kSortSmem * 8;   // rows of a stretch of the table: a bit each
 
-__device__ __forceinline__ void embed_cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+__device__ __forceinline__ unsigned embed_key(const EmbedGradParams& q, unsigned i) {
+  const long long id = q.ids[i];
+  return id >= 0 && id < q.vocab ? static_cast<unsigned>(id) : static_cast<unsigned>(q.vocab);
 }
 
-// A stable sort by digits from the lowest.  Warp w of the cluster holds places share w .. share (w + 1) - 1 and
-// counts their digits; where a digit's first place goes is the count of lower digits plus that of the same
-// digit in the warps before.
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradParams q) {
-  extern __shared__ unsigned sort_smem[];
+// One CTA, up to kSortFew places: a place's rank is the number of smaller (token, place).
+__device__ __forceinline__ void embed_sort_few(const EmbedGradParams& q, unsigned* smem) {
+  const unsigned i = threadIdx.x, n = static_cast<unsigned>(q.n);
+  smem[i] = i < n ? embed_key(q, i) : ~0u;
+  __syncthreads();
+  if (i >= n) return;
+  const unsigned key = smem[i];
+  unsigned rank = 0;
+  for (unsigned j = 0; j < n; j += 4) {
+    const uint4 k = *reinterpret_cast<const uint4*>(smem + j);
+    rank += (k.x < key || (k.x == key && j < i)) + (k.y < key || (k.y == key && j + 1 < i)) + (k.z < key || (k.z == key && j + 2 < i)) +
+            (k.w < key || (k.w == key && j + 3 < i));
+  }
+  if (ADAPT_IN_BOUNDS(rank, n, 51)) {
+    q.keys[1][rank] = key;   // (where an even number of passes leaves them)
+    q.places[1][rank] = i;
+  }
+}
+
+// By digits from the lowest.  Warp w of the cluster holds places share w .. share (w + 1) - 1 and counts their digits; a
+// digit's first place is the count of lower digits plus that of the same digit in the warps before.
+__device__ __forceinline__ void embed_sort_many(const EmbedGradParams& q, unsigned* smem, unsigned rank, unsigned parts) {
   __shared__ unsigned warp_sums[kSortWarps];
-  unsigned rank, parts;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned buckets = 1u << q.width;
-  unsigned* mine = sort_smem + warp * buckets;
-  unsigned* totals = sort_smem + kSortWarps * buckets;
+  unsigned* mine = smem + warp * buckets;
+  unsigned* totals = smem + kSortWarps * buckets;
+  unsigned* first = totals + buckets;
   const unsigned warps = parts * kSortWarps;
   const unsigned n = static_cast<unsigned>(q.n);
   const unsigned share = ((n + warps - 1) / warps + 31) & ~31u;
   const unsigned long long begin = static_cast<unsigned long long>(rank * kSortWarps + warp) * share;
   const unsigned from = begin < n ? static_cast<unsigned>(begin) : n, to = begin + share < n ? from + share : n;
-  const unsigned words = (static_cast<unsigned>(q.vocab) + 31) / 32;
-  for (unsigned i = rank * kSortThreads + threadIdx.x; i < words; i += parts * kSortThreads) q.present[i] = 0;
   for (int pass = 0; pass < q.passes; ++pass) {
     const unsigned* keys = q.keys[(pass + 1) & 1];
     const unsigned* places = q.places[(pass + 1) & 1];
     const int shift = pass * q.width;
-    auto key_at = [&](unsigned i) -> unsigned {
-      if (pass) return __ldcg(keys + i);
-      const long long id = q.ids[i];
-      return id >= 0 && id < q.vocab ? static_cast<unsigned>(id) : static_cast<unsigned>(q.vocab);
-    };
-    for (unsigned i = threadIdx.x; i < kSortWarps * buckets; i += kSortThreads) sort_smem[i] = 0;
+    auto key_at = [&](unsigned i) { return pass ? __ldcg(keys + i) : embed_key(q, i); };
+    for (unsigned i = threadIdx.x; i < kSortWarps * buckets / 4; i += kSortThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
+#pragma unroll 4
     for (unsigned i = from + lane; i < to; i += 32) atomicAdd(mine + ((key_at(i) >> shift) & (buckets - 1)), 1u);
     __syncthreads();
-    unsigned total = 0;
     if (threadIdx.x < buckets) {
+      unsigned count[kSortWarps], total = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWarps; ++w) count[w] = smem[w * buckets + threadIdx.x];
+#pragma unroll
       for (int w = 0; w < kSortWarps; ++w) {
-        const unsigned c = sort_smem[w * buckets + threadIdx.x];
-        sort_smem[w * buckets + threadIdx.x] = total;
-        total += c;
+        smem[w * buckets + threadIdx.x] = total;
+        total += count[w];
       }
       totals[threadIdx.x] = total;
     }
-    embed_cluster_sync();   // all totals are there (and, first, all bits are 0)
+    meet_cluster();   // all totals are there
     unsigned below = 0, all = 0;
     if (threadIdx.x < buckets) {
-      const unsigned at = static_cast<unsigned>(__cvta_generic_to_shared(totals + threadIdx.x));
+      const unsigned at = shared_address(totals + threadIdx.x);
+#pragma unroll 4
       for (unsigned r = 0; r < parts; ++r) {
-        unsigned a, c;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(at), "r"(r));
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(a) : "memory");
+        unsigned c;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(peer_address(at, r)) : "memory");
         if (r < rank) below += c;
         all += c;
       }
     }
     unsigned sum = all;   // running sum over the digits
+#pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const unsigned v = __shfl_up_sync(~0u, sum, d);
       if (lane >= d) sum += v;
@@ -176,6 +191,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradParam
     __syncthreads();
     if (warp == 0) {
       unsigned v = warp_sums[lane];
+#pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
         const unsigned w = __shfl_up_sync(~0u, v, d);
         if (lane >= d) v += w;
@@ -183,10 +199,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradParam
       warp_sums[lane] = v;
     }
     __syncthreads();
-    const unsigned first = sum - all + (warp ? warp_sums[warp - 1] : 0) + below;
-    if (threadIdx.x < buckets)
-      for (int w = 0; w < kSortWarps; ++w) sort_smem[w * buckets + threadIdx.x] += first;
-    embed_cluster_sync();   // the totals have been read; the CTA's first places are there
+    if (threadIdx.x < buckets) first[threadIdx.x] = sum - all + (warp ? warp_sums[warp - 1] : 0) + below;
+    __syncthreads();
     for (unsigned i = from; i < to; i += 32) {
       const unsigned at = i + lane;
       const bool live = at < to;
@@ -199,42 +213,88 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGradParam
       const unsigned peers = __match_any_sync(~0u, live ? digit : ~0u);
       const unsigned before = peers & ((1u << lane) - 1);
       unsigned goal = 0;
-      if (live) goal = mine[digit] + __popc(before);
+      if (live) goal = first[digit] + mine[digit] + __popc(before);
       __syncwarp();
       if (live && !before) mine[digit] += __popc(peers);
       __syncwarp();
-      if (live && ADAPT_IN_BOUNDS(goal, n, 40)) {
+      if (live && ADAPT_IN_BOUNDS(goal, n, 50)) {
         q.keys[pass & 1][goal] = key;
         q.places[pass & 1][goal] = place;
-        if (pass == 0 && key < static_cast<unsigned>(q.vocab)) atomicOr(q.present + (key >> 5), 1u << (key & 31));
       }
     }
-    embed_cluster_sync();   // what this pass wrote is there for the next
+    meet_cluster();   // what this pass wrote is there for the next, and its totals have been read
   }
 }
 
-// The first of the sorted places that holds `key`, which stands at place `at`.
-__device__ __forceinline__ int embed_first(const unsigned* keys, int at, unsigned key) {
-  int lo = 0, hi = at;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (keys[mid] < key) lo = mid + 1; else hi = mid;
+// 0 to every element of a row: whole 16-byte blocks, single elements at the ends.
+template <typename G>
+__device__ __forceinline__ void embed_blank(G* row, int dim, int lane) {
+  constexpr int V = 16 / sizeof(G);
+  const int skip = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(G));
+  for (int c = lane * V - skip; c < dim; c += 32 * V) {
+    if (c >= 0 && c + V <= dim) {
+      *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (c + k >= 0 && c + k < dim) row[c + k] = from_float<G>(0.0f);
+    }
   }
-  return lo;
 }
 
-// U parts of V columns for each thread, kEmbedThreads V apart.
-template <typename T, typename G, int V, int U>
+// The rows of tokens that do not occur, by every CTA from the `rank`-th on, `ctas` of them: a stretch of the table each,
+// a bit for each of its rows.
+template <typename G>
+__device__ __forceinline__ void embed_absent(const EmbedGradParams& q, unsigned* bits, int rank, int ctas) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = min(kAbsentRows, (q.vocab + ctas - 1) / ctas);
+  for (long long v0 = static_cast<long long>(rank) * per; v0 < q.vocab; v0 += static_cast<long long>(ctas) * per) {
+    const int rows = static_cast<int>(min(static_cast<long long>(per), q.vocab - v0));
+    __syncthreads();
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) bits[i] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int i = threadIdx.x; i < q.n; i += kSortThreads) {
+      const long long v = q.ids[i] - v0;
+      if (v >= 0 && v < rows) {
+        const unsigned bit = 1u << (v & 31);
+        if (!(reinterpret_cast<volatile unsigned*>(bits)[v >> 5] & bit)) atomicOr(bits + (v >> 5), bit);   // (frequent tokens are there already)
+      }
+    }
+    __syncthreads();
+    for (int v = warp; v < rows; v += kSortWarps)
+      if (!(bits[v >> 5] >> (v & 31) & 1)) embed_blank(static_cast<G*>(q.dtable) + (v0 + v) * q.ld_grad, q.dim, lane);
+  }
+}
+
+// The first cluster sorts; the others, if there are any, write rows of tokens that do not occur.
+template <typename G>
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedGradParams q) {
+  extern __shared__ __align__(16) unsigned sort_smem[];
+  let_next_kernel_start();
+  const unsigned parts = ctas_of_cluster();
+  const bool sorts = q.n > 0 && blockIdx.x < parts;
+  if (!sorts) {
+    const unsigned first = q.n > 0 ? parts : 0;
+    embed_absent<G>(q, sort_smem, blockIdx.x - first, gridDim.x - first);
+  } else if (q.passes == 0) {
+    embed_sort_few(q, sort_smem);
+  } else {
+    embed_sort_many(q, sort_smem, cta_in_cluster(), parts);
+  }
+}
+
+// U parts of V columns for each of a team's threads, lanes V apart.
+template <int V, int U>
 struct EmbedColumns {
-  int base;
-  int dim;
-  __device__ __forceinline__ EmbedColumns(int slice, int dim_) : base(slice * (kEmbedThreads * V * U) + static_cast<int>(threadIdx.x) * V), dim(dim_) {}
-  __device__ __forceinline__ int at(int u) const { return base + u * kEmbedThreads * V; }
+  int base, step, dim;
+  __device__ __forceinline__ EmbedColumns(int slice, int lane, int lanes, int dim_) : base((slice * lanes * U + lane) * V), step(lanes * V), dim(dim_) {}
+  __device__ __forceinline__ int at(int u) const { return base + u * step; }
   __device__ __forceinline__ bool in(int u) const { return at(u) < dim; }
 };
 
-template <typename T, typename G, int V, int U>
-__device__ __forceinline__ void embed_write(const EmbedGradParams& q, const EmbedColumns<T, G, V, U>& c, unsigned token, float (&sum)[U][V]) {
+template <typename G, int V, int U>
+__device__ __forceinline__ void embed_write(const EmbedGradParams& q, const EmbedColumns<V, U>& c, unsigned token, const float (&sum)[U][V]) {
   G* row = static_cast<G*>(q.dtable) + token * q.ld_grad;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -249,89 +309,135 @@ __device__ __forceinline__ void embed_write(const EmbedGradParams& q, const Embe
   }
 }
 
+constexpr int kEmbedBatch = 8;   // rows of dy that a thread has under way
+
+// Parts of rows as they lie in memory.
+template <typename T, int V> struct RawPart { typedef uint4 type; };
+template <typename T> struct RawPart<T, 1> { typedef T type; };
+template <typename T, int V>
+__device__ __forceinline__ void widen(const uint4& raw, float (&f)[V]) { unpack16<T>(raw, f); }
+template <typename T, int V>
+__device__ __forceinline__ void widen(const T& raw, float (&f)[1]) { f[0] = to_float(raw); }
+
 template <typename T, typename G, int V, int U>
-__global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(EmbedGradParams q) {
-  const int slice = blockIdx.x % q.slices, block = blockIdx.x / q.slices;
-  const EmbedColumns<T, G, V, U> c(slice, q.dim);
-  if (block >= q.token_ctas) {   // rows of tokens that do not occur
-    float zero[V] = {};
-    const int ctas = gridDim.x / q.slices - q.token_ctas;
-    for (int v = block - q.token_ctas; v < q.vocab; v += ctas) {
-      if (q.n && (q.present[v >> 5] >> (v & 31) & 1)) continue;
-      G* row = static_cast<G*>(q.dtable) + v * q.ld_grad;
+__global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGradParams q) {
+  extern __shared__ unsigned sorted[];   // tokens of the CTA's places, with one in front and one behind, then the places
+  typedef typename RawPart<T, V>::type Raw;
+  const int teams = kEmbedThreads / q.lanes, team = threadIdx.x / q.lanes;
+  const int slice = blockIdx.x % q.slices;
+  const long long cta_first = static_cast<long long>(blockIdx.x / q.slices) * teams * q.block;
+  const int count = static_cast<int>(min(static_cast<long long>(teams) * q.block, q.n - cta_first));
+  unsigned* keys = sorted + 1;
+  unsigned* places = sorted + teams * q.block + 2;
+  wait_for_previous_kernel();
+  {
+    const unsigned* all_keys = q.keys[(q.passes + 1) & 1] + cta_first;
+    const unsigned* all_places = q.places[(q.passes + 1) & 1] + cta_first;
+    for (int i = static_cast<int>(threadIdx.x) - 1; i <= count; i += kEmbedThreads) {
+      const long long p = cta_first + i;
+      keys[i] = p >= 0 && p < q.n ? all_keys[i] : ~0u;
+      if (i >= 0 && i < count) places[i] = all_places[i];
+    }
+  }
+  __syncthreads();
+  const int from = team * q.block, to = min(from + q.block, count);
+  if (from >= count) return;
+  const EmbedColumns<V, U> c(slice, threadIdx.x % q.lanes, q.lanes, q.dim);
+  float sum[U][V] = {};
+  int start = from;   // of the token at hand
+  float* partial = q.partial + 2 * (cta_first / q.block + team) * q.dim;
+  for (int i = from; i < to; i += kEmbedBatch) {
+    if (keys[i] >= static_cast<unsigned>(q.vocab)) return;   // places without a token, sorted to the end
+    Raw raw[kEmbedBatch][U];
+#pragma unroll
+    for (int j = 0; j < kEmbedBatch; ++j) {
+      if (i + j >= to || keys[i + j] >= static_cast<unsigned>(q.vocab) || !ADAPT_IN_BOUNDS(places[i + j], q.n, 52)) continue;
+      const T* row = static_cast<const T*>(q.dy) + places[i + j] * q.ld_dy;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (c.in(u)) store_part<G, V>(row + c.at(u), zero);
+        if (c.in(u)) raw[j][u] = __ldg(reinterpret_cast<const Raw*>(row + c.at(u)));
     }
-    return;
-  }
-  const unsigned* keys = q.keys[(q.passes + 1) & 1];
-  const unsigned* places = q.places[(q.passes + 1) & 1];
-  const int begin = block * q.chunk, end = min(begin + q.chunk, q.n);
-  int p = begin, first = begin;   // a piece's first place, its token's first place
-  unsigned key = keys[p];
-  if (p > 0 && keys[p - 1] == key) {   // a token that began in front: its first piece that begins here
-    first = embed_first(keys, p, key);
-    const int next = first + (p - first + q.piece - 1) / q.piece * q.piece;
-    if (next + q.piece <= q.n && keys[next + q.piece - 1] == key) p = next;
-    else while (p < q.n && keys[p] == key) ++p;   // (the piece in front takes the rest, fewer than a piece)
-  }
-  while (p < end) {
-    key = keys[p];
-    if (key >= static_cast<unsigned>(q.vocab)) return;   // places without a token, sorted to the end
-    if (p != begin && keys[p - 1] != key) first = p;
-    const bool more = p + 2 * q.piece <= q.n && keys[p + 2 * q.piece - 1] == key;
-    int stop = more ? p + q.piece : p + 1;
-    if (!more) while (stop < q.n && keys[stop] == key) ++stop;
-    float sum[U][V] = {};
-    for (int i = p; i < stop; ++i) {
-      const T* row = static_cast<const T*>(q.dy) + places[i] * q.ld_dy;
+#pragma unroll
+    for (int j = 0; j < kEmbedBatch; ++j) {
+      if (i + j >= to || keys[i + j] >= static_cast<unsigned>(q.vocab)) continue;
+      const unsigned key = keys[i + j];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (!c.in(u)) continue;
         float f[V];
-        load_part<T, V>(row + c.at(u), f);
+        widen<T, V>(raw[j][u], f);
+        if (c.in(u)) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) sum[u][k] += f[k];
+          for (int k = 0; k < V; ++k) sum[u][k] += f[k];
+        }
       }
-    }
-    if (more || p != first) {   // one of several pieces; those begin at least a piece apart
-      float* to = q.partial + static_cast<long long>(p / q.piece) * q.dim;
+      const bool ends = keys[i + j + 1] != key;
+      if (!ends && i + j + 1 < to) continue;
+      const bool began = start > from || keys[from - 1] != key;   // here, and not in the block in front
+      if (ends && began) {
+        embed_write<G, V, U>(q, c, key, sum);
+      } else {
+        float* half = partial + (began ? q.dim : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < V; ++k)
+            if (c.in(u)) half[c.at(u) + k] = sum[u][k];
+      }
+      start = i + j + 1;
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-          if (c.in(u)) to[c.at(u) + k] = sum[u][k];
-    } else {
-      embed_write<T, G, V, U>(q, c, key, sum);
+        for (int k = 0; k < V; ++k) sum[u][k] = 0.0f;
     }
-    p = stop;
   }
 }
 
-// Joins the pieces of a token that has several: the CTAs of block b look for a token that begins in places
-// b piece .. (b + 1) piece - 1 and has two pieces at least (there is one at most).
-template <typename T, typename G, int V, int U>
-__global__ __launch_bounds__(kEmbedThreads) void embed_join_kernel(EmbedGradParams q) {
-  const int slice = blockIdx.x % q.slices, block = blockIdx.x / q.slices;
+// A CTA looks whether a token that begins in block b goes on, and joins 128 of its columns: the warps take the
+// blocks behind in turn.
+constexpr int kJoinWarps = 8;
+constexpr int kJoinColumns = 128;
+
+template <typename G>
+__global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const EmbedGradParams q) {
+  __shared__ float part[kJoinWarps][kJoinColumns];
+  const int slices = (q.dim + kJoinColumns - 1) / kJoinColumns, slice = blockIdx.x % slices;
+  const long long b = blockIdx.x / slices, end = (b + 1) * q.block;
+  wait_for_previous_kernel();
   const unsigned* keys = q.keys[(q.passes + 1) & 1];
-  const int end = min((block + 1) * q.piece, q.n);
-  // the token of the block's last place is the only one that can reach a piece beyond
-  const unsigned key = keys[end - 1];
-  if (key >= static_cast<unsigned>(q.vocab)) return;
-  const int first = embed_first(keys, end - 1, key);
-  if (first < block * q.piece || first + 2 * q.piece > q.n || keys[first + 2 * q.piece - 1] != key) return;
-  const EmbedColumns<T, G, V, U> c(slice, q.dim);
-  float sum[U][V] = {};
-  for (int p = first; p + q.piece <= q.n && keys[p + q.piece - 1] == key; p += q.piece) {
-    const float* from = q.partial + static_cast<long long>(p / q.piece) * q.dim;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (c.in(u)) sum[u][k] += from[c.at(u) + k];
+  if (end >= q.n) return;
+  const unsigned key = keys[end];
+  if (key >= static_cast<unsigned>(q.vocab) || keys[end - 1] != key) return;
+  if (b > 0 && keys[b * q.block - 1] == key) return;   // (it began further in front)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // the blocks behind that begin with the token
+  const long long blocks = (q.n + q.block - 1) / q.block - b - 1;
+  long long count = 1;
+  for (bool more = true; more;) {
+    const long long j = count + lane;
+    const unsigned on = __ballot_sync(~0u, j < blocks && keys[end + j * q.block] == key);
+    more = on == ~0u;
+    count += more ? 32 : __ffs(~on) - 1;
   }
-  embed_write<T, G, V, U>(q, c, key, sum);
+  float sum[4] = {};
+  const int c0 = slice * kJoinColumns + lane;   // columns 32 apart
+  const float* from = q.partial + 2 * (b + 1) * q.dim;
+#pragma unroll 4
+  for (long long j = warp; j < count; j += kJoinWarps)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c0 + 32 * k < q.dim) sum[k] += __ldcg(from + 2 * j * q.dim + c0 + 32 * k);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) part[warp][lane + 32 * k] = sum[k];
+  __syncthreads();
+  const int c = slice * kJoinColumns + threadIdx.x;
+  if (threadIdx.x >= kJoinColumns || c >= q.dim) return;
+  float total = q.partial[(2 * b + 1) * q.dim + c];
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) total += part[w][threadIdx.x];
+  total *= q.scale;
+  G* to = static_cast<G*>(q.dtable) + key * q.ld_grad + c;
+  if (q.accumulate) total += to_float(*to);
+  *to = from_float<G>(total);
 }
 
 }  // namespace adapt
