@@ -16,17 +16,24 @@ constexpr int kSms = 148;   // of a B200
 
 bool in_int(int64_t v, int64_t least) { return v >= least && v <= 0x7FFFFFFF; }
 
-// Sorted places of a block: two rows of sums in fp32 at most go to memory and back for the block's rows of dy, and a
-// thousand blocks or so keep the device busy.
-int embed_block(int64_t n) { return n <= (1 << 15) ? 32 : n <= (1 << 17) ? 64 : 128; }
+// Sorted places of a block: as many blocks as fill the device six times over with CTAs of 256 threads of 16 bytes, while
+// two rows of sums in fp32 at most go to memory and back for each block.
+int embed_block(int64_t n, int64_t dim) {
+  const int64_t threads = std::min<int64_t>(kEmbedThreads, std::max<int64_t>(8, dim / 8));
+  int block = 8;
+  while (block < 128 && n * threads >= 2ll * block * kEmbedThreads * kSms * 6) block *= 2;
+  return block;
+}
 
 struct EmbedLayout {
-  size_t keys[2], places[2], partial, bytes;
+  size_t keys[2], places[2], joins, partial, bytes;
   EmbedLayout(int64_t n, int64_t dim) {
     size_t at = 0;
     auto take = [&](size_t b) { const size_t here = at; at = align_up(at + b, 256); return here; };
     for (int i = 0; i < 2; ++i) { keys[i] = take(4 * n); places[i] = take(4 * n); }
-    partial = take((n + embed_block(n) - 1) / embed_block(n) * 2 * dim * 4);
+    const int64_t blocks = (n + embed_block(n, dim) - 1) / embed_block(n, dim);
+    joins = take(4 * (blocks + 1));
+    partial = take(blocks * 2 * dim * 4);
     bytes = at;
   }
 };
@@ -98,7 +105,7 @@ int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_ta
                    (n == 1 || ld_out % wide == 0);
   const int64_t parts = vec ? dim / wide : dim;
   int lanes = 1;
-  while (lanes < kEmbedThreads && lanes * 4 < parts) lanes *= 2;
+  while (lanes < kEmbedThreads && lanes * kEmbedChunks < parts) lanes *= 2;
   const int rows = kEmbedThreads / lanes;
   const unsigned grid = static_cast<unsigned>((n + rows - 1) / rows);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
@@ -142,12 +149,13 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
     q.keys[i] = reinterpret_cast<unsigned*>(ws + lay.keys[i]);
     q.places[i] = reinterpret_cast<unsigned*>(ws + lay.places[i]);
   }
+  q.joins = reinterpret_cast<unsigned*>(ws + lay.joins);
   q.partial = reinterpret_cast<float*>(ws + lay.partial);
   int bits = 1;
   while (bits < 32 && (vocab >> bits)) ++bits;
   q.passes = n <= kSortFew ? 0 : (bits + kSortWidth - 1) / kSortWidth;
   q.width = q.passes ? (bits + q.passes - 1) / q.passes : 0;
-  q.block = embed_block(n);
+  q.block = embed_block(n, dim);
   const int wide = 16 / e;
   const bool vec = dim % wide == 0 && !misaligned(dy, 16) && !misaligned(dtable, 16) && (n <= 1 || ld_dy % wide == 0) &&
                    (vocab == 1 || ld_grad % wide == 0);
@@ -156,9 +164,8 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
   while (q.lanes < kEmbedThreads && q.lanes < parts_of_row) q.lanes *= 2;
   q.slices = static_cast<int>((parts_of_row + q.lanes - 1) / q.lanes);
   const int teams = kEmbedThreads / q.lanes;
-  const int64_t blocks = (n + q.block - 1) / q.block, sums = (blocks + teams - 1) / teams * q.slices,
-                joins = blocks * ((dim + kJoinColumns - 1) / kJoinColumns);
-  if (sums > 0x7FFFFFFF || joins > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
+  const int64_t blocks = (n + q.block - 1) / q.block, sums = (blocks + teams - 1) / teams * q.slices;
+  if (sums > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   int rc = ADAPT_OK;
   with_type(dtype, [&](auto t) {
@@ -196,6 +203,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
         if (err != cudaSuccess) { rc = cuda_fail(err, "token embedding, backward"); return; }
       }
       if (blocks > 1) {
+        const int64_t joins = std::min<int64_t>(kSms * 4, blocks * ((dim + kJoinColumns - 1) / kJoinColumns));
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
         const cudaError_t err = launch_behind(embed_join_kernel<G>, static_cast<unsigned>(joins), 32 * kJoinWarps, 0, stream, q);
         if (err != cudaSuccess) rc = cuda_fail(err, "token embedding, joined sums");

@@ -53,6 +53,7 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[V]) {
 
 // `lanes` threads (a power of two, up to the CTA) take a row; V elements at a time.
 constexpr int kEmbedThreads = 256;
+constexpr int kEmbedChunks = 4;   // that a thread has under way
 
 template <typename T, int V>
 __global__ __launch_bounds__(kEmbedThreads) void embedding_kernel(EmbedParams q, int lanes) {
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embedding_kernel(EmbedParams q,
   const T* row = static_cast<const T*>(q.table) + (id >= 0 && id < q.vocab ? id : 0) * q.ld_table;
   const float fill = id < 0 ? 0.0f : __int_as_float(0x7FC00000);
   const bool known = id >= 0 && id < q.vocab;
-  constexpr int kUnroll = 4;
+  constexpr int kUnroll = kEmbedChunks;
   for (int at = lane * V; at < q.dim; at += lanes * V * kUnroll) {
     float f[kUnroll][V];
 #pragma unroll
@@ -95,6 +96,7 @@ struct EmbedGradParams {
   bool accumulate;
   unsigned* keys[2];     // [n] tokens (vocab: none)
   unsigned* places[2];   // [n] their places
+  unsigned* joins;       // their number, then the blocks in which a token begins that goes on behind them
   float* partial;        // [blocks][2][dim] sums of a block's first token, which began in front, and of its last, which goes on
   int width, passes;     // digits of the sort (passes 0: by comparisons)
   int block;             // sorted places of a block
@@ -104,7 +106,8 @@ struct EmbedGradParams {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortWidth = 9;       // bits of a digit at most: two digits up to 262142 tokens
+constexpr int kSortWidth = 10;      // bits of a digit at most: two digits up to a million tokens
+constexpr int kSortHeld = 4;        // places of a lane that are held in registers
 constexpr int kSortMaxCluster = 16;
 constexpr int kSortFew = 1024;      // places that are sorted by comparisons
 constexpr int kSortSmem = (kSortWarps + 2) * (1 << kSortWidth) * 4;
@@ -153,10 +156,20 @@ __device__ __forceinline__ void embed_sort_many(const EmbedGradParams& q, unsign
     const unsigned* places = q.places[(pass + 1) & 1];
     const int shift = pass * q.width;
     auto key_at = [&](unsigned i) { return pass ? __ldcg(keys + i) : embed_key(q, i); };
+    unsigned held_key[kSortHeld], held_place[kSortHeld];   // the warp's first places, loaded at once
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k) {
+      const unsigned i = from + k * 32 + lane;
+      held_key[k] = i < to ? key_at(i) : 0;
+      held_place[k] = i < to ? (pass ? __ldcg(places + i) : i) : 0;
+    }
     for (unsigned i = threadIdx.x; i < kSortWarps * buckets / 4; i += kSortThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k)
+      if (from + k * 32 + lane < to) atomicAdd(mine + ((held_key[k] >> shift) & (buckets - 1)), 1u);
 #pragma unroll 4
-    for (unsigned i = from + lane; i < to; i += 32) atomicAdd(mine + ((key_at(i) >> shift) & (buckets - 1)), 1u);
+    for (unsigned i = from + kSortHeld * 32 + lane; i < to; i += 32) atomicAdd(mine + ((key_at(i) >> shift) & (buckets - 1)), 1u);
     __syncthreads();
     if (threadIdx.x < buckets) {
       unsigned count[kSortWarps], total = 0;
@@ -201,14 +214,7 @@ __device__ __forceinline__ void embed_sort_many(const EmbedGradParams& q, unsign
     __syncthreads();
     if (threadIdx.x < buckets) first[threadIdx.x] = sum - all + (warp ? warp_sums[warp - 1] : 0) + below;
     __syncthreads();
-    for (unsigned i = from; i < to; i += 32) {
-      const unsigned at = i + lane;
-      const bool live = at < to;
-      unsigned key = 0, place = 0;
-      if (live) {
-        key = key_at(at);
-        place = pass ? __ldcg(places + at) : at;
-      }
+    auto put = [&](bool live, unsigned key, unsigned place) {
       const unsigned digit = (key >> shift) & (buckets - 1);
       const unsigned peers = __match_any_sync(~0u, live ? digit : ~0u);
       const unsigned before = peers & ((1u << lane) - 1);
@@ -221,6 +227,22 @@ __device__ __forceinline__ void embed_sort_many(const EmbedGradParams& q, unsign
         q.keys[pass & 1][goal] = key;
         q.places[pass & 1][goal] = place;
       }
+    };
+#pragma unroll
+    for (int k = 0; k < kSortHeld; ++k)
+      if (from + k * 32 < to) put(from + k * 32 + lane < to, held_key[k], held_place[k]);
+    unsigned key = 0, place = 0;
+    auto load = [&](unsigned i) {
+      if (i < to) {
+        key = key_at(i);
+        place = pass ? __ldcg(places + i) : i;
+      }
+    };
+    load(from + kSortHeld * 32 + lane);
+    for (unsigned i = from + kSortHeld * 32; i < to; i += 32) {
+      const unsigned this_key = key, this_place = place;
+      load(i + 32 + lane);
+      put(i + lane < to, this_key, this_place);
     }
     meet_cluster();   // what this pass wrote is there for the next, and its totals have been read
   }
@@ -274,6 +296,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedGra
   let_next_kernel_start();
   const unsigned parts = ctas_of_cluster();
   const bool sorts = q.n > 0 && blockIdx.x < parts;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && q.n > 0) *q.joins = 0;
   if (!sorts) {
     const unsigned first = q.n > 0 ? parts : 0;
     embed_absent<G>(q, sort_smem, blockIdx.x - first, gridDim.x - first);
@@ -293,6 +316,22 @@ struct EmbedColumns {
   __device__ __forceinline__ bool in(int u) const { return at(u) < dim; }
 };
 
+// V elements of a gradient's row, in the types' 16 or 32 bytes.
+template <typename G, int V>
+__device__ __forceinline__ void load_row(const G* p, float (&f)[V]) {
+  if constexpr (V == 1) {
+    f[0] = to_float(*p);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; k += 16 / sizeof(G)) {
+      float part[16 / sizeof(G)];
+      unpack16<G>(*reinterpret_cast<const uint4*>(p + k), part);
+#pragma unroll
+      for (int j = 0; j < 16 / static_cast<int>(sizeof(G)); ++j) f[k + j] = part[j];
+    }
+  }
+}
+
 template <typename G, int V, int U>
 __device__ __forceinline__ void embed_write(const EmbedGradParams& q, const EmbedColumns<V, U>& c, unsigned token, const float (&sum)[U][V]) {
   G* row = static_cast<G*>(q.dtable) + token * q.ld_grad;
@@ -300,11 +339,14 @@ __device__ __forceinline__ void embed_write(const EmbedGradParams& q, const Embe
   for (int u = 0; u < U; ++u) {
     if (!c.in(u)) continue;
     float f[V];
+    if (q.accumulate) {
+      load_row<G, V>(row + c.at(u), f);
+    } else {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      f[k] = sum[u][k] * q.scale;
-      if (q.accumulate) f[k] += to_float(row[c.at(u) + k]);
+      for (int k = 0; k < V; ++k) f[k] = 0.0f;
     }
+#pragma unroll
+    for (int k = 0; k < V; ++k) f[k] += sum[u][k] * q.scale;
     store_part<G, V>(row + c.at(u), f);
   }
 }
@@ -320,7 +362,7 @@ template <typename T, int V>
 __device__ __forceinline__ void widen(const T& raw, float (&f)[1]) { f[0] = to_float(raw); }
 
 template <typename T, typename G, int V, int U>
-__global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGradParams q) {
+__global__ __launch_bounds__(kEmbedThreads, 3) void embed_sum_kernel(const EmbedGradParams q) {
   extern __shared__ unsigned sorted[];   // tokens of the CTA's places, with one in front and one behind, then the places
   typedef typename RawPart<T, V>::type Raw;
   const int teams = kEmbedThreads / q.lanes, team = threadIdx.x / q.lanes;
@@ -356,6 +398,8 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (c.in(u)) raw[j][u] = __ldg(reinterpret_cast<const Raw*>(row + c.at(u)));
+      if (q.accumulate && keys[i + j + 1] != keys[i + j] && c.in(0))   // what the sum will be added to
+        asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const G*>(q.dtable) + keys[i + j] * q.ld_grad + c.at(0)));
     }
 #pragma unroll
     for (int j = 0; j < kEmbedBatch; ++j) {
@@ -376,6 +420,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
       if (ends && began) {
         embed_write<G, V, U>(q, c, key, sum);
       } else {
+        if (began && c.base == 0) q.joins[1 + atomicAdd(q.joins, 1u)] = static_cast<unsigned>(cta_first / q.block) + team;
         float* half = partial + (began ? q.dim : 0);
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -392,52 +437,55 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   }
 }
 
-// A CTA looks whether a token that begins in block b goes on, and joins 128 of its columns: the warps take the
-// blocks behind in turn.
+// Joins the sums of tokens that go on beyond the block in which they begin: a CTA takes 128 columns of one after the other,
+// its warps the blocks behind in turn.
 constexpr int kJoinWarps = 8;
 constexpr int kJoinColumns = 128;
 
 template <typename G>
 __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const EmbedGradParams q) {
   __shared__ float part[kJoinWarps][kJoinColumns];
-  const int slices = (q.dim + kJoinColumns - 1) / kJoinColumns, slice = blockIdx.x % slices;
-  const long long b = blockIdx.x / slices, end = (b + 1) * q.block;
+  const unsigned slices = (q.dim + kJoinColumns - 1) / kJoinColumns;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   wait_for_previous_kernel();
   const unsigned* keys = q.keys[(q.passes + 1) & 1];
-  if (end >= q.n) return;
-  const unsigned key = keys[end];
-  if (key >= static_cast<unsigned>(q.vocab) || keys[end - 1] != key) return;
-  if (b > 0 && keys[b * q.block - 1] == key) return;   // (it began further in front)
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // the blocks behind that begin with the token
-  const long long blocks = (q.n + q.block - 1) / q.block - b - 1;
-  long long count = 1;
-  for (bool more = true; more;) {
-    const long long j = count + lane;
-    const unsigned on = __ballot_sync(~0u, j < blocks && keys[end + j * q.block] == key);
-    more = on == ~0u;
-    count += more ? 32 : __ffs(~on) - 1;
-  }
-  float sum[4] = {};
-  const int c0 = slice * kJoinColumns + lane;   // columns 32 apart
-  const float* from = q.partial + 2 * (b + 1) * q.dim;
+  const unsigned long long items = static_cast<unsigned long long>(*q.joins) * slices;
+  for (unsigned long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const int slice = static_cast<int>(item % slices);
+    const long long b = q.joins[1 + item / slices], end = (b + 1) * q.block;
+    const unsigned key = keys[end];
+    // the blocks behind that begin with the token: it is the first of those
+    const long long blocks = (q.n + q.block - 1) / q.block - b - 1;
+    long long count = 1;
+    for (bool more = true; more;) {
+      const long long j = count + lane;
+      const unsigned on = __ballot_sync(~0u, j < blocks && keys[end + j * q.block] == key);
+      more = on == ~0u;
+      count += more ? 32 : __ffs(~on) - 1;
+    }
+    float sum[4] = {};
+    const int c0 = slice * kJoinColumns + lane;   // columns 32 apart
+    const float* from = q.partial + 2 * (b + 1) * q.dim;
 #pragma unroll 4
-  for (long long j = warp; j < count; j += kJoinWarps)
+    for (long long j = warp; j < count; j += kJoinWarps)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (c0 + 32 * k < q.dim) sum[k] += __ldcg(from + 2 * j * q.dim + c0 + 32 * k);
+      for (int k = 0; k < 4; ++k)
+        if (c0 + 32 * k < q.dim) sum[k] += __ldcg(from + 2 * j * q.dim + c0 + 32 * k);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) part[warp][lane + 32 * k] = sum[k];
-  __syncthreads();
-  const int c = slice * kJoinColumns + threadIdx.x;
-  if (threadIdx.x >= kJoinColumns || c >= q.dim) return;
-  float total = q.partial[(2 * b + 1) * q.dim + c];
+    for (int k = 0; k < 4; ++k) part[warp][lane + 32 * k] = sum[k];
+    __syncthreads();
+    const int c = slice * kJoinColumns + threadIdx.x;
+    if (threadIdx.x < kJoinColumns && c < q.dim) {
+      float total = q.partial[(2 * b + 1) * q.dim + c];
 #pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) total += part[w][threadIdx.x];
-  total *= q.scale;
-  G* to = static_cast<G*>(q.dtable) + key * q.ld_grad + c;
-  if (q.accumulate) total += to_float(*to);
-  *to = from_float<G>(total);
+      for (int w = 0; w < kJoinWarps; ++w) total += part[w][threadIdx.x];
+      total *= q.scale;
+      G* to = static_cast<G*>(q.dtable) + key * q.ld_grad + c;
+      if (q.accumulate) total += to_float(*to);
+      *to = from_float<G>(total);
+    }
+    __syncthreads();
+  }
 }
 
 }  // namespace adapt
