@@ -16,13 +16,23 @@ constexpr int kSms = 148;   // of a B200
 
 bool in_int(int64_t v, int64_t least) { return v >= least && v <= 0x7FFFFFFF; }
 
-// Sorted places of a block: as many blocks as fill the device six times over with CTAs of 256 threads of 16 bytes, while
-// two rows of sums in fp32 at most go to memory and back for each block.
+// How the rows of a gradient are dealt out: CTAs of `teams` teams of `lanes` threads, `slices` of them for a row.
+struct EmbedTeams {
+  int lanes = 8, teams, slices;
+  EmbedTeams(int64_t dim, int per_thread) {
+    const int64_t threads = (dim + per_thread - 1) / per_thread;
+    while (lanes < kEmbedThreads && lanes < threads) lanes *= 2;
+    teams = kEmbedThreads / lanes;
+    slices = static_cast<int>((threads + lanes - 1) / lanes);
+  }
+};
+
+// Sorted places of a block: so many that three CTAs an SM take all of them at once, but kStageRows at least.  Two rows
+// of sums in fp32 at most go to memory and back for a block.  (By the teams of 16-bit rows, whatever the type.)
 int embed_block(int64_t n, int64_t dim) {
-  const int64_t threads = std::min<int64_t>(kEmbedThreads, std::max<int64_t>(8, dim / 8));
-  int block = 8;
-  while (block < 128 && n * threads >= 2ll * block * kEmbedThreads * kSms * 6) block *= 2;
-  return block;
+  const EmbedTeams t(dim, 8);
+  const int64_t places = 3ll * kSms * t.teams, most = 8192 / t.teams;   // (64 KB of tokens and places)
+  return static_cast<int>(std::min(most, std::max<int64_t>(kStageRows, (n * t.slices + places - 1) / places)));
 }
 
 struct EmbedLayout {
@@ -32,7 +42,7 @@ struct EmbedLayout {
     auto take = [&](size_t b) { const size_t here = at; at = align_up(at + b, 256); return here; };
     for (int i = 0; i < 2; ++i) { keys[i] = take(4 * n); places[i] = take(4 * n); }
     const int64_t blocks = (n + embed_block(n, dim) - 1) / embed_block(n, dim);
-    joins = take(4 * (blocks + 1));
+    joins = take(8 * (blocks + 1));
     partial = take(blocks * 2 * dim * 4);
     bytes = at;
   }
@@ -149,7 +159,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
     q.keys[i] = reinterpret_cast<unsigned*>(ws + lay.keys[i]);
     q.places[i] = reinterpret_cast<unsigned*>(ws + lay.places[i]);
   }
-  q.joins = reinterpret_cast<unsigned*>(ws + lay.joins);
+  q.joins = reinterpret_cast<uint2*>(ws + lay.joins);
   q.partial = reinterpret_cast<float*>(ws + lay.partial);
   int bits = 1;
   while (bits < 32 && (vocab >> bits)) ++bits;
@@ -159,12 +169,10 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
   const int wide = 16 / e;
   const bool vec = dim % wide == 0 && !misaligned(dy, 16) && !misaligned(dtable, 16) && (n <= 1 || ld_dy % wide == 0) &&
                    (vocab == 1 || ld_grad % wide == 0);
-  const int64_t columns = vec ? wide : 4, parts_of_row = (dim + columns - 1) / columns;   // of a thread
-  q.lanes = 8;
-  while (q.lanes < kEmbedThreads && q.lanes < parts_of_row) q.lanes *= 2;
-  q.slices = static_cast<int>((parts_of_row + q.lanes - 1) / q.lanes);
-  const int teams = kEmbedThreads / q.lanes;
-  const int64_t blocks = (n + q.block - 1) / q.block, sums = (blocks + teams - 1) / teams * q.slices;
+  const EmbedTeams team(dim, wide);
+  q.lanes = team.lanes; q.slices = team.slices;
+  q.slot = team.lanes * 16 + (vec ? 0 : 16);
+  const int64_t blocks = (n + q.block - 1) / q.block, sums = (blocks + team.teams - 1) / team.teams * team.slices;
   if (sums > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);
   int rc = ADAPT_OK;
@@ -172,7 +180,6 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
     using T = decltype(t);
     auto go = [&](auto g) {
       using G = decltype(g);
-      constexpr int V = 16 / sizeof(T);
       int parts = 1, clusters = 1;
       while (q.passes && parts < kSortMaxCluster && n > 1024ll * parts) parts *= 2;
       if ((rc = sort_clusters<G>(parts, &clusters)) != ADAPT_OK) return;
@@ -195,15 +202,22 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
         if (err != cudaSuccess) { rc = cuda_fail(err, "sort of tokens"); return; }
       }
       if (n == 0) return;
-      const int smem = (2 * teams * q.block + 2) * 4;
+      const int64_t smem = 2ll * team.teams * kStageRows * q.slot + (2ll * team.teams * q.block + 2) * 4;
+      if (smem > 220 * 1024) { rc = ADAPT_ERR_INVALID_ARG; return; }   // (never: embed_block has a limit)
       {
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
-        const cudaError_t err = vec ? launch_behind(embed_sum_kernel<T, G, V, 1>, static_cast<unsigned>(sums), kEmbedThreads, smem, stream, q)
-                                    : launch_behind(embed_sum_kernel<T, G, 1, 4>, static_cast<unsigned>(sums), kEmbedThreads, smem, stream, q);
+        auto sum = [&](auto kernel) {
+          if (smem > 48 * 1024) {
+            const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+            if (err != cudaSuccess) return err;
+          }
+          return launch_behind(kernel, static_cast<unsigned>(sums), kEmbedThreads, static_cast<int>(smem), stream, q);
+        };
+        const cudaError_t err = vec ? sum(embed_sum_kernel<T, G, true>) : sum(embed_sum_kernel<T, G, false>);
         if (err != cudaSuccess) { rc = cuda_fail(err, "token embedding, backward"); return; }
       }
       if (blocks > 1) {
-        const int64_t joins = std::min<int64_t>(kSms * 4, blocks * ((dim + kJoinColumns - 1) / kJoinColumns));
+        const int64_t joins = std::min<int64_t>(kSms * 16, blocks * ((dim + kJoinColumns - 1) / kJoinColumns));
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
         const cudaError_t err = launch_behind(embed_join_kernel<G>, static_cast<unsigned>(joins), 32 * kJoinWarps, 0, stream, q);
         if (err != cudaSuccess) rc = cuda_fail(err, "token embedding, joined sums");

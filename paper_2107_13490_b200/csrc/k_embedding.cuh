@@ -96,12 +96,13 @@ struct EmbedGradParams {
   bool accumulate;
   unsigned* keys[2];     // [n] tokens (vocab: none)
   unsigned* places[2];   // [n] their places
-  unsigned* joins;       // their number, then the blocks in which a token begins that goes on behind them
+  uint2* joins;          // their number, then the blocks in which a token begins that goes on behind them, and the token
   float* partial;        // [blocks][2][dim] sums of a block's first token, which began in front, and of its last, which goes on
   int width, passes;     // digits of the sort (passes 0: by comparisons)
   int block;             // sorted places of a block
   int lanes;             // threads of a team
   int slices;            // teams side by side that share a row's columns
+  int slot;              // bytes of a row in a stage
 };
 
 constexpr int kSortThreads = 1024;
@@ -296,7 +297,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedGra
   let_next_kernel_start();
   const unsigned parts = ctas_of_cluster();
   const bool sorts = q.n > 0 && blockIdx.x < parts;
-  if (blockIdx.x == 0 && threadIdx.x == 0 && q.n > 0) *q.joins = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && q.n > 0) q.joins->x = 0;
   if (!sorts) {
     const unsigned first = q.n > 0 ? parts : 0;
     embed_absent<G>(q, sort_smem, blockIdx.x - first, gridDim.x - first);
@@ -306,15 +307,6 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const EmbedGra
     embed_sort_many(q, sort_smem, cta_in_cluster(), parts);
   }
 }
-
-// U parts of V columns for each of a team's threads, lanes V apart.
-template <int V, int U>
-struct EmbedColumns {
-  int base, step, dim;
-  __device__ __forceinline__ EmbedColumns(int slice, int lane, int lanes, int dim_) : base((slice * lanes * U + lane) * V), step(lanes * V), dim(dim_) {}
-  __device__ __forceinline__ int at(int u) const { return base + u * step; }
-  __device__ __forceinline__ bool in(int u) const { return at(u) < dim; }
-};
 
 // V elements of a gradient's row, in the types' 16 or 32 bytes.
 template <typename G, int V>
@@ -332,45 +324,31 @@ __device__ __forceinline__ void load_row(const G* p, float (&f)[V]) {
   }
 }
 
-template <typename G, int V, int U>
-__device__ __forceinline__ void embed_write(const EmbedGradParams& q, const EmbedColumns<V, U>& c, unsigned token, const float (&sum)[U][V]) {
-  G* row = static_cast<G*>(q.dtable) + token * q.ld_grad;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (!c.in(u)) continue;
-    float f[V];
-    if (q.accumulate) {
-      load_row<G, V>(row + c.at(u), f);
-    } else {
-#pragma unroll
-      for (int k = 0; k < V; ++k) f[k] = 0.0f;
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k) f[k] += sum[u][k] * q.scale;
-    store_part<G, V>(row + c.at(u), f);
-  }
-}
+// A team of threads sums over the rows of its block, V elements a thread; CTAs of 256 threads hold one team or several.
+// Rows come through two stages in shared memory, kStageRows of each team's, which bulk copies fill ahead: whole rows under
+// way cost neither registers nor instructions.  Rows between 16-byte boundaries (kAligned false) are copied with the
+// aligned blocks around them and read element by element, V of them `lanes` apart.
+constexpr int kStageRows = 8;
 
-constexpr int kEmbedBatch = 8;   // rows of dy that a thread has under way
-
-// Parts of rows as they lie in memory.
-template <typename T, int V> struct RawPart { typedef uint4 type; };
-template <typename T> struct RawPart<T, 1> { typedef T type; };
-template <typename T, int V>
-__device__ __forceinline__ void widen(const uint4& raw, float (&f)[V]) { unpack16<T>(raw, f); }
-template <typename T, int V>
-__device__ __forceinline__ void widen(const T& raw, float (&f)[1]) { f[0] = to_float(raw); }
-
-template <typename T, typename G, int V, int U>
-__global__ __launch_bounds__(kEmbedThreads, 3) void embed_sum_kernel(const EmbedGradParams q) {
-  extern __shared__ unsigned sorted[];   // tokens of the CTA's places, with one in front and one behind, then the places
-  typedef typename RawPart<T, V>::type Raw;
-  const int teams = kEmbedThreads / q.lanes, team = threadIdx.x / q.lanes;
-  const int slice = blockIdx.x % q.slices;
+template <typename T, typename G, bool kAligned>
+__global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGradParams q) {
+  constexpr int V = 16 / static_cast<int>(sizeof(T));
+  extern __shared__ __align__(128) unsigned char embed_smem[];
+  __shared__ __align__(8) unsigned long long bars[2];
+  const int teams = kEmbedThreads / q.lanes, team = threadIdx.x / q.lanes, lane = threadIdx.x % q.lanes, warp_lane = threadIdx.x & 31;
+  const int slice = blockIdx.x % q.slices, first_column = slice * q.lanes * V, columns = min(q.dim - first_column, q.lanes * V);
   const long long cta_first = static_cast<long long>(blockIdx.x / q.slices) * teams * q.block;
   const int count = static_cast<int>(min(static_cast<long long>(teams) * q.block, q.n - cta_first));
-  unsigned* keys = sorted + 1;
-  unsigned* places = sorted + teams * q.block + 2;
+  const int stage_bytes = teams * kStageRows * q.slot;
+  // tokens of the CTA's places, with one in front and one behind, then the places
+  unsigned* keys = reinterpret_cast<unsigned*>(embed_smem + 2 * stage_bytes) + 1;
+  unsigned* places = keys + teams * q.block + 1;
+  const unsigned full = shared_address(bars), vocab = static_cast<unsigned>(q.vocab);
+  if (threadIdx.x == 0) {
+    barrier_init(full, 1);
+    barrier_init(full + 8, 1);
+    barrier_init_fence();
+  }
   wait_for_previous_kernel();
   {
     const unsigned* all_keys = q.keys[(q.passes + 1) & 1] + cta_first;
@@ -382,64 +360,102 @@ __global__ __launch_bounds__(kEmbedThreads, 3) void embed_sum_kernel(const Embed
     }
   }
   __syncthreads();
-  const int from = team * q.block, to = min(from + q.block, count);
-  if (from >= count) return;
-  const EmbedColumns<V, U> c(slice, threadIdx.x % q.lanes, q.lanes, q.dim);
-  float sum[U][V] = {};
-  int start = from;   // of the token at hand
-  float* partial = q.partial + 2 * (cta_first / q.block + team) * q.dim;
-  for (int i = from; i < to; i += kEmbedBatch) {
-    if (keys[i] >= static_cast<unsigned>(q.vocab)) return;   // places without a token, sorted to the end
-    Raw raw[kEmbedBatch][U];
-#pragma unroll
-    for (int j = 0; j < kEmbedBatch; ++j) {
-      if (i + j >= to || keys[i + j] >= static_cast<unsigned>(q.vocab) || !ADAPT_IN_BOUNDS(places[i + j], q.n, 52)) continue;
-      const T* row = static_cast<const T*>(q.dy) + places[i + j] * q.ld_dy;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c.in(u)) raw[j][u] = __ldg(reinterpret_cast<const Raw*>(row + c.at(u)));
-      if (q.accumulate && keys[i + j + 1] != keys[i + j] && c.in(0))   // what the sum will be added to
-        asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const G*>(q.dtable) + keys[i + j] * q.ld_grad + c.at(0)));
-    }
-#pragma unroll
-    for (int j = 0; j < kEmbedBatch; ++j) {
-      if (i + j >= to || keys[i + j] >= static_cast<unsigned>(q.vocab)) continue;
-      const unsigned key = keys[i + j];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float f[V];
-        widen<T, V>(raw[j][u], f);
-        if (c.in(u)) {
-#pragma unroll
-          for (int k = 0; k < V; ++k) sum[u][k] += f[k];
-        }
+  auto row_at = [&](int i) { return static_cast<const T*>(q.dy) + places[i] * q.ld_dy + first_column; };
+  auto live = [&](int i) { return i < count && keys[i] < vocab && ADAPT_IN_BOUNDS(places[i], q.n, 52); };
+  // by the first warp: the rows of a step
+  auto fill = [&](int step) {
+    unsigned bytes = 0;
+    for (int pass = 0; pass < 2; ++pass) {   // what will come is said before it is asked for
+      for (int r = warp_lane; r < teams * kStageRows; r += 32) {
+        const int of = r / kStageRows, in = step * kStageRows + r % kStageRows, i = of * q.block + in;
+        if (in >= q.block || !live(i)) continue;
+        const T* row = row_at(i);
+        const unsigned skip = kAligned ? 0 : static_cast<unsigned>(reinterpret_cast<uintptr_t>(row) & 15u);
+        const unsigned size = (skip + columns * static_cast<unsigned>(sizeof(T)) + 15) & ~15u;
+        if (pass == 0) { bytes += size; continue; }
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     :: "r"(shared_address(embed_smem) + (step & 1) * stage_bytes + r * q.slot), "l"(reinterpret_cast<const unsigned char*>(row) - skip),
+                        "r"(size), "r"(full + 8 * (step & 1)) : "memory");
+        if (q.accumulate && keys[i + 1] != keys[i])   // what the sum will be added to
+          asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const G*>(q.dtable) + keys[i] * q.ld_grad + first_column));
       }
-      const bool ends = keys[i + j + 1] != key;
-      if (!ends && i + j + 1 < to) continue;
+      if (pass == 0) {
+        bytes = __reduce_add_sync(~0u, bytes);
+        if (warp_lane == 0) barrier_expect_bytes(full + 8 * (step & 1), bytes);
+        __syncwarp();
+      }
+    }
+  };
+  const int steps = (min(q.block, count) + kStageRows - 1) / kStageRows;
+  if (threadIdx.x < 32) {
+    fill(0);
+    if (steps > 1) fill(1);
+  }
+  const int from = team * q.block, to = min(from + q.block, count);
+  float sum[V] = {};
+  int start = from;   // of the token at hand
+  float* partial = q.partial + 2 * (cta_first / q.block + team) * q.dim + first_column;
+  auto column = [&](int k) { return kAligned ? lane * V + k : lane + k * q.lanes; };
+  const bool in = lane * V < columns;   // (kAligned)
+  for (int step = 0; step < steps; ++step) {
+    const bool ok = barrier_wait(full + 8 * (step & 1), (step >> 1) & 1);
+    const unsigned char* stage = embed_smem + (step & 1) * stage_bytes + team * kStageRows * q.slot;
+    for (int r = 0; r < kStageRows; ++r) {
+      const int i = from + step * kStageRows + r;
+      if (i >= to || keys[i] >= vocab) break;
+      const unsigned key = keys[i];
+      if (kAligned) {
+        float f[V];
+        if (in) {
+          unpack16<T>(*reinterpret_cast<const uint4*>(stage + r * q.slot + lane * 16), f);
+#pragma unroll
+          for (int k = 0; k < V; ++k) sum[k] += f[k];
+        }
+      } else {
+        const T* row = reinterpret_cast<const T*>(stage + r * q.slot + (reinterpret_cast<uintptr_t>(row_at(i)) & 15u));
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (column(k) < columns) sum[k] += to_float(row[column(k)]);
+      }
+      if (!ok) sum[0] = __int_as_float(0x7FC00000);   // (a wait that ran out leaves NaN)
+      const bool ends = keys[i + 1] != key;
+      if (!ends && i + 1 < to) continue;
       const bool began = start > from || keys[from - 1] != key;   // here, and not in the block in front
       if (ends && began) {
-        embed_write<G, V, U>(q, c, key, sum);
-      } else {
-        if (began && c.base == 0) q.joins[1 + atomicAdd(q.joins, 1u)] = static_cast<unsigned>(cta_first / q.block) + team;
-        float* half = partial + (began ? q.dim : 0);
+        G* row = static_cast<G*>(q.dtable) + key * q.ld_grad + first_column;
+        if (kAligned) {
+          if (in) {
+            float f[V] = {};
+            if (q.accumulate) load_row<G, V>(row + lane * V, f);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+            for (int k = 0; k < V; ++k) f[k] += sum[k] * q.scale;
+            store_part<G, V>(row + lane * V, f);
+          }
+        } else {
 #pragma unroll
           for (int k = 0; k < V; ++k)
-            if (c.in(u)) half[c.at(u) + k] = sum[u][k];
+            if (column(k) < columns) row[column(k)] = from_float<G>(sum[k] * q.scale + (q.accumulate ? to_float(row[column(k)]) : 0.0f));
+        }
+      } else {
+        if (began && lane == 0 && slice == 0)
+          q.joins[1 + atomicAdd(&q.joins->x, 1u)] = make_uint2(static_cast<unsigned>(cta_first / q.block) + team, key);
+        float* half = partial + (began ? q.dim : 0);
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (column(k) < columns) half[column(k)] = sum[k];
       }
-      start = i + j + 1;
+      start = i + 1;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < V; ++k) sum[u][k] = 0.0f;
+      for (int k = 0; k < V; ++k) sum[k] = 0.0f;
     }
+    __syncthreads();   // the stage has been read
+    if (threadIdx.x < 32 && step + 2 < steps) fill(step + 2);
   }
 }
 
 // Joins the sums of tokens that go on beyond the block in which they begin: a CTA takes 128 columns of one after the other,
 // its warps the blocks behind in turn.
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 4;
 constexpr int kJoinColumns = 128;
 
 template <typename G>
@@ -449,23 +465,24 @@ __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const Embed
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   wait_for_previous_kernel();
   const unsigned* keys = q.keys[(q.passes + 1) & 1];
-  const unsigned long long items = static_cast<unsigned long long>(*q.joins) * slices;
+  const unsigned long long items = static_cast<unsigned long long>(q.joins->x) * slices;
   for (unsigned long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int slice = static_cast<int>(item % slices);
-    const long long b = q.joins[1 + item / slices], end = (b + 1) * q.block;
-    const unsigned key = keys[end];
+    const uint2 join = q.joins[1 + item / slices];
+    const long long b = join.x, end = (b + 1) * q.block;
+    const int c0 = slice * kJoinColumns + lane;   // columns 32 apart
+    const float* from = q.partial + 2 * (b + 1) * q.dim;
+    const float own = q.partial[(2 * b + 1) * q.dim + min(slice * kJoinColumns + static_cast<int>(threadIdx.x), q.dim - 1)];
     // the blocks behind that begin with the token: it is the first of those
     const long long blocks = (q.n + q.block - 1) / q.block - b - 1;
     long long count = 1;
     for (bool more = true; more;) {
       const long long j = count + lane;
-      const unsigned on = __ballot_sync(~0u, j < blocks && keys[end + j * q.block] == key);
+      const unsigned on = __ballot_sync(~0u, j < blocks && keys[end + j * q.block] == join.y);
       more = on == ~0u;
       count += more ? 32 : __ffs(~on) - 1;
     }
     float sum[4] = {};
-    const int c0 = slice * kJoinColumns + lane;   // columns 32 apart
-    const float* from = q.partial + 2 * (b + 1) * q.dim;
 #pragma unroll 4
     for (long long j = warp; j < count; j += kJoinWarps)
 #pragma unroll
@@ -475,17 +492,18 @@ __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const Embed
     for (int k = 0; k < 4; ++k) part[warp][lane + 32 * k] = sum[k];
     __syncthreads();
     const int c = slice * kJoinColumns + threadIdx.x;
-    if (threadIdx.x < kJoinColumns && c < q.dim) {
-      float total = q.partial[(2 * b + 1) * q.dim + c];
+    if (c < q.dim) {
+      float total = own;
 #pragma unroll
       for (int w = 0; w < kJoinWarps; ++w) total += part[w][threadIdx.x];
       total *= q.scale;
-      G* to = static_cast<G*>(q.dtable) + key * q.ld_grad + c;
+      G* to = static_cast<G*>(q.dtable) + join.y * q.ld_grad + c;
       if (q.accumulate) total += to_float(*to);
       *to = from_float<G>(total);
     }
     __syncthreads();
   }
 }
+static_assert(32 * kJoinWarps == kJoinColumns, "a thread a column");
 
 }  // namespace adapt
