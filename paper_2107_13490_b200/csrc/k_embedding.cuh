@@ -7,9 +7,9 @@
 // The gradient takes three launches.  The first sorts the tokens (stable, so that a token's occurrences stay in order) in
 // one cluster, whose CTAs exchange their digit counts through shared memory, while the other clusters write the rows of
 // tokens that do not occur, most of the table as a rule.  The second sums over blocks of the sorted places, one
-// block a team of threads, so that frequent tokens are summed by many; where a token goes on beyond a block's end,
-// its sums so far are left in memory, and the third launch joins them in the order of the blocks.  So every sum has one
-// order, whatever the timing, and no row of dy is read twice.
+// block a team of threads.  A token of no more places than a block belongs to the team in whose block it begins; more
+// frequent ones are cut at the blocks' ends, the sums of their pieces are left in memory, and the third launch joins
+// them in the order of the blocks.  So every sum has one order, whatever the timing, and no row of dy is read twice.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -97,7 +97,7 @@ struct EmbedGradParams {
   unsigned* keys[2];     // [n] tokens (vocab: none)
   unsigned* places[2];   // [n] their places
   uint2* joins;          // their number, then the blocks in which a token begins that goes on behind them, and the token
-  float* partial;        // [blocks][2][dim] sums of a block's first token, which began in front, and of its last, which goes on
+  float* partial;        // [blocks][2][dim] sums of a block's first token, which began in front, and of its last, which goes on (where they are cut)
   int width, passes;     // digits of the sort (passes 0: by comparisons)
   int block;             // sorted places of a block
   int lanes;             // threads of a team
@@ -340,9 +340,12 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   const long long cta_first = static_cast<long long>(blockIdx.x / q.slices) * teams * q.block;
   const int count = static_cast<int>(min(static_cast<long long>(teams) * q.block, q.n - cta_first));
   const int stage_bytes = teams * kStageRows * q.slot;
-  // tokens of the CTA's places, with one in front and one behind, then the places
-  unsigned* keys = reinterpret_cast<unsigned*>(embed_smem + 2 * stage_bytes) + 1;
-  unsigned* places = keys + teams * q.block + 1;
+  // tokens and places of the CTA's places, of a block in front and of one behind
+  const int around = q.block + 1, held = teams * q.block + 2 * around;
+  unsigned* keys = reinterpret_cast<unsigned*>(embed_smem + 2 * stage_bytes) + around;
+  unsigned* places = keys + held;
+  __shared__ int begins[kEmbedThreads / 8], ends_at[kEmbedThreads / 8];   // what the teams take
+  __shared__ bool cut_front[kEmbedThreads / 8];
   const unsigned full = shared_address(bars), vocab = static_cast<unsigned>(q.vocab);
   if (threadIdx.x == 0) {
     barrier_init(full, 1);
@@ -353,22 +356,54 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   {
     const unsigned* all_keys = q.keys[(q.passes + 1) & 1] + cta_first;
     const unsigned* all_places = q.places[(q.passes + 1) & 1] + cta_first;
-    for (int i = static_cast<int>(threadIdx.x) - 1; i <= count; i += kEmbedThreads) {
+    for (int i = static_cast<int>(threadIdx.x) - around; i < count + around; i += kEmbedThreads) {
       const long long p = cta_first + i;
-      keys[i] = p >= 0 && p < q.n ? all_keys[i] : ~0u;
-      if (i >= 0 && i < count) places[i] = all_places[i];
+      const bool known = p >= 0 && p < q.n;
+      keys[i] = known ? all_keys[i] : ~0u;   // (in front of the first, too: equal to no token)
+      places[i] = known ? all_places[i] : 0;
     }
   }
   __syncthreads();
+  if (threadIdx.x < static_cast<unsigned>(teams)) {
+    const int from = static_cast<int>(threadIdx.x) * q.block, to = min(from + q.block, count);
+    int begin = from, end = to;
+    bool front = false;
+    // the first place in [lo, hi) whose token is not below `least` (there are no places in front of the first)
+    auto search = [&](int lo, int hi, unsigned least) {
+      lo = max(lo, static_cast<int>(max(-cta_first, static_cast<long long>(-around))));
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (keys[mid] < least) lo = mid + 1; else hi = mid;
+      }
+      return lo;
+    };
+    if (from < count) {
+      if (keys[from - 1] == keys[from]) {   // its token's places, as far as a block away
+        const int first = search(from - around, from, keys[from]), stop = search(from + 1, from + q.block + 1, keys[from] + 1);
+        front = stop - first > q.block;
+        if (!front) begin = stop;   // the team in front takes it
+      }
+      if (keys[to] == keys[to - 1]) {
+        const int first = search(to - around, to, keys[to]), stop = search(to + 1, to + q.block + 1, keys[to] + 1);
+        if (stop - first <= q.block) end = stop;   // (then it begins in this block)
+      }
+      begin = min(begin, end);
+    } else {
+      begin = end = from;
+    }
+    begins[threadIdx.x] = begin;
+    ends_at[threadIdx.x] = end;
+    cut_front[threadIdx.x] = front;
+  }
+  __syncthreads();
   auto row_at = [&](int i) { return static_cast<const T*>(q.dy) + places[i] * q.ld_dy + first_column; };
-  auto live = [&](int i) { return i < count && keys[i] < vocab && ADAPT_IN_BOUNDS(places[i], q.n, 52); };
   // by the first warp: the rows of a step
   auto fill = [&](int step) {
     unsigned bytes = 0;
     for (int pass = 0; pass < 2; ++pass) {   // what will come is said before it is asked for
       for (int r = warp_lane; r < teams * kStageRows; r += 32) {
-        const int of = r / kStageRows, in = step * kStageRows + r % kStageRows, i = of * q.block + in;
-        if (in >= q.block || !live(i)) continue;
+        const int of = r / kStageRows, i = begins[of] + step * kStageRows + r % kStageRows;
+        if (i >= ends_at[of] || keys[i] >= vocab || !ADAPT_IN_BOUNDS(places[i], q.n, 52)) continue;
         const T* row = row_at(i);
         const unsigned skip = kAligned ? 0 : static_cast<unsigned>(reinterpret_cast<uintptr_t>(row) & 15u);
         const unsigned size = (skip + columns * static_cast<unsigned>(sizeof(T)) + 15) & ~15u;
@@ -386,12 +421,14 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
       }
     }
   };
-  const int steps = (min(q.block, count) + kStageRows - 1) / kStageRows;
+  int most = 0;
+  for (int t = 0; t < teams; ++t) most = max(most, ends_at[t] - begins[t]);
+  const int steps = (most + kStageRows - 1) / kStageRows;
   if (threadIdx.x < 32) {
-    fill(0);
+    if (steps > 0) fill(0);
     if (steps > 1) fill(1);
   }
-  const int from = team * q.block, to = min(from + q.block, count);
+  const int from = begins[team], to = ends_at[team];
   float sum[V] = {};
   int start = from;   // of the token at hand
   float* partial = q.partial + 2 * (cta_first / q.block + team) * q.dim + first_column;
@@ -420,7 +457,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
       if (!ok) sum[0] = __int_as_float(0x7FC00000);   // (a wait that ran out leaves NaN)
       const bool ends = keys[i + 1] != key;
       if (!ends && i + 1 < to) continue;
-      const bool began = start > from || keys[from - 1] != key;   // here, and not in the block in front
+      const bool began = start > from || !cut_front[team];   // here, and not in the block in front
       if (ends && began) {
         G* row = static_cast<G*>(q.dtable) + key * q.ld_grad + first_column;
         if (kAligned) {
@@ -455,7 +492,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
 
 // Joins the sums of tokens that go on beyond the block in which they begin: a CTA takes 128 columns of one after the other,
 // its warps the blocks behind in turn.
-constexpr int kJoinWarps = 4;
+constexpr int kJoinWarps = 8;
 constexpr int kJoinColumns = 128;
 
 template <typename G>
@@ -472,7 +509,7 @@ __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const Embed
     const long long b = join.x, end = (b + 1) * q.block;
     const int c0 = slice * kJoinColumns + lane;   // columns 32 apart
     const float* from = q.partial + 2 * (b + 1) * q.dim;
-    const float own = q.partial[(2 * b + 1) * q.dim + min(slice * kJoinColumns + static_cast<int>(threadIdx.x), q.dim - 1)];
+    const float own = q.partial[(2 * b + 1) * q.dim + min(slice * kJoinColumns + static_cast<int>(threadIdx.x % kJoinColumns), q.dim - 1)];
     // the blocks behind that begin with the token: it is the first of those
     const long long blocks = (q.n + q.block - 1) / q.block - b - 1;
     long long count = 1;
@@ -483,7 +520,7 @@ __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const Embed
       count += more ? 32 : __ffs(~on) - 1;
     }
     float sum[4] = {};
-#pragma unroll 4
+#pragma unroll 8
     for (long long j = warp; j < count; j += kJoinWarps)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -492,7 +529,7 @@ __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const Embed
     for (int k = 0; k < 4; ++k) part[warp][lane + 32 * k] = sum[k];
     __syncthreads();
     const int c = slice * kJoinColumns + threadIdx.x;
-    if (c < q.dim) {
+    if (threadIdx.x < kJoinColumns && c < q.dim) {
       float total = own;
 #pragma unroll
       for (int w = 0; w < kJoinWarps; ++w) total += part[w][threadIdx.x];
@@ -504,6 +541,5 @@ __global__ __launch_bounds__(32 * kJoinWarps) void embed_join_kernel(const Embed
     __syncthreads();
   }
 }
-static_assert(32 * kJoinWarps == kJoinColumns, "a thread a column");
 
 }  // namespace adapt
