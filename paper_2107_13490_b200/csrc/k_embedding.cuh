@@ -388,6 +388,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
         if (stop - first <= q.block) end = stop;   // (then it begins in this block)
       }
       begin = min(begin, end);
+      end = search(begin, end, vocab);   // (places without a token are sorted to the end)
     } else {
       begin = end = from;
     }
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
     for (int pass = 0; pass < 2; ++pass) {   // what will come is said before it is asked for
       for (int r = warp_lane; r < teams * kStageRows; r += 32) {
         const int of = r / kStageRows, i = begins[of] + step * kStageRows + r % kStageRows;
-        if (i >= ends_at[of] || keys[i] >= vocab || !ADAPT_IN_BOUNDS(places[i], q.n, 52)) continue;
+        if (i >= ends_at[of] || !ADAPT_IN_BOUNDS(places[i], q.n, 52)) continue;
         const T* row = row_at(i);
         const unsigned skip = kAligned ? 0 : static_cast<unsigned>(reinterpret_cast<uintptr_t>(row) & 15u);
         const unsigned size = (skip + columns * static_cast<unsigned>(sizeof(T)) + 15) & ~15u;
@@ -430,35 +431,39 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   }
   const int from = begins[team], to = ends_at[team];
   float sum[V] = {};
-  int start = from;   // of the token at hand
+  bool began = !cut_front[team];   // the token at hand: here, and not in the block in front
   float* partial = q.partial + 2 * (cta_first / q.block + team) * q.dim + first_column;
   auto column = [&](int k) { return kAligned ? lane * V + k : lane + k * q.lanes; };
   const bool in = lane * V < columns;   // (kAligned)
+  const unsigned base16 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(static_cast<const T*>(q.dy) + first_column)) & 15u;
+  const unsigned step16 = static_cast<unsigned>(q.ld_dy * sizeof(T)) & 15u;
   for (int step = 0; step < steps; ++step) {
     const bool ok = barrier_wait(full + 8 * (step & 1), (step >> 1) & 1);
+    if (!ok) sum[0] = __int_as_float(0x7FC00000);   // (a wait that ran out leaves NaN)
     const unsigned char* stage = embed_smem + (step & 1) * stage_bytes + team * kStageRows * q.slot;
-    for (int r = 0; r < kStageRows; ++r) {
-      const int i = from + step * kStageRows + r;
-      if (i >= to || keys[i] >= vocab) break;
-      const unsigned key = keys[i];
-      if (kAligned) {
-        float f[V];
-        if (in) {
+    const int i0 = from + step * kStageRows, rows = min(kStageRows, to - i0);
+    unsigned last = 0;   // rows after which a sum is written: a token's last, and the team's
+#pragma unroll
+    for (int r = 0; r < kStageRows; ++r)
+      if (r < rows && (keys[i0 + r + 1] != keys[i0 + r] || i0 + r + 1 == to)) last |= 1u << r;
+    for (int r = 0; r < rows;) {
+      const int stop = last >> r ? r + __ffs(last >> r) : rows;
+#pragma unroll 2
+      for (; r < stop; ++r) {
+        if (kAligned) {
+          float f[V];
           unpack16<T>(*reinterpret_cast<const uint4*>(stage + r * q.slot + lane * 16), f);
 #pragma unroll
           for (int k = 0; k < V; ++k) sum[k] += f[k];
-        }
-      } else {
-        const T* row = reinterpret_cast<const T*>(stage + r * q.slot + (reinterpret_cast<uintptr_t>(row_at(i)) & 15u));
+        } else {   // (beyond the columns it adds up what lies there, which goes nowhere)
+          const T* row = reinterpret_cast<const T*>(stage + r * q.slot + ((base16 + places[i0 + r] * step16) & 15u));
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-          if (column(k) < columns) sum[k] += to_float(row[column(k)]);
+          for (int k = 0; k < V; ++k) sum[k] += to_float(row[column(k)]);
+        }
       }
-      if (!ok) sum[0] = __int_as_float(0x7FC00000);   // (a wait that ran out leaves NaN)
-      const bool ends = keys[i + 1] != key;
-      if (!ends && i + 1 < to) continue;
-      const bool began = start > from || !cut_front[team];   // here, and not in the block in front
-      if (ends && began) {
+      if (!(last >> (r - 1) & 1)) break;   // the token goes on in the next step
+      const unsigned key = keys[i0 + r - 1];
+      if (began && keys[i0 + r] != key) {
         G* row = static_cast<G*>(q.dtable) + key * q.ld_grad + first_column;
         if (kAligned) {
           if (in) {
@@ -481,7 +486,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
         for (int k = 0; k < V; ++k)
           if (column(k) < columns) half[column(k)] = sum[k];
       }
-      start = i + 1;
+      began = true;
 #pragma unroll
       for (int k = 0; k < V; ++k) sum[k] = 0.0f;
     }
