@@ -116,7 +116,7 @@ int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_ta
                    (n == 1 || ld_out % wide == 0);
   const int64_t parts = vec ? dim / wide : dim;
   int lanes = 1;
-  while (lanes < kEmbedThreads && lanes * kEmbedChunks < parts) lanes *= 2;
+  while (lanes < kEmbedThreads && lanes * 4 < parts) lanes *= 2;
   const int rows = kEmbedThreads / lanes;
   const unsigned grid = static_cast<unsigned>((n + rows - 1) / rows);
   cudaStream_t stream = static_cast<cudaStream_t>(stream_handle);

@@ -29,15 +29,7 @@ struct EmbedParams {
   float scale;
 };
 
-// A row's elements from..from+V-1 (scaled by nothing) to and from registers.
-template <typename T, int V>
-__device__ __forceinline__ void load_part(const T* p, float (&f)[V]) {
-  if constexpr (V == 1) {
-    f[0] = to_float(*p);
-  } else {
-    unpack16<T>(__ldg(reinterpret_cast<const uint4*>(p)), f);
-  }
-}
+// A row's elements from..from+V-1 from registers.
 template <typename T, int V>
 __device__ __forceinline__ void store_part(T* p, const float (&f)[V]) {
   if constexpr (V == 1) {
@@ -51,9 +43,16 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[V]) {
   }
 }
 
+// Parts of rows as they lie in memory, and their elements.
+template <typename T, int V> struct RawPart { typedef uint4 type; };
+template <typename T> struct RawPart<T, 1> { typedef T type; };
+template <typename T, int V>
+__device__ __forceinline__ void widen(const uint4& raw, float (&f)[V]) { unpack16<T>(raw, f); }
+template <typename T, int V>
+__device__ __forceinline__ void widen(const T& raw, float (&f)[1]) { f[0] = to_float(raw); }
+
 // `lanes` threads (a power of two, up to the CTA) take a row; V elements at a time.
 constexpr int kEmbedThreads = 256;
-constexpr int kEmbedChunks = 4;   // that a thread has under way
 
 template <typename T, int V>
 __global__ __launch_bounds__(kEmbedThreads) void embedding_kernel(EmbedParams q, int lanes) {
@@ -65,21 +64,24 @@ __global__ __launch_bounds__(kEmbedThreads) void embedding_kernel(EmbedParams q,
   const T* row = static_cast<const T*>(q.table) + (id >= 0 && id < q.vocab ? id : 0) * q.ld_table;
   const float fill = id < 0 ? 0.0f : __int_as_float(0x7FC00000);
   const bool known = id >= 0 && id < q.vocab;
-  constexpr int kUnroll = kEmbedChunks;
+  constexpr int kUnroll = 4;   // parts that a thread has under way, as they lie in memory
+  typedef typename RawPart<T, V>::type Raw;
   for (int at = lane * V; at < q.dim; at += lanes * V * kUnroll) {
-    float f[kUnroll][V];
+    Raw raw[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int c = at + u * lanes * V;
-      if (known && c < q.dim) load_part<T, V>(row + c, f[u]);
+      if (known && c < q.dim) raw[u] = __ldg(reinterpret_cast<const Raw*>(row + c));
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int c = at + u * lanes * V;
       if (c >= q.dim) break;
+      float f[V];
+      widen<T, V>(raw[u], f);
 #pragma unroll
-      for (int k = 0; k < V; ++k) f[u][k] = known ? f[u][k] * q.scale : fill;
-      store_part<T, V>(out + c, f[u]);
+      for (int k = 0; k < V; ++k) f[k] = known ? f[k] * q.scale : fill;
+      store_part<T, V>(out + c, f);
     }
   }
 }
