@@ -321,20 +321,20 @@ struct NormRows {
   unsigned stage, parity;    // the stage of the row at hand, its barrier's phase
   const unsigned char* at;   // this thread's place in the stage
   int part;                  // of the row, for this CTA
-  long long group;           // clusters take the rows in turn
-  long long groups;
-  int skip;                  // elements between a 16-byte boundary and the rows' first element
+  unsigned group, groups;    // clusters take the rows in turn
+  int offset;                // column of the CTA's first element: below 0 where rows begin behind a 16-byte boundary
   unsigned in;               // which of the thread's elements are elements of the row (kEdges)
   __device__ __forceinline__ NormRows(const NormParams& q_, const NormRing& r, unsigned char* smem, unsigned long long* b)
       : q(q_), ring(r), stages(smem), bars(shared_address(b)), stage(0), parity(0), at(smem + threadIdx.x * 16), part(0),
-        group(blockIdx.x), groups(gridDim.x), skip(0), in(~0u) {
+        group(blockIdx.x), groups(gridDim.x), offset(0), in(~0u) {
     if (ring.parts > 1) {
       part = cta_in_cluster();
       group = blockIdx.x / ring.parts;
       groups = gridDim.x / ring.parts;
+      offset = part * kElems * static_cast<int>(blockDim.x);
     }
     if constexpr (kEdges) {
-      skip = static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + group * q.ld_block) & 15u) / sizeof(T));
+      offset -= static_cast<int>((reinterpret_cast<uintptr_t>(static_cast<const T*>(q.block) + group * q.ld_block) & 15u) / sizeof(T));
       in = 0;
 #pragma unroll
       for (int j = 0; j < kElems; ++j) {
@@ -350,7 +350,7 @@ struct NormRows {
         if (ring.weights[w] >= 0)
           for (int c = threadIdx.x; c < width; c += blockDim.x)
             reinterpret_cast<float*>(smem + ring.weights[w])[c] =
-                first() + c < 0 || first() + c >= q.dim ? 0.0f : from[w] ? __ldg(from[w] + first() + c) : 1.0f;
+                offset + c < 0 || offset + c >= q.dim ? 0.0f : from[w] ? __ldg(from[w] + offset + c) : 1.0f;
     }
     if (threadIdx.x == 0) {
       for (int s = 0; s < ring.stages; ++s) barrier_init(bars + 8 * s, 1);
@@ -359,8 +359,7 @@ struct NormRows {
     }
     if (ring.parts > 1) meet_cluster(); else __syncthreads();
   }
-  __device__ __forceinline__ int first() const { return part * kElems * static_cast<int>(blockDim.x) - skip; }   // column of the CTA
-  __device__ __forceinline__ int column(int i) const { return first() + (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V; }
+  __device__ __forceinline__ int column(int i) const { return offset + (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * V; }
   // Whether chunk i has an element of the row, and whether all of its elements are.
   __device__ __forceinline__ bool any(int i) const { return column(i) < q.dim; }
   __device__ __forceinline__ bool whole(int i) const { return !kEdges || ((in >> (i * V)) & ((1u << V) - 1)) == (1u << V) - 1; }
@@ -378,9 +377,9 @@ struct NormRows {
   }
   __device__ __forceinline__ bool has(int j) const { return !kEdges || (in >> j & 1); }
 
-  __device__ __forceinline__ void fill(int s, long long r) const {
-    if (r >= q.rows) return;
-    const int from_column = first(), columns = min(q.dim - from_column, kElems * static_cast<int>(blockDim.x));
+  __device__ __forceinline__ void fill(int s, unsigned r) const {
+    if (r >= static_cast<unsigned>(q.rows)) return;
+    const int from_column = offset, columns = min(q.dim - from_column, kElems * static_cast<int>(blockDim.x));
     if (columns <= 0) { barrier_expect_bytes(bars + 8 * s, 0); return; }
     const unsigned bytes = (columns * static_cast<int>(sizeof(T)) + 15) & ~15;
     barrier_expect_bytes(bars + 8 * s, ring.streams * bytes);
@@ -398,7 +397,7 @@ struct NormRows {
     return barrier_wait(bars + 8 * stage, parity) ? 0.0f : __int_as_float(0x7FC00000);
   }
   // Called when every thread has read what it needs of the row `r`.
-  __device__ __forceinline__ void release(long long r) {
+  __device__ __forceinline__ void release(unsigned r) {
     if (threadIdx.x == 0) fill(stage, r + ring.stages * groups);
     at += ring.streams * ring.stage_row;
     if (++stage == static_cast<unsigned>(ring.stages)) { stage = 0; parity ^= 1; at = stages + threadIdx.x * 16; }
@@ -497,7 +496,7 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
     }
     return make_float2(mean, rsqrtf(fmaf(sums.one(s), inv, q.eps)));
   };
-  for (long long r = rows.group; r < q.rows; r += rows.groups) {
+  for (unsigned r = rows.group; r < static_cast<unsigned>(q.rows); r += rows.groups) {
     const float poison = rows.ready();
     Two v[kPairs];
 #pragma unroll
@@ -577,10 +576,10 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) of_after[kAfter ? k : 0] = of_before[kBefore ? k : 0] = of_gate[kForAll ? k : 0] = both(0.0f);
   const float4* statistics = reinterpret_cast<const float4*>(q.stats_in);
-  float4 next = rows.group < q.rows ? __ldg(statistics + rows.group) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (long long r = rows.group; r < q.rows; r += rows.groups) {
+  float4 next = rows.group < static_cast<unsigned>(q.rows) ? __ldg(statistics + rows.group) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (unsigned r = rows.group; r < static_cast<unsigned>(q.rows); r += rows.groups) {
     const float4 st = next;
-    if (r + rows.groups < q.rows) next = __ldg(statistics + r + rows.groups);
+    if (r + rows.groups < static_cast<unsigned>(q.rows)) next = __ldg(statistics + r + rows.groups);
     const float poison = rows.ready();
     const float mean_a = -st.x * st.y, mean_b = -st.z * st.w, scale_b = q.scale * st.w, residual_b = q.residual_scale * st.w;
     // norm_before(y) and the gate; then the gradient of norm_after's output, and that output
@@ -714,8 +713,8 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
     }
   }
   if (!q.partial) return;
-  const long long plane = rows.groups * q.dim;
-  float* mine = q.partial + rows.group * q.dim;
+  const long long plane = static_cast<long long>(rows.groups) * q.dim;
+  float* mine = q.partial + static_cast<long long>(rows.group) * q.dim;
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     if (!rows.any(i)) break;
