@@ -37,7 +37,7 @@ int run_rows(const RowsParams& q, int dtype, cudaStream_t stream) {
 
 int run_copy(const CopyParams& q, cudaStream_t stream) {
   LaunchScope ls(ADAPT_KERNEL_INT8_ROWS, stream);
-  int8_copy_kernel<<<static_cast<unsigned>(q.rows), kCopyThreads, 0, stream>>>(q);
+  int8_copy_kernel<<<static_cast<unsigned>(q.part[0].rows) + static_cast<unsigned>(q.part[1].rows), kCopyThreads, 0, stream>>>(q);
   ADAPT_LAUNCH_OK("rows of codes");
   return ADAPT_OK;
 }
@@ -276,15 +276,18 @@ int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t
   if (rows <= kDotMaxRows) return run_dot(q, x, x_dtype, dtype, ldw, stream);
   signed char* ws = static_cast<signed char*>(workspace);
   int rc = ADAPT_OK;
-  if (lay.copy_w) {
-    const CopyParams c = {weight, ws + lay.w, n > 1 ? ldw : 0, lay.ld, q.n, q.k};
+  if (lay.copy_x || lay.copy_w) {
+    CopyParams c = {};
+    c.cols = q.k;
+    if (lay.copy_x) {
+      c.part[0] = {q.x, ws + lay.x, rows > 1 ? ldx : 0, lay.ld, q.rows};
+      q.x = c.part[0].to; q.ldx = lay.ld;
+    }
+    if (lay.copy_w) {
+      c.part[1] = {weight, ws + lay.w, n > 1 ? ldw : 0, lay.ld, q.n};
+      q.w = c.part[1].to; q.ldw = lay.ld;
+    }
     if ((rc = run_copy(c, stream)) != ADAPT_OK) return rc;
-    q.w = c.to; q.ldw = lay.ld;
-  }
-  if (lay.copy_x) {
-    const CopyParams c = {q.x, ws + lay.x, ldx, lay.ld, q.rows, q.k};
-    if ((rc = run_copy(c, stream)) != ADAPT_OK) return rc;
-    q.x = c.to; q.ldx = lay.ld;
   }
   if (lay.quantise) {
     RowsParams r = {};
@@ -294,8 +297,9 @@ int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t
     if ((rc = run_rows(r, x_dtype, stream)) != ADAPT_OK) return rc;
     q.x = r.codes; q.x_scales = r.scales; q.ldx = lay.ld;
   }
-  // (it reads weights before it waits for the kernel in front, which therefore must not be the one that writes them)
-  return run_tiles(q, dtype, lay.quantise || lay.copy_x, stream);
+  // (where activations are quantised as well, the weights' copies were complete when that kernel began)
+  q.w_late = lay.copy_w && !lay.quantise;
+  return run_tiles(q, dtype, lay.quantise || lay.copy_x || lay.copy_w, stream);
 }
 
 }  // extern "C"

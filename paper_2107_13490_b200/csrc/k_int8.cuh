@@ -113,6 +113,7 @@ struct LinearParams {
   long long ldx, ldw, ldy;
   int rows, n, k;
   bool x_one, w_one;   // one scale for all
+  bool w_late;         // the kernel in front writes the weights too
 };
 
 // 32 results of one token to 32-byte aligned memory, in whole sectors.
@@ -354,6 +355,7 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
       tile_load<false>(aligned + s * kStageBytes + kCtaRows * kDepth, &x_map, b * kDepth, token0, full + 8 * s);
     };
     const int first = min(to, from + kStages);
+    if (q.w_late) wait_for_previous_kernel();
     for (int b = from; b < first; ++b) weights(b);
     wait_for_previous_kernel();
     for (int b = from; b < first; ++b) tokens(b);
@@ -461,12 +463,13 @@ __global__ __launch_bounds__(kNarrowThreads) void int8_narrow_kernel(const __gri
 
 // ---- codes into rows that the TMA unit can read ------------------------------------------------------------
 
-struct CopyParams {
+struct CopyRows {
   const signed char* from;
   signed char* to;
   long long ld_from, ld_to;   // ld_to a multiple of 16
-  int rows, cols;
+  int rows;
 };
+struct CopyParams { CopyRows part[2]; int cols; };   // activations and weights, either may have no rows
 
 // 16 bytes that begin at byte `o` of two aligned blocks.
 __device__ __forceinline__ uint4 shift_bytes(const uint4& lo, const uint4& hi, unsigned o) {
@@ -489,14 +492,17 @@ constexpr int kCopyThreads = 128;
 // Only aligned blocks that hold a byte of the row are read.
 __global__ __launch_bounds__(kCopyThreads) void int8_copy_kernel(CopyParams q) {
   let_next_kernel_start();
-  const signed char* row = q.from + blockIdx.x * q.ld_from;
+  const bool second = blockIdx.x >= static_cast<unsigned>(q.part[0].rows);
+  const CopyRows& p = q.part[second];
+  const long long r = blockIdx.x - (second ? q.part[0].rows : 0);
+  const signed char* row = p.from + r * p.ld_from;
   for (int c = threadIdx.x * 16; c < q.cols; c += kCopyThreads * 16) {
     const unsigned o = static_cast<unsigned>(reinterpret_cast<uintptr_t>(row + c) & 15u);
     const uint4* block = reinterpret_cast<const uint4*>(row + c - o);
     const uint4 lo = __ldg(block);
     uint4 hi = make_uint4(0, 0, 0, 0);
     if (static_cast<int>(o) + min(16, q.cols - c) > 16) hi = __ldg(block + 1);
-    *reinterpret_cast<uint4*>(q.to + blockIdx.x * q.ld_to + c) = shift_bytes(lo, hi, o);
+    *reinterpret_cast<uint4*>(p.to + r * p.ld_to + c) = shift_bytes(lo, hi, o);
   }
 }
 
