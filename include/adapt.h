@@ -651,7 +651,7 @@ size_t adapt_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t ch
  *          that is >= vocab gives a row of NaN
  *   scale  finite
  *   out    DEVICE [n][dim], leading dimension ld_out >= dim, of the table's type; no overlap
- * Limits: vocab, n, dim < 2^31. */
+ * Limits: vocab, n, dim <= 2^30. */
 int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_table, int dtype,
                     const int64_t* ids, int64_t n, float scale, void* out, int64_t ld_out,
                     void* stream);
@@ -665,7 +665,7 @@ int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_ta
  *               dtype or ADAPT_DTYPE_F32.  Rows of tokens that do not occur are 0, or, with
  *               accumulate, left as they are
  *   workspace   DEVICE scratch of adapt_embedding_workspace_bytes, 256-byte aligned; needed
- * Limits: vocab, n, dim < 2^31. */
+ * Limits: vocab, n, dim <= 2^30. */
 int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_dy, int dtype,
                              const int64_t* ids, int64_t vocab, float scale, int accumulate,
                              void* dtable, int64_t ld_grad, int grad_dtype, void* workspace,
@@ -740,7 +740,7 @@ size_t adapt_block_norm_workspace_bytes(int64_t rows, int64_t dim);
  *   x       DEVICE [rows][cols], leading dimension ldx
  *   codes   DEVICE int8 [rows][cols], leading dimension ld_codes >= cols
  *   scales  DEVICE float[rows]
- * Limits: rows < 2^31, cols < 2^31. */
+ * Limits: rows, cols <= 2^30. */
 int adapt_int8_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype,
                     int8_t* codes, int64_t ld_codes, float* scales, void* stream);
 
@@ -761,7 +761,7 @@ int adapt_int8_rows(const void* x, int64_t rows, int64_t cols, int64_t ldx, int 
  * Any codes are legal, -128 too.  The sum is exact (int32); then come the scales, one after the
  * other, and the bias in fp32.  Codes with a 16-byte aligned address and a leading dimension
  * that is a multiple of 16 are read as they are; where there are more than 2 rows, others are
- * first copied to the workspace.  Limits: rows, n < 2^31, k <= ADAPT_INT8_MAX_K. */
+ * first copied to the workspace.  Limits: rows, n <= 2^30, k <= ADAPT_INT8_MAX_K. */
 int adapt_int8_linear(const void* x, int x_dtype, const float* x_scales, int64_t x_scale_count,
                       const int8_t* weight, const float* weight_scales,
                       int64_t weight_scale_count, const float* bias, int64_t rows, int64_t n,

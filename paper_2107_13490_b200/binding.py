@@ -847,8 +847,8 @@ def adapt_gated_scan_backward(x: torch.Tensor, gate: torch.Tensor, dy: torch.Ten
 
 def adapt_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
-    """adapt_embedding of adapt.h: scale * table[ids].  table [vocab, dim]; ids int64 of any shape, negative =
-    no token (a row of 0); returns [*ids.shape, dim]."""
+    """adapt_embedding of adapt.h: scale * table[ids].  table [vocab, dim]; ids int64 of any shape (copied where
+    not contiguous), negative = no token (a row of 0); returns [*ids.shape, dim]."""
     return _run("embedding", stream, table, ids, scale, out)
 
 

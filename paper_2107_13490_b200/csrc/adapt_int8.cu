@@ -13,7 +13,8 @@ namespace {
 
 constexpr int kSms = 148;   // of a B200
 
-bool in_int(int64_t v, int64_t least) { return v >= least && v <= 0x7FFFFFFF; }
+// (with room for what is added to a size before it is compared)
+bool in_int(int64_t v, int64_t least) { return v >= least && v <= (1 << 30); }
 
 int run_rows(const RowsParams& q, int dtype, cudaStream_t stream) {
   const int e = elem_bytes(dtype), wide = 16 / e;
@@ -164,7 +165,7 @@ Cut choose_cut(int64_t rows, int64_t n, int64_t k) {
   Cut best = {0, 1};
   int64_t least = up(up(rows, kWideTile) * up(n, kWideTile), kSms / 2) * (blocks * kDepth * 9 / 2 + 1000) + 6000;
   for (int tokens = 16; tokens <= 256; tokens *= 2) {
-    if (tokens >= 2 * rows && tokens > 16) break;
+    if ((tokens >= 2 * rows && tokens > 16) || up(rows, tokens) > 65535) continue;   // (a grid's second extent)
     for (int split = 1; split <= narrow_split(tokens) && blocks >= 2 * split; split *= 2) {
       const int64_t waves = up(across * up(rows, tokens) * split, kSms), depth = up(blocks, split) * kDepth;
       const int64_t per = std::max<int64_t>(2 * (kCtaRows + tokens), 100 * tokens / 64);   // hundredths of a clock a code
@@ -198,7 +199,6 @@ int run_tiles(const LinearParams& q, int dtype, bool early, cudaStream_t stream)
     return rc;
   }
   const int tokens = cut.tokens, split = cut.split, across = (q.n + kCtaRows - 1) / kCtaRows, down = (q.rows + tokens - 1) / tokens;
-  if (down > 65535 || static_cast<int64_t>(across) * split > 0x7FFFFFFF) return ADAPT_ERR_INVALID_ARG;
   if ((rc = tile_map(&x_map, q.x, q.rows, q.k, q.ldx, tokens)) != ADAPT_OK || (rc = tile_map(&w_map, q.w, q.n, q.k, q.ldw, kCtaRows)) != ADAPT_OK)
     return rc;
   with_type(dtype, [&](auto t) {

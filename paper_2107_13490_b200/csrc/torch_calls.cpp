@@ -378,10 +378,10 @@ int64_t count(PyObject* o, const char* why) {
   need(!beyond && v >= 0, why);
   return v;
 }
-const int64_t* tokens(const at::Tensor& ids, const at::Tensor& x) {
-  need(ids.device() == x.device() && ids.scalar_type() == at::kLong && ids.is_contiguous(),
-       "tokens: a contiguous int64 tensor on the device of its partner");
-  return static_cast<const int64_t*>(ids.const_data_ptr());
+// Tokens in order (copied where they do not lie so: a column of a batch).
+at::Tensor tokens(const at::Tensor& ids, const at::Tensor& x) {
+  need(ids.device() == x.device() && ids.scalar_type() == at::kLong, "tokens: an int64 tensor on the device of its partner");
+  return ids.contiguous();
 }
 // [tokens..., dim] as rows: contiguous, or a matrix with unit inner stride.
 Matrix rows_of(const at::Tensor& t, int64_t n, int64_t dim) {
@@ -394,10 +394,11 @@ Matrix rows_of(const at::Tensor& t, int64_t n, int64_t dim) {
 // (table, ids, scale, out) -> out
 PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 4, [&] {
-    const at::Tensor &table = tensor(a[0]), &ids = tensor(a[1]);
+    const at::Tensor& table = tensor(a[0]);
     const int dtype = elem(table);
     const Matrix m = matrix(table);
-    const int64_t* pi = tokens(ids, table);
+    const at::Tensor ids = tokens(tensor(a[1]), table);
+    const int64_t* pi = static_cast<const int64_t*>(ids.const_data_ptr());
     const float scale = static_cast<float>(real(a[2]));
     at::Tensor out;
     if (const at::Tensor* given = maybe(a[3])) {
@@ -419,10 +420,11 @@ PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // (dy, ids, vocab, scale, dtype, dtable, accumulate) -> dtable
 PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&] {
-    const at::Tensor &dy = tensor(a[0]), &ids = tensor(a[1]);
+    const at::Tensor& dy = tensor(a[0]);
     const int dtype = elem(dy);
     need(dy.dim() >= 1, "a row for each token");
-    const int64_t* pi = tokens(ids, dy);
+    const at::Tensor ids = tokens(tensor(a[1]), dy);
+    const int64_t* pi = static_cast<const int64_t*>(ids.const_data_ptr());
     const Matrix m = rows_of(dy, ids.numel(), dy.size(dy.dim() - 1));
     const int64_t vocab = count(a[2], "the vocabulary is a whole number");
     const float scale = static_cast<float>(real(a[3]));

@@ -70,6 +70,15 @@ def test_forward_layouts(dtype):
             assert (out[:, :at] == 7).all() and (out[:, at + dim:] == 7).all()
 
 
+def test_tokens_in_any_order():
+    """A column of a batch of tokens, and a transposed batch."""
+    table, batch = rand(30, 16), draw_ids(60, 30, "even").reshape(6, 10)
+    for ids in (batch[:, 3], batch.t(), batch[::2]):
+        assert torch.equal(B.adapt_embedding(table, ids), table[ids])
+        dy = rand(*ids.shape, 16)
+        assert torch.equal(B.adapt_embedding_backward(dy, ids, 30), B.adapt_embedding_backward(dy, ids.contiguous(), 30))
+
+
 def test_values_pass_unchanged():
     table = torch.tensor([[math.inf, -math.inf, math.nan, 0.0, 1e-45]], device="cuda")
     out = B.adapt_embedding(table, torch.zeros(2, dtype=torch.int64, device="cuda"))
