@@ -28,13 +28,15 @@ struct EmbedTeams {
   }
 };
 
-// Sorted places of a block: so many that three CTAs an SM take all of them at once, but kStageRows at least, and a 4096th (a token may
+constexpr int kEmbedLeast = 8;
+
+// Sorted places of a block: so many that three CTAs an SM take all of them at once, but kEmbedLeast at least, and a 4096th (a token may
 // be in all of them).  Two rows
 // of sums in fp32 at most go to memory and back for a block.  (By the teams of 16-bit rows, whatever the type.)
 int embed_block(int64_t n, int64_t dim) {
   const EmbedTeams t(dim, 8);
   const int64_t places = 3ll * kSms * t.teams, most = 8192 / (t.teams + 2);   // (64 KB of tokens and places)
-  return static_cast<int>(std::min(most, std::max({static_cast<int64_t>(kStageRows), n / 4096, (n * t.slices + places - 1) / places})));
+  return static_cast<int>(std::min(most, std::max({static_cast<int64_t>(kEmbedLeast), n / 4096, (n * t.slices + places - 1) / places})));
 }
 
 struct EmbedLayout {
@@ -204,7 +206,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
         if (err != cudaSuccess) { rc = cuda_fail(err, "sort of tokens"); return; }
       }
       if (n == 0) return;
-      const int64_t smem = 2ll * team.teams * kStageRows * q.slot + 2ll * (team.teams * q.block + 2 * (q.block + 1)) * 4;
+      const int64_t smem = 1ll * kStages * team.teams * kStageRows * q.slot + 2ll * (team.teams * q.block + 2 * (q.block + 1)) * 4;
       if (smem > 220 * 1024) { rc = ADAPT_ERR_INVALID_ARG; return; }   // (never: embed_block has a limit)
       {
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);
@@ -213,7 +215,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
             const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
             if (err != cudaSuccess) return err;
           }
-          return launch_behind(kernel, static_cast<unsigned>(sums), kEmbedThreads, static_cast<int>(smem), stream, q);
+          return launch_behind(kernel, static_cast<unsigned>(sums), kSumThreads, static_cast<int>(smem), stream, q);
         };
         const cudaError_t err = vec ? sum(embed_sum_kernel<T, G, true>) : sum(embed_sum_kernel<T, G, false>);
         if (err != cudaSuccess) { rc = cuda_fail(err, "token embedding, backward"); return; }

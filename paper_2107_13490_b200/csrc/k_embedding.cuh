@@ -327,16 +327,19 @@ __device__ __forceinline__ void load_row(const G* p, float (&f)[V]) {
 }
 
 // A team of threads sums over the rows of its block, V elements a thread; CTAs of 256 threads hold one team or several.
-// Rows come through two stages in shared memory, kStageRows of each team's, which bulk copies fill ahead: whole rows under
-// way cost neither registers nor instructions.  Rows between 16-byte boundaries (kAligned false) are copied with the
+// Rows come through stages in shared memory, kStageRows of each team's, which a warp of its own fills ahead by bulk copies:
+// whole rows under way cost neither registers nor instructions.  (With two stages that the summing warps fill themselves,
+// the copies' latency shows: 16384 rows of 2048 bf16 28 -> NEWFIG us.)  Rows between 16-byte boundaries (kAligned false) are copied with the
 // aligned blocks around them and read element by element, V of them `lanes` apart.
-constexpr int kStageRows = 8;
+constexpr int kStageRows = 4;
+constexpr int kStages = 4;
+constexpr int kSumThreads = kEmbedThreads + 32;
 
 template <typename T, typename G, bool kAligned>
-__global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGradParams q) {
+__global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradParams q) {
   constexpr int V = 16 / static_cast<int>(sizeof(T));
   extern __shared__ __align__(128) unsigned char embed_smem[];
-  __shared__ __align__(8) unsigned long long bars[2];
+  __shared__ __align__(8) unsigned long long bars[2 * kStages];
   const int teams = kEmbedThreads / q.lanes, team = threadIdx.x / q.lanes, lane = threadIdx.x % q.lanes, warp_lane = threadIdx.x & 31;
   const int slice = blockIdx.x % q.slices, first_column = slice * q.lanes * V, columns = min(q.dim - first_column, q.lanes * V);
   const long long cta_first = static_cast<long long>(blockIdx.x / q.slices) * teams * q.block;
@@ -344,21 +347,23 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   const int stage_bytes = teams * kStageRows * q.slot;
   // tokens and places of the CTA's places, of a block in front and of one behind
   const int around = q.block + 1, held = teams * q.block + 2 * around;
-  unsigned* keys = reinterpret_cast<unsigned*>(embed_smem + 2 * stage_bytes) + around;
+  unsigned* keys = reinterpret_cast<unsigned*>(embed_smem + kStages * stage_bytes) + around;
   unsigned* places = keys + held;
   __shared__ int begins[kEmbedThreads / 8], ends_at[kEmbedThreads / 8];   // what the teams take
   __shared__ bool cut_front[kEmbedThreads / 8];
-  const unsigned full = shared_address(bars), vocab = static_cast<unsigned>(q.vocab);
+  const unsigned full = shared_address(bars), empty = full + 8 * kStages, vocab = static_cast<unsigned>(q.vocab);
   if (threadIdx.x == 0) {
-    barrier_init(full, 1);
-    barrier_init(full + 8, 1);
+    for (int s = 0; s < kStages; ++s) {
+      barrier_init(full + 8 * s, 1);
+      barrier_init(empty + 8 * s, kEmbedThreads / 32);
+    }
     barrier_init_fence();
   }
   wait_for_previous_kernel();
   {
     const unsigned* all_keys = q.keys[(q.passes + 1) & 1] + cta_first;
     const unsigned* all_places = q.places[(q.passes + 1) & 1] + cta_first;
-    for (int i = static_cast<int>(threadIdx.x) - around; i < count + around; i += kEmbedThreads) {
+    for (int i = static_cast<int>(threadIdx.x) - around; i < count + around; i += kSumThreads) {
       const long long p = cta_first + i;
       const bool known = p >= 0 && p < q.n;
       keys[i] = known ? all_keys[i] : ~0u;   // (in front of the first, too: equal to no token)
@@ -400,36 +405,39 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   }
   __syncthreads();
   auto row_at = [&](int i) { return static_cast<const T*>(q.dy) + places[i] * q.ld_dy + first_column; };
-  // by the first warp: the rows of a step
-  auto fill = [&](int step) {
-    unsigned bytes = 0;
-    for (int pass = 0; pass < 2; ++pass) {   // what will come is said before it is asked for
-      for (int r = warp_lane; r < teams * kStageRows; r += 32) {
-        const int of = r / kStageRows, i = begins[of] + step * kStageRows + r % kStageRows;
-        if (i >= ends_at[of] || !ADAPT_IN_BOUNDS(places[i], q.n, 52)) continue;
-        const T* row = row_at(i);
-        const unsigned skip = kAligned ? 0 : static_cast<unsigned>(reinterpret_cast<uintptr_t>(row) & 15u);
-        const unsigned size = (skip + columns * static_cast<unsigned>(sizeof(T)) + 15) & ~15u;
-        if (pass == 0) { bytes += size; continue; }
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     :: "r"(shared_address(embed_smem) + (step & 1) * stage_bytes + r * q.slot), "l"(reinterpret_cast<const unsigned char*>(row) - skip),
-                        "r"(size), "r"(full + 8 * (step & 1)) : "memory");
-        if (q.accumulate && keys[i + 1] != keys[i])   // what the sum will be added to
-          asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const G*>(q.dtable) + keys[i] * q.ld_grad + first_column));
-      }
-      if (pass == 0) {
-        bytes = __reduce_add_sync(~0u, bytes);
-        if (warp_lane == 0) barrier_expect_bytes(full + 8 * (step & 1), bytes);
-        __syncwarp();
-      }
-    }
-  };
   int most = 0;
   for (int t = 0; t < teams; ++t) most = max(most, ends_at[t] - begins[t]);
   const int steps = (most + kStageRows - 1) / kStageRows;
-  if (threadIdx.x < 32) {
-    if (steps > 0) fill(0);
-    if (steps > 1) fill(1);
+  if (threadIdx.x >= kEmbedThreads) {   // the rows of the steps, ahead
+    for (int step = 0; step < steps; ++step) {
+      const int s = step % kStages;
+      const bool ok = barrier_wait(empty + 8 * s, ((step / kStages) & 1) ^ 1);
+      if (!__all_sync(~0u, ok)) return;   // (those who sum find no data then)
+      auto size_of = [&](const T* row) {
+        const unsigned skip = kAligned ? 0 : static_cast<unsigned>(reinterpret_cast<uintptr_t>(row) & 15u);
+        return (skip + columns * static_cast<unsigned>(sizeof(T)) + 15) & ~15u;
+      };
+      auto each = [&](auto f) {
+        for (int r = warp_lane; r < teams * kStageRows; r += 32) {
+          const int of = r / kStageRows, i = begins[of] + step * kStageRows + r % kStageRows;
+          if (i < ends_at[of] && ADAPT_IN_BOUNDS(places[i], q.n, 52)) f(r, i, row_at(i));
+        }
+      };
+      unsigned bytes = 0;   // what will come is said before it is asked for
+      each([&](int, int, const T* row) { bytes += size_of(row); });
+      bytes = __reduce_add_sync(~0u, bytes);
+      if (warp_lane == 0) barrier_expect_bytes(full + 8 * s, bytes);
+      __syncwarp();
+      each([&](int r, int i, const T* row) {
+        const unsigned skip = kAligned ? 0 : static_cast<unsigned>(reinterpret_cast<uintptr_t>(row) & 15u);
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     :: "r"(shared_address(embed_smem) + s * stage_bytes + r * q.slot), "l"(reinterpret_cast<const unsigned char*>(row) - skip),
+                        "r"(size_of(row)), "r"(full + 8 * s) : "memory");
+        if (q.accumulate && keys[i + 1] != keys[i])   // what the sum will be added to
+          asm volatile("prefetch.global.L2 [%0];" :: "l"(static_cast<const G*>(q.dtable) + keys[i] * q.ld_grad + first_column));
+      });
+    }
+    return;
   }
   const int from = begins[team], to = ends_at[team];
   float sum[V] = {};
@@ -440,9 +448,10 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
   const unsigned base16 = static_cast<unsigned>(reinterpret_cast<uintptr_t>(static_cast<const T*>(q.dy) + first_column)) & 15u;
   const unsigned step16 = static_cast<unsigned>(q.ld_dy * sizeof(T)) & 15u;
   for (int step = 0; step < steps; ++step) {
-    const bool ok = barrier_wait(full + 8 * (step & 1), (step >> 1) & 1);
+    const int s = step % kStages;
+    const bool ok = barrier_wait(full + 8 * s, (step / kStages) & 1);
     if (!ok) sum[0] = __int_as_float(0x7FC00000);   // (a wait that ran out leaves NaN)
-    const unsigned char* stage = embed_smem + (step & 1) * stage_bytes + team * kStageRows * q.slot;
+    const unsigned char* stage = embed_smem + s * stage_bytes + team * kStageRows * q.slot;
     const int i0 = from + step * kStageRows, rows = min(kStageRows, to - i0);
     unsigned last = 0;   // rows after which a sum is written: a token's last, and the team's
 #pragma unroll
@@ -492,8 +501,8 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedGra
 #pragma unroll
       for (int k = 0; k < V; ++k) sum[k] = 0.0f;
     }
-    __syncthreads();   // the stage has been read
-    if (threadIdx.x < 32 && step + 2 < steps) fill(step + 2);
+    __syncwarp();
+    if (warp_lane == 0) barrier_arrive(empty + 8 * s);   // the warp has read the stage
   }
 }
 
