@@ -170,6 +170,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
   q.passes = n <= kSortFew ? 0 : (bits + kSortWidth - 1) / kSortWidth;
   q.width = q.passes ? (bits + q.passes - 1) / q.passes : 0;
   q.block = embed_block(n, dim);
+  q.cut = q.block / 2;   // (a team takes three halves of a block at most)
   const int wide = 16 / e;
   const bool vec = dim % wide == 0 && !misaligned(dy, 16) && !misaligned(dtable, 16) && (n <= 1 || ld_dy % wide == 0) &&
                    (vocab == 1 || ld_grad % wide == 0);
@@ -206,7 +207,7 @@ int adapt_embedding_backward(const void* dy, int64_t n, int64_t dim, int64_t ld_
         if (err != cudaSuccess) { rc = cuda_fail(err, "sort of tokens"); return; }
       }
       if (n == 0) return;
-      const int64_t smem = 1ll * kStages * team.teams * kStageRows * q.slot + 2ll * (team.teams * q.block + 2 * (q.block + 1)) * 4;
+      const int64_t smem = 1ll * kStages * team.teams * kStageRows * q.slot + 2ll * (team.teams * q.block + 2 * (q.cut + 1)) * 4;
       if (smem > 220 * 1024) { rc = ADAPT_ERR_INVALID_ARG; return; }   // (never: embed_block has a limit)
       {
         LaunchScope ls(ADAPT_KERNEL_EMBEDDING_BACKWARD, stream);

@@ -7,7 +7,7 @@
 // The gradient takes three launches.  The first sorts the tokens (stable, so that a token's occurrences stay in order) in
 // one cluster, whose CTAs exchange their digit counts through shared memory, while the other clusters write the rows of
 // tokens that do not occur, most of the table as a rule.  The second sums over blocks of the sorted places, one
-// block a team of threads.  A token of no more places than a block belongs to the team in whose block it begins; more
+// block a team of threads.  A token of up to half a block's places belongs to the team in whose block it begins; more
 // frequent ones are cut at the blocks' ends, the sums of their pieces are left in memory, and the third launch joins
 // them in the order of the blocks.  So every sum has one order, whatever the timing, and no row of dy is read twice.
 #pragma once
@@ -102,6 +102,7 @@ struct EmbedGradParams {
   float* partial;        // [blocks][2][dim] sums of a block's first token, which began in front, and of its last, which goes on (where they are cut)
   int width, passes;     // digits of the sort (passes 0: by comparisons)
   int block;             // sorted places of a block
+  int cut;               // places of a token (up to a block's) that is cut where a block ends
   int lanes;             // threads of a team
   int slices;            // teams side by side that share a row's columns
   int slot;              // bytes of a row in a stage
@@ -345,8 +346,8 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradP
   const long long cta_first = static_cast<long long>(blockIdx.x / q.slices) * teams * q.block;
   const int count = static_cast<int>(min(static_cast<long long>(teams) * q.block, q.n - cta_first));
   const int stage_bytes = teams * kStageRows * q.slot;
-  // tokens and places of the CTA's places, of a block in front and of one behind
-  const int around = q.block + 1, held = teams * q.block + 2 * around;
+  // tokens and places of the CTA's places, and of some in front and behind
+  const int around = q.cut + 1, held = teams * q.block + 2 * around;
   unsigned* keys = reinterpret_cast<unsigned*>(embed_smem + kStages * stage_bytes) + around;
   unsigned* places = keys + held;
   __shared__ int begins[kEmbedThreads / 8], ends_at[kEmbedThreads / 8];   // what the teams take
@@ -385,14 +386,14 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradP
       return lo;
     };
     if (from < count) {
-      if (keys[from - 1] == keys[from]) {   // its token's places, as far as a block away
-        const int first = search(from - around, from, keys[from]), stop = search(from + 1, from + q.block + 1, keys[from] + 1);
-        front = stop - first > q.block;
+      if (keys[from - 1] == keys[from]) {   // its token's places, as far as it matters
+        const int first = search(from - around, from, keys[from]), stop = search(from + 1, from + q.cut + 1, keys[from] + 1);
+        front = stop - first > q.cut;
         if (!front) begin = stop;   // the team in front takes it
       }
       if (keys[to] == keys[to - 1]) {
-        const int first = search(to - around, to, keys[to]), stop = search(to + 1, to + q.block + 1, keys[to] + 1);
-        if (stop - first <= q.block) end = stop;   // (then it begins in this block)
+        const int first = search(to - around, to, keys[to]), stop = search(to + 1, to + q.cut + 1, keys[to] + 1);
+        if (stop - first <= q.cut) end = stop;   // (then it begins in this block)
       }
       begin = min(begin, end);
       end = search(begin, end, vocab);   // (places without a token are sorted to the end)
