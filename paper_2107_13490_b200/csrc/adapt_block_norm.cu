@@ -19,8 +19,8 @@ namespace {
 
 constexpr int kSms = 148;   // of a B200
 
-// How a row is held: by CTAs of so many threads, `parts` of them, `per_sm` on an SM.  (There is room for up to 7 elements
-// between a boundary and an odd row.)  128 registers a thread backward, 64 forward.
+// How a row is held: by CTAs of so many threads, `parts` of them, `per_sm` on an SM (at most; a kernel's registers say how many).
+// There is room for up to 7 elements between a boundary and an odd row.
 struct NormShape {
   int parts = 1, threads, per_sm;
   NormShape(int64_t dim, int most, int of_sm, int ctas) {
@@ -32,21 +32,25 @@ struct NormShape {
   }
 };
 NormShape norm_forward(int64_t dim) { return NormShape(dim, kNormMaxThreads, 1024, 16); }
-NormShape norm_backward(int64_t dim) { return NormShape(dim, kNormBackwardThreads, 512, 8); }
+// (backward: CTAs of one warp, whose rows take a warp's latency each, as many as there is room for; of more, stages pay rather
+// than CTAs.  us: 65536 x 256 bf16 with 8 78, with 12 62; 32768 x 1024 fp32 with 8 87, with 10 95)
+NormShape norm_backward(int64_t dim) { return NormShape(dim, kNormBackwardThreads, 512, dim <= 32 * kNormElems ? 16 : 8); }
 static_assert(ADAPT_NORM_MAX_DIM <= kNormElems * kNormBackwardThreads * kNormMaxParts, "a cluster holds the longest row");
 
-// CTAs (or clusters) of a backward pass, each with sums of its own over its rows.
+// CTAs (or clusters) of a backward pass at most, each with sums of its own over its rows.
 int64_t norm_ctas(int64_t rows, int64_t dim) {
   const NormShape shape = norm_backward(dim);
   return std::min<int64_t>(rows, kSms * shape.per_sm / shape.parts);
 }
-// A multiple of the period, so that a CTA's rows lie alike; the CTAs that has more have no rows, and sums of 0.
+// A multiple of the period, so that a CTA's rows lie alike; the CTAs that are more have no rows, and sums of 0.
 unsigned norm_grid(int64_t ctas, int period) { return static_cast<unsigned>((ctas + period - 1) / period * period); }
 
 // How the rows come through shared memory, if they do: all tensors have to lie alike to the 16-byte boundary, row by row.
 struct NormPlan {
   NormRing ring = {};
-  int smem = 0, period = 1;   // rows whose numbers differ by a multiple of the period lie alike
+  int smem = 0, copy = 0, copies = 0;
+  bool used[3];
+  int period = 1;   // rows whose numbers differ by a multiple of the period lie alike
   bool staged = true, edges = false;
   NormPlan(const NormParams& q, int e, const NormShape& shape, std::initializer_list<std::pair<const void*, long long>> in,
            std::initializer_list<std::pair<const void*, long long>> out) {
@@ -65,16 +69,19 @@ struct NormPlan {
       edges = edges || misaligned(p, 16);
     while (period * by % 16) period *= 2;
     ring.parts = shape.parts;
-    const int width = kNormElems * shape.threads, per_sm = shape.per_sm;   // elements of a part
+    const int width = kNormElems * shape.threads;   // elements of a part
     if (edges && q.dim + 16 / e - 1 > width * shape.parts) staged = false;   // the elements before a boundary take room too
     ring.stage_row = shape.parts > 1 ? width * e : edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
     for (int& p : ring.place) p = p < 0 ? -1 : p * ring.stage_row;
-    const int stage = ring.streams * ring.stage_row, copy = edges ? width * 4 : 0;
-    const bool used[3] = {q.after != kNormNone, q.before != kNormNone, q.shared};
-    int copies = 0;
+    copy = edges ? width * 4 : 0;
+    used[0] = q.after != kNormNone; used[1] = q.before != kNormNone; used[2] = q.shared;
     for (bool u : used) copies += u ? copy : 0;
-    ring.stages = std::min(kNormMaxStages, std::max((200 * 1024 / per_sm - copies) / stage, (220 * 1024 - copies) / stage > 0 ? 1 : 0));
-    staged = staged && ring.stages > 0;
+    staged = staged && (220 * 1024 - copies) / (ring.streams * ring.stage_row) > 0;
+  }
+  // Stages and the rest of shared memory for so many CTAs on an SM.
+  void fit(int per_sm) {
+    const int stage = ring.streams * ring.stage_row;
+    ring.stages = std::min(kNormMaxStages, std::max((200 * 1024 / per_sm - copies) / stage, 1));
     smem = ring.stages * stage;
     smem = (smem + 15) / 16 * 16;
     for (int w = 0; w < 3; ++w) {
@@ -101,28 +108,44 @@ void with_form(const NormParams& q, bool edges, F f) {
   if (edges) norms(std::true_type{}); else norms(std::false_type{});
 }
 
-// Launches a kernel that may need more shared memory than a kernel has by itself.
+// What the device says of a kernel, once for each device; it may use all of an SM's shared memory from then on.
 template <auto kKernel>
-int norm_launch(unsigned groups, const NormShape& shape, int smem, cudaStream_t stream, const NormParams& q, const NormRing& ring) {
-  static std::atomic<uint64_t> ready{0};   // devices that know
+int norm_registers(int* out) {
+  static std::atomic<int> known[kMaxDevices];
   int device = 0;
   ADAPT_CUDA(cudaGetDevice(&device));
-  const uint64_t bit = 1ull << (device & 63);
-  if (!(ready.load() & bit)) {
+  std::atomic<int>& slot = known[device % kMaxDevices];
+  int n = slot.load();
+  if (!n) {
+    cudaFuncAttributes a = {};
+    ADAPT_CUDA(cudaFuncGetAttributes(&a, kKernel));
     ADAPT_CUDA(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
-    ready.fetch_or(bit);
+    slot.store(n = (a.numRegs + 7) / 8 * 8);
   }
+  *out = n;
+  return ADAPT_OK;
+}
+
+// Launches a kernel on as many CTAs as the device holds at once, and says how many (clusters) that are.
+template <auto kKernel>
+int norm_launch(int64_t rows, const NormShape& shape, NormPlan plan, cudaStream_t stream, const NormParams& q, int* groups) {
+  int registers = 0;
+  const int rc = norm_registers<kKernel>(&registers);
+  if (rc != ADAPT_OK) return rc;
+  const int per_sm = std::max(1, std::min(shape.per_sm, 65536 / (registers * shape.threads)));
+  plan.fit(per_sm);
+  *groups = static_cast<int>(norm_grid(std::min<int64_t>(rows, kSms * per_sm / shape.parts), plan.period));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(groups * shape.parts);
+  cfg.gridDim = dim3(static_cast<unsigned>(*groups * shape.parts));
   cfg.blockDim = dim3(shape.threads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = plan.smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = shape.parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = shape.parts > 1 ? 1 : 0;
-  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kKernel, q, ring));
+  ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kKernel, q, plan.ring));
   return ADAPT_OK;
 }
 
@@ -180,12 +203,12 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
     const NormPlan plan(q, e, shape, {{block, q.ld_block}, {residual, q.ld_residual}, {q.shared ? nullptr : gate, q.ld_gate},
                         {nullptr, 0}, {nullptr, 0}}, {{y, q.ld_y}, {normed, q.ld_normed}});
     if (plan.staged) {
-      const unsigned grid = norm_grid(std::min<int64_t>(rows, kSms * shape.per_sm / shape.parts), plan.period);
+      int groups = 0;
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
         with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
           rc = norm_launch<norm_row_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
-              grid, shape, plan.smem, stream, q, plan.ring);
+              rows, shape, plan, stream, q, &groups);
         });
       });
       return rc;
@@ -257,14 +280,12 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
                         {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
                         {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
     if (plan.staged && (q.after != kNormNone || d_normed)) {
-      const unsigned grid = norm_grid(ctas, plan.period);
-      sum.ctas = static_cast<int>(grid);
       if (!d_normed) q.before = kNormNone;   // (its gradient is not given)
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
         with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
           rc = norm_launch<norm_row_backward_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
-              grid, shape, plan.smem, stream, q, plan.ring);
+              rows, shape, plan, stream, q, &sum.ctas);
         });
       });
     } else {
