@@ -117,7 +117,7 @@ int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_ta
   const int wide = 16 / e;
   const bool vec = dim % wide == 0 && !misaligned(table, 16) && !misaligned(out, 16) && (vocab == 1 || ld_table % wide == 0) &&
                    (n == 1 || ld_out % wide == 0);
-  const int64_t parts = vec ? dim / wide : dim;
+  const int64_t parts = (dim + wide - 1) / wide + (vec ? 0 : 1);
   int lanes = 1;
   while (lanes < kEmbedThreads && lanes * 4 < parts) lanes *= 2;
   const int rows = kEmbedThreads / lanes;
@@ -126,8 +126,8 @@ int adapt_embedding(const void* table, int64_t vocab, int64_t dim, int64_t ld_ta
   LaunchScope ls(ADAPT_KERNEL_EMBEDDING, stream);
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (vec) embedding_kernel<T, 16 / sizeof(T)><<<grid, kEmbedThreads, 0, stream>>>(q, lanes);
-    else embedding_kernel<T, 1><<<grid, kEmbedThreads, 0, stream>>>(q, lanes);
+    if (vec) embedding_kernel<T, false><<<grid, kEmbedThreads, 0, stream>>>(q, lanes);
+    else embedding_kernel<T, true><<<grid, kEmbedThreads, 0, stream>>>(q, lanes);
   });
   ADAPT_LAUNCH_OK("token embedding");
   return ADAPT_OK;

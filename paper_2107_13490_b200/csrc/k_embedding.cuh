@@ -43,45 +43,51 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[V]) {
   }
 }
 
-// Parts of rows as they lie in memory, and their elements.
-template <typename T, int V> struct RawPart { typedef uint4 type; };
-template <typename T> struct RawPart<T, 1> { typedef T type; };
-template <typename T, int V>
-__device__ __forceinline__ void widen(const uint4& raw, float (&f)[V]) { unpack16<T>(raw, f); }
-template <typename T, int V>
-__device__ __forceinline__ void widen(const T& raw, float (&f)[1]) { f[0] = to_float(raw); }
-
-// `lanes` threads (a power of two, up to the CTA) take a row; V elements at a time.
+// `lanes` threads (a power of two, up to the CTA) take a row, 16 bytes of the output at a time and four such parts under
+// way, as they lie in memory.  kShift: tables or outputs that are not 16-byte aligned.  Then a part is a 16-byte block of the
+// output, and the table's is shifted out of the two blocks that hold it; the ends of a row go element by element.
 constexpr int kEmbedThreads = 256;
 
-template <typename T, int V>
+template <typename T, bool kShift>
 __global__ __launch_bounds__(kEmbedThreads) void embedding_kernel(EmbedParams q, int lanes) {
+  constexpr int V = 16 / static_cast<int>(sizeof(T)), kParts = 4;
   const int i = blockIdx.x * (kEmbedThreads / lanes) + threadIdx.x / lanes;
   if (i >= q.n) return;
   const int lane = threadIdx.x & (lanes - 1);
   const long long id = q.ids[i];
   T* out = static_cast<T*>(q.out) + i * q.ld_out;
-  const T* row = static_cast<const T*>(q.table) + (id >= 0 && id < q.vocab ? id : 0) * q.ld_table;
-  const float fill = id < 0 ? 0.0f : __int_as_float(0x7FC00000);
   const bool known = id >= 0 && id < q.vocab;
-  constexpr int kUnroll = 4;   // parts that a thread has under way, as they lie in memory
-  typedef typename RawPart<T, V>::type Raw;
-  for (int at = lane * V; at < q.dim; at += lanes * V * kUnroll) {
-    Raw raw[kUnroll];
+  const T* row = static_cast<const T*>(q.table) + (known ? id : 0) * q.ld_table;
+  const float fill = id < 0 ? 0.0f : __int_as_float(0x7FC00000);
+  const int skip = kShift ? static_cast<int>((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(T)) : 0;
+  const unsigned shift = kShift ? static_cast<unsigned>(reinterpret_cast<uintptr_t>(row - skip) & 15u) : 0;
+  auto whole = [&](int c) { return !kShift || (c >= 0 && c + V <= q.dim); };
+  for (int at = lane * V - skip; at < q.dim; at += lanes * V * kParts) {
+    uint4 low[kParts], high[kParts];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kParts; ++u) {
       const int c = at + u * lanes * V;
-      if (known && c < q.dim) raw[u] = __ldg(reinterpret_cast<const Raw*>(row + c));
+      low[u] = high[u] = make_uint4(0, 0, 0, 0);
+      if (!known || c >= q.dim || !whole(c)) continue;
+      const uint4* block = reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(row + c) - shift);
+      low[u] = __ldg(block);
+      if (kShift && shift) high[u] = __ldg(block + 1);
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kParts; ++u) {
       const int c = at + u * lanes * V;
       if (c >= q.dim) break;
-      float f[V];
-      widen<T, V>(raw[u], f);
+      if (whole(c)) {
+        float f[V];
+        unpack16<T>(kShift ? shift_bytes(low[u], high[u], shift) : low[u], f);
 #pragma unroll
-      for (int k = 0; k < V; ++k) f[k] = known ? f[k] * q.scale : fill;
-      store_part<T, V>(out + c, f);
+        for (int k = 0; k < V; ++k) f[k] = known ? f[k] * q.scale : fill;
+        *reinterpret_cast<uint4*>(out + c) = pack16<T>(f);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (c + k >= 0 && c + k < q.dim) out[c + k] = from_float<T>(known ? to_float(row[c + k]) * q.scale : fill);
+      }
     }
   }
 }
@@ -135,7 +141,7 @@ __device__ __forceinline__ void embed_sort_few(const EmbedGradParams& q, unsigne
     rank += (k.x < key || (k.x == key && j < i)) + (k.y < key || (k.y == key && j + 1 < i)) + (k.z < key || (k.z == key && j + 2 < i)) +
             (k.w < key || (k.w == key && j + 3 < i));
   }
-  if (ADAPT_IN_BOUNDS(rank, n, 51)) {
+  if (ADAPT_IN_BOUNDS(rank, n, 71)) {
     q.keys[1][rank] = key;   // (where an even number of passes leaves them)
     q.places[1][rank] = i;
   }
@@ -227,7 +233,7 @@ __device__ __forceinline__ void embed_sort_many(const EmbedGradParams& q, unsign
       __syncwarp();
       if (live && !before) mine[digit] += __popc(peers);
       __syncwarp();
-      if (live && ADAPT_IN_BOUNDS(goal, n, 50)) {
+      if (live && ADAPT_IN_BOUNDS(goal, n, 70)) {
         q.keys[pass & 1][goal] = key;
         q.places[pass & 1][goal] = place;
       }
@@ -329,9 +335,9 @@ __device__ __forceinline__ void load_row(const G* p, float (&f)[V]) {
 
 // A team of threads sums over the rows of its block, V elements a thread; CTAs of 256 threads hold one team or several.
 // Rows come through stages in shared memory, kStageRows of each team's, which a warp of its own fills ahead by bulk copies:
-// whole rows under way cost neither registers nor instructions.  (With two stages that the summing warps fill themselves,
-// the copies' latency shows: 16384 rows of 2048 bf16 28 -> NEWFIG us.)  Rows between 16-byte boundaries (kAligned false) are copied with the
-// aligned blocks around them and read element by element, V of them `lanes` apart.
+// whole rows under way cost neither registers nor instructions.  (Filled by the warps that sum, from two stages, narrow rows
+// waited for it: 131072 rows of 64 bf16 100 us, so 91.)  Rows between 16-byte boundaries (kAligned false) are copied
+// with the aligned blocks around them and read element by element, V of them `lanes` apart.
 constexpr int kStageRows = 4;
 constexpr int kStages = 4;
 constexpr int kSumThreads = kEmbedThreads + 32;
@@ -421,7 +427,7 @@ __global__ __launch_bounds__(kSumThreads) void embed_sum_kernel(const EmbedGradP
       auto each = [&](auto f) {
         for (int r = warp_lane; r < teams * kStageRows; r += 32) {
           const int of = r / kStageRows, i = begins[of] + step * kStageRows + r % kStageRows;
-          if (i < ends_at[of] && ADAPT_IN_BOUNDS(places[i], q.n, 52)) f(r, i, row_at(i));
+          if (i < ends_at[of] && ADAPT_IN_BOUNDS(places[i], q.n, 72)) f(r, i, row_at(i));
         }
       };
       unsigned bytes = 0;   // what will come is said before it is asked for

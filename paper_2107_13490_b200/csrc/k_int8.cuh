@@ -471,22 +471,6 @@ struct CopyRows {
 };
 struct CopyParams { CopyRows part[2]; int cols; };   // activations and weights, either may have no rows
 
-// 16 bytes that begin at byte `o` of two aligned blocks.
-__device__ __forceinline__ uint4 shift_bytes(const uint4& lo, const uint4& hi, unsigned o) {
-  unsigned w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-  if (o & 8) {
-#pragma unroll
-    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-  }
-  if (o & 4) {
-#pragma unroll
-    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-  }
-  const unsigned bits = (o & 3) * 8;
-  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
-                    __funnelshift_r(w[3], w[4], bits));
-}
-
 constexpr int kCopyThreads = 128;
 
 // Only aligned blocks that hold a byte of the row are read.
