@@ -22,19 +22,30 @@ constexpr int kSms = 148;   // of a B200
 // How a row is held: by CTAs of so many threads, `parts` of them, `per_sm` on an SM (at most; a kernel's registers say how many).
 // There is room for up to 7 elements between a boundary and an odd row.
 struct NormShape {
-  int parts = 1, threads, per_sm;
-  NormShape(int64_t dim, int most, int of_sm, int ctas) {
+  int elems, rows, parts = 1, threads, per_sm;   // of a thread, at a time
+  NormShape(int64_t dim, int elems_, int rows_, int most, int of_sm, int ctas) : elems(elems_), rows(rows_) {
     const int64_t room = dim + (dim % 8 ? 7 : 0);
-    while (room > static_cast<int64_t>(kNormElems) * most * parts) parts *= 2;
-    const int64_t unit = 32ll * kNormElems * parts;
+    while (room > static_cast<int64_t>(elems) * most * parts) parts *= 2;
+    const int64_t unit = 32ll * elems * parts;
     threads = static_cast<int>((room + unit - 1) / unit) * 32;
     per_sm = std::max(1, std::min(ctas, of_sm / threads));
   }
 };
-NormShape norm_forward(int64_t dim) { return NormShape(dim, kNormMaxThreads, 1024, 16); }
+NormShape norm_forward(int64_t dim) { return NormShape(dim, kNormElems, 1, kNormMaxThreads, 1024, 16); }
 // (backward: CTAs of one warp, whose rows take a warp's latency each, as many as there is room for; of more, stages pay rather
 // than CTAs.  us: 65536 x 256 bf16 with 8 78, with 12 62; 32768 x 1024 fp32 with 8 87, with 10 95)
-NormShape norm_backward(int64_t dim) { return NormShape(dim, kNormBackwardThreads, 512, dim <= 32 * kNormElems ? 16 : 8); }
+NormShape norm_backward(int64_t dim) { return NormShape(dim, kNormElems, 1, kNormBackwardThreads, 512, dim <= 32 * kNormElems ? 16 : 8); }
+// Two rows at a time, by no more CTAs; where they pay.  Above, more CTAs do, and rows of up to 512 are a warp's, 16 CTAs on an SM.
+// us, by ones and by pairs, 2^25 elements: 256 bf16 with both norms and a gate 149, 130; 384 152, 167; 768 156, 135; 1024 124, 126;
+// with one norm fp32 768 85, 75; 1024 86, 73; 2048 86, 74; 2560 80, 95; 16384 rows of 2039 bf16 82, 94
+NormShape norm_backward_pairs(int64_t dim) {
+  return NormShape(dim, kNormPairElems, 2, kNormPairThreads, 512, dim <= 32 * kNormPairElems ? 16 : 8);
+}
+bool norm_in_pairs(int64_t dim, int norms) {
+  const int64_t room = dim + (dim % 8 ? 7 : 0), warp = 32 * kNormPairElems;
+  return room <= warp || (room > 2 * warp && room <= (norms == 1 && dim % 8 == 0 ? 8 * warp : 4 * warp));
+}
+static_assert(8 * 32 * kNormPairElems <= kNormPairElems * kNormPairThreads, "a CTA holds a pair of rows");
 static_assert(ADAPT_NORM_MAX_DIM <= kNormElems * kNormBackwardThreads * kNormMaxParts, "a cluster holds the longest row");
 
 // CTAs (or clusters) of a backward pass at most, each with sums of its own over its rows.
@@ -69,19 +80,19 @@ struct NormPlan {
       edges = edges || misaligned(p, 16);
     while (period * by % 16) period *= 2;
     ring.parts = shape.parts;
-    const int width = kNormElems * shape.threads;   // elements of a part
+    const int width = shape.elems * shape.threads;   // elements of a part
     if (edges && q.dim + 16 / e - 1 > width * shape.parts) staged = false;   // the elements before a boundary take room too
     ring.stage_row = shape.parts > 1 ? width * e : edges ? (q.dim * e + 15 + 15) / 16 * 16 : q.dim * e;
     for (int& p : ring.place) p = p < 0 ? -1 : p * ring.stage_row;
     copy = edges ? width * 4 : 0;
     used[0] = q.after != kNormNone; used[1] = q.before != kNormNone; used[2] = q.shared;
     for (bool u : used) copies += u ? copy : 0;
-    staged = staged && (220 * 1024 - copies) / (ring.streams * ring.stage_row) > 0;
+    staged = staged && (220 * 1024 - copies) / (ring.streams * ring.stage_row) >= shape.rows;
   }
   // Stages and the rest of shared memory for so many CTAs on an SM.
-  void fit(int per_sm) {
+  void fit(int per_sm, int rows) {
     const int stage = ring.streams * ring.stage_row;
-    ring.stages = std::min(kNormMaxStages, std::max((200 * 1024 / per_sm - copies) / stage, 1));
+    ring.stages = std::min(kNormMaxStages, std::max((200 * 1024 / per_sm - copies) / stage, rows)) / rows * rows;   // whole turns
     smem = ring.stages * stage;
     smem = (smem + 15) / 16 * 16;
     for (int w = 0; w < 3; ++w) {
@@ -133,7 +144,7 @@ int norm_launch(int64_t rows, const NormShape& shape, NormPlan plan, cudaStream_
   const int rc = norm_registers<kKernel>(&registers);
   if (rc != ADAPT_OK) return rc;
   const int per_sm = std::max(1, std::min(shape.per_sm, 65536 / (registers * shape.threads)));
-  plan.fit(per_sm);
+  plan.fit(per_sm, shape.rows);
   *groups = static_cast<int>(norm_grid(std::min<int64_t>(rows, kSms * per_sm / shape.parts), plan.period));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(*groups * shape.parts));
@@ -275,17 +286,29 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   int rc = ADAPT_OK;
   {
     LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM_BACKWARD, stream);
-    const NormShape shape = norm_backward(dim);
-    const NormPlan plan(q, e, shape, {{block, q.ld_block}, {residual, q.ld_residual},
-                        {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
-                        {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
+    auto plan_for = [&](const NormShape& shape) {
+      return NormPlan(q, e, shape, {{block, q.ld_block}, {residual, q.ld_residual},
+                      {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
+                      {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
+    };
+    NormShape shape = norm_backward(dim);
+    NormPlan plan = plan_for(shape);
+    if (norm_in_pairs(dim, (q.after != kNormNone) + (d_normed != nullptr))) {
+      const NormPlan pairs = plan_for(norm_backward_pairs(dim));
+      if (pairs.staged) {   // (there may be no room before a boundary)
+        shape = norm_backward_pairs(dim);
+        plan = pairs;
+      }
+    }
     if (plan.staged && (q.after != kNormNone || d_normed)) {
       if (!d_normed) q.before = kNormNone;   // (its gradient is not given)
       with_type(dtype, [&](auto t) {
         using T = decltype(t);
         with_form(q, plan.edges, [&](auto edges, auto after, auto before, auto kind) {
-          rc = norm_launch<norm_row_backward_kernel<T, decltype(edges)::value, decltype(after)::value, decltype(before)::value, decltype(kind)::value>>(
-              rows, shape, plan, stream, q, &sum.ctas);
+          constexpr bool E = decltype(edges)::value, A = decltype(after)::value, B = decltype(before)::value;
+          constexpr int K = decltype(kind)::value;
+          rc = shape.rows == 2 ? norm_launch<norm_pair_backward_kernel<T, E, A, B, K>>(rows, shape, plan, stream, q, &sum.ctas)
+                               : norm_launch<norm_row_backward_kernel<T, E, A, B, K>>(rows, shape, plan, stream, q, &sum.ctas);
         });
       });
     } else {

@@ -269,45 +269,54 @@ __device__ __forceinline__ Two kept_open(Two k) {
 }
 __device__ __forceinline__ Two kept_slope(Two k) { return make_float2(fmaf(-fabsf(k.x), fabsf(k.x), fabsf(k.x)), fmaf(-fabsf(k.y), fabsf(k.y), fabsf(k.y))); }
 
-// Sums over a CTA, in one of two sets of places in turn, so that one barrier each is enough.
 constexpr int kNormMaxParts = 4;
 
-template <int kThreads>
+// Sums over a CTA, up to kMost at a time, in one of two sets of places in turn, so that one barrier each is enough.
+template <int kThreads, int kMost>
 struct CtaSums {
-  float2 (*places)[kThreads / 32];
-  float2 (*parts)[kNormMaxParts];   // a sum of each CTA of the cluster
+  float (*places)[kMost][kThreads / 32];
+  float (*parts)[kNormMaxParts][kMost];   // sums of each CTA of the cluster
   int turn, part, count;
-  template <bool kTwo>
-  __device__ __forceinline__ float2 over_warp(float a, float b) const {
+  template <int N>
+  __device__ __forceinline__ static void over_warp(float (&v)[N]) {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) {
-      a += __shfl_xor_sync(~0u, a, d);
-      if (kTwo) b += __shfl_xor_sync(~0u, b, d);
-    }
-    return make_float2(a, b);
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] += __shfl_xor_sync(~0u, v[j], d);
   }
-  template <bool kTwo>
-  __device__ __forceinline__ float2 meet(float a, float b) {
-    float2 s = over_warp<kTwo>(a, b);
-    if (blockDim.x == 32) { __syncwarp(); return s; }   // (rows so short are not shared)
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
+    over_warp(v);
+    if (blockDim.x == 32) { __syncwarp(); return; }   // (rows so short are not shared)
     const int lane = threadIdx.x & 31;
-    if (lane == 0) places[turn][threadIdx.x >> 5] = s;
+    if (lane == 0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) places[turn][j][threadIdx.x >> 5] = v[j];
+    }
     __syncthreads();
-    s = lane < static_cast<int>(blockDim.x >> 5) ? places[turn][lane] : make_float2(0.0f, 0.0f);
-    s = over_warp<kTwo>(s.x, s.y);
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = lane < static_cast<int>(blockDim.x >> 5) ? places[turn][j][lane] : 0.0f;
+    over_warp(v);
     if (count > 1) {
-      if (threadIdx.x < static_cast<unsigned>(count))
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(peer_address(shared_address(&parts[turn][part]), threadIdx.x)), "f"(s.x), "f"(s.y)
-                     : "memory");
+      if (threadIdx.x < static_cast<unsigned>(count)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(peer_address(shared_address(&parts[turn][part][j]), threadIdx.x)), "f"(v[j]) : "memory");
+      }
       meet_cluster();
-      s = make_float2(0.0f, 0.0f);
-      for (int p = 0; p < count; ++p) { const float2 t = parts[turn][p]; s.x += t.x; s.y += t.y; }
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = 0.0f;
+      for (int p = 0; p < count; ++p)
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] += parts[turn][p][j];
     }
     turn ^= 1;
-    return s;
   }
-  __device__ __forceinline__ float one(float a) { return meet<false>(a, 0.0f).x; }
-  __device__ __forceinline__ float2 two(float a, float b) { return meet<true>(a, b); }
+  __device__ __forceinline__ float one(float a) {
+    float v[1] = {a};
+    (*this)(v);
+    return v[0];
+  }
 };
 
 // The rows of a CTA in order, read ahead into the ring by its first thread, and the columns of a thread.
@@ -392,9 +401,9 @@ struct NormRows {
                      :: "r"(shared_address(stages) + s * ring.streams * ring.stage_row + ring.place[i]), "l"(static_cast<const T*>(from[i]) + r * ld[i] + from_column),
                         "r"(bytes), "r"(bars + 8 * s) : "memory");
   }
-  // Waits for the row's data; 0, or NaN where they never came.
-  __device__ __forceinline__ float ready() const {
-    return barrier_wait(bars + 8 * stage, parity) ? 0.0f : __int_as_float(0x7FC00000);
+  // Waits for the row's data (or the next row's); 0, or NaN where they never came.
+  __device__ __forceinline__ float ready(int behind = 0) const {
+    return barrier_wait(bars + 8 * (stage + behind), parity) ? 0.0f : __int_as_float(0x7FC00000);
   }
   // Called when every thread has read what it needs of the row `r`.
   __device__ __forceinline__ void release(unsigned r) {
@@ -404,8 +413,8 @@ struct NormRows {
   }
   // Chunk i of stream kStream; 0 for what is not in the row.
   template <int kStream>
-  __device__ __forceinline__ void read(int i, Two (&f)[P]) const {
-    const uint4 raw = *reinterpret_cast<const uint4*>(at + ring.place[kStream] + i * blockDim.x * 16);
+  __device__ __forceinline__ void read(int i, Two (&f)[P], int behind = 0) const {   // (1: of the next row, in the next stage)
+    const uint4 raw = *reinterpret_cast<const uint4*>(at + behind * ring.streams * ring.stage_row + ring.place[kStream] + i * blockDim.x * 16);
     float v[V];
     unpack16<T>(raw, v);
     if (kEdges && !whole(i)) {
@@ -470,10 +479,9 @@ __global__ __launch_bounds__(kNormMaxThreads, 1) void norm_row_kernel(const Norm
   constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kNormElems / 2;
   extern __shared__ __align__(128) unsigned char norm_smem[];
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
-  __shared__ float2 places[2][kNormMaxThreads / 32];
+  __shared__ float places[2][1][kNormMaxThreads / 32], parts[2][kNormMaxParts][1];
   Rows rows(q, ring, norm_smem, bars);
-  __shared__ float2 parts[2][kNormMaxParts];
-  CtaSums<kNormMaxThreads> sums{places, parts, 0, rows.part, ring.parts};
+  CtaSums<kNormMaxThreads, 1> sums{places, parts, 0, rows.part, ring.parts};
   const float inv = 1.0f / static_cast<float>(q.dim);
   // mean and 1 / deviation; the deviation around the mean, in a second sum
   auto statistics = [&](const Two (&v)[kPairs], int kind) {
@@ -567,10 +575,9 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
   constexpr bool kForAll = kGate == kGateForAll;
   extern __shared__ __align__(128) unsigned char norm_smem[];
   __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
-  __shared__ float2 places[2][kNormBackwardThreads / 32];
+  __shared__ float places[2][2][kNormBackwardThreads / 32], parts[2][kNormMaxParts][2];
   Rows rows(q, ring, norm_smem, bars);
-  __shared__ float2 parts[2][kNormMaxParts];
-  CtaSums<kNormBackwardThreads> sums{places, parts, 0, rows.part, ring.parts};
+  CtaSums<kNormBackwardThreads, 2> sums{places, parts, 0, rows.part, ring.parts};
   const float inv = 1.0f / static_cast<float>(q.dim);
   Two of_after[kAfter ? kPairs : 1], of_before[kBefore ? kPairs : 1], of_gate[kForAll ? kPairs : 1];   // sums over rows
 #pragma unroll
@@ -637,8 +644,9 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
           s = sum(s, d);
         }
       }
-      m = sums.two(sh.x + sh.y, s.x + s.y + poison);
-      m.x *= inv;
+      float t[2] = {sh.x + sh.y, s.x + s.y + poison};
+      sums(t);
+      m = make_float2(t[0] * inv, t[1]);
       m.y = q.before == kNormLayer ? m.y * inv : poison;
     }
     Two sh = both(0.0f), s = sh;
@@ -693,8 +701,9 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
       for (int k = 0; k < P; ++k) one[i * P + k] = d[k];
     }
     if (kAfter) {
-      m = sums.two(sh.x + sh.y, s.x + s.y + poison);
-      m.x *= inv;
+      float t[2] = {sh.x + sh.y, s.x + s.y + poison};
+      sums(t);
+      m = make_float2(t[0] * inv, t[1]);
       m.y = q.after == kNormLayer ? m.y * inv : poison;
     } else {
       __syncthreads();
@@ -710,6 +719,199 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
       for (int k = 0; k < P; ++k)
         f[k] = kAfter ? times_plus(two[i * P + k], by_x, times_plus(one[i * P + k], st.y, by_y)) : one[i * P + k];
       rows.write(q.d_block, r * q.ld_d_block, i, f);
+    }
+  }
+  if (!q.partial) return;
+  const long long plane = static_cast<long long>(rows.groups) * q.dim;
+  float* mine = q.partial + static_cast<long long>(rows.group) * q.dim;
+#pragma unroll
+  for (int i = 0; i < kChunks; ++i) {
+    if (!rows.any(i)) break;
+    if (kForAll) rows.write_sums(mine, i, of_gate + (kForAll ? i * P : 0));
+    if (kAfter) rows.write_sums(mine + plane, i, of_after + (kAfter ? i * P : 0));
+    if (kBefore) rows.write_sums(mine + 2 * plane, i, of_before + (kBefore ? i * P : 0));
+  }
+}
+
+// The same for shorter rows, two at a time: they share the reading of the weights and the rounds of sums, and each one's
+// latencies hide behind the other's.  A thread holds eight elements of both; the ring has an even number of stages.
+constexpr int kNormPairElems = 8;
+constexpr int kNormPairThreads = 256;
+
+template <typename T, bool kEdges, bool kAfter, bool kBefore, int kGate>
+__global__ __launch_bounds__(kNormPairThreads, 2) void norm_pair_backward_kernel(const NormParams q, const NormRing ring) {
+  typedef NormRows<T, kNormPairElems, kEdges> Rows;
+  constexpr int P = Rows::P, kChunks = Rows::kChunks, kPairs = kNormPairElems / 2;
+  constexpr bool kForAll = kGate == kGateForAll;
+  extern __shared__ __align__(128) unsigned char norm_smem[];
+  __shared__ __align__(8) unsigned long long bars[kNormMaxStages];
+  __shared__ float places[2][4][kNormPairThreads / 32], parts[2][kNormMaxParts][4];
+  Rows rows(q, ring, norm_smem, bars);
+  CtaSums<kNormPairThreads, 4> sums{places, parts, 0, rows.part, ring.parts};
+  const float inv = 1.0f / static_cast<float>(q.dim);
+  const unsigned total = static_cast<unsigned>(q.rows);
+  const bool sigmoid = kGate == kGateEachSigmoid || (kForAll && q.sigmoid);
+  Two of_after[kAfter ? kPairs : 1], of_before[kBefore ? kPairs : 1], of_gate[kForAll ? kPairs : 1];   // sums over rows
+#pragma unroll
+  for (int k = 0; k < kPairs; ++k) of_after[kAfter ? k : 0] = of_before[kBefore ? k : 0] = of_gate[kForAll ? k : 0] = both(0.0f);
+  const float4* statistics = reinterpret_cast<const float4*>(q.stats_in);
+  auto statistic = [&](unsigned r) { return r < total ? __ldg(statistics + r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f); };
+  float4 next[2] = {statistic(rows.group), statistic(rows.group + rows.groups)};
+  for (unsigned r = rows.group; r < total; r += 2 * rows.groups) {
+    const bool second = r + rows.groups < total;
+    const float4 st[2] = {next[0], next[1]};
+    next[0] = statistic(r + 2 * rows.groups);
+    next[1] = statistic(r + 3 * rows.groups);
+    const float poison[2] = {rows.ready(), second ? rows.ready(1) : 0.0f};
+    // of both rows: norm_before(y) and the gate; then the gradient of norm_after's output, and that output
+    Two one[2][kPairs], two[2][kPairs];
+    auto block_hat = [&](int j, int i, const Two (&w)[P], Two (&hat)[P], Two (&value)[P]) {
+      rows.template read<0>(i, hat, j);
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        if (kAfter) hat[k] = times_plus(hat[k], st[j].y, -st[j].x * st[j].y);
+        value[k] = kAfter ? times(hat[k], w[k]) : hat[k];
+      }
+    };
+    auto keep_gate = [&](int j, int i, const Two (&for_all)[P]) {
+      if (kGate == kGateNone) return;
+      Two g[P];
+      if (!kForAll) rows.template read<2>(i, g, j);
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const Two v = kForAll ? for_all[k] : g[k];
+        two[j][i * P + k] = sigmoid ? gate_kept(v) : v;
+      }
+    };
+    auto opened = [&](Two kept) { return sigmoid ? kept_open(kept) : kept; };
+    float2 m[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+    if (kBefore) {
+      Two sh[2] = {both(0.0f), both(0.0f)}, s[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        if (!rows.any(i)) break;
+        Two wa[P], wb[P], wg[P];
+        if (kAfter) rows.template weights<0>(i, wa);
+        rows.template weights<1>(i, wb);
+        if (kForAll) rows.template weights<2>(i, wg);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (j && !second) continue;
+          const float mean_b = -st[j].z * st[j].w;
+          Two hat[P], y[P], f[P], base[P];
+          block_hat(j, i, wa, hat, y);
+          keep_gate(j, i, wg);
+          if (q.residual) {
+            rows.template read<1>(i, f, j);
+#pragma unroll
+            for (int k = 0; k < P; ++k) base[k] = times_plus(f[k], q.residual_scale * st[j].w, mean_b);
+          } else {
+#pragma unroll
+            for (int k = 0; k < P; ++k) base[k] = both(mean_b);
+          }
+          rows.template read<4>(i, f, j);   // (0 beyond the row, so that nothing there counts)
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            if (kGate != kGateNone) y[k] = times(y[k], opened(two[j][i * P + k]));
+            const Two y_hat = times_plus(y[k], q.scale * st[j].w, base[k]);
+            one[j][i * P + k] = y_hat;
+            of_before[kBefore ? i * P + k : 0] = times_plus(f[k], y_hat, of_before[kBefore ? i * P + k : 0]);
+            const Two d = times(f[k], wb[k]);
+            sh[j] = times_plus(d, y_hat, sh[j]);
+            s[j] = sum(s[j], d);
+          }
+        }
+      }
+      float t[4] = {sh[0].x + sh[0].y, s[0].x + s[0].y, sh[1].x + sh[1].y, s[1].x + s[1].y};
+      sums(t);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) m[j] = make_float2(t[2 * j] * inv, q.before == kNormLayer ? t[2 * j + 1] * inv : 0.0f);
+    }
+    Two sh[2] = {both(0.0f), both(0.0f)}, s[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (!rows.any(i)) break;
+      Two wa[P], wb[P], wg[P];
+      if (kAfter) rows.template weights<0>(i, wa);
+      if (kBefore) rows.template weights<1>(i, wb);
+      if (kForAll && !kBefore) rows.template weights<2>(i, wg);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (j && !second) continue;
+        const unsigned row = r + j * rows.groups;
+        Two hat[P], value[P], d[P], f[P];
+        block_hat(j, i, wa, hat, value);
+        if (!kBefore) keep_gate(j, i, wg);
+        if (q.d_y) {
+          rows.template read<3>(i, d, j);
+        } else {
+#pragma unroll
+          for (int k = 0; k < P; ++k) d[k] = both(0.0f);
+        }
+        if (kBefore) {
+          rows.template read<4>(i, f, j);
+#pragma unroll
+          for (int k = 0; k < P; ++k)
+            d[k] = times_plus(times_plus(one[j][i * P + k], -m[j].x, times_plus(f[k], wb[k], -m[j].y)), st[j].w, d[k]);
+        }
+        if (kEdges) rows.blank(i, d);
+        if (q.d_residual) {
+#pragma unroll
+          for (int k = 0; k < P; ++k) f[k] = times(d[k], q.residual_scale);
+          rows.write(q.d_residual, row * q.ld_d_residual, i, f);
+        }
+#pragma unroll
+        for (int k = 0; k < P; ++k) d[k] = times(d[k], q.scale);
+        if (kGate != kGateNone) {
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            f[k] = times(d[k], value[k]);
+            if (sigmoid) f[k] = times(f[k], kept_slope(two[j][i * P + k]));
+            d[k] = times(d[k], opened(two[j][i * P + k]));
+            if (kForAll) of_gate[kForAll ? i * P + k : 0] = sum(of_gate[kForAll ? i * P + k : 0], f[k]);
+          }
+          if (!kForAll && q.d_gate) rows.write(q.d_gate, row * q.ld_d_gate, i, f);
+        }
+        if (kAfter) {
+#pragma unroll
+          for (int k = 0; k < P; ++k) {
+            of_after[kAfter ? i * P + k : 0] = times_plus(d[k], hat[k], of_after[kAfter ? i * P + k : 0]);
+            d[k] = times(d[k], wa[k]);
+            sh[j] = times_plus(d[k], hat[k], sh[j]);
+            s[j] = sum(s[j], d[k]);
+            two[j][i * P + k] = hat[k];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < P; ++k) one[j][i * P + k] = d[k];
+      }
+    }
+    if (kAfter) {
+      float t[4] = {sh[0].x + sh[0].y, s[0].x + s[0].y, sh[1].x + sh[1].y, s[1].x + s[1].y};
+      sums(t);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) m[j] = make_float2(t[2 * j] * inv, q.after == kNormLayer ? t[2 * j + 1] * inv : 0.0f);
+    } else {
+      __syncthreads();
+    }
+    rows.release(r);
+    rows.release(r + rows.groups);
+    if (!q.d_block) continue;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (!rows.any(i)) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (j && !second) continue;
+        Two f[P];
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+          f[k] = one[j][i * P + k];
+          if (kAfter) f[k] = times_plus(two[j][i * P + k], -m[j].x * st[j].y, times_plus(f[k], st[j].y, -m[j].y * st[j].y));
+          f[k].x += poison[j];
+        }
+        rows.write(q.d_block, (r + j * rows.groups) * q.ld_d_block, i, f);
+      }
     }
   }
   if (!q.partial) return;
