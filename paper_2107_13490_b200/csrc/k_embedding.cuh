@@ -36,10 +36,10 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[V]) {
     *p = from_float<T>(f[0]);
   } else if constexpr (V * sizeof(T) == 32) {   // fp32 gradients of 16-bit rows
     const float a[4] = {f[0], f[1], f[2], f[3]}, b[4] = {f[4], f[5], f[6], f[7]};
-    reinterpret_cast<uint4*>(p)[0] = pack16<float>(a);
-    reinterpret_cast<uint4*>(p)[1] = pack16<float>(b);
+    __stcs(reinterpret_cast<uint4*>(p), pack16<float>(a));
+    __stcs(reinterpret_cast<uint4*>(p) + 1, pack16<float>(b));
   } else {
-    *reinterpret_cast<uint4*>(p) = pack16<T>(f);
+    __stcs(reinterpret_cast<uint4*>(p), pack16<T>(f));
   }
 }
 
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embedding_kernel(EmbedParams q,
         unpack16<T>(kShift ? shift_bytes(low[u], high[u], shift) : low[u], f);
 #pragma unroll
         for (int k = 0; k < V; ++k) f[k] = known ? f[k] * q.scale : fill;
-        *reinterpret_cast<uint4*>(out + c) = pack16<T>(f);
+        __stcs(reinterpret_cast<uint4*>(out + c), pack16<T>(f));
       } else {
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -265,7 +265,7 @@ __device__ __forceinline__ void embed_blank(G* row, int dim, int lane) {
   const int skip = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(G));
   for (int c = lane * V - skip; c < dim; c += 32 * V) {
     if (c >= 0 && c + V <= dim) {
-      *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+      __stcs(reinterpret_cast<uint4*>(row + c), make_uint4(0, 0, 0, 0));
     } else {
 #pragma unroll
       for (int k = 0; k < V; ++k)
