@@ -74,6 +74,15 @@ def test_sizes(dtype, kind, rows, dim):
     check(v, d_y, d_n, kind, kind)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("after,before,gate", [(RMS, LAYER, "each"), (LAYER, NONE, "shared"), (NONE, RMS, "none")])
+@pytest.mark.parametrize("rows,dim", [(9999, 72), (4999, 1000), (4997, 1001), (3001, 2040), (3001, 2047), (1201, 4096)])
+def test_many_rows(dtype, after, before, gate, rows, dim):
+    """Each CTA walks over several rounds of its ring of stages, with a last round of one row or two."""
+    v, d_y, d_n = make(rows, dim, dtype, gate)
+    check(v, d_y, d_n, after, before)
+
+
 @pytest.mark.parametrize("dim", [1, 2, 3, 5, 7])
 def test_narrowest_rows(dim):
     for after, before in ((RMS, LAYER), (LAYER, RMS), (NONE, RMS), (LAYER, NONE)):
