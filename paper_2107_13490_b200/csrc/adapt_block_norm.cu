@@ -19,34 +19,10 @@ namespace {
 
 constexpr int kSms = 148;   // of a B200
 
-// How a row is held: by CTAs of so many threads, `parts` of them, `per_sm` on an SM (at most; a kernel's registers say how many).
-// There is room for up to 7 elements between a boundary and an odd row.
-struct NormShape {
-  int elems, rows, parts = 1, threads, per_sm;   // of a thread, at a time
-  NormShape(int64_t dim, int elems_, int rows_, int most, int of_sm, int ctas) : elems(elems_), rows(rows_) {
-    const int64_t room = dim + (dim % 8 ? 7 : 0);
-    while (room > static_cast<int64_t>(elems) * most * parts) parts *= 2;
-    const int64_t unit = 32ll * elems * parts;
-    threads = static_cast<int>((room + unit - 1) / unit) * 32;
-    per_sm = std::max(1, std::min(ctas, of_sm / threads));
-  }
-};
-NormShape norm_forward(int64_t dim) { return NormShape(dim, kNormElems, 1, kNormMaxThreads, 1024, 16); }
-// (backward: CTAs of one warp, whose rows take a warp's latency each, as many as there is room for; of more, stages pay rather
-// than CTAs.  us: 65536 x 256 bf16 with 8 78, with 12 62; 32768 x 1024 fp32 with 8 87, with 10 95)
-NormShape norm_backward(int64_t dim) { return NormShape(dim, kNormElems, 1, kNormBackwardThreads, 512, dim <= 32 * kNormElems ? 16 : 8); }
-// Two rows at a time, by no more CTAs; where they pay.  Above, more CTAs do, and rows of up to 512 are a warp's, 16 CTAs on an SM.
-// us, by ones and by pairs, 2^25 elements: 256 bf16 with both norms and a gate 149, 130; 384 152, 167; 768 156, 135; 1024 124, 126;
-// with one norm fp32 768 85, 75; 1024 86, 73; 2048 86, 74; 2560 80, 95; 16384 rows of 2039 bf16 82, 94
-NormShape norm_backward_pairs(int64_t dim) {
-  return NormShape(dim, kNormPairElems, 2, kNormPairThreads, 512, dim <= 32 * kNormPairElems ? 16 : 8);
-}
-bool norm_in_pairs(int64_t dim, int norms) {
-  const int64_t room = dim + (dim % 8 ? 7 : 0), warp = 32 * kNormPairElems;
-  return room <= warp || (room > 2 * warp && room <= (norms == 1 && dim % 8 == 0 ? 8 * warp : 4 * warp));
-}
-static_assert(8 * 32 * kNormPairElems <= kNormPairElems * kNormPairThreads, "a CTA holds a pair of rows");
-static_assert(ADAPT_NORM_MAX_DIM <= kNormElems * kNormBackwardThreads * kNormMaxParts, "a cluster holds the longest row");
+// (norm_room is largest one below the limit, where it is odd)
+static_assert(norm_room(ADAPT_NORM_MAX_DIM) <= kNormElems * kNormBackwardThreads * kNormMaxParts &&
+                  norm_room(ADAPT_NORM_MAX_DIM - 1) <= kNormElems * kNormBackwardThreads * kNormMaxParts,
+              "a cluster holds the longest row, and the longest odd one");
 
 // CTAs (or clusters) of a backward pass at most, each with sums of its own over its rows.
 int64_t norm_ctas(int64_t rows, int64_t dim) {

@@ -12,6 +12,7 @@
 #include <stdint.h>
 
 #include "k_elem.cuh"
+#include "norm_shape.h"
 #include "tensor_core.cuh"
 
 namespace adapt {
@@ -212,9 +213,6 @@ __global__ __launch_bounds__(kNormThreads) void norm_any_backward_kernel(NormPar
 //
 // Rows that one CTA cannot hold are shared by the CTAs of a cluster, which add up their sums through shared memory.
 
-constexpr int kNormElems = 16;             // elements of a thread
-constexpr int kNormMaxThreads = 1024;      // of a CTA, forward
-constexpr int kNormBackwardThreads = 512;  // and backward
 constexpr int kNormMaxStages = 4;
 
 struct NormRing {
@@ -268,8 +266,6 @@ __device__ __forceinline__ Two kept_open(Two k) {
   return make_float2(signbit(k.x) ? fabsf(k.x) : most.x, signbit(k.y) ? fabsf(k.y) : most.y);
 }
 __device__ __forceinline__ Two kept_slope(Two k) { return make_float2(fmaf(-fabsf(k.x), fabsf(k.x), fabsf(k.x)), fmaf(-fabsf(k.y), fabsf(k.y), fabsf(k.y))); }
-
-constexpr int kNormMaxParts = 4;
 
 // Sums over a CTA, up to kMost at a time, in one of two sets of places in turn, so that one barrier each is enough.
 template <int kThreads, int kMost>
@@ -735,9 +731,6 @@ __global__ __launch_bounds__(kNormBackwardThreads, 1) void norm_row_backward_ker
 
 // The same for shorter rows, two at a time: they share the reading of the weights and the rounds of sums, and each one's
 // latencies hide behind the other's.  A thread holds eight elements of both; the ring has an even number of stages.
-constexpr int kNormPairElems = 8;
-constexpr int kNormPairThreads = 256;
-
 template <typename T, bool kEdges, bool kAfter, bool kBefore, int kGate>
 __global__ __launch_bounds__(kNormPairThreads, 2) void norm_pair_backward_kernel(const NormParams q, const NormRing ring) {
   typedef NormRows<T, kNormPairElems, kEdges> Rows;
