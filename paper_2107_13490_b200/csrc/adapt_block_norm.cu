@@ -250,6 +250,7 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
     return ADAPT_ERR_INVALID_ARG;
   q.stats_in = stats; q.d_y = d_y; q.d_normed = d_normed; q.d_block = d_block; q.d_residual = d_residual; q.d_gate = d_gate;
   q.d_weight_after = d_weight_after; q.d_weight_before = d_weight_before;
+  if (!d_normed) q.residual = nullptr;   // (only the norm before the next block looks at it; its gradient needs d_y alone)
   const int64_t ctas = norm_ctas(rows, dim);
   NormColumns sum = {};
   sum.out[0] = q.shared ? static_cast<float*>(d_gate) : nullptr;
@@ -266,7 +267,7 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   {
     LaunchScope ls(ADAPT_KERNEL_BLOCK_NORM_BACKWARD, stream);
     auto plan_for = [&](const NormShape& shape) {
-      return NormPlan(q, e, shape, {{block, q.ld_block}, {residual, q.ld_residual},
+      return NormPlan(q, e, shape, {{block, q.ld_block}, {q.residual, q.ld_residual},
                       {q.shared ? nullptr : gate, q.ld_gate}, {d_y, q.ld_d_y}, {d_normed, q.ld_d_normed}},
                       {{d_block, q.ld_d_block}, {d_residual, q.ld_d_residual}, {q.shared ? nullptr : d_gate, q.ld_d_gate}});
     };
