@@ -29,6 +29,14 @@ int64_t norm_ctas(int64_t rows, int64_t dim) {
   const NormShape shape = norm_backward(dim);
   return std::min<int64_t>(rows, kSms * shape.per_sm / shape.parts);
 }
+// CTAs of the kernel for any layout, which takes a whole row whatever its length: as many on an SM as have the shared memory for one, up
+// to 4, or as many as the kernels above take of short rows.  (us by 1, 2, 4 and 8 on an SM, both norms and a gate, bf16: 16384 x 1024 886,
+// 470, 284, 271; 16384 x 4096 3828, 2106, 1140, 1189; 4096 x 16384 4397, 2730, 2173 by 3; 65536 x 384 561 by 8, 461 by 16)
+int64_t norm_any_ctas(int64_t rows, int64_t dim) {
+  const int fit = static_cast<int>(220 * 1024 / (dim * 4 + 1024));
+  return std::min<int64_t>(rows, kSms * std::min(fit, std::max(norm_backward(dim).per_sm, 4)));
+}
+static_assert(220 * 1024 / (ADAPT_NORM_MAX_DIM * 4 + 1024) >= 1, "an SM holds the longest row");
 // A multiple of the period, so that a CTA's rows lie alike; the CTAs that are more have no rows, and sums of 0.
 int64_t norm_grid(int64_t ctas, int period) { return (ctas + period - 1) / period * period; }
 
@@ -217,7 +225,7 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate, 
 
 size_t adapt_block_norm_workspace_bytes(int64_t rows, int64_t dim) {
   if (rows < 1 || rows > 0x7FFFFFFF || dim < 1 || dim > ADAPT_NORM_MAX_DIM) return 0;
-  return 3 * sizeof(float) * static_cast<size_t>(norm_grid(norm_ctas(rows, dim), 8)) * dim;
+  return 3 * sizeof(float) * static_cast<size_t>(std::max(norm_grid(norm_ctas(rows, dim), 8), norm_any_ctas(rows, dim))) * dim;
 }
 
 int adapt_block_norm_backward(const void* block, const void* residual, const void* gate, const float* weight_after,
@@ -251,11 +259,10 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
   q.stats_in = stats; q.d_y = d_y; q.d_normed = d_normed; q.d_block = d_block; q.d_residual = d_residual; q.d_gate = d_gate;
   q.d_weight_after = d_weight_after; q.d_weight_before = d_weight_before;
   if (!d_normed) q.residual = nullptr;   // (only the norm before the next block looks at it; its gradient needs d_y alone)
-  const int64_t ctas = norm_ctas(rows, dim);
   NormColumns sum = {};
   sum.out[0] = q.shared ? static_cast<float*>(d_gate) : nullptr;
   sum.out[1] = d_weight_after; sum.out[2] = d_weight_before;
-  sum.ctas = static_cast<int>(ctas); sum.dim = q.dim;
+  sum.dim = q.dim;
   const bool sums = sum.out[0] || sum.out[1] || sum.out[2];
   if (sums) {
     if (!workspace || misaligned(workspace, 256)) return ADAPT_ERR_INVALID_ARG;
@@ -292,11 +299,12 @@ int adapt_block_norm_backward(const void* block, const void* residual, const voi
         });
       });
     } else {
+      sum.ctas = static_cast<int>(norm_any_ctas(rows, dim));
       with_type(dtype, [&](auto t) {
         const auto kernel = norm_any_backward_kernel<decltype(t)>;
         const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ADAPT_NORM_MAX_DIM * 4);
         if (err != cudaSuccess) rc = cuda_fail(err, "block norm, backward");
-        else kernel<<<static_cast<unsigned>(ctas), kNormThreads, q.dim * 4, stream>>>(q);
+        else kernel<<<static_cast<unsigned>(sum.ctas), kNormThreads, q.dim * 4, stream>>>(q);
       });
     }
     if (rc != ADAPT_OK) return rc;

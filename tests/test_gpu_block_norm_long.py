@@ -26,3 +26,15 @@ def test_lengths_at_the_borders_of_shapes(dtype, kind, rows, dim):
 def test_many_long_rows(dtype, after, before, gate, rows, dim):
     v, d_y, d_n = make(rows, dim, dtype, gate)
     check(v, d_y, d_n, after, before)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gate", ["each", "shared"])
+@pytest.mark.parametrize("rows,dim", [(1300, 1024), (700, 4096), (613, 9000), (451, 16384), (301, 20001), (151, 32768)])
+def test_many_rows_that_lie_otherwise(dtype, gate, rows, dim):
+    """The residual begins behind the other tensors' 16-byte boundaries; CTAs take several rows each."""
+    v, d_y, d_n = make(rows, dim, dtype, gate)
+    buf = torch.zeros((rows, dim + 8), dtype=dtype, device="cuda")
+    buf[:, 1:1 + dim] = v["residual"]
+    v["residual"] = buf[:, 1:1 + dim]
+    check(v, d_y, d_n, RMS, LAYER)

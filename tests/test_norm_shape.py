@@ -3,6 +3,8 @@ cluster and the places that their sums have, wherever the row begins.  Compiled 
 import os
 import subprocess
 
+from paper_2107_13490_b200 import binding as B
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2107_13490_b200", "csrc")
 SOURCE = """
 #include <cstdio>
@@ -36,3 +38,10 @@ def test_every_length_fits(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, str(tmp_path / "norm_shape.cpp"), "-o", program], check=True)
     r = subprocess.run([program], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_long_rows_have_sums_of_a_cta_on_every_sm():
+    """Rows that lie otherwise go to CTAs of which each takes a whole row: no fewer than there are SMs (148)."""
+    for dim in (1, 8, 333, 1000, 4096, 8192, 8193, 9000, 16384, 16385, 20001, B.NORM_MAX_DIM):
+        assert B.adapt_block_norm_workspace_bytes(100000, dim) >= 3 * 4 * 148 * dim, dim
+        assert B.adapt_block_norm_workspace_bytes(3, dim) >= 3 * 4 * 3 * dim, dim
