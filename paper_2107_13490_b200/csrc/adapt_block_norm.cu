@@ -121,20 +121,39 @@ int norm_registers(int* out) {
   return ADAPT_OK;
 }
 
+// Clusters of a launch that the device holds at once: of 4 and more CTAs not every SM has a place, since a cluster lies within one of
+// the device's groups of SMs (33 clusters of 4, 15 of 8).  The answer to the last question of each device is kept.
+template <auto kKernel>
+int norm_clusters(const cudaLaunchConfig_t& cfg, int* out) {
+  static std::atomic<uint64_t> known[kMaxDevices];   // threads (11 bits), shared memory (18), CTAs of a cluster (4), clusters
+  int device = 0, n = 0;
+  ADAPT_CUDA(cudaGetDevice(&device));
+  std::atomic<uint64_t>& slot = known[device % kMaxDevices];
+  const uint64_t asked = cfg.blockDim.x | cfg.dynamicSmemBytes << 11 | static_cast<uint64_t>(cfg.attrs[0].val.clusterDim.x) << 29, last = slot.load();
+  if (last && (last & ((1ull << 33) - 1)) == asked) {
+    n = static_cast<int>(last >> 33);
+  } else {
+    ADAPT_CUDA(cudaOccupancyMaxActiveClusters(&n, kKernel, &cfg));
+    slot.store(asked | static_cast<uint64_t>(n) << 33);
+  }
+  *out = n;
+  return ADAPT_OK;
+}
+
 // Launches a kernel on as many CTAs as the device holds at once, and says how many (clusters) that are: a CTA that had to wait
-// for another's end would begin its share of the rows then.  (us, 32768 x 4095 fp16 with 152 CTAs backward 1684, with 144 954)
+// for another's end would begin its share of the rows then.  (us, 32768 x 4095 fp16 with 152 CTAs backward 1684, with 144 954;
+// 2048 x 32768 bf16 with 37 clusters 765, with 33 443)
 template <auto kKernel>
 int norm_launch(int64_t rows, const NormShape& shape, NormPlan plan, cudaStream_t stream, const NormParams& q, int* groups) {
   int registers = 0;
-  const int rc = norm_registers<kKernel>(&registers);
+  int rc = norm_registers<kKernel>(&registers);
   if (rc != ADAPT_OK) return rc;
   int per_sm = std::max(1, std::min(shape.per_sm, 65536 / (registers * shape.threads)));
   plan.fit(per_sm, shape.rows);
   while (per_sm > 1 && per_sm * (plan.smem + 2048) > 228 * 1024) plan.fit(--per_sm, shape.rows);
-  const int held = kSms * per_sm / shape.parts;
-  *groups = static_cast<int>(std::min<int64_t>(norm_grid(rows, plan.period), held / plan.period * plan.period));
+  int held = kSms * per_sm / shape.parts;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(*groups * shape.parts));
+  cfg.gridDim = dim3(static_cast<unsigned>(held * shape.parts));
   cfg.blockDim = dim3(shape.threads);
   cfg.dynamicSmemBytes = plan.smem;
   cfg.stream = stream;
@@ -143,6 +162,13 @@ int norm_launch(int64_t rows, const NormShape& shape, NormPlan plan, cudaStream_
   attr[0].val.clusterDim.x = shape.parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = shape.parts > 1 ? 1 : 0;
+  if (shape.parts > 1) {
+    int clusters = 0;
+    if ((rc = norm_clusters<kKernel>(cfg, &clusters)) != ADAPT_OK) return rc;
+    held = std::min(held, clusters);
+  }
+  *groups = static_cast<int>(std::min<int64_t>(norm_grid(rows, plan.period), std::max(1, held / plan.period) * plan.period));
+  cfg.gridDim = dim3(static_cast<unsigned>(*groups * shape.parts));
   ADAPT_CUDA(cudaLaunchKernelEx(&cfg, kKernel, q, plan.ring));
   return ADAPT_OK;
 }
