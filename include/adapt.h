@@ -711,11 +711,14 @@ int adapt_block_norm(const void* block, const void* residual, const void* gate,
 /* Its gradient.  y is recomputed in fp32 from the inputs, which must be as they were.
  *   stats     as adapt_block_norm wrote it for the same inputs
  *   d_y, d_normed  DEVICE [rows][dim], gradients of y and normed; either may be NULL (0), not
- *             both; d_normed needs before
+ *             both; d_normed needs before.  Without d_normed the residual is not read
  *   d_block, d_residual, d_gate  DEVICE [rows][dim], each may be NULL; a shared gate's d_gate is
  *             DEVICE float[dim], the sum over the rows.  d_residual may be d_y (same leading
  *             dimension), no other overlap
- *   d_weight_after, d_weight_before  DEVICE float[dim], each may be NULL
+ *   d_weight_after, d_weight_before  DEVICE float[dim], each may be NULL.  d_weight_before needs
+ *             d_normed (without it that gradient is 0, and not written).  Where there are no
+ *             rows, both and a shared gate's d_gate are written as 0, d_y and d_normed not
+ *             looked at
  *   strides   HOST int64[8] = leading dimensions of block, residual, gate, d_y, d_normed,
  *             d_block, d_residual, d_gate, or NULL: dim.  Inputs may have 0
  *   workspace DEVICE scratch of adapt_block_norm_workspace_bytes, 256-byte aligned; needed where a

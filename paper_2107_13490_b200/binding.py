@@ -908,7 +908,8 @@ def adapt_block_norm_backward(block: torch.Tensor, stats: torch.Tensor, d_y: Opt
                               want_residual: bool = True, want_gate: bool = True, want_weights: bool = True,
                               d_residual: Optional[torch.Tensor] = None, stream=None) -> BlockNormGradients:
     """adapt_block_norm_backward of adapt.h, for the inputs and options of adapt_block_norm and its ``stats``;
-    gradients of what was given there and is wanted.  ``d_residual`` may be ``d_y`` (in place)."""
+    gradients of what was given there and is wanted.  ``d_weight_before`` needs ``d_normed``: without it that gradient
+    is 0 and None is returned.  ``d_residual`` may be ``d_y`` (in place)."""
     return BlockNormGradients(*_run("block_norm_backward", stream, block, residual, gate, weight_after, weight_before,
                                     after, before, gate_mode, scale, residual_scale, eps, stats, d_y, d_normed,
                                     want_block, want_residual, want_gate, want_weights, d_residual))

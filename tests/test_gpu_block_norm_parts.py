@@ -26,3 +26,16 @@ def test_the_residual_is_not_looked_at_without_the_second_norm_s_gradient(dtype,
     for n in ("d_block", "d_gate", "d_weight_after"):
         assert torch.equal(getattr(got, n), getattr(want, n)), n
     assert want.d_residual is None and got.d_residual.shape == (rows, dim)
+
+
+def test_the_second_norm_s_weight_has_no_gradient_without_the_output_s():
+    v, d_y, d_n = make(40, 256, torch.float32)
+    how = dict(after=RMS, before=RMS, eps=EPS)
+    stats = B.adapt_block_norm(**v, **how, want_stats=True).stats
+    g = B.adapt_block_norm_backward(stats=stats, d_y=d_y, **v, **how)
+    assert g.d_weight_before is None and g.d_weight_after is not None
+    # what is left out is 0
+    assert (B.adapt_block_norm_backward(stats=stats, d_y=d_y, d_normed=torch.zeros_like(d_n), **v, **how).d_weight_before == 0).all()
+    none = {n: t[:0] if t.dim() == 2 else t for n, t in v.items()}
+    g = B.adapt_block_norm_backward(stats=stats[:0], d_y=d_y[:0], d_normed=d_n[:0], **none, **how)
+    assert (g.d_weight_before == 0).all() and (g.d_weight_after == 0).all()
