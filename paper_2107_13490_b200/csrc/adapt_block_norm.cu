@@ -17,8 +17,6 @@ static_assert(ADAPT_NORM_NONE == kNormNone && ADAPT_NORM_RMS == kNormRms && ADAP
 
 namespace {
 
-constexpr int kSms = 148;   // of a B200
-
 // (norm_room is largest one below the limit, where it is odd)
 static_assert(norm_room(ADAPT_NORM_MAX_DIM) <= kNormElems * kNormBackwardThreads * kNormMaxParts &&
                   norm_room(ADAPT_NORM_MAX_DIM - 1) <= kNormElems * kNormBackwardThreads * kNormMaxParts,

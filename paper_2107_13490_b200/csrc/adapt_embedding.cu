@@ -12,11 +12,6 @@ using namespace adapt;
 
 namespace {
 
-constexpr int kSms = 148;   // of a B200
-
-// (with room for what is added to a size before it is compared)
-bool in_int(int64_t v, int64_t least) { return v >= least && v <= (1 << 30); }
-
 // How the rows of a gradient are dealt out: CTAs of `teams` teams of `lanes` threads, `slices` of them for a row.
 struct EmbedTeams {
   int lanes = 8, teams, slices;

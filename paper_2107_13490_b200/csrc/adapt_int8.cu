@@ -11,11 +11,6 @@ using namespace adapt;
 
 namespace {
 
-constexpr int kSms = 148;   // of a B200
-
-// (with room for what is added to a size before it is compared)
-bool in_int(int64_t v, int64_t least) { return v >= least && v <= (1 << 30); }
-
 int run_rows(const RowsParams& q, int dtype, cudaStream_t stream) {
   const int e = elem_bytes(dtype), wide = 16 / e;
   // a row in the registers of up to 256 threads, 8 chunks each

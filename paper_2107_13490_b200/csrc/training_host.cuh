@@ -1,4 +1,4 @@
-// Host side that the training-step operators' entry points share.
+// Host side that the entry points of the training-step operators and of those around the layers share.
 #pragma once
 
 #include <cstdint>
@@ -8,6 +8,12 @@
 #include "k_elem.cuh"
 
 namespace adapt {
+
+// SMs of a B200.  A constant: workspaces are sized without a device, and grids and cuts go by the same number.
+constexpr int kSms = 148;
+
+// Whether a size is in a kernel's reach (with room for what is added to it before it is compared).
+inline bool in_int(int64_t v, int64_t least) { return v >= least && v <= (1 << 30); }
 
 // Bytes of an element, 0 for an unknown type.
 inline int elem_bytes(int dtype) {
