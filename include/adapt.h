@@ -691,6 +691,7 @@ size_t adapt_embedding_workspace_bytes(int64_t n, int64_t dim, int64_t vocab);
  *            (same leading dimension), normed too where y is not it; no other overlap
  *   weight_after, weight_before  DEVICE float[dim] or NULL: 1
  *   eps      >= 0 and finite; scale, residual_scale finite
+ *            Means are taken in fp32, of squares too: for values of y and block up to 1e17
  *   stats_out  DEVICE float[rows][4] or NULL: {mean, 1 / deviation} of block and of y, what the
  *            backward pass starts from
  * Limits: rows < 2^31, dim <= ADAPT_NORM_MAX_DIM. */

@@ -34,8 +34,9 @@ inline NormShape norm_backward(int64_t dim) {
   return NormShape(dim, kNormElems, 1, kNormBackwardThreads, 512, dim <= 32 * kNormElems ? 16 : 8);
 }
 // Two rows at a time, by no more CTAs; where they pay.  Above, more CTAs do, and rows of up to 512 are a warp's, 16 CTAs on an SM.
-// us, by ones and by pairs, 2^25 elements: 256 bf16 with both norms and a gate 149, 130; 384 152, 167; 768 156, 135; 1024 124, 126;
-// with one norm fp32 768 85, 75; 1024 86, 73; 2048 86, 74; 2560 80, 95; 16384 rows of 2039 bf16 82, 94
+// us, by ones and by pairs, 2^25 elements: 256 bf16 with both norms and a gate 149, 130; 384 152, 167; 640 183, 158; 768 156, 135;
+// without the gate 1000 117, 103; 1024 110, 101; with one norm fp32 768 85, 75; 1024 86, 73; 2048 86, 74; 2560 80, 95; 16384 rows of
+// 2039 bf16 82, 94.  The rule does not see the gate: with one 896 135, 139; 1000 128, 129; 1024 123, 126
 inline NormShape norm_backward_pairs(int64_t dim) {
   return NormShape(dim, kNormPairElems, 2, kNormPairThreads, 512, dim <= 32 * kNormPairElems ? 16 : 8);
 }
